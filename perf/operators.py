@@ -251,7 +251,7 @@ def _append(pool, k, v, table, seq_len, q_start, page):
     where = _places(table, seq_len, q_start, k.shape[0], page)
     for name, x in (("k", k), ("v", v)):
         g = x.float().unflatten(-1, (-1, GROUP))
-        lo, hi = g.amin(-1).clamp(-65504, 65504), g.amax(-1).clamp(-65504, 65504)
+        lo, hi = g.amin(-1).clamp(-65000, 65000), g.amax(-1).clamp(-65000, 65000)
         step, base = ((hi - lo) / 15).half(), lo.half()
         s = step.float()
         code = torch.round((g - base.float()[..., None]) * torch.where(s > 0, 1 / s, torch.zeros_like(s))[..., None])
