@@ -63,8 +63,10 @@ typedef enum {
     TSVD_E_TOOBIG = 9,  /* request exceeds a fixed capacity (tsvd_forward_static, TSVD_MAX_CONTRACTION) */
     TSVD_E_RANGE = 10,  /* tsvd_last_status only: a token's dynamic range exceeded what the
                            fixed-point digits resolve (see the note on arithmetic above)   */
-    TSVD_E_INTERNAL = 11 /* tsvd_last_status only, builds with -DTSVD_CHECK_BOUNDS: a kernel found
+    TSVD_E_INTERNAL = 11, /* tsvd_last_status only, builds with -DTSVD_CHECK_BOUNDS: a kernel found
                            one of its ring or tile indices outside its range              */
+    TSVD_E_INDEX = 12   /* tsvd_kv4_last_status only (tsvd_serving.h): a page number or a sequence length
+                           was outside its range                                           */
 } tsvd_status_t;
 
 /* Longest contraction (N and K) a handle may have: the digit sums of a row are combined in

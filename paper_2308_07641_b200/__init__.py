@@ -2,7 +2,9 @@
 
 `binding` mirrors the C entry points one to one; `TSVDLinear` is a small
 convenience over them for torch tensors (it owns a handle and passes data
-pointers and the current stream; it computes nothing itself).
+pointers and the current stream; it computes nothing itself).  `serving` holds
+what a served layer needs beside it: 8-bit linear layers and a 4-bit key/value
+cache with its attention (include/tsvd_serving.h).
 """
 from __future__ import annotations
 
@@ -10,6 +12,7 @@ from . import binding
 from .binding import (DTYPES, TSVD_BF16, TSVD_F32, TSVD_I8, TSVD_FLAG_OUT_F32,  # noqa: F401
                       TSVD_FLAG_PATH_DECODE, TSVD_FLAG_PATH_SIMPLE, TSVD_FLAG_PATH_TENSOR,
                       TSVD_FLAG_WIDE_X, TSVDError)
+from .serving import Int8Linear, KV4Cache, dequantize, quantize  # noqa: F401
 
 
 def device_activations(x_np, x_dtype: str):

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libtsvd.so")
 TSVD_F32, TSVD_BF16, TSVD_I8 = 0, 1, 2
 TSVD_OK = 0
 (TSVD_E_NULL, TSVD_E_SHAPE, TSVD_E_VALUE, TSVD_E_DTYPE, TSVD_E_ALIGN, TSVD_E_CUDA,
- TSVD_E_TIMEOUT, TSVD_E_NOMEM, TSVD_E_TOOBIG, TSVD_E_RANGE, TSVD_E_INTERNAL) = range(1, 12)
+ TSVD_E_TIMEOUT, TSVD_E_NOMEM, TSVD_E_TOOBIG, TSVD_E_RANGE, TSVD_E_INTERNAL, TSVD_E_INDEX) = range(1, 13)
 TSVD_MAX_CONTRACTION = 65280
 TSVD_STATIC_SCRATCH_BYTES = 4 << 20
 TSVD_FLAG_OUT_F32 = 0x1
@@ -32,13 +32,21 @@ TSVD_PACK_INDEX_LISTS = 0x1      # tsvd_pack flag
 TSVD_INDEX_MAX_COLUMNS = 32768
 TSVD_FLAG_TEST_STALL = 0x100
 TSVD_FLAG_WIDE_X = 0x200         # bf16 activations as four digits (outliers up to 2^16 of the bulk)
+# tsvd_serving.h
+TSVD_FLAG_OUT_BF16 = 0x2         # tsvd_i8_forward: bf16 results
+TSVD_FLAG_CAUSAL = 0x4           # tsvd_kv4_attend
+TSVD_I8_MAX_N = 131071
 
 DTYPES = {"f32": TSVD_F32, "bf16": TSVD_BF16, "i8": TSVD_I8}
 
-# every symbol include/tsvd.h declares
+# every symbol include/tsvd.h and include/tsvd_serving.h declare
 EXPORTS = ("tsvd_pack", "tsvd_forward", "tsvd_forward_ex", "tsvd_forward_host", "tsvd_forward_static",
            "tsvd_reserve", "tsvd_set_bias", "tsvd_ternarize", "tsvd_forward_v", "tsvd_forward_v_patches", "tsvd_im2col", "tsvd_last_status", "tsvd_plan", "tsvd_info", "tsvd_index_bytes", "tsvd_unpack", "tsvd_profile_enable", "tsvd_profile_read",
-           "tsvd_launch_count", "tsvd_destroy", "tsvd_strerror")
+           "tsvd_launch_count", "tsvd_destroy", "tsvd_strerror",
+           # include/tsvd_serving.h
+           "tsvd_quantize", "tsvd_dequantize", "tsvd_i8_pack", "tsvd_i8_forward", "tsvd_i8_reserve", "tsvd_i8_info",
+           "tsvd_i8_last_status", "tsvd_i8_destroy", "tsvd_kv4_create", "tsvd_kv4_append", "tsvd_kv4_read",
+           "tsvd_kv4_attend", "tsvd_kv4_info", "tsvd_kv4_last_status", "tsvd_kv4_destroy")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -108,6 +116,27 @@ def lib() -> ctypes.CDLL:
         L.tsvd_launch_count.restype = ctypes.c_ulonglong
         L.tsvd_destroy.argtypes = [vp]
         L.tsvd_destroy.restype = None
+        ll = ctypes.c_longlong
+        L.tsvd_quantize.argtypes = [vp, ci, ll, ci, ll, vp, ll, vp, vp]
+        L.tsvd_dequantize.argtypes = [vp, ll, vp, ll, ci, vp, ci, ll, vp]
+        L.tsvd_i8_pack.argtypes = [vp, ll, vp, vp, ci, ci, cu, ctypes.POINTER(vp)]
+        L.tsvd_i8_forward.argtypes = [vp, vp, ll, vp, vp, ll, ci, ci, cu, vp]
+        L.tsvd_i8_reserve.argtypes = [vp, ci, ci]
+        L.tsvd_i8_info.argtypes = [vp, ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(ctypes.c_size_t)]
+        L.tsvd_i8_last_status.argtypes = [vp]
+        L.tsvd_i8_destroy.argtypes = [vp]
+        L.tsvd_kv4_create.argtypes = [ci, ci, ci, ll, ctypes.POINTER(vp)]
+        L.tsvd_kv4_append.argtypes = [vp, vp, ll, vp, ll, ci, vp, ci, vp, vp, ci, ci, vp]
+        L.tsvd_kv4_read.argtypes = [vp, vp, ll, vp, ll, ci, vp, ci, vp, vp, ci, ci, vp]
+        L.tsvd_kv4_attend.argtypes = [vp, vp, ll, vp, ll, ci, ci, vp, ci, vp, vp, ci, ci, ci, ci, ctypes.c_float, ci, cu, vp]
+        L.tsvd_kv4_info.argtypes = [vp] + [ctypes.POINTER(ci)] * 3 + [ctypes.POINTER(ll), ctypes.POINTER(ctypes.c_size_t)]
+        L.tsvd_kv4_last_status.argtypes = [vp]
+        L.tsvd_kv4_destroy.argtypes = [vp]
+        for f in ("quantize", "dequantize", "i8_pack", "i8_forward", "i8_reserve", "i8_info", "i8_last_status", "kv4_create",
+                  "kv4_append", "kv4_read", "kv4_attend", "kv4_info", "kv4_last_status"):
+            getattr(L, "tsvd_" + f).restype = ci
+        L.tsvd_i8_destroy.restype = None
+        L.tsvd_kv4_destroy.restype = None
         L.tsvd_strerror.argtypes = [ci]
         L.tsvd_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -275,3 +304,92 @@ def tsvd_launch_count() -> int:
 def tsvd_destroy(h: int) -> None:
     if h:
         lib().tsvd_destroy(h)
+
+
+# ---- include/tsvd_serving.h: raw device pointers (torch.Tensor.data_ptr()) and a cudaStream_t value -----------------
+
+
+def tsvd_quantize(x_ptr: int, dtype: int, rows: int, cols: int, ldx: int, q_ptr: int, ldq: int, scale_ptr: int,
+                  stream: int = 0) -> None:
+    """Rows of x into 8-bit integers with one scale per row."""
+    _check(lib().tsvd_quantize(x_ptr, dtype, rows, cols, ldx, q_ptr, ldq, scale_ptr, stream or None), "tsvd_quantize")
+
+
+def tsvd_dequantize(q_ptr: int, ldq: int, scale_ptr: int, rows: int, cols: int, y_ptr: int, dtype: int, ldy: int,
+                    stream: int = 0) -> None:
+    _check(lib().tsvd_dequantize(q_ptr, ldq, scale_ptr, rows, cols, y_ptr, dtype, ldy, stream or None), "tsvd_dequantize")
+
+
+def tsvd_i8_pack(W_ptr: int, ldw: int, w_scale_ptr: int, bias_ptr: int, M: int, N: int, flags: int = 0) -> int:
+    """Host or device pointers of W int8 [M,N], w_scale and (or 0) bias float [M]; returns the handle."""
+    h = ctypes.c_void_p()
+    _check(lib().tsvd_i8_pack(W_ptr, ldw, w_scale_ptr, bias_ptr or None, M, N, flags, ctypes.byref(h)), "tsvd_i8_pack")
+    return h.value
+
+
+def tsvd_i8_forward(h: int, x_ptr: int, ldx: int, x_scale_ptr: int, y_ptr: int, ldy: int, B: int, dtype: int, flags: int = 0,
+                    stream: int = 0) -> None:
+    _check(lib().tsvd_i8_forward(h, x_ptr, ldx, x_scale_ptr or None, y_ptr, ldy, B, dtype, flags, stream or None),
+           "tsvd_i8_forward")
+
+
+def tsvd_i8_reserve(h: int, B_max: int, dtype: int) -> None:
+    _check(lib().tsvd_i8_reserve(h, B_max, dtype), "tsvd_i8_reserve")
+
+
+def tsvd_i8_info(h: int) -> dict:
+    M, N, pb = ctypes.c_int(), ctypes.c_int(), ctypes.c_size_t()
+    _check(lib().tsvd_i8_info(h, ctypes.byref(M), ctypes.byref(N), ctypes.byref(pb)), "tsvd_i8_info")
+    return {"M": M.value, "N": N.value, "packed_bytes": pb.value}
+
+
+def tsvd_i8_last_status(h: int) -> int:
+    return int(lib().tsvd_i8_last_status(h))
+
+
+def tsvd_i8_destroy(h: int) -> None:
+    if h:
+        lib().tsvd_i8_destroy(h)
+
+
+def tsvd_kv4_create(n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().tsvd_kv4_create(n_kv_heads, head_dim, page_tokens, n_pages, ctypes.byref(h)), "tsvd_kv4_create")
+    return h.value
+
+
+def tsvd_kv4_append(h: int, k_ptr: int, ldk: int, v_ptr: int, ldv: int, dtype: int, table_ptr: int, max_pages: int,
+                    seq_len_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, stream: int = 0) -> None:
+    _check(lib().tsvd_kv4_append(h, k_ptr, ldk, v_ptr, ldv, dtype, table_ptr, max_pages, seq_len_ptr, q_start_ptr or None, n_seq,
+                                 n_rows, stream or None), "tsvd_kv4_append")
+
+
+def tsvd_kv4_read(h: int, k_ptr: int, ldk: int, v_ptr: int, ldv: int, dtype: int, table_ptr: int, max_pages: int,
+                  seq_len_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, stream: int = 0) -> None:
+    _check(lib().tsvd_kv4_read(h, k_ptr, ldk, v_ptr, ldv, dtype, table_ptr, max_pages, seq_len_ptr, q_start_ptr or None, n_seq,
+                               n_rows, stream or None), "tsvd_kv4_read")
+
+
+def tsvd_kv4_attend(h: int, q_ptr: int, ldq: int, out_ptr: int, ldo: int, n_heads: int, dtype: int, table_ptr: int,
+                    max_pages: int, seq_len_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, max_q: int, max_kv: int,
+                    scale: float, window: int = 0, flags: int = 0, stream: int = 0) -> None:
+    _check(lib().tsvd_kv4_attend(h, q_ptr, ldq, out_ptr, ldo, n_heads, dtype, table_ptr, max_pages, seq_len_ptr,
+                                 q_start_ptr or None, n_seq, n_rows, max_q, max_kv, scale, window, flags, stream or None),
+           "tsvd_kv4_attend")
+
+
+def tsvd_kv4_info(h: int) -> dict:
+    a, b, c = ctypes.c_int(), ctypes.c_int(), ctypes.c_int()
+    n, pb = ctypes.c_longlong(), ctypes.c_size_t()
+    _check(lib().tsvd_kv4_info(h, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), ctypes.byref(n), ctypes.byref(pb)),
+           "tsvd_kv4_info")
+    return {"n_kv_heads": a.value, "head_dim": b.value, "page_tokens": c.value, "n_pages": n.value, "pool_bytes": pb.value}
+
+
+def tsvd_kv4_last_status(h: int) -> int:
+    return int(lib().tsvd_kv4_last_status(h))
+
+
+def tsvd_kv4_destroy(h: int) -> None:
+    if h:
+        lib().tsvd_kv4_destroy(h)

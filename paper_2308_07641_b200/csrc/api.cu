@@ -25,6 +25,7 @@ extern "C" const char* tsvd_strerror(tsvd_status_t s)
         case TSVD_E_TOOBIG: return "request exceeds a fixed capacity (static scratch, contraction length or index width)";
         case TSVD_E_RANGE: return "a token's dynamic range exceeded what the fixed-point digits resolve";
         case TSVD_E_INTERNAL: return "a checked build found an index outside its range";
+        case TSVD_E_INDEX: return "a page number or a sequence length is outside its range";
     }
     return "unknown status";
 }

@@ -1,0 +1,323 @@
+// Keys and values in 4 bits: the pool of pages, append, read, and the entry point of the attention.
+//
+// Per position, head and group of 32 numbers: step = fp16((hi - lo) / 15), base = fp16(lo),
+// code = clamp(rint((x - base) / step), 0, 15).
+#include <new>
+
+#include "serving.cuh"
+
+namespace {
+
+constexpr float kMost = 65000.0f;   // the largest magnitude kept: 15 steps above -kMost still are an fp16 number
+
+// Where row `row` of the batch lives: its page and place, or page = -1 (with the status bit) when that is out of range.
+struct Place { int page, at; };
+__device__ __forceinline__ Place place_of_row(const Kv4Geom& g, const Kv4Batch& b, int row, int* status)
+{
+    Place p{-1, 0};
+    const int s = kv4_seq_of_row(b, row);
+    if (s >= b.n_seq) return p;                       // behind the last sequence: not a row
+    const int end = b.q_start ? b.q_start[s + 1] : row + 1;
+    const long long pos = (long long)b.seq_len[s] - (end - row);
+    if (pos >= 0 && pos < (long long)b.max_pages * g.page_tokens) {
+        const int page = b.table[(long long)s * b.max_pages + pos / g.page_tokens];
+        if (page >= 0 && page < g.n_pages) {
+            p.page = page;
+            p.at = (int)(pos % g.page_tokens);
+        }
+    }
+    if (p.page < 0 && threadIdx.x == 0) atomicOr(status, KV4_DEV_INDEX);
+    return p;
+}
+
+// Eight consecutive numbers; VEC: the address is a multiple of 16 bytes.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8])
+{
+    if constexpr (VEC) {
+        alignas(16) T t[8];
+#pragma unroll
+        for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(t)[i] = reinterpret_cast<const uint4*>(p)[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(p[i]);
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8])
+{
+    alignas(16) T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = from_f32<T>(v[i]);
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<uint4*>(t)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = t[i];
+    }
+}
+
+// What one thread holds: eight numbers, a quarter of a group.  Item `u` of a row: key or value, head, word of eight.
+struct Item { int is_v, head, word; };
+__device__ __forceinline__ Item item_of(int u, int heads, int words)
+{
+    Item t;
+    t.word = u % words;
+    t.head = u / words % heads;
+    t.is_v = u / (words * heads);
+    return t;
+}
+// Byte offsets inside a 16-position block.
+__device__ __forceinline__ int code_offset(const Item& t, int dim, int at)
+{
+    const int w = t.word >> 2, j = t.word & 3;       // group, quarter
+    const int place = t.is_v ? t.word : j * (dim / KV4_GROUP) + w;
+    return (t.is_v ? 10 * dim : 0) + at * (dim / 2) + place * 4;
+}
+__device__ __forceinline__ int scale_offset(const Item& t, int dim, int at)
+{
+    return (t.is_v ? 18 * dim : 8 * dim) + at * (dim / 8) + (t.word >> 2) * 4;
+}
+
+// A block takes a row; the rows of a call go into different positions, so no two blocks write the same bytes.
+template <typename T, bool VEC>
+__global__ void kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv,
+                                  int* status)
+{
+    const int row = blockIdx.x;
+    const Place at = place_of_row(g, b, row, status);
+    if (at.page < 0) return;
+    const int words = g.dim / 8, items = 2 * g.heads * words;
+    for (int u = threadIdx.x; u < items; u += blockDim.x) {   // items is a multiple of 16: quads stay whole
+        const Item t = item_of(u, g.heads, words);
+        float x[8];
+        load8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + (long long)t.head * g.dim + t.word * 8, x);
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
+        const unsigned quad = 0xfu << (threadIdx.x & 28);
+        lo = fminf(lo, __shfl_xor_sync(quad, lo, 1));
+        hi = fmaxf(hi, __shfl_xor_sync(quad, hi, 1));
+        lo = fmaxf(fminf(lo, __shfl_xor_sync(quad, lo, 2)), -kMost);
+        hi = fminf(fmaxf(hi, __shfl_xor_sync(quad, hi, 2)), kMost);
+        lo = fminf(lo, kMost);
+        hi = fmaxf(hi, -kMost);
+        const __half step = __float2half_rn(__fdiv_rn(hi - lo, 15.0f)), base = __float2half_rn(lo);
+        const float s = __half2float(step), m = __half2float(base);
+        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = min(15, max(0, __float2int_rn(__fmul_rn(__fsub_rn(x[e], m), inv))));
+            word |= (uint32_t)c << (4 * ((e >> 1) + 4 * (e & 1)));
+        }
+        uint8_t* blk = g.block(at.page, t.head, at.at);
+        const int pos = at.at & (KV4_BLOCK - 1);
+        *reinterpret_cast<uint32_t*>(blk + code_offset(t, g.dim, pos)) = word;
+        if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + scale_offset(t, g.dim, pos)) = __halves2half2(step, base);
+    }
+}
+
+template <typename T, bool VEC>
+__global__ void kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __restrict__ v, long long ldv, int* status)
+{
+    const int row = blockIdx.x;
+    const Place at = place_of_row(g, b, row, status);
+    const int words = g.dim / 8, items = 2 * g.heads * words;
+    for (int u = threadIdx.x; u < items; u += blockDim.x) {
+        const Item t = item_of(u, g.heads, words);
+        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (at.page >= 0) {
+            const uint8_t* blk = g.block(at.page, t.head, at.at);
+            const int pos = at.at & (KV4_BLOCK - 1);
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(blk + code_offset(t, g.dim, pos));
+            const float2 sm = __half22float2(*reinterpret_cast<const __half2*>(blk + scale_offset(t, g.dim, pos)));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((word >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u), sm.x, sm.y);
+        }
+        store8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + (long long)t.head * g.dim + t.word * 8, x);
+    }
+}
+
+unsigned row_threads(const Kv4Geom& g)
+{
+    const int items = 2 * g.heads * (g.dim / 8);
+    return (unsigned)(items >= 512 ? 512 : (items + 31) / 32 * 32);
+}
+
+bool aligned16(const void* p, long long ld, size_t size) { return (((uintptr_t)p) & 15) == 0 && (ld * (long long)size) % 16 == 0; }
+
+tsvd_status_t check_batch(const tsvd_kv4_s* h, const int* page_table, int max_pages, const int* seq_len, int n_seq, int n_rows,
+                          const int* q_start)
+{
+    if (!h || !page_table || !seq_len) return TSVD_E_NULL;
+    if (max_pages < 1 || n_seq < 1 || n_rows < 0 || (!q_start && n_rows != n_seq)) return TSVD_E_SHAPE;
+    if (((uintptr_t)page_table | (uintptr_t)seq_len | (uintptr_t)q_start) & 3) return TSVD_E_ALIGN;
+    return TSVD_OK;
+}
+
+}  // namespace
+
+extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_tokens, long long n_pages, tsvd_kv4_t* out)
+{
+    if (!out) return TSVD_E_NULL;
+    *out = nullptr;
+    if (n_kv_heads < 1 || (head_dim != 64 && head_dim != 128) || page_tokens < 1 || page_tokens % KV4_BLOCK || n_pages < 1)
+        return TSVD_E_SHAPE;
+    if (n_pages > 0x7fffffffLL / page_tokens || n_kv_heads > 65535) return TSVD_E_TOOBIG;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return TSVD_E_CUDA; }
+    tsvd_kv4_s* h = new (std::nothrow) tsvd_kv4_s();
+    if (!h) return TSVD_E_NOMEM;
+    h->device = dev;
+    h->g.heads = n_kv_heads;
+    h->g.dim = head_dim;
+    h->g.page_tokens = page_tokens;
+    h->g.n_pages = (int)n_pages;
+    h->pool_bytes = (size_t)n_pages * h->g.page_bytes();
+    cudaError_t e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaMalloc(&h->g.pool, h->pool_bytes);
+    if (e == cudaSuccess) e = cudaMemset(h->g.pool, 0, h->pool_bytes);
+    if (e == cudaSuccess) e = cudaMalloc(&h->dev_status, sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(h->dev_status, 0, sizeof(int));
+    if (e != cudaSuccess) {
+        tsvd_kv4_destroy(h);
+        (void)cudaGetLastError();
+        return e == cudaErrorMemoryAllocation ? TSVD_E_NOMEM : TSVD_E_CUDA;
+    }
+    *out = h;
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long ldk, const void* v, long long ldv, tsvd_dtype_t dtype,
+                                         const int* page_table, int max_pages, const int* seq_len, const int* q_start, int n_seq,
+                                         int n_rows, void* stream)
+{
+    const tsvd_status_t ok = check_batch(h, page_table, max_pages, seq_len, n_seq, n_rows, q_start);
+    if (ok != TSVD_OK) return ok;
+    const long long width = (long long)h->g.heads * h->g.dim;
+    if (ldk < width || ldv < width) return TSVD_E_SHAPE;
+    if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
+    if (n_rows == 0) return TSVD_OK;
+    if (!k || !v) return TSVD_E_NULL;
+    const size_t size = dtype == TSVD_F32 ? 4 : 2;
+    if (((uintptr_t)k | (uintptr_t)v) & (size - 1)) return TSVD_E_ALIGN;
+    const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
+    const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
+    cudaStream_t st = (cudaStream_t)stream;
+    const unsigned t = row_threads(h->g);
+    auto go = [&](auto kernel, auto* kp, auto* vp) { kernel<<<(unsigned)n_rows, t, 0, st>>>(h->g, b, kp, ldk, vp, ldv, h->dev_status); };
+    if (dtype == TSVD_F32) {
+        if (vec) go(kv4_append_kernel<float, true>, (const float*)k, (const float*)v);
+        else go(kv4_append_kernel<float, false>, (const float*)k, (const float*)v);
+    } else {
+        if (vec) go(kv4_append_kernel<__nv_bfloat16, true>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
+        else go(kv4_append_kernel<__nv_bfloat16, false>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
+    }
+    TSVD_CUDA_OK(cudaGetLastError());
+    tsvd_count_launch();
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, void* v, long long ldv, tsvd_dtype_t dtype,
+                                       const int* page_table, int max_pages, const int* seq_len, const int* q_start, int n_seq,
+                                       int n_rows, void* stream)
+{
+    const tsvd_status_t ok = check_batch(h, page_table, max_pages, seq_len, n_seq, n_rows, q_start);
+    if (ok != TSVD_OK) return ok;
+    const long long width = (long long)h->g.heads * h->g.dim;
+    if (ldk < width || ldv < width) return TSVD_E_SHAPE;
+    if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
+    if (n_rows == 0) return TSVD_OK;
+    if (!k || !v) return TSVD_E_NULL;
+    const size_t size = dtype == TSVD_F32 ? 4 : 2;
+    if (((uintptr_t)k | (uintptr_t)v) & (size - 1)) return TSVD_E_ALIGN;
+    const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
+    const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
+    cudaStream_t st = (cudaStream_t)stream;
+    const unsigned t = row_threads(h->g);
+    auto go = [&](auto kernel, auto* kp, auto* vp) { kernel<<<(unsigned)n_rows, t, 0, st>>>(h->g, b, kp, ldk, vp, ldv, h->dev_status); };
+    if (dtype == TSVD_F32) {
+        if (vec) go(kv4_read_kernel<float, true>, (float*)k, (float*)v);
+        else go(kv4_read_kernel<float, false>, (float*)k, (float*)v);
+    } else {
+        if (vec) go(kv4_read_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
+        else go(kv4_read_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
+    }
+    TSVD_CUDA_OK(cudaGetLastError());
+    tsvd_count_launch();
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long ldq, void* out, long long ldo, int n_heads,
+                                         tsvd_dtype_t dtype, const int* page_table, int max_pages, const int* seq_len,
+                                         const int* q_start, int n_seq, int n_rows, int max_q, int max_kv, float scale, int window,
+                                         unsigned flags, void* stream)
+{
+    const tsvd_status_t ok = check_batch(h, page_table, max_pages, seq_len, n_seq, n_rows, q_start);
+    if (ok != TSVD_OK) return ok;
+    if (n_heads < 1 || n_heads % h->g.heads || n_heads > 65535) return TSVD_E_SHAPE;
+    const long long width = (long long)n_heads * h->g.dim;
+    if (ldq < width || ldo < width || max_q < 1 || max_kv < 0 || window < 0 || !(scale == scale)) return TSVD_E_SHAPE;
+    if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
+    if (flags & ~(TSVD_FLAG_CAUSAL | TSVD_FLAG_PATH_SIMPLE)) return TSVD_E_DTYPE;
+    if (n_rows == 0) return TSVD_OK;
+    if (!q || !out) return TSVD_E_NULL;
+    if ((((uintptr_t)q | (uintptr_t)out) & 15) || ldq % 8 || ldo % 8) return TSVD_E_ALIGN;
+    AttendArgs a{};
+    a.h = h;
+    a.b = Kv4Batch{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
+    a.q = q;
+    a.ldq = ldq;
+    a.out = out;
+    a.ldo = ldo;
+    a.n_heads = n_heads;
+    a.dtype = dtype;
+    a.max_q = max_q < n_rows ? max_q : n_rows;
+    const long long room = (long long)max_pages * h->g.page_tokens;
+    a.max_kv = (int)(max_kv && max_kv < room ? max_kv : room < 0x7fffffffLL ? room : 0x7fffffffLL);
+    a.scale = scale;
+    a.window = window;
+    a.causal = flags & TSVD_FLAG_CAUSAL;
+    a.stream = (cudaStream_t)stream;
+    return kv4_attend_simple(a);
+}
+
+extern "C" tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages, size_t* pool_bytes)
+{
+    if (!h) return TSVD_E_NULL;
+    if (n_kv_heads) *n_kv_heads = h->g.heads;
+    if (head_dim) *head_dim = h->g.dim;
+    if (page_tokens) *page_tokens = h->g.page_tokens;
+    if (n_pages) *n_pages = h->g.n_pages;
+    if (pool_bytes) *pool_bytes = h->pool_bytes;
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status_t tsvd_kv4_last_status(tsvd_kv4_t h)
+{
+    if (!h) return TSVD_E_NULL;
+    int word = 0;
+    TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
+    if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));
+    return (word & KV4_DEV_TIMEOUT) ? TSVD_E_TIMEOUT : (word & KV4_DEV_INDEX) ? TSVD_E_INDEX : TSVD_OK;
+}
+
+extern "C" void tsvd_kv4_destroy(tsvd_kv4_t h)
+{
+    if (!h) return;
+    const int dev = h->device;
+    int prev = dev;
+    if (cudaGetDevice(&prev) == cudaSuccess && prev != dev) cudaSetDevice(dev);
+    cudaDeviceSynchronize();
+    if (h->g.pool) cudaFree(h->g.pool);
+    if (h->dev_status) cudaFree(h->dev_status);
+    if (h->parts) cudaFree(h->parts);
+    if (h->tickets) cudaFree(h->tickets);
+    (void)cudaGetLastError();
+    delete h;
+    if (prev != dev) cudaSetDevice(prev);
+}
