@@ -1,102 +1,36 @@
 // 8-bit integers with a scale for each token and channel: quantisation of rows, and the linear layer on them.
 #include <new>
 
+#include "rows8.cuh"
 #include "serving.cuh"
 
 namespace {
 
-constexpr float kSmallest = 7.888609e-31f;   // 2^-100: below it 127 / a is no longer safely finite
-
-// q = rint(x * (127 / a)); 0 for a row without values of any size, the (poisoned) scale says when a is not finite
-__device__ __forceinline__ float inverse_step(float a) { return a >= kSmallest ? __fdiv_rn(127.0f, a) : 0.0f; }
-__device__ __forceinline__ int quantised(float x, float inv) { return __float2int_rn(__fmul_rn(x, inv)); }
-
-// |a| and |b| compared as integers: the larger magnitude, and a NaN (whose bits exceed infinity's) wins over everything
-__device__ __forceinline__ uint32_t max_magnitude(uint32_t m, float v) { return max(m, __float_as_uint(v) & 0x7fffffffu); }
-
-__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* slots)
-{
-    m = __reduce_max_sync(0xffffffffu, m);
-    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = m;
-    __syncthreads();
-    const unsigned n = blockDim.x >> 5;
-    m = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < n ? slots[threadIdx.x & 31] : 0u);
-    __syncthreads();
-    return m;
-}
-
-// A block per row; the row is read twice (the second time from cache).
+// Sixteen columns a thread: 16 bytes of q, 64 (fp32) or 32 (bf16) bytes of y where `wide`.
 template <typename T>
-__global__ void quantize_rows_kernel(const T* __restrict__ x, int cols, long long ldx, int8_t* __restrict__ q, long long ldq,
-                                     float* __restrict__ scale)
+__global__ void dequantize_rows_kernel(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale, int rows, int cols,
+                                       T* __restrict__ y, long long ldy, bool wide)
 {
-    __shared__ uint32_t slots[32];
-    const T* row = x + (long long)blockIdx.x * ldx;
-    uint32_t m = 0;
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) m = max_magnitude(m, to_f32(row[c]));
-    const float a = __uint_as_float(block_max(m, slots));
-    const float inv = inverse_step(a);
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) q[(long long)blockIdx.x * ldq + c] = (int8_t)quantised(to_f32(row[c]), inv);
-    if (threadIdx.x == 0) scale[blockIdx.x] = __fdiv_rn(a, 127.0f);
-}
-
-template <typename T>
-__global__ void dequantize_rows_kernel(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale, int cols,
-                                       T* __restrict__ y, long long ldy)
-{
-    const float s = scale[blockIdx.x];
-    for (int c = threadIdx.x; c < cols; c += blockDim.x)
-        y[(long long)blockIdx.x * ldy + c] = from_f32<T>((float)q[(long long)blockIdx.x * ldq + c] * s);
-}
-
-// Activations into tensor-core order: [block of 128 columns][token group of 8], zeros beyond the last column.
-template <typename T>
-__global__ void stage_rows_kernel(const T* __restrict__ x, int cols, long long ldx, const float* __restrict__ x_scale,
-                                  int col_blocks, int groups, uint8_t* __restrict__ tiles, float* __restrict__ scale)
-{
-    __shared__ uint32_t slots[32];
-    const int b = blockIdx.x;
-    const T* row = x + (long long)b * ldx;
-    float inv = 1.0f, step = 1.0f;
-    if constexpr (sizeof(T) > 1) {
-        uint32_t m = 0;
-        for (int c = threadIdx.x; c < cols; c += blockDim.x) m = max_magnitude(m, to_f32(row[c]));
-        const float a = __uint_as_float(block_max(m, slots));
-        inv = inverse_step(a);
-        step = __fdiv_rn(a, 127.0f);
-    } else {
-        if (x_scale) step = x_scale[b];
-    }
-    for (int c = threadIdx.x; c < col_blocks * 128; c += blockDim.x) {
-        int v = 0;
-        if (c < cols) {
-            if constexpr (sizeof(T) > 1) v = quantised(to_f32(row[c]), inv);
-            else v = row[c];
+    const int units = (cols + 15) / 16;
+    const long long total = (long long)rows * units;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+        const int row = (int)(i / units), c = (int)(i - (long long)row * units) * 16;
+        const float s = scale[row];
+        rows8::Unit<int8_t, false> u;
+        const int8_t* src = q + (long long)row * ldq;
+        T* dst = y + (long long)row * ldy + c;
+        if (wide && c + 16 <= cols) {
+            u.u = __ldg(reinterpret_cast<const uint4*>(src + c));
+            const int8_t* b = reinterpret_cast<const int8_t*>(&u.u);
+            alignas(16) T t[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = from_f32<T>((float)b[e] * s);
+#pragma unroll
+            for (int e = 0; e < (int)sizeof(T); ++e) reinterpret_cast<uint4*>(dst)[e] = reinterpret_cast<uint4*>(t)[e];
+        } else {
+            for (int e = 0; e < 16 && c + e < cols; ++e) dst[e] = from_f32<T>((float)src[c + e] * s);
         }
-        tiles[((size_t)(c >> 7) * groups + (b >> 3)) * 1024 + i8_group_offset(b & 7, c & 127)] = (uint8_t)(int8_t)v;
     }
-    if (threadIdx.x == 0) scale[b] = step;
-}
-
-// Simple product: a block takes 32 channels x 8 tokens, a thread one of each.
-__global__ void i8_product_simple_kernel(const int8_t* __restrict__ W, const uint8_t* __restrict__ xt, const float* __restrict__ xs,
-                                         const float* __restrict__ ws, const float* __restrict__ bias, int M, int B, int col_blocks,
-                                         int groups, void* y, long long ldy, int out_bf16)
-{
-    const int m = blockIdx.x * 32 + threadIdx.x, b = blockIdx.y * 8 + threadIdx.y;
-    if (m >= M || b >= B) return;
-    int sum = 0;
-    for (int kb = 0; kb < col_blocks; ++kb) {
-        const int8_t* w = W + ((size_t)(m >> 7) * col_blocks + kb) * 16384 + (size_t)((m & 127) >> 3) * 1024;
-        const uint8_t* x = xt + ((size_t)kb * groups + (b >> 3)) * 1024;
-        for (int c = 0; c < 128; c += 4)
-            sum = __dp4a(*reinterpret_cast<const int*>(w + i8_group_offset(m & 7, c)),
-                         *reinterpret_cast<const int*>(x + i8_group_offset(b & 7, c)), sum);
-    }
-    float v = (float)sum * xs[b] * ws[m];
-    if (bias) v += bias[m];
-    if (out_bf16) reinterpret_cast<__nv_bfloat16*>(y)[(long long)b * ldy + m] = __float2bfloat16_rn(v);
-    else reinterpret_cast<float*>(y)[(long long)b * ldy + m] = v;
 }
 
 __global__ void i8_tile_weights_kernel(const int8_t* __restrict__ W, long long ldw, int rows, int N, int col_blocks,
@@ -111,8 +45,6 @@ __global__ void i8_tile_weights_kernel(const int8_t* __restrict__ W, long long l
 
 bool misaligned(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
 
-unsigned row_threads(long long cols) { return cols >= 2048 ? 256u : cols >= 512 ? 128u : 64u; }
-
 }  // namespace
 
 extern "C" tsvd_status_t tsvd_quantize(const void* x, tsvd_dtype_t dtype, long long rows, int cols, long long ldx, int8_t* q,
@@ -123,12 +55,8 @@ extern "C" tsvd_status_t tsvd_quantize(const void* x, tsvd_dtype_t dtype, long l
     if (rows == 0) return TSVD_OK;
     if (!x || !q || !scale) return TSVD_E_NULL;
     if (misaligned(x, dtype == TSVD_F32 ? 4 : 2) || misaligned(scale, 4)) return TSVD_E_ALIGN;
-    cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == TSVD_F32)
-        quantize_rows_kernel<float><<<(unsigned)rows, row_threads(cols), 0, st>>>((const float*)x, cols, ldx, q, ldq, scale);
-    else
-        quantize_rows_kernel<__nv_bfloat16><<<(unsigned)rows, row_threads(cols), 0, st>>>((const __nv_bfloat16*)x, cols, ldx, q, ldq, scale);
-    TSVD_CUDA_OK(cudaGetLastError());
+    const rows8::RowMajor out{q, ldq, (((uintptr_t)q) & 15) == 0 && (rows == 1 || ldq % 16 == 0)};
+    TSVD_CUDA_OK(rows8::quantize(x, dtype, (int)rows, cols, ldx, nullptr, out, scale, (cudaStream_t)stream));
     tsvd_count_launch();
     return TSVD_OK;
 }
@@ -142,10 +70,13 @@ extern "C" tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const f
     if (!q || !scale || !y) return TSVD_E_NULL;
     if (misaligned(y, dtype == TSVD_F32 ? 4 : 2) || misaligned(scale, 4)) return TSVD_E_ALIGN;
     cudaStream_t st = (cudaStream_t)stream;
+    const bool wide = (((uintptr_t)q | (uintptr_t)y) & 15) == 0 && (rows == 1 || (ldq % 16 == 0 && ldy * (dtype == TSVD_F32 ? 4 : 2) % 16 == 0));
+    const long long blocks = (rows * ((cols + 15) / 16) + 127) / 128;
+    const unsigned grid = (unsigned)(blocks < 148LL * 64 ? blocks : 148LL * 64);
     if (dtype == TSVD_F32)
-        dequantize_rows_kernel<float><<<(unsigned)rows, row_threads(cols), 0, st>>>(q, ldq, scale, cols, (float*)y, ldy);
+        dequantize_rows_kernel<float><<<grid, 128, 0, st>>>(q, ldq, scale, (int)rows, cols, (float*)y, ldy, wide);
     else
-        dequantize_rows_kernel<__nv_bfloat16><<<(unsigned)rows, row_threads(cols), 0, st>>>(q, ldq, scale, cols, (__nv_bfloat16*)y, ldy);
+        dequantize_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(q, ldq, scale, (int)rows, cols, (__nv_bfloat16*)y, ldy, wide);
     TSVD_CUDA_OK(cudaGetLastError());
     tsvd_count_launch();
     return TSVD_OK;
@@ -216,9 +147,11 @@ extern "C" tsvd_status_t tsvd_i8_pack(const int8_t* W, long long ldw, const floa
     h->device = dev;
     h->M = M;
     h->N = N;
+    if (cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { (void)cudaGetLastError(); delete h; return TSVD_E_CUDA; }
     h->row_tiles = (M + 127) / 128;
     h->col_blocks = (N + 127) / 128;
-    const tsvd_status_t st = i8_fill(h, W, ldw, w_scale, bias);
+    tsvd_status_t st = i8_fill(h, W, ldw, w_scale, bias);
+    if (st == TSVD_OK) st = i8_product_prepare();
     if (st != TSVD_OK) { i8_free(h); return st; }
     *out = h;
     return TSVD_OK;
@@ -226,8 +159,8 @@ extern "C" tsvd_status_t tsvd_i8_pack(const int8_t* W, long long ldw, const floa
 
 static size_t i8_ws_bytes(const tsvd_i8_s* h, int B)
 {
-    const size_t padded = ((size_t)B + 255) / 256 * 256;
-    return padded * ((size_t)h->col_blocks * 128 + sizeof(float));
+    const size_t groups = ((size_t)B + 7) / 8;
+    return groups * 8 * ((size_t)h->col_blocks * 128 + sizeof(float));
 }
 
 static tsvd_status_t i8_grow(tsvd_i8_s* h, int B)
@@ -237,7 +170,6 @@ static tsvd_status_t i8_grow(tsvd_i8_s* h, int B)
     TSVD_CUDA_OK(cudaDeviceSynchronize());
     if (h->ws) { cudaFree(h->ws); h->ws = nullptr; h->ws_bytes = 0; }
     TSVD_CUDA_OK(cudaMalloc(&h->ws, need));
-    TSVD_CUDA_OK(cudaMemset(h->ws, 0, need));
     h->ws_bytes = need;
     return TSVD_OK;
 }
@@ -265,22 +197,12 @@ extern "C" tsvd_status_t tsvd_i8_forward(tsvd_i8_t h, const void* x, long long l
         return TSVD_E_ALIGN;
     const tsvd_status_t grown = i8_grow(h, B);
     if (grown != TSVD_OK) return grown;
-    cudaStream_t st = (cudaStream_t)stream;
-    const int groups = (B + 255) / 256 * 32;
-    float* xs = reinterpret_cast<float*>(h->ws + (size_t)groups * 8 * h->col_blocks * 128);
-    const unsigned threads = row_threads((long long)h->col_blocks * 128);
-    if (dtype == TSVD_F32)
-        stage_rows_kernel<float><<<(unsigned)B, threads, 0, st>>>((const float*)x, h->N, ldx, nullptr, h->col_blocks, groups, h->ws, xs);
-    else if (dtype == TSVD_BF16)
-        stage_rows_kernel<__nv_bfloat16><<<(unsigned)B, threads, 0, st>>>((const __nv_bfloat16*)x, h->N, ldx, nullptr, h->col_blocks, groups, h->ws, xs);
-    else
-        stage_rows_kernel<int8_t><<<(unsigned)B, threads, 0, st>>>((const int8_t*)x, h->N, ldx, x_scale, h->col_blocks, groups, h->ws, xs);
-    TSVD_CUDA_OK(cudaGetLastError());
-    i8_product_simple_kernel<<<dim3((unsigned)(h->M + 31) / 32, (unsigned)(B + 7) / 8), dim3(32, 8), 0, st>>>(
-        h->W, h->ws, xs, h->w_scale, h->bias, h->M, B, h->col_blocks, groups, y, ldy, y_bf16);
-    TSVD_CUDA_OK(cudaGetLastError());
-    tsvd_count_launch(2);
-    return TSVD_OK;
+    const int groups = (B + 7) / 8;
+    float* xs = reinterpret_cast<float*>(h->ws + (size_t)groups * 1024 * h->col_blocks);
+    const rows8::Tiles out{h->ws, groups};
+    TSVD_CUDA_OK(rows8::quantize(x, dtype, B, h->N, ldx, x_scale, out, xs, (cudaStream_t)stream));
+    tsvd_count_launch();
+    return i8_product(h, h->ws, xs, B, y, ldy, y_bf16, (cudaStream_t)stream);
 }
 
 extern "C" tsvd_status_t tsvd_i8_info(tsvd_i8_t h, int* M, int* N, size_t* packed_bytes)

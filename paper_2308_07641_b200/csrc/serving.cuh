@@ -23,6 +23,7 @@ __host__ __device__ inline size_t i8_group_offset(int row_in_group, int col_in_b
 
 struct tsvd_i8_s {
     int device = 0;
+    int sms = 0;
     int M = 0, N = 0;
     int row_tiles = 0, col_blocks = 0;   // 128 each
     int8_t* W = nullptr;                 // device, row_tiles * col_blocks * 16 KiB
@@ -32,6 +33,10 @@ struct tsvd_i8_s {
     size_t ws_bytes = 0;
     int* dev_status = nullptr;
 };
+
+// i8_mma.cu: the product of B tokens in tensor-core order (x, then their scales) with the handle's weights
+tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, cudaStream_t st);
+tsvd_status_t i8_product_prepare();   // once for the current device, before the first product
 
 // ---- the 4-bit cache ------------------------------------------------------------------------------------------------
 // A page is [kv head][block of 16 positions], a block 20 * head_dim bytes:
