@@ -183,6 +183,11 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     if (e == cudaSuccess) e = cudaMemset(h->g.pool, 0, h->pool_bytes);
     if (e == cudaSuccess) e = cudaMalloc(&h->dev_status, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(h->dev_status, 0, sizeof(int));
+    const size_t tickets = kv4_decode_tickets(h->sms) * sizeof(unsigned);
+    if (e == cudaSuccess) e = cudaMalloc(&h->parts, kv4_decode_parts_bytes(h->sms, head_dim));
+    if (e == cudaSuccess) e = cudaMalloc(&h->tickets, tickets);
+    if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, tickets);
+    if (e == cudaSuccess && kv4_decode_prepare() != TSVD_OK) e = cudaErrorUnknown;
     if (e != cudaSuccess) {
         tsvd_kv4_destroy(h);
         (void)cudaGetLastError();
@@ -283,7 +288,8 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     a.window = window;
     a.causal = flags & TSVD_FLAG_CAUSAL;
     a.stream = (cudaStream_t)stream;
-    return kv4_attend_simple(a);
+    if (dtype == TSVD_F32 || (flags & TSVD_FLAG_PATH_SIMPLE)) return kv4_attend_simple(a);
+    return kv4_attend_decode(a);
 }
 
 extern "C" tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages, size_t* pool_bytes)
@@ -303,6 +309,7 @@ extern "C" tsvd_status_t tsvd_kv4_last_status(tsvd_kv4_t h)
     int word = 0;
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));
+    if (word & KV4_DEV_TIMEOUT) TSVD_CUDA_OK(cudaMemset(h->tickets, 0, kv4_decode_tickets(h->sms) * sizeof(unsigned)));
     return (word & KV4_DEV_TIMEOUT) ? TSVD_E_TIMEOUT : (word & KV4_DEV_INDEX) ? TSVD_E_INDEX : TSVD_OK;
 }
 

@@ -123,4 +123,8 @@ struct AttendArgs {
     bool causal;
     cudaStream_t stream;
 };
-tsvd_status_t kv4_attend_simple(const AttendArgs& a);
+tsvd_status_t kv4_attend_simple(const AttendArgs& a);   // kv4_simple.cu
+tsvd_status_t kv4_attend_decode(const AttendArgs& a);   // kv4_decode.cu: few rows, bf16
+tsvd_status_t kv4_decode_prepare();                     // once for the current device
+size_t kv4_decode_parts_bytes(int sms, int dim);        // its scratch
+size_t kv4_decode_tickets(int sms);

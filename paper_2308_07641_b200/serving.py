@@ -24,40 +24,43 @@ def _code(dtype, what: str) -> int:
 
 
 def _stream(x) -> int:
-    import torch
-    return torch.cuda.current_stream(x.device).cuda_stream
+    """torch's current stream on x's device (the raw value: a Stream object costs 2 us to make)."""
+    from torch._C import _cuda_getCurrentRawStream
+    return _cuda_getCurrentRawStream(x.get_device())
 
 
 def _rows(x, what: str):
-    """A CUDA tensor [rows, cols] with contiguous rows; returns its row stride."""
-    if not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+    """A CUDA tensor [rows, cols] with contiguous rows; returns (rows, cols, row stride)."""
+    if not x.is_cuda or x.dim() != 2:
         raise TSVDError(binding.TSVD_E_SHAPE, what)
-    return max(x.stride(0), x.shape[1])
+    rows, cols = x.shape
+    ld, one = x.stride()
+    if one != 1 and cols > 1:
+        raise TSVDError(binding.TSVD_E_SHAPE, what)
+    return rows, cols, ld if ld > cols else cols
 
 
 def quantize(x):
     """8-bit integers with one scale per row: x float32 or bfloat16 [rows, cols] (row stride >= cols) ->
     (q int8 [rows, cols], its rows 16-byte aligned; scale float32 [rows]); x is about q * scale[:, None]."""
     import torch
-    ldx = _rows(x, "quantize")
-    rows, cols = x.shape
+    rows, cols, ldx = _rows(x, "quantize")
     ldq = (cols + 15) & ~15
-    q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    q = torch.empty_strided((rows, cols), (ldq, 1), dtype=torch.int8, device=x.device)
+    scale = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=x.device)
     binding.tsvd_quantize(x.data_ptr(), _code(x.dtype, "quantize"), rows, cols, ldx, q.data_ptr(), ldq, scale.data_ptr(), _stream(x))
-    return q[:, :cols] if ldq != cols else q, scale
+    return q, scale
 
 
 def dequantize(q, scale, dtype=None):
     """q * scale[:, None] as float32 (default) or bfloat16."""
     import torch
-    ldq = _rows(q, "dequantize")
+    rows, cols, ldq = _rows(q, "dequantize")
     if q.dtype != torch.int8 or scale.dtype != torch.float32:
         raise TSVDError(binding.TSVD_E_DTYPE, "dequantize")
-    rows, cols = q.shape
     if scale.shape != (rows,) or not scale.is_cuda or not scale.is_contiguous():
         raise TSVDError(binding.TSVD_E_SHAPE, "dequantize")
-    y = torch.empty((rows, cols), dtype=dtype or torch.float32, device=q.device)
+    y = torch.empty_strided((rows, cols), (cols, 1), dtype=dtype or torch.float32, device=q.device)
     binding.tsvd_dequantize(q.data_ptr(), ldq, scale.data_ptr(), rows, cols, y.data_ptr(), _code(y.dtype, "dequantize"), cols, _stream(q))
     return y
 
@@ -87,21 +90,26 @@ class Int8Linear:
         """x: CUDA tensor [B, N], row stride >= N: float32 or bfloat16 (quantised on the way), or int8 with x_scale
         float32 [B] (None: ones).  Returns [B, M]: bfloat16 for bfloat16 x, else float32, unless flags say otherwise."""
         import torch
-        ldx = _rows(x, "Int8Linear.forward")
-        B = x.shape[0]
+        B, N, ldx = _rows(x, "Int8Linear.forward")
         dt = _code(x.dtype, "Int8Linear.forward")
-        if x.shape[1] != self.N or (x_scale is not None and (x_scale.shape != (B,) or not x_scale.is_contiguous() or not x_scale.is_cuda)):
+        if N != self.N:
             raise TSVDError(binding.TSVD_E_SHAPE, "Int8Linear.forward")
-        if x_scale is not None and x_scale.dtype != torch.float32:
-            raise TSVDError(binding.TSVD_E_DTYPE, "Int8Linear.forward")
+        if x_scale is not None:
+            if x_scale.shape != (B,) or not x_scale.is_contiguous() or not x_scale.is_cuda:
+                raise TSVDError(binding.TSVD_E_SHAPE, "Int8Linear.forward")
+            if x_scale.dtype != torch.float32:
+                raise TSVDError(binding.TSVD_E_DTYPE, "Int8Linear.forward")
         want = torch.bfloat16 if (flags & binding.TSVD_FLAG_OUT_BF16 or (dt == TSVD_BF16 and not flags & binding.TSVD_FLAG_OUT_F32)) \
             else torch.float32
+        ldy = self.M
         if out is None:
-            out = torch.empty((B, self.M), dtype=want, device=x.device)
-        elif out.dtype != want or out.shape != (B, self.M):
+            out = torch.empty_strided((B, ldy), (ldy, 1), dtype=want, device=x.device)
+        elif out.dtype != want or out.shape != (B, ldy):
             raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != want else binding.TSVD_E_SHAPE, "Int8Linear.forward")
+        else:
+            ldy = _rows(out, "Int8Linear.forward")[2]
         binding.tsvd_i8_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else 0, out.data_ptr(),
-                                _rows(out, "Int8Linear.forward"), B, dt, flags, _stream(x))
+                                ldy, B, dt, flags, _stream(x))
         return out
 
     __call__ = forward
@@ -132,42 +140,52 @@ class KV4Cache:
         self.handle = binding.tsvd_kv4_create(n_kv_heads, head_dim, page_tokens, n_pages)
         self.n_kv_heads, self.head_dim, self.n_pages, self.page_tokens = n_kv_heads, head_dim, n_pages, page_tokens
 
-    def _heads(self, x, heads: int, what: str) -> int:
-        """A CUDA tensor [rows, heads, head_dim] whose rows lie in one piece; returns the row stride."""
-        if not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or x.stride(2) != 1 or (
-                heads > 1 and x.stride(1) != self.head_dim):
+    def _heads(self, x, what: str):
+        """A CUDA tensor [rows, heads, head_dim] whose rows lie in one piece; returns (rows, heads, row stride)."""
+        if not x.is_cuda or x.dim() != 3:
             raise TSVDError(binding.TSVD_E_SHAPE, what)
-        return max(x.stride(0), heads * self.head_dim)
+        rows, heads, dim = x.shape
+        ld, per_head, one = x.stride()
+        if dim != self.head_dim or one != 1 or (heads > 1 and per_head != dim):
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        return rows, heads, ld if ld > heads * dim else heads * dim
 
     def _batch(self, page_table, seq_len, q_start, rows: int, what: str):
         import torch
-        for t in (page_table, seq_len) + ((q_start,) if q_start is not None else ()):
-            if t.dtype != torch.int32:
-                raise TSVDError(binding.TSVD_E_DTYPE, what)
-            if not t.is_cuda or not t.is_contiguous():
-                raise TSVDError(binding.TSVD_E_SHAPE, what)
-        if page_table.dim() != 2 or seq_len.shape != (page_table.shape[0],) or (
-                q_start is not None and q_start.shape != (page_table.shape[0] + 1,)):
+        int32 = torch.int32
+        if page_table.dtype != int32 or seq_len.dtype != int32 or (q_start is not None and q_start.dtype != int32):
+            raise TSVDError(binding.TSVD_E_DTYPE, what)
+        if page_table.dim() != 2 or seq_len.dim() != 1 or not (page_table.is_cuda and seq_len.is_cuda) or not (
+                page_table.is_contiguous() and seq_len.is_contiguous()):
             raise TSVDError(binding.TSVD_E_SHAPE, what)
         n_seq, max_pages = page_table.shape
-        return (page_table.data_ptr(), max_pages, seq_len.data_ptr(), q_start.data_ptr() if q_start is not None else 0, n_seq, rows)
+        if seq_len.shape[0] != n_seq:
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        start = 0
+        if q_start is not None:
+            if q_start.dim() != 1 or q_start.shape[0] != n_seq + 1 or not q_start.is_cuda or not q_start.is_contiguous():
+                raise TSVDError(binding.TSVD_E_SHAPE, what)
+            start = q_start.data_ptr()
+        return page_table.data_ptr(), max_pages, seq_len.data_ptr(), start, n_seq, rows
 
     def append(self, k, v, page_table, seq_len, q_start=None) -> None:
         """Put k, v [rows, n_kv_heads, head_dim] (float32 or bfloat16) at the last positions of their sequences."""
         if k.dtype != v.dtype or k.shape != v.shape:
             raise TSVDError(binding.TSVD_E_DTYPE if k.dtype != v.dtype else binding.TSVD_E_SHAPE, "KV4Cache.append")
-        ldk, ldv = self._heads(k, self.n_kv_heads, "KV4Cache.append"), self._heads(v, self.n_kv_heads, "KV4Cache.append")
-        batch = self._batch(page_table, seq_len, q_start, k.shape[0], "KV4Cache.append")
+        (rows, heads, ldk), (_, _, ldv) = self._heads(k, "KV4Cache.append"), self._heads(v, "KV4Cache.append")
+        if heads != self.n_kv_heads:
+            raise TSVDError(binding.TSVD_E_SHAPE, "KV4Cache.append")
+        batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.append")
         binding.tsvd_kv4_append(self.handle, k.data_ptr(), ldk, v.data_ptr(), ldv, _code(k.dtype, "KV4Cache.append"), *batch, _stream(k))
 
     def read(self, rows: int, page_table, seq_len, q_start=None, dtype=None):
         """(k, v) [rows, n_kv_heads, head_dim] as the cache holds them: float32 (default) or bfloat16."""
         import torch
-        shape = (rows, self.n_kv_heads, self.head_dim)
-        k = torch.empty(shape, dtype=dtype or torch.float32, device=seq_len.device)
-        v = torch.empty_like(k)
-        batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.read")
         ld = self.n_kv_heads * self.head_dim
+        shape, strides = (rows, self.n_kv_heads, self.head_dim), (ld, self.head_dim, 1)
+        k = torch.empty_strided(shape, strides, dtype=dtype or torch.float32, device=seq_len.device)
+        v = torch.empty_strided(shape, strides, dtype=k.dtype, device=k.device)
+        batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.read")
         binding.tsvd_kv4_read(self.handle, k.data_ptr(), ld, v.data_ptr(), ld, _code(k.dtype, "KV4Cache.read"), *batch, _stream(k))
         return k, v
 
@@ -177,16 +195,17 @@ class KV4Cache:
         last positions of their sequences (append their keys first).  max_q, max_kv: bounds on the rows and the positions
         of one sequence, where the caller knows them.  Returns a tensor like q."""
         import torch
-        n_heads = q.shape[1] if q.dim() == 3 else 0
-        ldq = self._heads(q, n_heads, "KV4Cache.attend")
-        batch = self._batch(page_table, seq_len, q_start, q.shape[0], "KV4Cache.attend")
+        rows, n_heads, ldq = self._heads(q, "KV4Cache.attend")
+        batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.attend")
         if max_q is None:
-            max_q = 1 if q_start is None else max(1, q.shape[0])
+            max_q = 1 if q_start is None else max(1, rows)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            ldo = n_heads * self.head_dim
+            out = torch.empty_strided((rows, n_heads, self.head_dim), (ldo, self.head_dim, 1), dtype=q.dtype, device=q.device)
         elif out.dtype != q.dtype or out.shape != q.shape:
             raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != q.dtype else binding.TSVD_E_SHAPE, "KV4Cache.attend")
-        ldo = self._heads(out, n_heads, "KV4Cache.attend")
+        else:
+            ldo = self._heads(out, "KV4Cache.attend")[2]
         if scale is None:
             scale = 1.0 / math.sqrt(self.head_dim)
         if causal:
