@@ -449,6 +449,8 @@ def test_attend_sharp_and_flat_softmax(new):
     b = Batch([777], 2, 128, 64, seed=4)
     b.check(4, [new], qmul=40.0)
     b.check(4, [new], qmul=0.0)
+    b.check(4, [new], scale=0.0, window=300)
+    b.check(4, [new], qmul=1e-30)
 
 
 @pytest.mark.parametrize("new", [1, 200])
