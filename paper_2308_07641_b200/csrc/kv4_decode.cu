@@ -3,11 +3,13 @@
 //     out = sum_j p_j v_j / sum_j p_j,   p_j = exp2(c q.k_j - ref),   c = scale log2(e)
 //
 // Work.  An item is (sequence, key/value head, group of 8 NT query rows: the heads that share the key/value head, of one
-// or several tokens); its unit is a block of 16 cached positions.  All units of the call, item after item, are cut into
-// equal runs, one for each block of a persistent grid, so ragged batches and single long sequences spread alike.  A block's
-// eight warps take the run's units in turn; each warp has its own ring of units in shared memory, filled by bulk copies
-// that run ahead across item borders.  At an item's end the warps' sums meet in shared memory; an item that spans blocks
-// leaves its parts in scratch, and the block that finishes last adds them in their order (so results do not depend on it).
+// or several tokens); its unit is two blocks of 16 cached positions.  All units of the call, item after item, are cut into
+// equal runs, one for each warp of a persistent grid, so ragged batches and single long sequences spread alike, and no warp
+// waits for another until its run is done.  Each warp keeps a ring of units in shared memory that it fills by bulk copies,
+// ahead across item borders.  A warp writes the items that lie in its run; of one that reaches beyond it, at either end, it
+// keeps its part.  At the end the block adds its warps' parts; what still lacks other blocks' parts goes to scratch, and the
+// block that finishes last adds those in their order (so results do not depend on it).  Few short items get a block each
+// instead, which saves that last step.
 //
 // Arithmetic.  mma.sync m16n8k16 in fp16 with fp32 sums, the cached side as the 16-row operand, the query rows as the
 // 8-column one.  Scores use the codes as they are: a mask and an or make fp16 pairs 1024 + code, or 1024 + 16 code for the
@@ -25,9 +27,13 @@ namespace {
 
 using namespace ptx;
 
-constexpr int DEC_WARPS = 7;             // warps that compute; one more feeds their rings
-constexpr int DEC_THREADS = (DEC_WARPS + 1) * 32;
-constexpr int DEC_QUEUE = 4;             // items that the feeding warp may be ahead
+constexpr int DEC_MAX_STAGES = 6;
+constexpr int DEC_QUEUE = 8;             // items that the copies may be ahead: more than DEC_MAX_STAGES
+constexpr int DEC_APART = 6;             // units a warp up to which items get a block each: a step over scratch costs as much
+constexpr int DEC_STATIC = 13 * 1024;    // room for what the kernel declares
+constexpr int DEC_WARPS = 8;             // two on each quarter of an SM: up to 255 registers a thread
+constexpr int DEC_UNIT = 2 * KV4_BLOCK;  // positions of a unit
+
 constexpr float kSlack = 8.0f;           // how far (log2) a score may pass the reference before it moves
 constexpr float kNone = -1e30f;          // the reference before the first score
 
@@ -42,13 +48,21 @@ struct DecParams {
     int max_q;
     float c;             // scale * log2(e)
     int window, causal;
-    int min_share;       // units of a run at least
+    int stages;          // units of a warp's ring
+    int keep_cols;       // query rows of an item that can hold anything: what is kept of a part
     float* parts;        // [grid][2][rows][D + 2]
     unsigned* tickets;   // [grid]
     int* status;
+    int sms;
 };
 
-__device__ __forceinline__ uint32_t lop_or(uint32_t x, uint32_t mask) { return (x & mask) | 0x64006400u; }
+// (x & mask) | 0x64006400 in one instruction
+__device__ __forceinline__ uint32_t lop_or(uint32_t x, uint32_t mask)
+{
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(0x64006400u));
+    return y;
+}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -79,27 +93,12 @@ __device__ __forceinline__ float ex2(float x)
 }
 __device__ __forceinline__ float2 halves(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
-__device__ __forceinline__ void warps_sync() { asm volatile("bar.sync 1, %0;" ::"n"(DEC_WARPS * 32) : "memory"); }
-__device__ __forceinline__ bool any_of_the_warps(bool x)
-{
-    uint32_t y;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.red.or.pred q, 1, %2, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(y)
-        : "r"((uint32_t)x), "n"(DEC_WARPS * 32)
-        : "memory");
-    return y != 0;
-}
-
 template <int WORDS>
 struct alignas(4 * WORDS) Words { uint32_t w[WORDS]; };
 
-// What one sequence brings (the lanes of the feeding warp hold 32 sequences, one each).
+// What one sequence brings.
 struct Seq {
-    int rows, len, first, items, blk0, units;   // units of one item; blk0: its first block
+    int rows, len, first, items, unit0, units;  // units of one item; unit0: its first, counted from position 0
     int all;                                    // its rows, those beyond max_q (which are not computed) included
 };
 
@@ -110,8 +109,8 @@ __device__ __forceinline__ Seq load_seq(const DecParams& p, int s)
     if (s >= p.b.n_seq) return q;
     q.first = kv4_first_row(p.b, s);
     q.all = kv4_first_row(p.b, s + 1) - q.first;
-    q.rows = min(q.all, p.max_q);
-    if (q.rows <= 0) { q.rows = 0; return q; }
+    q.rows = min(min(q.all, p.max_q), p.b.n_rows - q.first);
+    if (q.rows <= 0 || q.first < 0) { q.rows = 0; return q; }
     q.len = p.b.seq_len[s];
     const long long room = (long long)p.b.max_pages * p.g.page_tokens;
     const long long seen = q.len < 0 ? 0 : min((long long)q.len, room);
@@ -121,67 +120,87 @@ __device__ __forceinline__ Seq load_seq(const DecParams& p, int s)
     if (p.window) lo = max(0LL, pos0 - p.window + 1);
     if (p.causal) hi = min(hi, pos0 + q.rows);
     q.items = p.g.heads * ((q.rows * p.group + ROWS - 1) / ROWS);
-    q.blk0 = (int)(lo / KV4_BLOCK);
-    q.units = hi > lo ? (int)((hi + KV4_BLOCK - 1) / KV4_BLOCK) - q.blk0 : 1;   // an item that sees nothing still writes zeros
+    q.unit0 = (int)(lo / DEC_UNIT);
+    q.units = hi > lo ? (int)((hi + DEC_UNIT - 1) / DEC_UNIT) - q.unit0 : 1;   // an item that sees nothing still writes zeros
     return q;
 }
 
-// An item as the computing warps get it.
+// A warp's share of an item.
 struct Item {
     int first_row, n_rows;     // of the call; (row, head) pairs of the item's sequence and head in all
     int head, row0;            // the pairs row0 .. are this item's
     int len, pos0;             // positions that can be seen at all; position of the sequence's first row
-    int blk0, unit0, unit1, units;
-    int b_first, b_last;       // the blocks of the grid that share it
+    int at0, unit0, unit1, units;    // position of its unit 0; units [unit0, unit1) of `units` are the warp's
+    long long u0;              // where the item begins in the call's list of units
 };
 
-template <int D, int NT, int STAGES>
-__global__ void __launch_bounds__(DEC_THREADS, NT == 1 ? 2 : 1)
+// The run behind a warp's copies (what changes with every unit is in registers).
+struct Feed {
+    int s, item, page_at;
+    Seq q;
+    long long item_u0, u1;
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(DEC_WARPS * 32, 1)
 kv4_decode_kernel(const DecParams p)
 {
-    constexpr int ROWS = 8 * NT, W = D / KV4_GROUP, UNIT = 20 * D, VW = D / 64;   // VW: words of value codes per thread and key
+    constexpr int WARPS = DEC_WARPS;
+    constexpr int ROWS = 8 * NT, W = D / KV4_GROUP, BLOCK = 20 * D, UNIT = 2 * BLOCK;
+    constexpr int VW = D / 64;   // words of value codes per thread and key
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 127) & ~(uintptr_t)127);
-    float* meet = reinterpret_cast<float*>(ring + DEC_WARPS * STAGES * UNIT);       // [warps][ROWS][D]
-    __shared__ uint64_t full[DEC_WARPS][STAGES], empty[DEC_WARPS][STAGES], item_full[DEC_QUEUE], item_empty[DEC_QUEUE];
-    __shared__ uint8_t there[DEC_WARPS][STAGES];
-    __shared__ Item queue[DEC_QUEUE];
-    __shared__ float ref_2[2][DEC_WARPS][ROWS], sum_2[2][DEC_WARPS][ROWS];   // one pair is read while the next item's is written
+    float* heads_kept = reinterpret_cast<float*>(ring + (size_t)WARPS * p.stages * UNIT);   // [warps][keep_cols][D]
+    __shared__ uint64_t full[WARPS][DEC_MAX_STAGES];
+    __shared__ uint8_t there[WARPS][DEC_MAX_STAGES];
+    __shared__ Item queue[WARPS][DEC_QUEUE];
+    __shared__ Feed feeds[WARPS];
+    // What a warp keeps of an item that began before its run (0; the numbers in heads_kept) or ends after it (1; the numbers
+    // in the warp's own ring, which is then idle).
+    __shared__ float kept_ref[2][WARPS][ROWS], kept_sum[2][WARPS][ROWS];
+    __shared__ Item kept[2][WARPS];
     __shared__ int ctl_[2];
     __shared__ unsigned last_s;
     volatile int* ctl = ctl_;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
 
-    if (threadIdx.x == 0) {
-        ctl[0] = 0;
-        ctl[1] = kWaitLimitDefault;
-        for (int w = 0; w < DEC_WARPS; ++w)
-            for (int i = 0; i < STAGES; ++i) { mbar_init(&full[w][i], 1); mbar_init(&empty[w][i], 1); }
-        for (int i = 0; i < DEC_QUEUE; ++i) { mbar_init(&item_full[i], 1); mbar_init(&item_empty[i], DEC_WARPS); }
+    if (threadIdx.x == 0) { ctl[0] = 0; ctl[1] = kWaitLimitDefault; }
+    if (threadIdx.x < WARPS) {
+        for (int i = 0; i < p.stages; ++i) mbar_init(&full[threadIdx.x][i], 1);
+        kept[0][threadIdx.x].units = kept[1][threadIdx.x].units = 0;
         fence_mbar_init();
     }
     __syncthreads();
     pdl_launch_dependents();
     pdl_wait();
 
-    if (warp == DEC_WARPS) {
-        // ================= the feeding warp: the block's run of units, item by item =================
-        long long total = 0;
-        for (int s0 = 0; s0 < p.b.n_seq; s0 += 32) {
-            const Seq q = load_seq<ROWS>(p, s0 + lane);
-            total += (long long)q.items * q.units;
-        }
-        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)p.min_share);
-        const long long u0 = share * blockIdx.x, u1 = min(u0 + share, total);
-        int q_at = 0;
-        uint32_t q_phase = 0;
-        if (u0 < u1) {
-            int base = 0, s = 0, item = 0, unit = 0;     // base: the sequences that the lanes hold
-            long long item_u0 = 0;                       // where the item begins in the call's list of units
-            Seq mine = load_seq<ROWS>(p, lane);
-            for (long long before = 0;;) {
-                const long long n = (long long)mine.items * mine.units;
+    // ---- the warp's run of units ----
+    long long total = 0;
+    int total_items = 0, most = 0;
+    Seq mine = load_seq<ROWS>(p, lane);
+    for (int s0 = 0;; mine = load_seq<ROWS>(p, s0 + lane)) {
+        total += (long long)mine.items * mine.units;
+        total_items += mine.items;
+        most = max(most, mine.units);
+        s0 += 32;
+        if (s0 >= p.b.n_seq) break;
+    }
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    total_items = __reduce_add_sync(0xffffffffu, total_items);
+    most = __reduce_max_sync(0xffffffffu, most);
+    const bool apart = total_items <= (int)gridDim.x && most <= DEC_APART * WARPS;
+    const long long runs = (long long)gridDim.x * WARPS;
+    const long long run = apart ? (most + WARPS - 1) / WARPS : max((total + runs - 1) / runs, 2LL), share = run * WARPS;
+    if (apart) total = share * total_items;                    // a block's share for each item, whatever its length
+    Feed& f = feeds[warp];
+    {
+        const long long u0 = run * ((long long)blockIdx.x * WARPS + warp), u1 = min(u0 + run, total);
+        long long before = 0;
+        if (p.b.n_seq > 32) mine = load_seq<ROWS>(p, lane);
+        if (u0 < u1)
+            for (int s0 = 0; s0 < p.b.n_seq; mine = load_seq<ROWS>(p, s0 + lane)) {
+                const int span = apart ? (int)share : mine.units;
+                const long long n = (long long)mine.items * span;
                 long long scan = n;
                 for (int o = 1; o < 32; o <<= 1) {
                     const long long v = __shfl_up_sync(0xffffffffu, scan, o);
@@ -189,116 +208,121 @@ kv4_decode_kernel(const DecParams p)
                 }
                 const unsigned holds = __ballot_sync(0xffffffffu, before + scan > u0);
                 if (holds) {
-                    const int l = __ffs(holds) - 1;
-                    const long long start = before + __shfl_sync(0xffffffffu, scan - n, l);
-                    const int units = __shfl_sync(0xffffffffu, mine.units, l);
-                    s = base + l;
-                    item = (int)((u0 - start) / units);
-                    unit = (int)((u0 - start) % units);
-                    item_u0 = u0 - unit;
+                    if (lane == __ffs(holds) - 1) {
+                        const unsigned in = (unsigned)(u0 - before - (scan - n));
+                        f.s = s0 + lane;
+                        f.item = (int)(in / (unsigned)span) - 1;          // the step to the first item adds one
+                        f.q = mine;
+                        f.item_u0 = u0 - in % (unsigned)span - span;
+                    }
                     break;
                 }
                 before += __shfl_sync(0xffffffffu, scan, 31);
-                base += 32;
-                mine = load_seq<ROWS>(p, base + lane);
+                s0 += 32;
             }
-            const int per_page = p.g.page_tokens / KV4_BLOCK;
-            int stage = 0;                               // of the ring that this lane feeds
-            uint32_t phase = 0;
-            bool ok = true;
-            while (ok) {
-                const int who = s - base;
-                const int units = __shfl_sync(0xffffffffu, mine.units, who), items = __shfl_sync(0xffffffffu, mine.items, who);
-                const int blk0 = __shfl_sync(0xffffffffu, mine.blk0, who), len = __shfl_sync(0xffffffffu, mine.len, who);
-                const int rows = __shfl_sync(0xffffffffu, mine.rows, who), first = __shfl_sync(0xffffffffu, mine.first, who);
-                const int all = __shfl_sync(0xffffffffu, mine.all, who);
-                const int unit1 = (int)min((long long)units, u1 - item_u0), head = item % p.g.heads;
-                if (lane == 0) {
-                    ok = mbar_wait(&item_empty[q_at], q_phase ^ 1, ctl);
-                    if (ok) {
-                        Item it;
-                        it.first_row = first;
-                        it.n_rows = rows * p.group;
-                        it.head = head;
-                        it.row0 = item / p.g.heads * ROWS;
-                        it.len = (int)max(0LL, min((long long)len, (long long)p.b.max_pages * p.g.page_tokens));
-                        it.pos0 = len - all;
-                        it.blk0 = blk0;
-                        it.unit0 = unit;
-                        it.unit1 = unit1;
-                        it.units = units;
-                        it.b_first = (int)(item_u0 / share);
-                        it.b_last = (int)((item_u0 + units - 1) / share);
-                        queue[q_at] = it;
-                        mbar_arrive(&item_full[q_at]);
-                    }
-                }
-                if (!__shfl_sync(0xffffffffu, ok, 0)) break;
-                if (++q_at == DEC_QUEUE) { q_at = 0; q_phase ^= 1; }
-                // lane w: units unit + w, + DEC_WARPS, ... into the ring of warp w; a page number is asked for one turn ahead
-                auto page_of = [&](int u) {
-                    const int blk = blk0 + u;
-                    if (u >= unit1 || (long long)blk * KV4_BLOCK >= len || blk / per_page >= p.b.max_pages) return -2;   // no such position
-                    return p.b.table[(long long)s * p.b.max_pages + blk / per_page];
-                };
-                if (lane < DEC_WARPS) {
-                    int page = page_of(unit + lane);
-                    for (int u = unit + lane; u < unit1; u += DEC_WARPS) {
-                        const int next = page_of(u + DEC_WARPS);
-                        if (!mbar_wait(&empty[lane][stage], phase ^ 1, ctl)) { ok = false; break; }
-                        const bool in = page >= 0 && page < p.g.n_pages;
-                        there[lane][stage] = in;
-                        if (in) {
-                            mbar_arrive_expect_tx(&full[lane][stage], UNIT);
-                            bulk_g2s(ring + (lane * STAGES + stage) * UNIT, p.g.block(page, head, (blk0 + u) % per_page * KV4_BLOCK), UNIT,
-                                     &full[lane][stage]);
-                        } else {
-                            if (page != -2) atomicOr(p.status, KV4_DEV_INDEX);
-                            mbar_arrive(&full[lane][stage]);
-                        }
-                        page = next;
-                        if (++stage == STAGES) { stage = 0; phase ^= 1; }
-                    }
-                }
-                ok = __all_sync(0xffffffffu, ok);
-                // the next item
-                item_u0 += units;
-                if (item_u0 >= u1) break;
-                unit = 0;
-                if (++item == items) {
-                    item = 0;
-                    int more = 0;
-                    do {
-                        if (++s == base + 32) { base += 32; mine = load_seq<ROWS>(p, base + lane); }
-                        more = __shfl_sync(0xffffffffu, mine.items, s - base);
-                    } while (more == 0 && s < p.b.n_seq);
-                    if (more == 0) break;                // only if the lengths changed meanwhile
-                }
-            }
-            // where a wait gave up, copies in flight are waited for (with a limit)
-            if (ctl[0] && lane < DEC_WARPS)
-                for (int i = 0; i < STAGES; ++i)
-                    for (int n = 0; n < 4096 && !mbar_try_wait_64(&full[lane][i], i < stage ? phase : phase ^ 1); ++n) { }
+        __syncwarp();
+        if (lane == 0) {
+            f.u1 = u1;
+            if (u0 >= u1) { f.u1 = f.item_u0 = 0; f.q.units = 0; }   // nothing to do
         }
         __syncwarp();
-        if (lane == 0 && mbar_wait(&item_empty[q_at], q_phase ^ 1, ctl)) {
-            queue[q_at].units = 0;                       // the end
-            mbar_arrive(&item_full[q_at]);
-        }
-        return;
     }
+    const int per_page = p.g.page_tokens / KV4_BLOCK;
+    // The whole warp moves along the run together; one lane writes and copies.
+    const uint8_t* ptr = nullptr;        // the next block, null where its page number is out of range
+    int in_page = 0, in_item = 0;        // blocks left in the page, units left in the warp's share of the item
+    int next_page = 0, pushed = 0;       // a page number is asked for one page ahead
+    auto ask_page = [&](int at) {        // -2: no such position
+        return at < p.b.max_pages && (long long)at * p.g.page_tokens < f.q.len ? p.b.table[(long long)f.s * p.b.max_pages + at] : -2;
+    };
+    auto open_page = [&](int page, int in) {
+        ptr = nullptr;
+        if (page >= 0 && page < p.g.n_pages) ptr = p.g.block(page, f.item % p.g.heads, in * KV4_BLOCK);
+        else if (page != -2 && lane == 0) atomicOr(p.status, KV4_DEV_INDEX);
+        in_page = per_page - in;
+        next_page = ask_page(f.page_at + 1);
+    };
+    auto turn_page = [&]() {
+        __syncwarp();
+        if (lane == 0) ++f.page_at;
+        __syncwarp();
+        open_page(next_page, 0);
+    };
+    auto next_item = [&]() -> bool {     // false: the run is done
+        __syncwarp();
+        if (lane == 0) {
+            const int span = apart ? (int)share : f.q.units;
+            f.item_u0 += span;
+            if (f.item_u0 < f.u1 && ++f.item == f.q.items) {
+                f.item = 0;
+                do f.q = load_seq<ROWS>(p, ++f.s); while (f.q.items == 0 && f.s < p.b.n_seq);
+                if (f.q.items == 0) f.u1 = 0;                  // only if the lengths changed meanwhile
+            }
+        }
+        __syncwarp();
+        const long long run_u0 = run * ((long long)blockIdx.x * WARPS + warp), item_u0 = f.item_u0, u1 = f.u1;
+        const int unit0 = (int)max(0LL, run_u0 - item_u0), unit1 = (int)min((long long)f.q.units, u1 - item_u0);
+        if (item_u0 >= u1 || unit0 >= unit1) return false;     // (unit0 >= unit1: an item apart, shorter than the block's share)
+        const int blk = (f.q.unit0 + unit0) * 2;
+        if (lane == 0) {
+            Item& it = queue[warp][pushed % DEC_QUEUE];
+            it.first_row = f.q.first;
+            it.n_rows = f.q.rows * p.group;
+            it.head = f.item % p.g.heads;
+            it.row0 = f.item / p.g.heads * ROWS;
+            it.len = (int)max(0LL, min((long long)f.q.len, (long long)p.b.max_pages * p.g.page_tokens));
+            it.pos0 = f.q.len - f.q.all;
+            it.at0 = f.q.unit0 * DEC_UNIT;
+            it.unit0 = unit0;
+            it.unit1 = unit1;
+            it.units = f.q.units;
+            it.u0 = item_u0;
+            f.page_at = blk / per_page;
+        }
+        __syncwarp();
+        ++pushed;
+        in_item = unit1 - unit0;
+        open_page(ask_page(blk / per_page), blk % per_page);
+        return true;
+    };
+    bool more = true;
+    // The next unit of the run into slot `st`.  What is out of range is replaced by the pool's first block (its numbers are
+    // finite) and hidden.
+    auto feed = [&](int st) {
+        if (!more || (in_item == 0 && !(more = next_item()))) return;
+        if (in_page == 0) turn_page();
+        const uint8_t *a = ptr, *b;
+        const bool joined = in_page >= 2;
+        if (joined) {
+            b = ptr ? ptr + BLOCK : nullptr;
+            in_page -= 2;
+        } else {
+            turn_page();
+            b = ptr;
+            --in_page;
+        }
+        ptr = b ? b + BLOCK : nullptr;
+        --in_item;
+        if (lane == 0) {
+            uint8_t* to = ring + (size_t)(warp * p.stages + st) * UNIT;
+            there[warp][st] = (a ? 1 : 0) | (b ? 2 : 0);
+            mbar_arrive_expect_tx(&full[warp][st], UNIT);
+            if (joined && a) {
+                bulk_g2s(to, a, UNIT, &full[warp][st]);
+            } else {
+                bulk_g2s(to, a ? a : p.g.pool, BLOCK, &full[warp][st]);
+                bulk_g2s(to + BLOCK, b ? b : p.g.pool, BLOCK, &full[warp][st]);
+            }
+        }
+    };
+    for (int i = 0; i < p.stages; ++i) feed(i);
+    __syncwarp();
 
-    // ================= the computing warps =================
-    const int r = lane >> 2, j = lane & 3;
-    int stage = 0, q_at = 0;
-    uint32_t phase = 0, q_phase = 0;
+    int stage = 0;
+    uint32_t phase = 0;
     bool ok = true;
-    for (int turn = 0;; turn ^= 1) {
-        float (*ref_s)[ROWS] = ref_2[turn], (*sum_s)[ROWS] = sum_2[turn];
-        if (!mbar_wait(&item_full[q_at], q_phase, ctl)) ok = false;
-        if (any_of_the_warps(!ok)) break;          // a wait gave up: all leave together
-        if (queue[q_at].units == 0) break;
-        const Item it = queue[q_at];
+    for (int popped = 0; popped < pushed; ++popped) {
+        const Item it = queue[warp][popped % DEC_QUEUE];
 
         // ---- the item's query rows ----
         uint32_t qf[NT][2 * W][2];           // [..][MMA step][word]: column r
@@ -383,22 +407,24 @@ kv4_decode_kernel(const DecParams p)
         all_hi = __reduce_min_sync(0xffffffffu, all_hi);
 
         // ---- its units ----
-        for (int u = it.unit0 + warp; u < it.unit1; u += DEC_WARPS) {
-            if (!mbar_wait(&full[warp][stage], phase, ctl)) { ok = false; break; }
-            const uint8_t* blk = ring + (warp * STAGES + stage) * UNIT;
-            if (there[warp][stage]) {
-                const int pos_blk = (it.blk0 + u) * KV4_BLOCK;
-                // rows r and r + 8 of the score tile are the block's positions kr and kr + 8
-                const int kr = (r >> 1) + 4 * (r & 1);
+        for (int u = it.unit0; u < it.unit1; ++u) {
+            if (!(ok = mbar_wait(&full[warp][stage], phase, ctl))) break;
+            const uint8_t* unit = ring + (size_t)(warp * p.stages + stage) * UNIT;
+            const int at = it.at0 + u * DEC_UNIT, here = there[warp][stage];
+            // rows r and r + 8 of a block's score tile are its positions kr and kr + 8
+            const int kr = (r >> 1) + 4 * (r & 1);
+            float sc[2][NT][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t* blk = unit + h * BLOCK;
                 Words<W> kw[2], ks[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    kw[h] = *reinterpret_cast<const Words<W>*>(blk + (kr + 8 * h) * (D / 2) + j * 4 * W);
-                    ks[h] = *reinterpret_cast<const Words<W>*>(blk + 8 * D + (kr + 8 * h) * (D / 8));
+                for (int x = 0; x < 2; ++x) {
+                    kw[x] = *reinterpret_cast<const Words<W>*>(blk + (kr + 8 * x) * (D / 2) + j * 4 * W);
+                    ks[x] = *reinterpret_cast<const Words<W>*>(blk + 8 * D + (kr + 8 * x) * (D / 8));
                 }
-                float sc[NT][4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.0f;
+                for (int t = 0; t < NT; ++t) sc[h][t][0] = sc[h][t][1] = sc[h][t][2] = sc[h][t][3] = 0.0f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const uint32_t x0 = kw[0].w[w], x1 = kw[1].w[w], y0 = x0 >> 8, y1 = x1 >> 8;
@@ -410,68 +436,78 @@ kv4_decode_kernel(const DecParams p)
                         float d[4] = {off[t][w][0], off[t][w][1], off[t][w][0], off[t][w][1]};
                         mma_f16(d, a[0], a[1], a[2], a[3], qf[t][2 * w][0], qf[t][2 * w][1]);
                         mma_f16(d, a[4], a[5], a[6], a[7], qf[t][2 * w + 1][0], qf[t][2 * w + 1][1]);
-                        sc[t][0] = fmaf(s0.y, qsum[t][w][0], fmaf(s0.x, d[0], sc[t][0]));
-                        sc[t][1] = fmaf(s0.y, qsum[t][w][1], fmaf(s0.x, d[1], sc[t][1]));
-                        sc[t][2] = fmaf(s1.y, qsum[t][w][0], fmaf(s1.x, d[2], sc[t][2]));
-                        sc[t][3] = fmaf(s1.y, qsum[t][w][1], fmaf(s1.x, d[3], sc[t][3]));
+                        sc[h][t][0] = fmaf(s0.y, qsum[t][w][0], fmaf(s0.x, d[0], sc[h][t][0]));
+                        sc[h][t][1] = fmaf(s0.y, qsum[t][w][1], fmaf(s0.x, d[1], sc[h][t][1]));
+                        sc[h][t][2] = fmaf(s1.y, qsum[t][w][0], fmaf(s1.x, d[2], sc[h][t][2]));
+                        sc[h][t][3] = fmaf(s1.y, qsum[t][w][1], fmaf(s1.x, d[3], sc[h][t][3]));
                     }
                 }
-                if (pos_blk < all_lo || pos_blk + KV4_BLOCK > all_hi) {
+            }
+            if (at < all_lo || at + DEC_UNIT > all_hi || here != 3) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const int pos = pos_blk + kr + (k & 2 ? 8 : 0);
+                            const int pos = at + h * KV4_BLOCK + kr + (k & 2 ? 8 : 0);
                             // hidden whatever the scale's sign: the product below has to be -inf
-                            if (pos < lo[t][k & 1] || pos >= hi[t][k & 1]) sc[t][k] = cmul[t][k & 1] < 0.0f ? INFINITY : -INFINITY;
+                            if (pos < lo[t][k & 1] || pos >= hi[t][k & 1] || !(here >> h & 1)) sc[h][t][k] = cmul[t][k & 1] < 0.0f ? INFINITY : -INFINITY;
                         }
-                }
-                float e[NT][4];
-                bool over = false;
+            }
+            float e[2][NT][4];
+            bool over = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        e[t][k] = fmaf(sc[t][k], cmul[t][k & 1], -ref[t][k & 1]);
-                        over |= e[t][k] > kSlack;
+                        e[h][t][k] = fmaf(sc[h][t][k], cmul[t][k & 1], -ref[t][k & 1]);
+                        over |= e[h][t][k] > kSlack;
                     }
-                if (__any_sync(0xffffffffu, over)) {
+            if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float x = sc[t][k] * cmul[t][k], y = sc[t][k + 2] * cmul[t][k];
-                            float m = fmaxf(ref[t][k], fmaxf(x, y));
-                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                            const float keep = ex2(ref[t][k] - m);       // 0 before the first score
-                            ref[t][k] = m;
-                            sum[t][k] *= keep;
+                    for (int k = 0; k < 2; ++k) {
+                        float x[4] = {sc[0][t][k] * cmul[t][k], sc[0][t][k + 2] * cmul[t][k], sc[1][t][k] * cmul[t][k], sc[1][t][k + 2] * cmul[t][k]};
+                        float m = fmaxf(fmaxf(ref[t][k], fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        const float keep = ex2(ref[t][k] - m);       // 0 before the first score
+                        ref[t][k] = m;
+                        sum[t][k] *= keep;
 #pragma unroll
-                            for (int i = 0; i < D / 16; ++i) { o[t][i][k] *= keep; o[t][i][k + 2] *= keep; }
-                            e[t][k] = x - m;
-                            e[t][k + 2] = y - m;
-                        }
-                }
+                        for (int i = 0; i < D / 16; ++i) { o[t][i][k] *= keep; o[t][i][k + 2] *= keep; }
+                        e[0][t][k] = x[0] - m;
+                        e[0][t][k + 2] = x[1] - m;
+                        e[1][t][k] = x[2] - m;
+                        e[1][t][k + 2] = x[3] - m;
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t* blk = unit + h * BLOCK;
                 uint32_t pb[NT][2];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) e[t][k] = ex2(e[t][k]);
-                    sum[t][0] += e[t][0] + e[t][2];
-                    sum[t][1] += e[t][1] + e[t][3];
-                    pb[t][0] = transpose8(h2(e[t][0], e[t][1]));
-                    pb[t][1] = transpose8(h2(e[t][2], e[t][3]));
+                    for (int k = 0; k < 4; ++k) e[h][t][k] = ex2(e[h][t][k]);
+                    sum[t][0] += e[h][t][0] + e[h][t][2];
+                    sum[t][1] += e[h][t][1] + e[h][t][3];
+                    pb[t][0] = transpose8(h2(e[h][t][0], e[h][t][1]));
+                    pb[t][1] = transpose8(h2(e[h][t][2], e[h][t][3]));
                 }
                 // values: this thread's key pairs (j, j + 4) and (j + 8, j + 12), numbers D/8 r .. of each
                 const uint8_t* vb = blk + 10 * D;
                 Words<VW> vw[4];
                 uint32_t vs[4];
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    vw[h] = *reinterpret_cast<const Words<VW>*>(vb + (j + 4 * h) * (D / 2) + r * 4 * VW);
-                    vs[h] = *reinterpret_cast<const uint32_t*>(blk + 18 * D + (j + 4 * h) * (D / 8) + (r * W / 8) * 4);
+                for (int x = 0; x < 4; ++x) {
+                    vw[x] = *reinterpret_cast<const Words<VW>*>(vb + (j + 4 * x) * (D / 2) + r * 4 * VW);
+                    vs[x] = *reinterpret_cast<const uint32_t*>(blk + 18 * D + (j + 4 * x) * (D / 8) + (r * W / 8) * 4);
                 }
                 const uint32_t st0 = __byte_perm(vs[0], vs[1], 0x5410), bs0 = __byte_perm(vs[0], vs[1], 0x7632);
                 const uint32_t st1 = __byte_perm(vs[2], vs[3], 0x5410), bs1 = __byte_perm(vs[2], vs[3], 0x7632);
@@ -493,63 +529,94 @@ kv4_decode_kernel(const DecParams p)
                 }
             }
             __syncwarp();                      // every lane has read the slot
-            if (lane == 0) mbar_arrive(&empty[warp][stage]);
-            if (++stage == STAGES) { stage = 0; phase ^= 1; }
+            feed(stage);
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1; }
         }
+        if (!ok) break;
 
-        // ---- the warps' sums ----
+        // ---- write it, or keep it ----
+        const int which = it.unit0 > 0 ? 0 : 1;                // began before the run: 0
+        const bool whole = it.unit0 == 0 && it.unit1 == it.units;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                float v = sum[t][k];
-                v += __shfl_xor_sync(0xffffffffu, v, 4);
-                v += __shfl_xor_sync(0xffffffffu, v, 8);
-                v += __shfl_xor_sync(0xffffffffu, v, 16);
-                if (r == 0) {
-                    ref_s[warp][8 * t + 2 * j + k] = ref[t][k];
-                    sum_s[warp][8 * t + 2 * j + k] = v;
+                float l = sum[t][k];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                const int col = 8 * t + 2 * j + k, row = it.row0 + col;
+                if (row >= it.n_rows) continue;
+                if (whole) {
+                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                    __nv_bfloat16* to = p.out + (long long)(it.first_row + row / p.group) * p.ldo +
+                                        (long long)(it.head * p.group + row % p.group) * D + (D / 8) * r;
+#pragma unroll
+                    for (int i = 0; i < D / 16; i += 4) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {          // tile i: numbers 2 i and the next
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(o[t][i + x][k] * inv, o[t][i + x][k + 2] * inv);
+                            w[x] = *reinterpret_cast<const uint32_t*>(&b);
+                        }
+                        *reinterpret_cast<uint4*>(to + 2 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                } else {
+                    float* to = which ? reinterpret_cast<float*>(ring + (size_t)warp * p.stages * UNIT) : heads_kept + (size_t)warp * p.keep_cols * D;
+                    to += col * D + (D / 8) * r;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<float2*>(to + 2 * i) = make_float2(o[t][i][k], o[t][i][k + 2]);
+                    if (r == 0) { kept_ref[which][warp][col] = ref[t][k]; kept_sum[which][warp][col] = l; }
                 }
             }
-        warps_sync();
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int col = 8 * t + 2 * j + k;
-                float top = kNone;
-#pragma unroll
-                for (int w = 0; w < DEC_WARPS; ++w) top = fmaxf(top, ref_s[w][col]);
-                const float f = ex2(ref[t][k] - top);
-                float* to = meet + (warp * ROWS + col) * D + (D / 8) * r;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)       // tile 4 x + n: numbers 8 x + 2 n and the next
-                    *reinterpret_cast<float2*>(to + 2 * i) = make_float2(o[t][i][k] * f, o[t][i][k + 2] * f);
-            }
-        warps_sync();
+        if (!whole && lane == 0) kept[which][warp] = it;
+    }
+    if (!ok) {
+        // a wait gave up: the warp's copies in flight are waited for (with a limit)
+        if (lane == 0) atomicOr(p.status, KV4_DEV_TIMEOUT);
+        for (int i = 0; i < p.stages; ++i)
+            for (int n = 0; n < 4096 && !mbar_try_wait_64(&full[warp][i], i < stage ? phase ^ 1 : phase); ++n) { }
+    }
+
+    // ================= the block's parts: chains of warps that share an item =================
+    __syncthreads();
+    constexpr int THREADS = WARPS * 32, PART = ROWS * (D + 2);
+    // In the order of the units: warp 0's part of an item from before, then each warp's item that ends after it, with the
+    // parts of the warps that follow.
+    for (int a = -1; a < WARPS; ++a) {
+        const int from = a < 0 ? 0 : a;
+        const Item it = kept[a < 0 ? 0 : 1][from];
+        if (it.units == 0) continue;
+        int to = from;                                         // the last warp of the chain
+        bool ends = it.unit1 == it.units;
+        while (!ends && to + 1 < WARPS && kept[0][to + 1].units != 0) {
+            ++to;
+            ends = kept[0][to].unit1 == kept[0][to].units;
+        }
         const int cols = min(ROWS, it.n_rows - it.row0);
-        const bool starts = it.unit0 == 0, whole = starts && it.unit1 == it.units;
+        const bool starts = a >= 0, whole = starts && ends;
         auto write = [&](int col, int d, float4 v, float l) {
             const int row = it.row0 + col;
             const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            __nv_bfloat162 a = __floats2bfloat162_rn(v.x * inv, v.y * inv), b = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+            __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
             *reinterpret_cast<uint2*>(p.out + (long long)(it.first_row + row / p.group) * p.ldo +
                                       (long long)(it.head * p.group + row % p.group) * D + d) =
-                make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+                make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
         };
-        constexpr int PART = ROWS * (D + 2);
         float* part = p.parts + ((size_t)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
-        for (int i = threadIdx.x; i < cols * (D / 4); i += DEC_WARPS * 32) {
+        for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
             const int col = i / (D / 4), d = i % (D / 4) * 4;
             float top = kNone, l = 0.0f;
-#pragma unroll
-            for (int w = 0; w < DEC_WARPS; ++w) top = fmaxf(top, ref_s[w][col]);
             float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-            for (int w = 0; w < DEC_WARPS; ++w) {
-                const float4 x = *reinterpret_cast<const float4*>(meet + (w * ROWS + col) * D + d);
-                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-                l += ex2(ref_s[w][col] - top) * sum_s[w][col];
+            for (int w = from; w <= to; ++w) top = fmaxf(top, kept_ref[starts && w == from][w][col]);
+            for (int w = from; w <= to; ++w) {
+                const bool own = starts && w == from;
+                const float* src = own ? reinterpret_cast<const float*>(ring + (size_t)w * p.stages * UNIT) : heads_kept + (size_t)w * p.keep_cols * D;
+                const float4 x = *reinterpret_cast<const float4*>(src + col * D + d);
+                const float f = ex2(kept_ref[own][w][col] - top);
+                v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+                l = fmaf(kept_sum[own][w][col], f, l);
             }
             if (whole) {
                 write(col, d, v, l);
@@ -559,25 +626,25 @@ kv4_decode_kernel(const DecParams p)
             }
         }
         if (!whole) {
-            // ---- the parts of an item that spans blocks ----
+            const int b_first = (int)(it.u0 / share), b_last = (int)((it.u0 + it.units - 1) / share);
             __threadfence();
-            warps_sync();
+            __syncthreads();
             if (threadIdx.x == 0) {
-                const unsigned n = (unsigned)(it.b_last - it.b_first + 1);
-                const unsigned seen = atomicAdd(&p.tickets[it.b_first], 1u);
+                const unsigned n = (unsigned)(b_last - b_first + 1);
+                const unsigned seen = atomicAdd(&p.tickets[b_first], 1u);
                 last_s = seen + 1 == n;
-                if (seen + 1 == n) p.tickets[it.b_first] = 0;
+                if (seen + 1 == n) p.tickets[b_first] = 0;
                 __threadfence();
             }
-            warps_sync();
+            __syncthreads();
             if (last_s) {
-                for (int i = threadIdx.x; i < cols * (D / 4); i += DEC_WARPS * 32) {
+                for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
                     const int col = i / (D / 4), d = i % (D / 4) * 4;
                     float top = kNone, l = 0.0f;
                     float4 v = make_float4(0, 0, 0, 0);
 #pragma unroll 8
-                    for (int b = it.b_first; b <= it.b_last; ++b) {
-                        const float* src = p.parts + ((size_t)b * 2 + (b == it.b_first ? 1 : 0)) * PART;
+                    for (int b = b_first; b <= b_last; ++b) {
+                        const float* src = p.parts + ((size_t)b * 2 + (b == b_first ? 1 : 0)) * PART;
                         const float t = __ldcg(src + ROWS * D + col), ls = __ldcg(src + ROWS * (D + 1) + col);
                         const float4 x = __ldcg(reinterpret_cast<const float4*>(src + col * D + d));
                         const float nt = fmaxf(top, t);
@@ -591,43 +658,37 @@ kv4_decode_kernel(const DecParams p)
                 }
             }
         }
-        if (lane == 0) mbar_arrive(&item_empty[q_at]);
-        if (++q_at == DEC_QUEUE) { q_at = 0; q_phase ^= 1; }
     }
-    if (!ok && lane == 0) atomicOr(p.status, KV4_DEV_TIMEOUT);
 }
 
-template <int D, int NT, int STAGES>
-constexpr size_t smem_bytes() { return 128 + (size_t)DEC_WARPS * STAGES * 20 * D + sizeof(float) * DEC_WARPS * 8 * NT * D; }
-
-template <int D, int NT, int STAGES>
-tsvd_status_t launch(const DecParams& p, int blocks, cudaStream_t st)
+template <int D, int NT>
+tsvd_status_t launch(DecParams p, long long items, long long units_most, cudaStream_t st)
 {
-    PdlLaunch l((unsigned)blocks, DEC_THREADS, smem_bytes<D, NT, STAGES>(), st);
-    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_decode_kernel<D, NT, STAGES>, p));
+    constexpr size_t kRoom = 227 * 1024 - DEC_STATIC;          // beside what the kernel declares itself
+    const size_t kept = sizeof(float) * DEC_WARPS * p.keep_cols * D;
+    const size_t unit = (size_t)DEC_WARPS * 40 * D;
+    p.stages = (int)std::min<size_t>(DEC_MAX_STAGES, (kRoom - 128 - kept) / unit);
+    const long long blocks = std::min((long long)p.sms, std::max(items, (units_most + DEC_WARPS - 1) / DEC_WARPS));
+    PdlLaunch l((unsigned)blocks, DEC_WARPS * 32, 128 + kept + p.stages * unit, st);
+    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_decode_kernel<D, NT>, p));
     tsvd_count_launch();
     return TSVD_OK;
-}
-
-template <int D, int NT, int STAGES>
-cudaError_t prepare()
-{
-    return cudaFuncSetAttribute(kv4_decode_kernel<D, NT, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, NT, STAGES>());
 }
 
 constexpr int kRowsMost = 16;      // rows of an item: 8 or 16
 
 }  // namespace
 
-size_t kv4_decode_parts_bytes(int sms, int dim) { return sizeof(float) * (size_t)(2 * sms) * 2 * kRowsMost * (dim + 2); }
-size_t kv4_decode_tickets(int sms) { return (size_t)(2 * sms); }
+size_t kv4_decode_parts_bytes(int sms, int dim) { return sizeof(float) * (size_t)sms * 2 * kRowsMost * (dim + 2); }
+size_t kv4_decode_tickets(int sms) { return (size_t)sms; }
 
 tsvd_status_t kv4_decode_prepare()
 {
-    TSVD_CUDA_OK((prepare<128, 1, 4>()));
-    TSVD_CUDA_OK((prepare<64, 1, 8>()));
-    TSVD_CUDA_OK((prepare<128, 2, 8>()));
-    TSVD_CUDA_OK((prepare<64, 2, 8>()));
+    const int most = 227 * 1024 - DEC_STATIC;
+    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
+    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<64, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
+    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
+    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<64, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
     return TSVD_OK;
 }
 
@@ -646,16 +707,15 @@ tsvd_status_t kv4_attend_decode(const AttendArgs& a)
     p.c = fabsf(a.scale) < 1e-18f ? 1e-18f : a.scale * 1.4426950408889634f;
     p.window = a.window;
     p.causal = a.causal;
-    p.min_share = 16;
     p.parts = a.h->parts;
     p.tickets = a.h->tickets;
     p.status = a.h->dev_status;
+    p.sms = a.h->sms;
     const long long rows = (long long)a.max_q * p.group;
     const bool two = rows > 8;
+    p.keep_cols = (int)std::min<long long>(rows, two ? 16 : 8);
     const long long items = (long long)a.b.n_seq * p.g.heads * ((rows + (two ? 15 : 7)) / (two ? 16 : 8));
-    const long long most = items * (((long long)a.max_kv + KV4_BLOCK - 1) / KV4_BLOCK + 1);
-    const long long blocks = std::min((long long)a.h->sms * (two ? 1 : 2), (most + p.min_share - 1) / p.min_share);
-    if (p.g.dim == 128)
-        return two ? launch<128, 2, 8>(p, (int)blocks, a.stream) : launch<128, 1, 4>(p, (int)blocks, a.stream);
-    return two ? launch<64, 2, 8>(p, (int)blocks, a.stream) : launch<64, 1, 8>(p, (int)blocks, a.stream);
+    const long long most = items * (((long long)a.max_kv + DEC_UNIT - 1) / DEC_UNIT + 1);
+    if (p.g.dim == 128) return two ? launch<128, 2>(p, items, most, a.stream) : launch<128, 1>(p, items, most, a.stream);
+    return two ? launch<64, 2>(p, items, most, a.stream) : launch<64, 1>(p, items, most, a.stream);
 }
