@@ -187,7 +187,7 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     if (e == cudaSuccess) e = cudaMalloc(&h->parts, kv4_decode_parts_bytes(h->sms, head_dim));
     if (e == cudaSuccess) e = cudaMalloc(&h->tickets, tickets);
     if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, tickets);
-    if (e == cudaSuccess && kv4_decode_prepare() != TSVD_OK) e = cudaErrorUnknown;
+    if (e == cudaSuccess && (kv4_decode_prepare() != TSVD_OK || kv4_prefill_prepare() != TSVD_OK)) e = cudaErrorUnknown;
     if (e != cudaSuccess) {
         tsvd_kv4_destroy(h);
         (void)cudaGetLastError();
@@ -289,7 +289,7 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     a.causal = flags & TSVD_FLAG_CAUSAL;
     a.stream = (cudaStream_t)stream;
     if (dtype == TSVD_F32 || (flags & TSVD_FLAG_PATH_SIMPLE)) return kv4_attend_simple(a);
-    return kv4_attend_decode(a);
+    return (long long)a.max_q * (n_heads / h->g.heads) <= 32 ? kv4_attend_decode(a) : kv4_attend_prefill(a);
 }
 
 extern "C" tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages, size_t* pool_bytes)

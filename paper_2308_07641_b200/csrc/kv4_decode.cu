@@ -16,8 +16,8 @@
 // odd nibbles, whose q is divided by 16 beforehand; 1024 sum q comes off through the accumulator's start value, and step and
 // base of the group are applied to the fp32 sum: s (q.code) + b (sum q).  So scores carry no rounding of k at all.  q enters
 // as fp16 after division by a power of two per row (exact up to 2^-24 of the row's largest).  Values become fp16 numbers
-// code * step + base (one rounding); probabilities fp16, at most 2^8 above the reference, which moves only when a score
-// passes it by more than 8 (in units of log2): no exchange between lanes otherwise.
+// code * step + base (one rounding); probabilities fp16, relative to a reference that moves only when a score passes the
+// one it was set by by more than 5 (in units of log2): no exchange between lanes otherwise.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -34,7 +34,9 @@ constexpr int DEC_STATIC = 13 * 1024;    // room for what the kernel declares
 constexpr int DEC_WARPS = 8;             // two on each quarter of an SM: up to 255 registers a thread
 constexpr int DEC_UNIT = 2 * KV4_BLOCK;  // positions of a unit
 
-constexpr float kSlack = 8.0f;           // how far (log2) a score may pass the reference before it moves
+// Probabilities are 2^(score - reference): 2^10 where the reference was set, up to 2^15 before it moves, so that fp16
+// reaches down to 2^-35 of it.
+constexpr float kSet = 10.0f, kMove = 15.0f;
 constexpr float kNone = -1e30f;          // the reference before the first score
 
 struct DecParams {
@@ -464,7 +466,7 @@ kv4_decode_kernel(const DecParams p)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         e[h][t][k] = fmaf(sc[h][t][k], cmul[t][k & 1], -ref[t][k & 1]);
-                        over |= e[h][t][k] > kSlack;
+                        over |= e[h][t][k] > kMove;
                     }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -472,10 +474,10 @@ kv4_decode_kernel(const DecParams p)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         float x[4] = {sc[0][t][k] * cmul[t][k], sc[0][t][k + 2] * cmul[t][k], sc[1][t][k] * cmul[t][k], sc[1][t][k + 2] * cmul[t][k]};
-                        float m = fmaxf(fmaxf(ref[t][k], fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
+                        float m = fmaxf(fmaxf(ref[t][k] + kSet, fmaxf(x[0], x[1])), fmaxf(x[2], x[3]));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) - kSet;
                         const float keep = ex2(ref[t][k] - m);       // 0 before the first score
                         ref[t][k] = m;
                         sum[t][k] *= keep;

@@ -1,0 +1,570 @@
+// Attention over the 4-bit cache for many query rows (prompts, and pieces of prompts behind earlier context): bound by the
+// tensor cores and the exponentials.
+//
+//     out = sum_j p_j v_j / sum_j p_j,   p_j = exp2(c q.k_j - ref),   c = scale log2(e)
+//
+// A block takes up to two tiles of 128 query rows of one sequence and key/value head -- (token, head) pairs of the heads
+// that share it -- and walks over tiles of 128 cached positions:
+//   warp 13     copies the packed positions into shared memory, keys and values in turn
+//   warps 8-11  turn codes into fp16 numbers, code * step + base, in the order the tensor cores read (keys with head_dim
+//               contiguous, values likewise: the second product takes them as an MN-major operand, so nothing is transposed)
+//   warp 12     issues tcgen05.mma: scores S = Q K^T into tensor memory, then O += P V with P from tensor memory
+//   warps 0-3 and 4-7, one row a thread: running maximum, exponentials, P as fp16 over S's own columns, the sum
+// The two row tiles alternate, so that the products of one run while the other's exponentials do.  A row's reference moves
+// only when a score passes the one it was set by by more than 5 (log2), so that O, which stays in tensor memory, is seldom rescaled.
+//
+// Arithmetic: q as fp16 after division by a power of two per row (exact down to 2^-24 of the row's largest; the power goes
+// into the row's factor c), keys and values as fp16 (one rounding), probabilities as fp16, sums in fp32.
+#include <algorithm>
+
+#include "serving.cuh"
+#include "sm100_ptx.cuh"
+
+namespace {
+
+using namespace ptx;
+
+constexpr int PRE_THREADS = 14 * 32;
+constexpr int PRE_ROWS = 128;            // rows of a tile
+constexpr int PRE_KEYS = 128;            // positions of a tile
+constexpr int PRE_HIDE = 8;              // tiles whose hidden blocks are remembered: more than any copy can be ahead
+// Probabilities are 2^(score - reference): 2^10 where the reference was set, up to 2^15 before it moves, so that fp16
+// reaches down to 2^-35 of it.
+constexpr float kSet = 10.0f, kMove = 15.0f;
+constexpr float kNone = -1e30f;
+
+struct PreParams {
+    Kv4Geom g;
+    Kv4Batch b;
+    const __nv_bfloat16* q;
+    long long ldq;
+    __nv_bfloat16* out;
+    long long ldo;
+    int group, max_q;
+    int tiles;               // pairs of row tiles of a sequence and head
+    float c;
+    float sign;              // of the scale: goes into q
+    int window, causal;
+    int* status;
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t lop_or(uint32_t x, uint32_t mask)
+{
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(0x64006400u));
+    return y;
+}
+__device__ __forceinline__ uint32_t h2(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t hfma(uint32_t a, uint32_t b, uint32_t c)
+{
+    const __half2 v = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Eight numbers of a group from their codes: pairs in order, step and base in both halves.
+__device__ __forceinline__ uint4 numbers(uint32_t x, uint32_t step, uint32_t base)
+{
+    constexpr uint32_t kOne = 0x3c003c00u, kMinus1024 = 0xe400e400u, kSixteenth = 0x2c002c00u, kMinus64 = 0xd400d400u;
+    const uint32_t y = x >> 8;
+    uint4 v;
+    v.x = hfma(hfma(lop_or(x, 0x000f000fu), kOne, kMinus1024), step, base);
+    v.y = hfma(hfma(lop_or(x, 0x00f000f0u), kSixteenth, kMinus64), step, base);
+    v.z = hfma(hfma(lop_or(y, 0x000f000fu), kOne, kMinus1024), step, base);
+    v.w = hfma(hfma(lop_or(y, 0x00f000f0u), kSixteenth, kMinus64), step, base);
+    return v;
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+          "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// kind::f16, both operands fp16, fp32 sums; B_MN: the N x K operand has N contiguous.
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn)
+{
+    return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// MN-major operand, 128-byte swizzle: rows of 64 numbers (one k each), eight rows a 1 KiB group, 64 numbers to the next
+// `apart` bytes later.
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t apart)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(apart >> 4) << 16;
+    d |= (uint64_t)(1024u >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+__device__ __forceinline__ void umma_f16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+
+// Shared memory (1024-aligned): Q [2 tiles][D/64][128 rows][128 B] | K [2][D/64][128][128 B] | V [2][D/64][128][128 B] |
+// packed halves [STAGES][8 blocks][10 D bytes]
+template <int D>
+struct Layout {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTile = kHalves * 16384;
+    static constexpr int kPacked = 8 * 10 * D;              // keys or values of a tile of positions
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kQ = 0, kK = 2 * kTile, kV = 4 * kTile, kStg = 6 * kTile;
+    static constexpr int kBytes = kStg + kStages * kPacked;
+};
+
+template <int D>
+__global__ void __launch_bounds__(PRE_THREADS, 1)
+kv4_prefill_kernel(const PreParams p)
+{
+    using L = Layout<D>;
+    constexpr int W = D / KV4_GROUP;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    __shared__ uint64_t stg_full[L::kStages], stg_empty[L::kStages], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full[2], p_full[2],
+        o_done[2], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ uint8_t hidden[PRE_HIDE];
+    __shared__ int ctl_[2];
+    volatile int* ctl = ctl_;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // ---- which rows: pairs of tiles with the most positions first ----
+    pdl_launch_dependents();
+    pdl_wait();
+    const int per = p.g.heads * p.b.n_seq;
+    const int pair = p.tiles - 1 - (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
+    const int head = rest % p.g.heads, s = rest / p.g.heads;
+    const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
+    const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
+    const int row_base = pair * 2 * PRE_ROWS;
+    if (row_base >= n_rows) return;
+    const int len = p.b.seq_len[s];
+    const long long room = (long long)p.b.max_pages * p.g.page_tokens;
+    if (len > room && threadIdx.x == 0) atomicOr(p.status, KV4_DEV_INDEX);
+    const int len_in = (int)max(0LL, min((long long)len, room));
+    const int pos0 = len - all;                             // position of the sequence's first row
+    auto row_hi = [&](int row) { return p.causal ? max(0, min(pos0 + row / p.group + 1, len_in)) : len_in; };
+    auto row_lo = [&](int row) { return p.window ? max(0, pos0 + row / p.group - p.window + 1) : 0; };
+    int t_lo[2], t_hi[2];                                   // tiles of positions [t_lo, t_hi) that each row tile sees
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int r0 = row_base + x * PRE_ROWS, r1 = min(r0 + PRE_ROWS, n_rows) - 1;
+        t_lo[x] = t_hi[x] = 0;
+        if (r1 >= r0 && row_hi(r1) > row_lo(r0)) {
+            t_lo[x] = row_lo(r0) / PRE_KEYS;
+            t_hi[x] = (row_hi(r1) + PRE_KEYS - 1) / PRE_KEYS;
+        }
+    }
+    const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
+    const int k_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), k_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < L::kStages; ++i) { mbar_init(&stg_full[i], 8); mbar_init(&stg_empty[i], 4); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&k_full[i], 4);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_full[i], 4);
+            mbar_init(&v_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&o_done[i], 1);
+        }
+        mbar_init(&q_full, 8);
+        mbar_init(&drained, 1);
+        ctl[0] = 0;
+        ctl[1] = kWaitLimitDefault;
+        fence_mbar_init();
+    }
+    if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;                        // S or P of tile x: column 128 x; O: column 256 + 128 x
+
+    if (warp < 8) {
+        // ================= rows: one a thread =================
+        const int x = warp >> 2, r = threadIdx.x & 127, row = row_base + x * PRE_ROWS + r;
+        const bool live = row < n_rows;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        float cm;
+        {   // the row of q, divided by the power of two at or below its largest (2^-60 at least)
+            const __nv_bfloat16* src = p.q + (long long)(first + (live ? row / p.group : 0)) * p.ldq +
+                                       (long long)(head * p.group + (live ? row % p.group : 0)) * D;
+            float top = 0.0f;
+            uint4 v[D / 8];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+                v[i] = live ? *reinterpret_cast<const uint4*>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
+            }
+            const int e = min(max((int)(__float_as_uint(top) >> 23), 67), 253) - 127;
+            const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
+            cm = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
+            uint8_t* to = smem + L::kQ + x * L::kTile + r * 128;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                uint32_t h[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * down, __uint_as_float(w[k] & 0xffff0000u) * down);
+                *reinterpret_cast<uint4*>(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full);
+        }
+        const int lo = live ? row_lo(row) : 0, hi = live ? row_hi(row) : 0x7fffffff;
+        const int all_lo = __reduce_max_sync(0xffffffffu, lo), all_hi = __reduce_min_sync(0xffffffffu, hi);
+        const uint32_t t_s = t_lane + 128u * x, t_o = t_lane + 256u + 128u * x;
+        float ref = kNone, sum = 0.0f;
+        uint32_t ph = 0;
+        bool ok = true;
+        const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
+        for (int k = a; k < b; ++k) {
+            if (!(ok = mbar_wait(&s_full[x], ph, ctl))) break;
+            tc_fence_after_sync();
+            const int at = k * PRE_KEYS;
+            const uint32_t hide = hidden[k % PRE_HIDE];
+            const bool edge = at < all_lo || at + PRE_KEYS > all_hi || hide;
+            auto masked = [&](uint32_t (&v)[32], int c0) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int pos = at + c0 + i;
+                    if (pos < lo || pos >= hi || (hide >> ((c0 + i) >> 4) & 1)) v[i] = 0xff800000u;
+                }
+            };
+            float top = -INFINITY;
+#pragma unroll
+            for (int c0 = 0; c0 < PRE_KEYS; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld32(t_s + c0, v);
+                tmem_ld_wait();
+                if (edge) masked(v, c0);
+                float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[1]);
+#pragma unroll
+                for (int i = 2; i < 32; i += 2) { m0 = fmaxf(m0, __uint_as_float(v[i])); m1 = fmaxf(m1, __uint_as_float(v[i + 1])); }
+                top = fmaxf(top, fmaxf(m0, m1));
+            }
+            top *= cm;
+            const bool over = top > ref + kMove;
+            if (__any_sync(0xffffffffu, over)) {
+                const float to = over ? top - kSet : ref, keep = ex2(ref - to);    // 0 before the first score
+                ref = to;
+                sum *= keep;
+                if (k > a) {
+                    if (!(ok = mbar_wait(&o_done[x], ph ^ 1, ctl))) break;   // the product of the tile before
+                    tc_fence_after_sync();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(t_o + c0, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * keep);
+                        tmem_st32(t_o + c0, v);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c0 = 0; c0 < PRE_KEYS; c0 += 32) {
+                uint32_t v[32], w[16];
+                tmem_ld32(t_s + c0, v);
+                tmem_ld_wait();
+                if (edge) masked(v, c0);
+                float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float e0 = ex2(fmaf(__uint_as_float(v[2 * i]), cm, -ref)), e1 = ex2(fmaf(__uint_as_float(v[2 * i + 1]), cm, -ref));
+                    s0 += e0;
+                    s1 += e1;
+                    w[i] = h2(e0, e1);
+                }
+                sum += s0 + s1;
+                tmem_st16(t_s + c0 / 2, w);                  // over columns whose scores have been read
+            }
+            tmem_st_wait();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[x]);
+            ph ^= 1;
+        }
+        if (ok && b > a) ok = mbar_wait(&o_done[x], ph ^ 1, ctl);
+        tc_fence_after_sync();
+        if (ok) {
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            __nv_bfloat16* to = p.out + (long long)(first + (live ? row / p.group : 0)) * p.ldo +
+                                (long long)(head * p.group + (live ? row % p.group : 0)) * D;
+#pragma unroll
+            for (int c0 = 0; c0 < D; c0 += 32) {
+                uint32_t v[32] = {};
+                if (b > a) {
+                    tmem_ld32(t_o + c0, v);
+                    tmem_ld_wait();
+                }
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v[i + 2 * k]) * inv, __uint_as_float(v[i + 2 * k + 1]) * inv);
+                            w[k] = *reinterpret_cast<const uint32_t*>(&y);
+                        }
+                        *reinterpret_cast<uint4*>(to + c0 + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+        }
+        tc_fence_before_sync();
+    } else if (warp < 12) {
+        // ================= numbers from codes =================
+        const int w4 = warp - 8, j = lane & 3, idx = lane >> 2;
+        int st = 0;
+        uint32_t sph = 0, ph[2] = {0, 0};                   // phases of the two stages
+        bool ok = true;
+        for (int k = k_lo; k < k_hi && ok; ++k) {
+            const int buf = (k - k_lo) & 1;
+            // keys: lane (position, j) has one word of every group; positions in the order 0 4 1 5 ... keep the stores apart
+            if (!(ok = mbar_wait(&stg_full[st], sph, ctl) && mbar_wait(&k_empty[buf], ph[buf] ^ 1, ctl))) break;
+            const uint8_t* src = smem + L::kStg + st * L::kPacked;
+            uint8_t* dst = smem + L::kK + buf * L::kTile;
+            const int kr = (idx >> 1) + 4 * (idx & 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = i * 32 + w4 * 8 + kr, pos = key & 15;
+                const uint8_t* blk = src + (key >> 4) * (10 * D);
+                uint32_t code[W], sb[W];
+                if constexpr (W == 4) {
+                    const uint4 cw = *reinterpret_cast<const uint4*>(blk + pos * (D / 2) + j * 16), sw = *reinterpret_cast<const uint4*>(blk + 8 * D + pos * (D / 8));
+                    code[0] = cw.x; code[1] = cw.y; code[2] = cw.z; code[3] = cw.w;
+                    sb[0] = sw.x; sb[1] = sw.y; sb[2] = sw.z; sb[3] = sw.w;
+                } else {
+                    const uint2 cw = *reinterpret_cast<const uint2*>(blk + pos * (D / 2) + j * 8), sw = *reinterpret_cast<const uint2*>(blk + 8 * D + pos * (D / 8));
+                    code[0] = cw.x; code[1] = cw.y;
+                    sb[0] = sw.x; sb[1] = sw.y;
+                }
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    *reinterpret_cast<uint4*>(dst + (w >> 1) * 16384 + key * 128 + (((4 * (w & 1) + j) ^ (key & 7)) << 4)) =
+                        numbers(code[w], __byte_perm(sb[w], 0, 0x1010), __byte_perm(sb[w], 0, 0x3232));
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&k_full[buf]); mbar_arrive(&stg_empty[st]); }
+            if (++st == L::kStages) { st = 0; sph ^= 1; }
+            // values: lane (position, j) has D / 4 consecutive numbers; the upper two quarters start elsewhere
+            if (!(ok = mbar_wait(&stg_full[st], sph, ctl) && mbar_wait(&v_empty[buf], ph[buf] ^ 1, ctl))) break;
+            src = smem + L::kStg + st * L::kPacked;
+            dst = smem + L::kV + buf * L::kTile;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = i * 32 + w4 * 8 + idx, pos = key & 15;
+                const uint8_t* blk = src + (key >> 4) * (10 * D);
+                if constexpr (W == 4) {
+                    uint4 cw = *reinterpret_cast<const uint4*>(blk + pos * (D / 2) + j * 16);
+                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + 8 * D + pos * (D / 8) + j * 4);
+                    const uint32_t step = __byte_perm(sb, 0, 0x1010), base = __byte_perm(sb, 0, 0x3232);
+                    const int turn = j & 2;                  // numbers 32 j + 8 (i ^ turn) .. at turn i
+                    if (turn) cw = make_uint4(cw.z, cw.w, cw.x, cw.y);
+                    const uint32_t code[4] = {cw.x, cw.y, cw.z, cw.w};
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        *reinterpret_cast<uint4*>(dst + (j >> 1) * 16384 + key * 128 + (((4 * (j & 1) + (n ^ turn)) ^ (key & 7)) << 4)) =
+                            numbers(code[n], step, base);
+                } else {
+                    const uint2 cw = *reinterpret_cast<const uint2*>(blk + pos * (D / 2) + j * 8);
+                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + 8 * D + pos * (D / 8) + (j >> 1) * 4);
+                    const uint32_t step = __byte_perm(sb, 0, 0x1010), base = __byte_perm(sb, 0, 0x3232);
+                    *reinterpret_cast<uint4*>(dst + key * 128 + (((2 * j) ^ (key & 7)) << 4)) = numbers(cw.x, step, base);
+                    *reinterpret_cast<uint4*>(dst + key * 128 + (((2 * j + 1) ^ (key & 7)) << 4)) = numbers(cw.y, step, base);
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&v_full[buf]); mbar_arrive(&stg_empty[st]); }
+            if (++st == L::kStages) { st = 0; sph ^= 1; }
+            ph[buf] ^= 1;
+        }
+    } else if (warp == 12) {
+        // ================= products =================
+        if (elect_one() && k_hi > k_lo) {
+            constexpr uint32_t kQk = idesc_f16(PRE_ROWS, PRE_KEYS, false), kPv = idesc_f16(PRE_ROWS, D, true);
+            const uint32_t base = smem_u32(smem);
+            auto scores = [&](int x, int buf) {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {           // 16 numbers a step: 32 bytes of a 128-byte row
+                    const uint32_t at = (uint32_t)(i >> 2) * 16384u + (uint32_t)(i & 3) * 32u;
+                    umma_f16_ss(tmem + 128u * x, umma_desc_k_sw128(base + L::kQ + x * L::kTile + at), umma_desc_k_sw128(base + L::kK + buf * L::kTile + at),
+                                kQk, i > 0);
+                }
+                umma_commit(&s_full[x]);
+            };
+            auto values = [&](int x, int buf, bool more) {
+#pragma unroll
+                for (int i = 0; i < PRE_KEYS / 16; ++i)      // 16 positions a step: 16 rows of values, 8 columns of P
+                    umma_f16_ts(tmem + 256u + 128u * x, tmem + 128u * x + 8u * i,
+                                umma_desc_mn_sw128(base + L::kV + buf * L::kTile + (uint32_t)i * 2048u, 16384u), kPv, more || i > 0);
+                umma_commit(&o_done[x]);
+            };
+            bool ok = mbar_wait(&q_full, 0, ctl) && mbar_wait(&k_full[0], 0, ctl);
+            uint32_t pph[2] = {0, 0};
+            if (ok) {
+                tc_fence_after_sync();
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (t_lo[x] == k_lo && t_hi[x] > k_lo) scores(x, 0);
+                umma_commit(&k_empty[0]);
+            }
+            for (int k = k_lo; k < k_hi && ok; ++k) {
+                const int i = k - k_lo, buf = i & 1, nbuf = buf ^ 1;
+                const uint32_t ph = (uint32_t)(i >> 1) & 1, nph = (uint32_t)((i + 1) >> 1) & 1;
+                if (!(ok = mbar_wait(&v_full[buf], ph, ctl))) break;
+                bool have = false;                           // the next keys
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (k >= t_lo[x] && k < t_hi[x]) {
+                        if (!(ok = mbar_wait(&p_full[x], pph[x], ctl))) break;
+                        pph[x] ^= 1;
+                        tc_fence_after_sync();
+                        values(x, buf, k > t_lo[x]);
+                    }
+                    if (k + 1 >= t_lo[x] && k + 1 < t_hi[x]) {
+                        if (!have && !(ok = mbar_wait(&k_full[nbuf], nph, ctl))) break;
+                        have = true;
+                        tc_fence_after_sync();
+                        scores(x, nbuf);
+                    }
+                }
+                if (!ok) break;
+                umma_commit(&v_empty[buf]);
+                if (k + 1 < k_hi) umma_commit(&k_empty[nbuf]);
+            }
+            // every product has ended before the block does
+            umma_commit(&drained);
+            for (int n = 0; n < (1 << 16) && !mbar_try_wait_64(&drained, 0); ++n) { }
+        }
+        __syncwarp();
+    } else {
+        // ================= packed positions: lane i copies block i of a tile, keys and values in turn =================
+        const int per_page = p.g.page_tokens / KV4_BLOCK;
+        int st = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int k = k_lo; k < k_hi && ok; ++k) {
+            const int blk = k * (PRE_KEYS / KV4_BLOCK) + (lane & 7);
+            const uint8_t* src = nullptr;
+            if ((long long)blk * KV4_BLOCK < len_in) {
+                const int page = p.b.table[(long long)s * p.b.max_pages + blk / per_page];
+                if (page >= 0 && page < p.g.n_pages) src = p.g.block(page, head, blk % per_page * KV4_BLOCK);
+                else if (lane < 8) atomicOr(p.status, KV4_DEV_INDEX);
+            }
+            // what is out of range is replaced by the pool's first block (its numbers are finite) and hidden
+            const uint32_t gone = __ballot_sync(0xffffffffu, src == nullptr) & 0xffu;
+            if (!src) src = p.g.pool;
+            for (int half = 0; half < 2 && ok; ++half) {
+                ok = mbar_wait(&stg_empty[st], ph ^ 1, ctl);
+                if (ok && half == 0 && lane == 0) hidden[k % PRE_HIDE] = (uint8_t)gone;
+                __syncwarp();
+                if (ok && lane < 8) {
+                    mbar_arrive_expect_tx(&stg_full[st], 10 * D);
+                    bulk_g2s(smem + L::kStg + st * L::kPacked + lane * (10 * D), src + half * (10 * D), 10 * D, &stg_full[st]);
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (ok && ++st == L::kStages) { st = 0; ph ^= 1; }
+            }
+        }
+        // where a wait gave up, copies in flight are waited for (with a limit)
+        if (ctl[0])
+            for (int i = 0; i < L::kStages; ++i)
+                for (int n = 0; n < 4096 && !mbar_try_wait_64(&stg_full[i], i < st ? ph : ph ^ 1); ++n) { }
+        __syncwarp();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (threadIdx.x == 0 && ctl[0]) atomicOr(p.status, KV4_DEV_TIMEOUT);
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+tsvd_status_t launch(const PreParams& p, cudaStream_t st)
+{
+    const long long blocks = (long long)p.tiles * p.g.heads * p.b.n_seq;
+    if (blocks > 0x7fffffffLL) return TSVD_E_TOOBIG;
+    PdlLaunch l((unsigned)blocks, PRE_THREADS, Layout<D>::kBytes + 1024, st);
+    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_prefill_kernel<D>, p));
+    tsvd_count_launch();
+    return TSVD_OK;
+}
+
+}  // namespace
+
+tsvd_status_t kv4_prefill_prepare()
+{
+    TSVD_CUDA_OK(cudaFuncSetAttribute(kv4_prefill_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<128>::kBytes + 1024));
+    TSVD_CUDA_OK(cudaFuncSetAttribute(kv4_prefill_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<64>::kBytes + 1024));
+    return TSVD_OK;
+}
+
+tsvd_status_t kv4_attend_prefill(const AttendArgs& a)
+{
+    PreParams p{};
+    p.g = a.h->g;
+    p.b = a.b;
+    p.q = (const __nv_bfloat16*)a.q;
+    p.ldq = a.ldq;
+    p.out = (__nv_bfloat16*)a.out;
+    p.ldo = a.ldo;
+    p.group = a.n_heads / a.h->g.heads;
+    p.max_q = a.max_q;
+    p.tiles = (int)(((long long)a.max_q * p.group + 2 * PRE_ROWS - 1) / (2 * PRE_ROWS));
+    // (a scale of 0 is a tiny one: hidden positions become -inf through the product with it)
+    p.c = std::max(fabsf(a.scale) * 1.4426950408889634f, 1e-18f);
+    p.sign = a.scale < 0.0f ? -1.0f : 1.0f;
+    p.window = a.window;
+    p.causal = a.causal;
+    p.status = a.h->dev_status;
+    return p.g.dim == 128 ? launch<128>(p, a.stream) : launch<64>(p, a.stream);
+}
