@@ -24,7 +24,10 @@ namespace {
 
 using namespace ptx;
 
-constexpr int PRE_THREADS = 14 * 32;
+constexpr int PRE_THREADS = 16 * 32;     // four warpgroups (14 warps have work)
+// Registers: 512 threads x 128 at launch; the rows' two warpgroups take 184 a thread, the others keep 72.
+constexpr int kRegsRows = 184, kRegsRest = 72;
+static_assert(256 * kRegsRows + 256 * kRegsRest <= PRE_THREADS * 128, "more than the block was launched with would wait for ever");
 constexpr int PRE_ROWS = 128;            // rows of a tile
 constexpr int PRE_KEYS = 128;            // positions of a tile
 constexpr int PRE_HIDE = 8;              // tiles whose hidden blocks are remembered: more than any copy can be ahead
@@ -69,6 +72,29 @@ __device__ __forceinline__ uint32_t hfma(uint32_t a, uint32_t b, uint32_t c)
 {
     const __half2 v = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+// two at once: (a, b) * m + c, and a sum
+__device__ __forceinline__ float2 fma2(float2 a, float2 m, float2 c)
+{
+    float2 y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(y))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(m)), "l"(reinterpret_cast<unsigned long long&>(c)));
+    return y;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 y;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long&>(y))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+    return y;
 }
 // Eight numbers of a group from their codes: pairs in order, step and base in both halves.
 __device__ __forceinline__ uint4 numbers(uint32_t x, uint32_t step, uint32_t base)
@@ -138,6 +164,9 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
         : "memory");
 }
+
+template <int WORDS>
+struct alignas(4 * WORDS) Words { uint32_t w[WORDS]; };
 
 // Shared memory (1024-aligned): Q [2 tiles][D/64][128 rows][128 B] | K [2][D/64][128][128 B] | V [2][D/64][128][128 B] |
 // packed halves [STAGES][8 blocks][10 D bytes]
@@ -221,6 +250,7 @@ kv4_prefill_kernel(const PreParams p)
     const uint32_t tmem = tmem_slot;                        // S or P of tile x: column 128 x; O: column 256 + 128 x
 
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRows));
         // ================= rows: one a thread =================
         const int x = warp >> 2, r = threadIdx.x & 127, row = row_base + x * PRE_ROWS + r;
         const bool live = row < n_rows;
@@ -268,26 +298,30 @@ kv4_prefill_kernel(const PreParams p)
             const int at = k * PRE_KEYS;
             const uint32_t hide = hidden[k % PRE_HIDE];
             const bool edge = at < all_lo || at + PRE_KEYS > all_hi || hide;
-            auto masked = [&](uint32_t (&v)[32], int c0) {
+            uint32_t v[4][32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int pos = at + c0 + i;
-                    if (pos < lo || pos >= hi || (hide >> ((c0 + i) >> 4) & 1)) v[i] = 0xff800000u;
-                }
-            };
-            float top = -INFINITY;
+            for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, v[c]);
+            tmem_ld_wait();
+            if (edge) {
 #pragma unroll
-            for (int c0 = 0; c0 < PRE_KEYS; c0 += 32) {
-                uint32_t v[32];
-                tmem_ld32(t_s + c0, v);
-                tmem_ld_wait();
-                if (edge) masked(v, c0);
-                float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[1]);
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 2; i < 32; i += 2) { m0 = fmaxf(m0, __uint_as_float(v[i])); m1 = fmaxf(m1, __uint_as_float(v[i + 1])); }
-                top = fmaxf(top, fmaxf(m0, m1));
+                    for (int i = 0; i < 32; ++i) {
+                        const int pos = at + 32 * c + i;
+                        if (pos < lo || pos >= hi || (hide >> (2 * c + (i >> 4)) & 1)) v[c][i] = 0xff800000u;
+                    }
             }
-            top *= cm;
+            float top;
+            {
+                float m[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    m[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
+#pragma unroll
+                    for (int i = 2; i < 32; i += 2) m[c] = max3(m[c], __uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1]));
+                }
+                top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * cm;
+            }
             const bool over = top > ref + kMove;
             if (__any_sync(0xffffffffu, over)) {
                 const float to = over ? top - kSet : ref, keep = ex2(ref - to);    // 0 before the first score
@@ -297,33 +331,32 @@ kv4_prefill_kernel(const PreParams p)
                     if (!(ok = mbar_wait(&o_done[x], ph ^ 1, ctl))) break;   // the product of the tile before
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(t_o + c0, v);
+                    for (int c0 = 0; c0 < D; c0 += 16) {
+                        uint32_t u[16];
+                        tmem_ld16(t_o + c0, u);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * keep);
-                        tmem_st32(t_o + c0, v);
+                        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * keep);
+                        tmem_st16(t_o + c0, u);
                     }
                 }
             }
+            const float2 cm2 = make_float2(cm, cm), ref2 = make_float2(-ref, -ref);
+            float2 s2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-            for (int c0 = 0; c0 < PRE_KEYS; c0 += 32) {
-                uint32_t v[32], w[16];
-                tmem_ld32(t_s + c0, v);
-                tmem_ld_wait();
-                if (edge) masked(v, c0);
-                float s0 = 0.0f, s1 = 0.0f;
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float e0 = ex2(fmaf(__uint_as_float(v[2 * i]), cm, -ref)), e1 = ex2(fmaf(__uint_as_float(v[2 * i + 1]), cm, -ref));
-                    s0 += e0;
-                    s1 += e1;
-                    w[i] = h2(e0, e1);
+                    float2 e = fma2(make_float2(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), cm2, ref2);
+                    e.x = ex2(e.x);
+                    e.y = ex2(e.y);
+                    s2[i & 1] = add2(s2[i & 1], e);
+                    w[i] = h2(e.x, e.y);
                 }
-                sum += s0 + s1;
-                tmem_st16(t_s + c0 / 2, w);                  // over columns whose scores have been read
+                tmem_st16(t_s + 16 * c, w);                  // over the scores, which have all been read
             }
+            sum += (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
             tmem_st_wait();
             tc_fence_before_sync();
             __syncwarp();
@@ -359,6 +392,7 @@ kv4_prefill_kernel(const PreParams p)
         }
         tc_fence_before_sync();
     } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         // ================= numbers from codes =================
         const int w4 = warp - 8, j = lane & 3, idx = lane >> 2;
         int st = 0;
@@ -371,24 +405,21 @@ kv4_prefill_kernel(const PreParams p)
             const uint8_t* src = smem + L::kStg + st * L::kPacked;
             uint8_t* dst = smem + L::kK + buf * L::kTile;
             const int kr = (idx >> 1) + 4 * (idx & 1);
+            Words<W> code[4], sb[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = i * 32 + w4 * 8 + kr, pos = key & 15;
                 const uint8_t* blk = src + (key >> 4) * (10 * D);
-                uint32_t code[W], sb[W];
-                if constexpr (W == 4) {
-                    const uint4 cw = *reinterpret_cast<const uint4*>(blk + pos * (D / 2) + j * 16), sw = *reinterpret_cast<const uint4*>(blk + 8 * D + pos * (D / 8));
-                    code[0] = cw.x; code[1] = cw.y; code[2] = cw.z; code[3] = cw.w;
-                    sb[0] = sw.x; sb[1] = sw.y; sb[2] = sw.z; sb[3] = sw.w;
-                } else {
-                    const uint2 cw = *reinterpret_cast<const uint2*>(blk + pos * (D / 2) + j * 8), sw = *reinterpret_cast<const uint2*>(blk + 8 * D + pos * (D / 8));
-                    code[0] = cw.x; code[1] = cw.y;
-                    sb[0] = sw.x; sb[1] = sw.y;
-                }
+                code[i] = *reinterpret_cast<const Words<W>*>(blk + pos * (D / 2) + j * 4 * W);
+                sb[i] = *reinterpret_cast<const Words<W>*>(blk + 8 * D + pos * (D / 8));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = i * 32 + w4 * 8 + kr;
 #pragma unroll
                 for (int w = 0; w < W; ++w)
                     *reinterpret_cast<uint4*>(dst + (w >> 1) * 16384 + key * 128 + (((4 * (w & 1) + j) ^ (key & 7)) << 4)) =
-                        numbers(code[w], __byte_perm(sb[w], 0, 0x1010), __byte_perm(sb[w], 0, 0x3232));
+                        numbers(code[i].w[w], __byte_perm(sb[i].w[w], 0, 0x1010), __byte_perm(sb[i].w[w], 0, 0x3232));
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -398,27 +429,30 @@ kv4_prefill_kernel(const PreParams p)
             if (!(ok = mbar_wait(&stg_full[st], sph, ctl) && mbar_wait(&v_empty[buf], ph[buf] ^ 1, ctl))) break;
             src = smem + L::kStg + st * L::kPacked;
             dst = smem + L::kV + buf * L::kTile;
+            const int turn = W == 4 ? j & 2 : 0;             // the words of a lane in the order n ^ turn
+            uint32_t sv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = i * 32 + w4 * 8 + idx, pos = key & 15;
                 const uint8_t* blk = src + (key >> 4) * (10 * D);
-                if constexpr (W == 4) {
-                    uint4 cw = *reinterpret_cast<const uint4*>(blk + pos * (D / 2) + j * 16);
-                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + 8 * D + pos * (D / 8) + j * 4);
-                    const uint32_t step = __byte_perm(sb, 0, 0x1010), base = __byte_perm(sb, 0, 0x3232);
-                    const int turn = j & 2;                  // numbers 32 j + 8 (i ^ turn) .. at turn i
-                    if (turn) cw = make_uint4(cw.z, cw.w, cw.x, cw.y);
-                    const uint32_t code[4] = {cw.x, cw.y, cw.z, cw.w};
+                code[i] = *reinterpret_cast<const Words<W>*>(blk + pos * (D / 2) + j * 4 * W);
+                sv[i] = *reinterpret_cast<const uint32_t*>(blk + 8 * D + pos * (D / 8) + j * W / 4 * 4);
+            }
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
-                        *reinterpret_cast<uint4*>(dst + (j >> 1) * 16384 + key * 128 + (((4 * (j & 1) + (n ^ turn)) ^ (key & 7)) << 4)) =
-                            numbers(code[n], step, base);
-                } else {
-                    const uint2 cw = *reinterpret_cast<const uint2*>(blk + pos * (D / 2) + j * 8);
-                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + 8 * D + pos * (D / 8) + (j >> 1) * 4);
-                    const uint32_t step = __byte_perm(sb, 0, 0x1010), base = __byte_perm(sb, 0, 0x3232);
-                    *reinterpret_cast<uint4*>(dst + key * 128 + (((2 * j) ^ (key & 7)) << 4)) = numbers(cw.x, step, base);
-                    *reinterpret_cast<uint4*>(dst + key * 128 + (((2 * j + 1) ^ (key & 7)) << 4)) = numbers(cw.y, step, base);
+            for (int i = 0; i < 4; ++i) {
+                const int key = i * 32 + w4 * 8 + idx;
+                const uint32_t step = __byte_perm(sv[i], 0, 0x1010), base = __byte_perm(sv[i], 0, 0x3232);
+                if constexpr (W == 4) {
+                    if (turn) {
+                        const uint32_t a0 = code[i].w[0], a1 = code[i].w[1];
+                        code[i].w[0] = code[i].w[2]; code[i].w[1] = code[i].w[3];
+                        code[i].w[2] = a0; code[i].w[3] = a1;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < W; ++n) {                // numbers 8 W j + 8 (n ^ turn) ..
+                    const int unit = W * j + (n ^ turn);
+                    *reinterpret_cast<uint4*>(dst + (unit >> 3) * 16384 + key * 128 + (((unit & 7) ^ (key & 7)) << 4)) = numbers(code[i].w[n], step, base);
                 }
             }
             fence_proxy_async_smem();
@@ -427,7 +461,9 @@ kv4_prefill_kernel(const PreParams p)
             if (++st == L::kStages) { st = 0; sph ^= 1; }
             ph[buf] ^= 1;
         }
-    } else if (warp == 12) {
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+      if (warp == 12) {
         // ================= products =================
         if (elect_one() && k_hi > k_lo) {
             constexpr uint32_t kQk = idesc_f16(PRE_ROWS, PRE_KEYS, false), kPv = idesc_f16(PRE_ROWS, D, true);
@@ -486,7 +522,7 @@ kv4_prefill_kernel(const PreParams p)
             for (int n = 0; n < (1 << 16) && !mbar_try_wait_64(&drained, 0); ++n) { }
         }
         __syncwarp();
-    } else {
+      } else if (warp == 13) {
         // ================= packed positions: lane i copies block i of a tile, keys and values in turn =================
         const int per_page = p.g.page_tokens / KV4_BLOCK;
         int st = 0;
@@ -520,6 +556,7 @@ kv4_prefill_kernel(const PreParams p)
             for (int i = 0; i < L::kStages; ++i)
                 for (int n = 0; n < 4096 && !mbar_try_wait_64(&stg_full[i], i < st ? ph : ph ^ 1); ++n) { }
         __syncwarp();
+      }
     }
     tc_fence_before_sync();
     __syncthreads();
