@@ -192,39 +192,11 @@ kv4_prefill_kernel(const PreParams p)
         o_done[2], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ uint8_t hidden[PRE_HIDE];
+    __shared__ float row_up[2][PRE_ROWS];     // a row's factor: c times its power of two
+    __shared__ int2 row_at[2][PRE_ROWS];      // its row of the call and first number there; -1: none
     __shared__ int ctl_[2];
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    // ---- which rows: pairs of tiles with the most positions first ----
-    pdl_launch_dependents();
-    pdl_wait();
-    const int per = p.g.heads * p.b.n_seq;
-    const int pair = p.tiles - 1 - (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
-    const int head = rest % p.g.heads, s = rest / p.g.heads;
-    const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
-    const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
-    const int row_base = pair * 2 * PRE_ROWS;
-    if (row_base >= n_rows) return;
-    const int len = p.b.seq_len[s];
-    const long long room = (long long)p.b.max_pages * p.g.page_tokens;
-    if (len > room && threadIdx.x == 0) atomicOr(p.status, KV4_DEV_INDEX);
-    const int len_in = (int)max(0LL, min((long long)len, room));
-    const int pos0 = len - all;                             // position of the sequence's first row
-    auto row_hi = [&](int row) { return p.causal ? max(0, min(pos0 + row / p.group + 1, len_in)) : len_in; };
-    auto row_lo = [&](int row) { return p.window ? max(0, pos0 + row / p.group - p.window + 1) : 0; };
-    int t_lo[2], t_hi[2];                                   // tiles of positions [t_lo, t_hi) that each row tile sees
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int r0 = row_base + x * PRE_ROWS, r1 = min(r0 + PRE_ROWS, n_rows) - 1;
-        t_lo[x] = t_hi[x] = 0;
-        if (r1 >= r0 && row_hi(r1) > row_lo(r0)) {
-            t_lo[x] = row_lo(r0) / PRE_KEYS;
-            t_hi[x] = (row_hi(r1) + PRE_KEYS - 1) / PRE_KEYS;
-        }
-    }
-    const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
-    const int k_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), k_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kStages; ++i) { mbar_init(&stg_full[i], 8); mbar_init(&stg_empty[i], 4); }
@@ -243,6 +215,37 @@ kv4_prefill_kernel(const PreParams p)
         ctl[1] = kWaitLimitDefault;
         fence_mbar_init();
     }
+    // ---- which rows: pairs of tiles with the most positions first ----
+    pdl_launch_dependents();
+    pdl_wait();
+    const int per = p.g.heads * p.b.n_seq;
+    const int pair = p.tiles - 1 - (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
+    const int head = rest % p.g.heads, s = rest / p.g.heads;
+    const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
+    const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
+    const int row_base = pair * 2 * PRE_ROWS;
+    if (row_base >= n_rows) return;
+    const int len = p.b.seq_len[s];
+    const long long room = (long long)p.b.max_pages * p.g.page_tokens;
+    if (len > room && threadIdx.x == 0) atomicOr(p.status, KV4_DEV_INDEX);
+    const int len_in = (int)max(0LL, min((long long)len, room));
+    const int pos0 = len - all;                             // position of the sequence's first row
+    auto token_hi = [&](int token) { return p.causal ? max(0, min(pos0 + token + 1, len_in)) : len_in; };
+    auto token_lo = [&](int token) { return p.window ? max(0, pos0 + token - p.window + 1) : 0; };
+    int t_lo[2], t_hi[2];                                   // tiles of positions [t_lo, t_hi) that each row tile sees
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int r0 = row_base + x * PRE_ROWS, r1 = min(r0 + PRE_ROWS, n_rows) - 1;
+        t_lo[x] = t_hi[x] = 0;
+        const int lo = token_lo(r0 / p.group), hi = token_hi(r1 / p.group);
+        if (r1 >= r0 && hi > lo) {
+            t_lo[x] = lo / PRE_KEYS;
+            t_hi[x] = (hi + PRE_KEYS - 1) / PRE_KEYS;
+        }
+    }
+    const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
+    const int k_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), k_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
+
     if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
@@ -255,37 +258,46 @@ kv4_prefill_kernel(const PreParams p)
         const int x = warp >> 2, r = threadIdx.x & 127, row = row_base + x * PRE_ROWS + r;
         const bool live = row < n_rows;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const int wrow = r & ~31;                           // the warp's first row of the tile
+        const int token = row / p.group;
+        row_at[x][r] = make_int2(live ? first + token : -1, (head * p.group + row - token * p.group) * D);
+        __syncwarp();
+        uint8_t* own = smem + L::kQ + x * L::kTile;
         float cm;
-        {   // the row of q, divided by the power of two at or below its largest (2^-60 at least)
-            const __nv_bfloat16* src = p.q + (long long)(first + (live ? row / p.group : 0)) * p.ldq +
-                                       (long long)(head * p.group + (live ? row % p.group : 0)) * D;
-            float top = 0.0f;
-            uint4 v[D / 8];
+        {   // Q: the warp's 32 rows, D / 8 lanes a row, each row divided by the power of two at or below its largest (2^-60 at least)
+            constexpr int LANES = D / 8, ROWS = 32 / LANES;
+            const int u = lane % LANES;
+            uint4 v[LANES];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                v[i] = live ? *reinterpret_cast<const uint4*>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < LANES; ++i) {
+                const int2 from = row_at[x][wrow + i * ROWS + lane / LANES];
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (from.x >= 0) v[i] = *reinterpret_cast<const uint4*>(p.q + from.x * p.ldq + from.y + 8 * u);
+            }
+#pragma unroll
+            for (int i = 0; i < LANES; ++i) {
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                float top = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
-            }
-            const int e = min(max((int)(__float_as_uint(top) >> 23), 67), 253) - 127;
-            const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
-            cm = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
-            uint8_t* to = smem + L::kQ + x * L::kTile + r * 128;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const int e = min(max((int)(__float_as_uint(top) >> 23), 67), 253) - 127;
+                const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
+                const int rr = wrow + i * ROWS + lane / LANES;
+                if (u == 0) row_up[x][rr] = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
                 uint32_t h[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * down, __uint_as_float(w[k] & 0xffff0000u) * down);
-                *reinterpret_cast<uint4*>(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(own + (u >> 3) * 16384 + rr * 128 + (((u & 7) ^ (rr & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
             fence_proxy_async_smem();
             __syncwarp();
+            cm = row_up[x][r];
             if (lane == 0) mbar_arrive(&q_full);
         }
-        const int lo = live ? row_lo(row) : 0, hi = live ? row_hi(row) : 0x7fffffff;
+        const int lo = live ? token_lo(token) : 0, hi = live ? token_hi(token) : 0x7fffffff;
         const int all_lo = __reduce_max_sync(0xffffffffu, lo), all_hi = __reduce_min_sync(0xffffffffu, hi);
         const uint32_t t_s = t_lane + 128u * x, t_o = t_lane + 256u + 128u * x;
         float ref = kNone, sum = 0.0f;
@@ -367,8 +379,10 @@ kv4_prefill_kernel(const PreParams p)
         tc_fence_after_sync();
         if (ok) {
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            __nv_bfloat16* to = p.out + (long long)(first + (live ? row / p.group : 0)) * p.ldo +
-                                (long long)(head * p.group + (live ? row % p.group : 0)) * D;
+            // Through the tile's own Q, which the products are done with: the warp's 32 rows, 16 bytes of a row at unit
+            // u ^ row, then D / 8 lanes a row.
+            constexpr int LANES = D / 8, ROWS = 32 / LANES;
+            uint8_t* mine = own + wrow * (2 * D);
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t v[32] = {};
@@ -376,18 +390,25 @@ kv4_prefill_kernel(const PreParams p)
                     tmem_ld32(t_o + c0, v);
                     tmem_ld_wait();
                 }
-                if (live) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t w[4];
+                for (int i = 0; i < 32; i += 8) {
+                    uint32_t w[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v[i + 2 * k]) * inv, __uint_as_float(v[i + 2 * k + 1]) * inv);
-                            w[k] = *reinterpret_cast<const uint32_t*>(&y);
-                        }
-                        *reinterpret_cast<uint4*>(to + c0 + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        const __nv_bfloat162 y = __floats2bfloat162_rn(__uint_as_float(v[i + 2 * k]) * inv, __uint_as_float(v[i + 2 * k + 1]) * inv);
+                        w[k] = *reinterpret_cast<const uint32_t*>(&y);
                     }
+                    *reinterpret_cast<uint4*>(mine + lane * (2 * D) + ((((c0 + i) >> 3) ^ (lane & (LANES - 1))) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < LANES; ++i) {
+                const int rl = i * ROWS + lane / LANES, u = lane % LANES;
+                const int2 at = row_at[x][wrow + rl];
+                if (at.x >= 0)
+                    *reinterpret_cast<uint4*>(p.out + at.x * p.ldo + at.y + 8 * u) =
+                        *reinterpret_cast<const uint4*>(mine + rl * (2 * D) + ((u ^ (rl & (LANES - 1))) << 4));
             }
         }
         tc_fence_before_sync();
