@@ -10,7 +10,8 @@
 //               contiguous, values likewise: the second product takes them as an MN-major operand, so nothing is transposed)
 //   warp 12     issues tcgen05.mma: scores S = Q K^T into tensor memory, then O += P V with P from tensor memory
 //   warps 0-3 and 4-7, one row a thread: running maximum, exponentials, P as fp16 over S's own columns, the sum
-// The two row tiles alternate, so that the products of one run while the other's exponentials do.  A row's reference moves
+// A step is 64 positions.  Each row tile has two score buffers: the scores of the next step are formed while a step's
+// exponentials run, so a row never waits for a product.  A row's reference moves
 // only when a score passes the one it was set by by more than 5 (log2), so that O, which stays in tensor memory, is seldom rescaled.
 //
 // Arithmetic: q as fp16 after division by a power of two per row (exact down to 2^-24 of the row's largest; the power goes
@@ -24,12 +25,10 @@ namespace {
 
 using namespace ptx;
 
-constexpr int PRE_THREADS = 16 * 32;     // four warpgroups (14 warps have work)
-// Registers: 512 threads x 128 at launch; the rows' two warpgroups take 184 a thread, the others keep 72.
-constexpr int kRegsRows = 184, kRegsRest = 72;
-static_assert(256 * kRegsRows + 256 * kRegsRest <= PRE_THREADS * 128, "more than the block was launched with would wait for ever");
+constexpr int PRE_THREADS = 14 * 32;
 constexpr int PRE_ROWS = 128;            // rows of a tile
 constexpr int PRE_KEYS = 128;            // positions of a tile
+constexpr int PRE_STEP = 64;             // positions of a step: half a tile
 constexpr int PRE_HIDE = 8;              // tiles whose hidden blocks are remembered: more than any copy can be ahead
 // Probabilities are 2^(score - reference): 2^10 where the reference was set, up to 2^15 before it moves, so that fp16
 // reaches down to 2^-35 of it.
@@ -188,8 +187,8 @@ kv4_prefill_kernel(const PreParams p)
     constexpr int W = D / KV4_GROUP;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    __shared__ uint64_t stg_full[L::kStages], stg_empty[L::kStages], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full[2], p_full[2],
-        o_done[2], drained;
+    __shared__ uint64_t stg_full[L::kStages], stg_empty[L::kStages], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full, s_full[2][2], p_full[2][2],
+        o_done[2][2], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ uint8_t hidden[PRE_HIDE];
     __shared__ float row_up[2][PRE_ROWS];     // a row's factor: c times its power of two
@@ -205,9 +204,7 @@ kv4_prefill_kernel(const PreParams p)
             mbar_init(&k_empty[i], 1);
             mbar_init(&v_full[i], 4);
             mbar_init(&v_empty[i], 1);
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
-            mbar_init(&o_done[i], 1);
+            for (int h = 0; h < 2; ++h) { mbar_init(&s_full[i][h], 1); mbar_init(&p_full[i][h], 4); mbar_init(&o_done[i][h], 1); }
         }
         mbar_init(&q_full, 8);
         mbar_init(&drained, 1);
@@ -232,28 +229,28 @@ kv4_prefill_kernel(const PreParams p)
     const int pos0 = len - all;                             // position of the sequence's first row
     auto token_hi = [&](int token) { return p.causal ? max(0, min(pos0 + token + 1, len_in)) : len_in; };
     auto token_lo = [&](int token) { return p.window ? max(0, pos0 + token - p.window + 1) : 0; };
-    int t_lo[2], t_hi[2];                                   // tiles of positions [t_lo, t_hi) that each row tile sees
+    int t_lo[2], t_hi[2];                                   // steps [t_lo, t_hi) that each row tile sees
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int r0 = row_base + x * PRE_ROWS, r1 = min(r0 + PRE_ROWS, n_rows) - 1;
         t_lo[x] = t_hi[x] = 0;
         const int lo = token_lo(r0 / p.group), hi = token_hi(r1 / p.group);
         if (r1 >= r0 && hi > lo) {
-            t_lo[x] = lo / PRE_KEYS;
-            t_hi[x] = (hi + PRE_KEYS - 1) / PRE_KEYS;
+            t_lo[x] = lo / PRE_STEP;
+            t_hi[x] = (hi + PRE_STEP - 1) / PRE_STEP;
         }
     }
     const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
-    const int k_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), k_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
+    const int j_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), j_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
+    const int k_lo = j_lo / 2, k_hi = (j_hi + 1) / 2;       // tiles
 
     if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = tmem_slot;                        // S or P of tile x: column 128 x; O: column 256 + 128 x
+    const uint32_t tmem = tmem_slot;                        // S or P of tile x, buffer h: column 128 x + 64 h; O: column 256 + 128 x
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRows));
         // ================= rows: one a thread =================
         const int x = warp >> 2, r = threadIdx.x & 127, row = row_base + x * PRE_ROWS + r;
         const bool live = row < n_rows;
@@ -299,48 +296,48 @@ kv4_prefill_kernel(const PreParams p)
         }
         const int lo = live ? token_lo(token) : 0, hi = live ? token_hi(token) : 0x7fffffff;
         const int all_lo = __reduce_max_sync(0xffffffffu, lo), all_hi = __reduce_min_sync(0xffffffffu, hi);
-        const uint32_t t_s = t_lane + 128u * x, t_o = t_lane + 256u + 128u * x;
+        const uint32_t t_o = t_lane + 256u + 128u * x;
         float ref = kNone, sum = 0.0f;
-        uint32_t ph = 0;
+        uint32_t pho = 0, phs = 0;                          // of o_done and of s_full (bit h: odd steps have barriers of their own)
         bool ok = true;
         const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
         for (int k = a; k < b; ++k) {
-            if (!(ok = mbar_wait(&s_full[x], ph, ctl))) break;
+            const int h = k & 1, at = k * PRE_STEP;
+            if (!(ok = mbar_wait(&s_full[x][h], phs >> h & 1, ctl))) break;
+            phs ^= 1u << h;
             tc_fence_after_sync();
-            const int at = k * PRE_KEYS;
-            const uint32_t hide = hidden[k % PRE_HIDE];
-            const bool edge = at < all_lo || at + PRE_KEYS > all_hi || hide;
-            uint32_t v[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, v[c]);
+            const uint32_t t_s = t_lane + 128u * x + 64u * h;
+            uint32_t v[2][32];
+            tmem_ld32(t_s, v[0]);
+            tmem_ld32(t_s + 32, v[1]);
+            const uint32_t hide = hidden[(k >> 1) % PRE_HIDE] >> (4 * h) & 15;
+            const bool edge = at < all_lo || at + PRE_STEP > all_hi || hide;
             tmem_ld_wait();
             if (edge) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const int pos = at + 32 * c + i;
                         if (pos < lo || pos >= hi || (hide >> (2 * c + (i >> 4)) & 1)) v[c][i] = 0xff800000u;
                     }
             }
-            float top;
-            {
-                float m[4];
+            float m[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    m[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t* w = v[c >> 1] + 16 * (c & 1);
+                m[c] = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 #pragma unroll
-                    for (int i = 2; i < 32; i += 2) m[c] = max3(m[c], __uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1]));
-                }
-                top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * cm;
+                for (int i = 2; i < 16; i += 2) m[c] = max3(m[c], __uint_as_float(w[i]), __uint_as_float(w[i + 1]));
             }
+            const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * cm;
             const bool over = top > ref + kMove;
             if (__any_sync(0xffffffffu, over)) {
                 const float to = over ? top - kSet : ref, keep = ex2(ref - to);    // 0 before the first score
                 ref = to;
                 sum *= keep;
                 if (k > a) {
-                    if (!(ok = mbar_wait(&o_done[x], ph ^ 1, ctl))) break;   // the product of the tile before
+                    if (!(ok = mbar_wait(&o_done[x][h ^ 1], (pho >> (h ^ 1) & 1) ^ 1, ctl))) break;   // the product of the step before
                     tc_fence_after_sync();
 #pragma unroll 1
                     for (int c0 = 0; c0 < D; c0 += 16) {
@@ -356,7 +353,7 @@ kv4_prefill_kernel(const PreParams p)
             const float2 cm2 = make_float2(cm, cm), ref2 = make_float2(-ref, -ref);
             float2 s2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -372,10 +369,10 @@ kv4_prefill_kernel(const PreParams p)
             tmem_st_wait();
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[x]);
-            ph ^= 1;
+            if (lane == 0) mbar_arrive(&p_full[x][h]);
+            pho ^= 1u << h;
         }
-        if (ok && b > a) ok = mbar_wait(&o_done[x], ph ^ 1, ctl);
+        if (ok && b > a) ok = mbar_wait(&o_done[x][(b - 1) & 1], (pho >> ((b - 1) & 1) & 1) ^ 1, ctl);
         tc_fence_after_sync();
         if (ok) {
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -413,7 +410,6 @@ kv4_prefill_kernel(const PreParams p)
         }
         tc_fence_before_sync();
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         // ================= numbers from codes =================
         const int w4 = warp - 8, j = lane & 3, idx = lane >> 2;
         int st = 0;
@@ -483,60 +479,58 @@ kv4_prefill_kernel(const PreParams p)
             ph[buf] ^= 1;
         }
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
       if (warp == 12) {
         // ================= products =================
         if (elect_one() && k_hi > k_lo) {
-            constexpr uint32_t kQk = idesc_f16(PRE_ROWS, PRE_KEYS, false), kPv = idesc_f16(PRE_ROWS, D, true);
+            constexpr uint32_t kQk = idesc_f16(PRE_ROWS, PRE_STEP, false), kPv = idesc_f16(PRE_ROWS, D, true);
             const uint32_t base = smem_u32(smem);
-            auto scores = [&](int x, int buf) {
+            // Descriptors count addresses in 16 bytes, so that a step is one addition.
+            const uint64_t desc_q = umma_desc_k_sw128(base + L::kQ), desc_k = umma_desc_k_sw128(base + L::kK), desc_v = umma_desc_mn_sw128(base + L::kV, 16384u);
+            // step j of row tile x: half j & 1 of the tile of positions in stage (j / 2 - k_lo) & 1
+            auto scores = [&](int x, int j) {
+                const uint64_t q = desc_q + (uint32_t)(x * (L::kTile >> 4));
+                const uint64_t keys = desc_k + (uint32_t)((((j >> 1) - k_lo) & 1) * (L::kTile >> 4) + (j & 1) * (PRE_STEP * 128 >> 4));
+                const uint32_t to = tmem + 128u * x + 64u * (j & 1);
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {           // 16 numbers a step: 32 bytes of a 128-byte row
-                    const uint32_t at = (uint32_t)(i >> 2) * 16384u + (uint32_t)(i & 3) * 32u;
-                    umma_f16_ss(tmem + 128u * x, umma_desc_k_sw128(base + L::kQ + x * L::kTile + at), umma_desc_k_sw128(base + L::kK + buf * L::kTile + at),
-                                kQk, i > 0);
+                for (int i = 0; i < D / 16; ++i) {           // 16 numbers at a time: 32 bytes of a 128-byte row
+                    const uint32_t at = (uint32_t)((i >> 2) * (16384 >> 4) + (i & 3) * 2);
+                    umma_f16_ss(to, q + at, keys + at, kQk, i > 0);
                 }
-                umma_commit(&s_full[x]);
+                umma_commit(&s_full[x][j & 1]);
             };
-            auto values = [&](int x, int buf, bool more) {
+            auto values = [&](int x, int j, bool more) {
+                const uint64_t vals = desc_v + (uint32_t)((((j >> 1) - k_lo) & 1) * (L::kTile >> 4) + (j & 1) * (PRE_STEP * 128 >> 4));
+                const uint32_t to = tmem + 256u + 128u * x, probs = tmem + 128u * x + 64u * (j & 1);
 #pragma unroll
-                for (int i = 0; i < PRE_KEYS / 16; ++i)      // 16 positions a step: 16 rows of values, 8 columns of P
-                    umma_f16_ts(tmem + 256u + 128u * x, tmem + 128u * x + 8u * i,
-                                umma_desc_mn_sw128(base + L::kV + buf * L::kTile + (uint32_t)i * 2048u, 16384u), kPv, more || i > 0);
-                umma_commit(&o_done[x]);
+                for (int i = 0; i < PRE_STEP / 16; ++i)      // 16 positions at a time: 16 rows of values, 8 columns of P
+                    umma_f16_ts(to, probs + 8u * i, vals + (uint32_t)(i * (2048 >> 4)), kPv, more || i > 0);
+                umma_commit(&o_done[x][j & 1]);
             };
-            bool ok = mbar_wait(&q_full, 0, ctl) && mbar_wait(&k_full[0], 0, ctl);
-            uint32_t pph[2] = {0, 0};
-            if (ok) {
-                tc_fence_after_sync();
+            bool ok = mbar_wait(&q_full, 0, ctl);
+            uint32_t pph[2] = {0, 0};                        // phases of p_full (bit h)
+            for (int j = 2 * k_lo - 1; j < j_hi && ok; ++j) {
+                // the scores of the next step, then the values of this one
+                const int n = j + 1;
+                if (n < j_hi) {
+                    if (!(n & 1) && !(ok = mbar_wait(&k_full[((n >> 1) - k_lo) & 1], (uint32_t)((n >> 1) - k_lo) >> 1 & 1, ctl))) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (n >= t_lo[x] && n < t_hi[x]) scores(x, n);
+                    if (n & 1) umma_commit(&k_empty[((n >> 1) - k_lo) & 1]);
+                }
+                if (j < 2 * k_lo) continue;
+                if (!(j & 1) && !(ok = mbar_wait(&v_full[((j >> 1) - k_lo) & 1], (uint32_t)((j >> 1) - k_lo) >> 1 & 1, ctl))) break;
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    if (t_lo[x] == k_lo && t_hi[x] > k_lo) scores(x, 0);
-                umma_commit(&k_empty[0]);
-            }
-            for (int k = k_lo; k < k_hi && ok; ++k) {
-                const int i = k - k_lo, buf = i & 1, nbuf = buf ^ 1;
-                const uint32_t ph = (uint32_t)(i >> 1) & 1, nph = (uint32_t)((i + 1) >> 1) & 1;
-                if (!(ok = mbar_wait(&v_full[buf], ph, ctl))) break;
-                bool have = false;                           // the next keys
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (k >= t_lo[x] && k < t_hi[x]) {
-                        if (!(ok = mbar_wait(&p_full[x], pph[x], ctl))) break;
-                        pph[x] ^= 1;
+                    if (j >= t_lo[x] && j < t_hi[x]) {
+                        if (!(ok = mbar_wait(&p_full[x][j & 1], pph[x] >> (j & 1) & 1, ctl))) break;
+                        pph[x] ^= 1u << (j & 1);
                         tc_fence_after_sync();
-                        values(x, buf, k > t_lo[x]);
+                        values(x, j, j > t_lo[x]);
                     }
-                    if (k + 1 >= t_lo[x] && k + 1 < t_hi[x]) {
-                        if (!have && !(ok = mbar_wait(&k_full[nbuf], nph, ctl))) break;
-                        have = true;
-                        tc_fence_after_sync();
-                        scores(x, nbuf);
-                    }
-                }
                 if (!ok) break;
-                umma_commit(&v_empty[buf]);
-                if (k + 1 < k_hi) umma_commit(&k_empty[nbuf]);
+                if (j & 1) umma_commit(&v_empty[((j >> 1) - k_lo) & 1]);
             }
             // every product has ended before the block does
             umma_commit(&drained);
