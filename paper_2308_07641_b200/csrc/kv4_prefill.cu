@@ -14,8 +14,8 @@
 // exponentials run, so a row never waits for a product.  A row's reference moves
 // only when a score passes the one it was set by by more than 5 (log2), so that O, which stays in tensor memory, is seldom rescaled.
 //
-// Arithmetic: q as fp16 after division by a power of two per row (exact down to 2^-24 of the row's largest; the power goes
-// into the row's factor c), keys and values as fp16 (one rounding), probabilities as fp16, sums in fp32.
+// Arithmetic: q as fp16 after division by a power of two for 32 rows together (exact down to 2^-24 of their largest number,
+// which is far below what a score can show; the power goes into the factor c), keys and values as fp16 (one rounding), probabilities as fp16, sums in fp32.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -191,7 +191,6 @@ kv4_prefill_kernel(const PreParams p)
         o_done[2][2], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ uint8_t hidden[PRE_HIDE];
-    __shared__ float row_up[2][PRE_ROWS];     // a row's factor: c times its power of two
     __shared__ int2 row_at[2][PRE_ROWS];      // its row of the call and first number there; -1: none
     __shared__ int ctl_[2];
     volatile int* ctl = ctl_;
@@ -221,8 +220,8 @@ kv4_prefill_kernel(const PreParams p)
     const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
     const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
     const int row_base = pair * 2 * PRE_ROWS;
-    if (row_base >= n_rows) return;
     const int len = p.b.seq_len[s];
+    if (row_base >= n_rows) return;
     const long long room = (long long)p.b.max_pages * p.g.page_tokens;
     if (len > room && threadIdx.x == 0) atomicOr(p.status, KV4_DEV_INDEX);
     const int len_in = (int)max(0LL, min((long long)len, room));
@@ -261,7 +260,7 @@ kv4_prefill_kernel(const PreParams p)
         __syncwarp();
         uint8_t* own = smem + L::kQ + x * L::kTile;
         float cm;
-        {   // Q: the warp's 32 rows, D / 8 lanes a row, each row divided by the power of two at or below its largest (2^-60 at least)
+        {   // Q: the warp's 32 rows, D / 8 lanes a row, divided by the power of two at or below their largest number (2^-60 at least)
             constexpr int LANES = D / 8, ROWS = 32 / LANES;
             const int u = lane % LANES;
             uint4 v[LANES];
@@ -271,19 +270,18 @@ kv4_prefill_kernel(const PreParams p)
                 v[i] = make_uint4(0, 0, 0, 0);
                 if (from.x >= 0) v[i] = *reinterpret_cast<const uint4*>(p.q + from.x * p.ldq + from.y + 8 * u);
             }
+            uint32_t top = 0;                               // magnitudes compared as 16-bit integers, two at a time
+#pragma unroll
+            for (int i = 0; i < LANES; ++i)
+                top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu)), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
+            top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+            const int e = min(max((int)(top >> 7), 67), 253) - 127;
+            const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
+            cm = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                float top = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u))));
-#pragma unroll
-                for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const int e = min(max((int)(__float_as_uint(top) >> 23), 67), 253) - 127;
-                const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
                 const int rr = wrow + i * ROWS + lane / LANES;
-                if (u == 0) row_up[x][rr] = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
                 uint32_t h[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * down, __uint_as_float(w[k] & 0xffff0000u) * down);
@@ -291,7 +289,6 @@ kv4_prefill_kernel(const PreParams p)
             }
             fence_proxy_async_smem();
             __syncwarp();
-            cm = row_up[x][r];
             if (lane == 0) mbar_arrive(&q_full);
         }
         const int lo = live ? token_lo(token) : 0, hi = live ? token_hi(token) : 0x7fffffff;
