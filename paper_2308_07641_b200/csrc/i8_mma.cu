@@ -15,6 +15,7 @@ using namespace ptx;
 constexpr int I8_THREADS = 192;          // warps 0-3: epilogue; 4: copies; 5: tensor memory and MMA issue
 constexpr int I8_MAX_STAGES = 12;
 constexpr int I8_SMEM_LIMIT = 227 * 1024;
+constexpr int I8_OUT_BYTES = 2 * 16 * 128 * 4;   // results on their way out: 16 tokens of 128 channels, twice
 
 struct I8Params {
     const int8_t* W;
@@ -24,11 +25,12 @@ struct I8Params {
     const float* bias;       // the same, or null
     void* y;
     long long ldy;
-    int y_bf16;
+    int y_bf16, y_wide;      // y_wide: rows start on 16-byte boundaries
     int M, B;
     int KB;                  // blocks of 128 columns
     int groups;              // groups of 8 tokens in x
     int row_tiles, tok_tiles, NT;
+    int band;                // row tiles of a band: a band's tiles are walked token tile by token tile
     int stages;
     int* status;
 };
@@ -38,11 +40,25 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v)
     asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
+__device__ __forceinline__ float scaled(const I8Params&, int sum, float xs, float ws, float bias)
+{
+    return __fadd_rn(__fmul_rn(__fmul_rn((float)sum, xs), ws), bias);
+}
 __device__ __forceinline__ void store_y(const I8Params& p, int b, int m, int sum, float xs, float ws, float bias)
 {
-    const float v = __fadd_rn(__fmul_rn(__fmul_rn((float)sum, xs), ws), bias);
+    const float v = scaled(p, sum, xs, ws, bias);
     if (p.y_bf16) reinterpret_cast<__nv_bfloat16*>(p.y)[(long long)b * p.ldy + m] = __float2bfloat16_rn(v);
     else reinterpret_cast<float*>(p.y)[(long long)b * p.ldy + m] = v;
+}
+
+// Tile `i` of the call: bands of row tiles one after another, so that the blocks that run at the same time share both the
+// weights and the tokens that they read.
+__device__ __forceinline__ void tile_at(const I8Params& p, int i, int& rt, int& tt)
+{
+    const int per_band = p.band * p.tok_tiles, b = i / per_band, in = i - b * per_band;
+    const int rows = min(p.band, p.row_tiles - b * p.band);
+    tt = in / rows;
+    rt = b * p.band + in - tt * rows;
 }
 
 // CL = 1: persistent, a block walks over tiles (row tile fastest), two accumulators.
@@ -83,17 +99,20 @@ i8_mma_kernel(const I8Params p)
             // The weights of the first stages are requested before the kernel that writes the tokens has ended.
             int s = 0, ahead = 0;
             uint32_t ph = 0;
-            const int rt0 = first % p.row_tiles;
+            int rt0 = 0, tt0 = 0;
+            tile_at(p, min(first, tiles - 1), rt0, tt0);
             if (first < tiles)
                 for (int kb = kb0; kb < kb1 && ahead < p.stages; ++kb, ++ahead) {
-                    const uint32_t tok = (uint32_t)min(p.NT, p.groups * 8 - first / p.row_tiles * p.NT);
+                    const uint32_t tok = (uint32_t)min(p.NT, p.groups * 8 - tt0 * p.NT);
                     mbar_arrive_expect_tx(&full[ahead], 16384u + tok * 128u);
                     bulk_g2s(smem + (size_t)ahead * stage_bytes, p.W + ((size_t)rt0 * p.KB + kb) * 16384, 16384u, &full[ahead]);
                 }
             pdl_wait();
             bool ok = true;
             for (int tile = first; tile < tiles && ok; tile += step) {
-                const int rt = tile % p.row_tiles, t0 = tile / p.row_tiles * p.NT;
+                int rt, t0;
+                tile_at(p, tile, rt, t0);
+                t0 *= p.NT;
                 const uint32_t tok = (uint32_t)min(p.NT, p.groups * 8 - t0);   // groups behind the last token are not copied
                 for (int kb = kb0; kb < kb1; ++kb) {
                     uint8_t* at = smem + (size_t)s * stage_bytes;
@@ -140,10 +159,13 @@ i8_mma_kernel(const I8Params p)
         }
     } else {
         pdl_wait();
-        int a = 0;
+        int a = 0, flip = 0;
         uint32_t aph = 0;
+        uint8_t* out_stage = smem + (size_t)p.stages * stage_bytes;
         for (int tile = first; tile < tiles; tile += step) {
-            const int rt = tile % p.row_tiles, t0 = tile / p.row_tiles * p.NT;
+            int rt, t0;
+            tile_at(p, tile, rt, t0);
+            t0 *= p.NT;
             const int n = min(p.NT, p.B - t0);
             const int m = rt * 128 + warp * 32 + lane;
             const float ws = p.w_scale[m], bias = p.bias ? p.bias[m] : 0.0f;
@@ -152,14 +174,48 @@ i8_mma_kernel(const I8Params p)
             const uint32_t src = tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)a * 256u;
             if constexpr (CL == 1) {
                 if (!ok) break;
-                for (int j0 = 0; j0 < n; j0 += 16) {
+                // Through shared memory, 16 tokens at a time: a lane has one channel of them, the output wants a token's
+                // channels together.
+                const int c = warp * 32 + lane, width = min(128, p.M - rt * 128);
+                for (int j0 = 0; j0 < n; j0 += 16, flip ^= 1) {
                     uint32_t r[16];
                     tmem_ld16(src + (uint32_t)j0, r);
-                    tmem_ld_wait();
-                    if (m < p.M) {
+                    float xs[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (j0 + j < n) store_y(p, t0 + j0 + j, m, (int)r[j], __ldg(p.x_scale + t0 + j0 + j), ws, bias);
+                    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(xs + 4 * j) = __ldg(reinterpret_cast<const float4*>(p.x_scale + t0 + j0) + j);
+                    tmem_ld_wait();
+                    uint8_t* chunk = out_stage + flip * 16 * 128 * 4;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float v = scaled(p, (int)r[j], xs[j], ws, bias);
+                        if (p.y_bf16) reinterpret_cast<__nv_bfloat16*>(chunk)[j * 128 + c] = __float2bfloat16_rn(v);
+                        else reinterpret_cast<float*>(chunk)[j * 128 + c] = v;
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");   // one barrier a chunk: the other buffer's readers are through before it
+                    const int rows = min(16, n - j0), size = p.y_bf16 ? 2 : 4;
+                    uint8_t* to = reinterpret_cast<uint8_t*>(p.y) + ((long long)(t0 + j0) * p.ldy + (long long)rt * 128) * size;
+                    if (p.y_wide) {
+                        const int units = 128 * size / 16;            // of a token
+                        for (int i = threadIdx.x; i < rows * units; i += 128) {
+                            const int j = i / units, u = i - j * units;
+                            const uint4 w = *reinterpret_cast<const uint4*>(chunk + i * 16);
+                            uint8_t* at = to + (long long)j * p.ldy * size + u * 16;
+                            if ((u + 1) * 16 <= width * size) {
+                                *reinterpret_cast<uint4*>(at) = w;
+                            } else {                                  // the ragged end of a row, 2 or 4 bytes at a time
+                                const uint32_t part[4] = {w.x, w.y, w.z, w.w};
+                                for (int e = 0; e < 16 / size; ++e)
+                                    if (u * 16 + (e + 1) * size <= width * size) {
+                                        if (size == 4) reinterpret_cast<uint32_t*>(at)[e] = part[e];
+                                        else reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(part[e >> 1] >> (16 * (e & 1)));
+                                    }
+                            }
+                        }
+                    } else if (c < width) {
+                        for (int j = 0; j < rows; ++j) {
+                            if (p.y_bf16) reinterpret_cast<__nv_bfloat16*>(to)[(long long)j * p.ldy + c] = reinterpret_cast<__nv_bfloat16*>(chunk)[j * 128 + c];
+                            else reinterpret_cast<float*>(to)[(long long)j * p.ldy + c] = reinterpret_cast<float*>(chunk)[j * 128 + c];
+                        }
                     }
                 }
                 tc_fence_before_sync();
@@ -175,7 +231,9 @@ i8_mma_kernel(const I8Params p)
         // 128/CL of the tile each), slot [source][token][row], in the ring's memory.
         constexpr int OWN = 128 / CL;
         const bool works = first < tiles;
-        const int rt = first % p.row_tiles, t0 = first / p.row_tiles * p.NT;
+        int rt, t0;
+        tile_at(p, min(first, tiles - 1), rt, t0);
+        t0 *= p.NT;
         const int n = works ? min(p.NT, p.B - t0) : 0;
         cluster_sync_all();
         const bool ok = ctl[0] == 0;
@@ -214,8 +272,9 @@ template <int CL>
 tsvd_status_t launch(I8Params p, int blocks, cudaStream_t st)
 {
     const size_t stage = 16384 + (size_t)p.NT * 128;
-    p.stages = (int)std::min<size_t>(I8_MAX_STAGES, (I8_SMEM_LIMIT - 2048) / stage);
-    size_t ring = p.stages * stage;
+    const size_t out = CL == 1 ? I8_OUT_BYTES : 0;
+    p.stages = (int)std::min<size_t>(I8_MAX_STAGES, (I8_SMEM_LIMIT - 2048 - out) / stage);
+    size_t ring = p.stages * stage + out;
     if (CL > 1) {
         const int longest = (p.KB + CL - 1) / CL;
         p.stages = std::min(p.stages, std::max(longest, 1));
@@ -253,6 +312,7 @@ tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_sc
     p.y = y;
     p.ldy = ldy;
     p.y_bf16 = y_bf16;
+    p.y_wide = ((uintptr_t)y & 15) == 0 && (B == 1 || ldy * (y_bf16 ? 2 : 4) % 16 == 0);
     p.M = h->M;
     p.B = B;
     p.KB = h->col_blocks;
@@ -274,6 +334,7 @@ tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_sc
             if (best < 0 || cost < best) { best = cost; p.NT = nt; p.tok_tiles = (int)tok; cl = c; }
         }
     }
+    p.band = std::min(p.row_tiles, (sms + p.tok_tiles - 1) / p.tok_tiles);
     const int tiles = p.row_tiles * p.tok_tiles;
     switch (cl) {
         case 8: return launch<8>(p, tiles * 8, st);

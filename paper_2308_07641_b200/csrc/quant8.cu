@@ -160,7 +160,7 @@ extern "C" tsvd_status_t tsvd_i8_pack(const int8_t* W, long long ldw, const floa
 static size_t i8_ws_bytes(const tsvd_i8_s* h, int B)
 {
     const size_t groups = ((size_t)B + 7) / 8;
-    return groups * 8 * ((size_t)h->col_blocks * 128 + sizeof(float));
+    return groups * 8 * ((size_t)h->col_blocks * 128 + sizeof(float)) + 64;   // scales are read 16 at a time
 }
 
 static tsvd_status_t i8_grow(tsvd_i8_s* h, int B)
