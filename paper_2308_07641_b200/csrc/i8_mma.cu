@@ -61,6 +61,21 @@ __device__ __forceinline__ void tile_at(const I8Params& p, int i, int& rt, int& 
     rt = b * p.band + in - tt * rows;
 }
 
+// The 128 threads of the results agree whether any of them gave up (a wait that runs out is not seen by all at the same time).
+__device__ __forceinline__ bool any_of_128(bool x)
+{
+    uint32_t y;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.red.or.pred q, 1, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(y)
+        : "r"((uint32_t)x)
+        : "memory");
+    return y != 0;
+}
+
 // CL = 1: persistent, a block walks over tiles (row tile fastest), two accumulators.
 // CL > 1: one tile for each cluster of CL blocks, which share its contraction and meet through distributed shared memory.
 template <int CL>
@@ -173,7 +188,7 @@ i8_mma_kernel(const I8Params p)
             tc_fence_after_sync();
             const uint32_t src = tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)a * 256u;
             if constexpr (CL == 1) {
-                if (!ok) break;
+                if (any_of_128(!ok)) break;
                 // Through shared memory, 16 tokens at a time: a lane has one channel of them, the output wants a token's
                 // channels together.
                 const int c = warp * 32 + lane, width = min(128, p.M - rt * 128);

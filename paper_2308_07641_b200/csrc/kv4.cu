@@ -87,6 +87,8 @@ template <typename T, bool VEC>
 __global__ void kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv,
                                   int* status)
 {
+    pdl_launch_dependents();
+    pdl_wait();
     const int row = blockIdx.x;
     const Place at = place_of_row(g, b, row, status);
     if (at.page < 0) return;
@@ -124,6 +126,8 @@ __global__ void kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k
 template <typename T, bool VEC>
 __global__ void kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __restrict__ v, long long ldv, int* status)
 {
+    pdl_launch_dependents();
+    pdl_wait();
     const int row = blockIdx.x;
     const Place at = place_of_row(g, b, row, status);
     const int words = g.dim / 8, items = 2 * g.heads * words;
@@ -214,7 +218,11 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
     const unsigned t = row_threads(h->g);
-    auto go = [&](auto kernel, auto* kp, auto* vp) { kernel<<<(unsigned)n_rows, t, 0, st>>>(h->g, b, kp, ldk, vp, ldv, h->dev_status); };
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto kernel, auto* kp, auto* vp) {
+        PdlLaunch l((unsigned)n_rows, t, 0, st);
+        e = cudaLaunchKernelEx(&l.cfg, kernel, h->g, b, kp, ldk, vp, ldv, h->dev_status);
+    };
     if (dtype == TSVD_F32) {
         if (vec) go(kv4_append_kernel<float, true>, (const float*)k, (const float*)v);
         else go(kv4_append_kernel<float, false>, (const float*)k, (const float*)v);
@@ -222,7 +230,7 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
         if (vec) go(kv4_append_kernel<__nv_bfloat16, true>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
         else go(kv4_append_kernel<__nv_bfloat16, false>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
     }
-    TSVD_CUDA_OK(cudaGetLastError());
+    TSVD_CUDA_OK(e);
     tsvd_count_launch();
     return TSVD_OK;
 }
@@ -244,7 +252,11 @@ extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, voi
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
     const unsigned t = row_threads(h->g);
-    auto go = [&](auto kernel, auto* kp, auto* vp) { kernel<<<(unsigned)n_rows, t, 0, st>>>(h->g, b, kp, ldk, vp, ldv, h->dev_status); };
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto kernel, auto* kp, auto* vp) {
+        PdlLaunch l((unsigned)n_rows, t, 0, st);
+        e = cudaLaunchKernelEx(&l.cfg, kernel, h->g, b, kp, ldk, vp, ldv, h->dev_status);
+    };
     if (dtype == TSVD_F32) {
         if (vec) go(kv4_read_kernel<float, true>, (float*)k, (float*)v);
         else go(kv4_read_kernel<float, false>, (float*)k, (float*)v);
@@ -252,7 +264,7 @@ extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, voi
         if (vec) go(kv4_read_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
         else go(kv4_read_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
     }
-    TSVD_CUDA_OK(cudaGetLastError());
+    TSVD_CUDA_OK(e);
     tsvd_count_launch();
     return TSVD_OK;
 }

@@ -11,6 +11,8 @@ template <typename T>
 __global__ void dequantize_rows_kernel(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale, int rows, int cols,
                                        T* __restrict__ y, long long ldy, bool wide)
 {
+    pdl_launch_dependents();
+    pdl_wait();
     const int units = (cols + 15) / 16;
     const long long total = (long long)rows * units;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
@@ -73,11 +75,11 @@ extern "C" tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const f
     const bool wide = (((uintptr_t)q | (uintptr_t)y) & 15) == 0 && (rows == 1 || (ldq % 16 == 0 && ldy * (dtype == TSVD_F32 ? 4 : 2) % 16 == 0));
     const long long blocks = (rows * ((cols + 15) / 16) + 127) / 128;
     const unsigned grid = (unsigned)(blocks < 148LL * 64 ? blocks : 148LL * 64);
+    PdlLaunch l(grid, 128, 0, st);
     if (dtype == TSVD_F32)
-        dequantize_rows_kernel<float><<<grid, 128, 0, st>>>(q, ldq, scale, (int)rows, cols, (float*)y, ldy, wide);
+        TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, dequantize_rows_kernel<float>, q, ldq, scale, (int)rows, cols, (float*)y, ldy, wide));
     else
-        dequantize_rows_kernel<__nv_bfloat16><<<grid, 128, 0, st>>>(q, ldq, scale, (int)rows, cols, (__nv_bfloat16*)y, ldy, wide);
-    TSVD_CUDA_OK(cudaGetLastError());
+        TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, dequantize_rows_kernel<__nv_bfloat16>, q, ldq, scale, (int)rows, cols, (__nv_bfloat16*)y, ldy, wide));
     tsvd_count_launch();
     return TSVD_OK;
 }

@@ -9,24 +9,34 @@ import math
 from . import binding
 from .binding import DTYPES, TSVD_BF16, TSVD_F32, TSVD_I8, TSVDError
 
-_CODES: dict = {}
+# torch is loaded with the first call: the package's other parts do without it.  These calls last microseconds, so the front
+# looks up as little as it can: the raw stream (a Stream object costs 2 us to make), the library's functions directly.
+_CODES: dict = {}          # torch dtype -> the library's number
+_empty = _raw_stream = _i32 = _f32 = _i8 = _bf16 = None
+
+
+def _load() -> None:
+    global _empty, _raw_stream, _i32, _f32, _i8, _bf16
+    import torch
+    from torch._C import _cuda_getCurrentRawStream
+    _empty, _raw_stream = torch.empty_strided, _cuda_getCurrentRawStream
+    _i32, _f32, _i8, _bf16 = torch.int32, torch.float32, torch.int8, torch.bfloat16
+    _CODES.update({torch.float32: TSVD_F32, torch.bfloat16: TSVD_BF16, torch.int8: TSVD_I8})
 
 
 def _code(dtype, what: str) -> int:
     """The library's number of a torch dtype (float32, bfloat16 or int8)."""
     if not _CODES:
-        import torch
-        _CODES.update({torch.float32: TSVD_F32, torch.bfloat16: TSVD_BF16, torch.int8: TSVD_I8})
-    try:
-        return _CODES[dtype]
-    except KeyError:
-        raise TSVDError(binding.TSVD_E_DTYPE, what) from None
+        _load()
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TSVDError(binding.TSVD_E_DTYPE, what)
+    return code
 
 
 def _stream(x) -> int:
-    """torch's current stream on x's device (the raw value: a Stream object costs 2 us to make)."""
-    from torch._C import _cuda_getCurrentRawStream
-    return _cuda_getCurrentRawStream(x.get_device())
+    """torch's current stream on x's device."""
+    return _raw_stream(x.get_device())
 
 
 def _rows(x, what: str):
@@ -43,25 +53,30 @@ def _rows(x, what: str):
 def quantize(x):
     """8-bit integers with one scale per row: x float32 or bfloat16 [rows, cols] (row stride >= cols) ->
     (q int8 [rows, cols], its rows 16-byte aligned; scale float32 [rows]); x is about q * scale[:, None]."""
-    import torch
     rows, cols, ldx = _rows(x, "quantize")
+    code, device = _code(x.dtype, "quantize"), x.device
     ldq = (cols + 15) & ~15
-    q = torch.empty_strided((rows, cols), (ldq, 1), dtype=torch.int8, device=x.device)
-    scale = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=x.device)
-    binding.tsvd_quantize(x.data_ptr(), _code(x.dtype, "quantize"), rows, cols, ldx, q.data_ptr(), ldq, scale.data_ptr(), _stream(x))
+    q = _empty((rows, cols), (ldq, 1), dtype=_i8, device=device)
+    scale = _empty((rows,), (1,), dtype=_f32, device=device)
+    err = binding.lib().tsvd_quantize(x.data_ptr(), code, rows, cols, ldx, q.data_ptr(), ldq, scale.data_ptr(), _stream(x))
+    if err:
+        raise TSVDError(err, "tsvd_quantize")
     return q, scale
 
 
 def dequantize(q, scale, dtype=None):
     """q * scale[:, None] as float32 (default) or bfloat16."""
-    import torch
     rows, cols, ldq = _rows(q, "dequantize")
-    if q.dtype != torch.int8 or scale.dtype != torch.float32:
+    if _code(q.dtype, "dequantize") != TSVD_I8 or scale.dtype != _f32:
         raise TSVDError(binding.TSVD_E_DTYPE, "dequantize")
     if scale.shape != (rows,) or not scale.is_cuda or not scale.is_contiguous():
         raise TSVDError(binding.TSVD_E_SHAPE, "dequantize")
-    y = torch.empty_strided((rows, cols), (cols, 1), dtype=dtype or torch.float32, device=q.device)
-    binding.tsvd_dequantize(q.data_ptr(), ldq, scale.data_ptr(), rows, cols, y.data_ptr(), _code(y.dtype, "dequantize"), cols, _stream(q))
+    dtype = dtype or _f32
+    code = _code(dtype, "dequantize")
+    y = _empty((rows, cols), (cols, 1), dtype=dtype, device=q.device)
+    err = binding.lib().tsvd_dequantize(q.data_ptr(), ldq, scale.data_ptr(), rows, cols, y.data_ptr(), code, cols, _stream(q))
+    if err:
+        raise TSVDError(err, "tsvd_dequantize")
     return y
 
 
@@ -89,7 +104,6 @@ class Int8Linear:
     def forward(self, x, x_scale=None, out=None, flags: int = 0):
         """x: CUDA tensor [B, N], row stride >= N: float32 or bfloat16 (quantised on the way), or int8 with x_scale
         float32 [B] (None: ones).  Returns [B, M]: bfloat16 for bfloat16 x, else float32, unless flags say otherwise."""
-        import torch
         B, N, ldx = _rows(x, "Int8Linear.forward")
         dt = _code(x.dtype, "Int8Linear.forward")
         if N != self.N:
@@ -97,19 +111,20 @@ class Int8Linear:
         if x_scale is not None:
             if x_scale.shape != (B,) or not x_scale.is_contiguous() or not x_scale.is_cuda:
                 raise TSVDError(binding.TSVD_E_SHAPE, "Int8Linear.forward")
-            if x_scale.dtype != torch.float32:
+            if x_scale.dtype != _f32:
                 raise TSVDError(binding.TSVD_E_DTYPE, "Int8Linear.forward")
-        want = torch.bfloat16 if (flags & binding.TSVD_FLAG_OUT_BF16 or (dt == TSVD_BF16 and not flags & binding.TSVD_FLAG_OUT_F32)) \
-            else torch.float32
+        want = _bf16 if (flags & binding.TSVD_FLAG_OUT_BF16 or (dt == TSVD_BF16 and not flags & binding.TSVD_FLAG_OUT_F32)) else _f32
         ldy = self.M
         if out is None:
-            out = torch.empty_strided((B, ldy), (ldy, 1), dtype=want, device=x.device)
+            out = _empty((B, ldy), (ldy, 1), dtype=want, device=x.device)
         elif out.dtype != want or out.shape != (B, ldy):
             raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != want else binding.TSVD_E_SHAPE, "Int8Linear.forward")
         else:
             ldy = _rows(out, "Int8Linear.forward")[2]
-        binding.tsvd_i8_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else 0, out.data_ptr(),
-                                ldy, B, dt, flags, _stream(x))
+        err = binding.lib().tsvd_i8_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else None,
+                                            out.data_ptr(), ldy, B, dt, flags, _stream(x))
+        if err:
+            raise TSVDError(err, "tsvd_i8_forward")
         return out
 
     __call__ = forward
@@ -151,9 +166,9 @@ class KV4Cache:
         return rows, heads, ld if ld > heads * dim else heads * dim
 
     def _batch(self, page_table, seq_len, q_start, rows: int, what: str):
-        import torch
-        int32 = torch.int32
-        if page_table.dtype != int32 or seq_len.dtype != int32 or (q_start is not None and q_start.dtype != int32):
+        if not _CODES:
+            _load()
+        if page_table.dtype != _i32 or seq_len.dtype != _i32 or (q_start is not None and q_start.dtype != _i32):
             raise TSVDError(binding.TSVD_E_DTYPE, what)
         if page_table.dim() != 2 or seq_len.dim() != 1 or not (page_table.is_cuda and seq_len.is_cuda) or not (
                 page_table.is_contiguous() and seq_len.is_contiguous()):
@@ -161,7 +176,7 @@ class KV4Cache:
         n_seq, max_pages = page_table.shape
         if seq_len.shape[0] != n_seq:
             raise TSVDError(binding.TSVD_E_SHAPE, what)
-        start = 0
+        start = None
         if q_start is not None:
             if q_start.dim() != 1 or q_start.shape[0] != n_seq + 1 or not q_start.is_cuda or not q_start.is_contiguous():
                 raise TSVDError(binding.TSVD_E_SHAPE, what)
@@ -176,17 +191,22 @@ class KV4Cache:
         if heads != self.n_kv_heads:
             raise TSVDError(binding.TSVD_E_SHAPE, "KV4Cache.append")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.append")
-        binding.tsvd_kv4_append(self.handle, k.data_ptr(), ldk, v.data_ptr(), ldv, _code(k.dtype, "KV4Cache.append"), *batch, _stream(k))
+        err = binding.lib().tsvd_kv4_append(self.handle, k.data_ptr(), ldk, v.data_ptr(), ldv, _code(k.dtype, "KV4Cache.append"), *batch,
+                                            _stream(k))
+        if err:
+            raise TSVDError(err, "tsvd_kv4_append")
 
     def read(self, rows: int, page_table, seq_len, q_start=None, dtype=None):
         """(k, v) [rows, n_kv_heads, head_dim] as the cache holds them: float32 (default) or bfloat16."""
-        import torch
-        ld = self.n_kv_heads * self.head_dim
-        shape, strides = (rows, self.n_kv_heads, self.head_dim), (ld, self.head_dim, 1)
-        k = torch.empty_strided(shape, strides, dtype=dtype or torch.float32, device=seq_len.device)
-        v = torch.empty_strided(shape, strides, dtype=k.dtype, device=k.device)
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.read")
-        binding.tsvd_kv4_read(self.handle, k.data_ptr(), ld, v.data_ptr(), ld, _code(k.dtype, "KV4Cache.read"), *batch, _stream(k))
+        dtype, device, ld = dtype or _f32, seq_len.device, self.n_kv_heads * self.head_dim
+        code = _code(dtype, "KV4Cache.read")
+        shape, strides = (rows, self.n_kv_heads, self.head_dim), (ld, self.head_dim, 1)
+        k = _empty(shape, strides, dtype=dtype, device=device)
+        v = _empty(shape, strides, dtype=dtype, device=device)
+        err = binding.lib().tsvd_kv4_read(self.handle, k.data_ptr(), ld, v.data_ptr(), ld, code, *batch, _stream(seq_len))
+        if err:
+            raise TSVDError(err, "tsvd_kv4_read")
         return k, v
 
     def attend(self, q, page_table, seq_len, q_start=None, max_q=None, max_kv=None, causal=True, window=0, scale=None, out=None,
@@ -194,14 +214,13 @@ class KV4Cache:
         """Attention of q [rows, n_heads, head_dim] (bfloat16 or float32) over the cached keys and values; the rows are the
         last positions of their sequences (append their keys first).  max_q, max_kv: bounds on the rows and the positions
         of one sequence, where the caller knows them.  Returns a tensor like q."""
-        import torch
         rows, n_heads, ldq = self._heads(q, "KV4Cache.attend")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.attend")
         if max_q is None:
             max_q = 1 if q_start is None else max(1, rows)
         if out is None:
             ldo = n_heads * self.head_dim
-            out = torch.empty_strided((rows, n_heads, self.head_dim), (ldo, self.head_dim, 1), dtype=q.dtype, device=q.device)
+            out = _empty((rows, n_heads, self.head_dim), (ldo, self.head_dim, 1), dtype=q.dtype, device=q.device)
         elif out.dtype != q.dtype or out.shape != q.shape:
             raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != q.dtype else binding.TSVD_E_SHAPE, "KV4Cache.attend")
         else:
@@ -210,8 +229,10 @@ class KV4Cache:
             scale = 1.0 / math.sqrt(self.head_dim)
         if causal:
             flags |= binding.TSVD_FLAG_CAUSAL
-        binding.tsvd_kv4_attend(self.handle, q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads, _code(q.dtype, "KV4Cache.attend"), *batch,
-                                max_q, max_kv or 0, scale, window, flags, _stream(q))
+        err = binding.lib().tsvd_kv4_attend(self.handle, q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads,
+                                            _code(q.dtype, "KV4Cache.attend"), *batch, max_q, max_kv or 0, scale, window, flags, _stream(q))
+        if err:
+            raise TSVDError(err, "tsvd_kv4_attend")
         return out
 
     def status(self) -> int:
