@@ -3,6 +3,7 @@
 // Per position, head and group of 32 numbers: step = fp16((hi - lo) / 15), base = fp16(lo),
 // code = clamp(rint((x - base) / step), 0, 15).
 #include <new>
+#include <type_traits>
 
 #include "serving.cuh"
 
@@ -20,10 +21,11 @@ __device__ __forceinline__ Place place_of_row(const Kv4Geom& g, const Kv4Batch& 
     const int end = b.q_start ? b.q_start[s + 1] : row + 1;
     const long long pos = (long long)b.seq_len[s] - (end - row);
     if (pos >= 0 && pos < (long long)b.max_pages * g.page_tokens) {
-        const int page = b.table[(long long)s * b.max_pages + pos / g.page_tokens];
+        const unsigned at = (unsigned)pos, n = at / (unsigned)g.page_tokens;
+        const int page = b.table[(long long)s * b.max_pages + n];
         if (page >= 0 && page < g.n_pages) {
             p.page = page;
-            p.at = (int)(pos % g.page_tokens);
+            p.at = (int)(at - n * (unsigned)g.page_tokens);
         }
     }
     if (p.page < 0 && threadIdx.x == 0) atomicOr(status, KV4_DEV_INDEX);
@@ -61,42 +63,43 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8])
 }
 
 // What one thread holds: eight numbers, a quarter of a group.  Item `u` of a row: key or value, head, word of eight.
-struct Item { int is_v, head, word; };
-__device__ __forceinline__ Item item_of(int u, int heads, int words)
-{
-    Item t;
-    t.word = u % words;
-    t.head = u / words % heads;
-    t.is_v = u / (words * heads);
-    return t;
-}
-// Byte offsets inside a 16-position block.
-__device__ __forceinline__ int code_offset(const Item& t, int dim, int at)
-{
-    const int w = t.word >> 2, j = t.word & 3;       // group, quarter
-    const int place = t.is_v ? t.word : j * (dim / KV4_GROUP) + w;
-    return (t.is_v ? 10 * dim : 0) + at * (dim / 2) + place * 4;
-}
-__device__ __forceinline__ int scale_offset(const Item& t, int dim, int at)
-{
-    return (t.is_v ? 18 * dim : 8 * dim) + at * (dim / 8) + (t.word >> 2) * 4;
-}
+template <int D>
+struct Item {
+    int is_v, head, word;
+    __device__ __forceinline__ Item(int u, int heads)
+    {
+        word = u & (D / 8 - 1);
+        head = u / (D / 8);
+        is_v = head >= heads;
+        if (is_v) head -= heads;
+    }
+    // byte offsets inside a 16-position block
+    __device__ __forceinline__ int codes(int at) const
+    {
+        const int w = word >> 2, j = word & 3;           // group, quarter
+        const int place = is_v ? word : j * (D / KV4_GROUP) + w;
+        return (is_v ? 10 * D : 0) + at * (D / 2) + place * 4;
+    }
+    __device__ __forceinline__ int scales(int at) const { return (is_v ? 18 * D : 8 * D) + at * (D / 8) + (word >> 2) * 4; }
+};
 
 // A block takes a row; the rows of a call go into different positions, so no two blocks write the same bytes.
-template <typename T, bool VEC>
-__global__ void kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv,
-                                  int* status)
+template <typename T, bool VEC, int D>
+__global__ void __launch_bounds__(512)
+kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv, int* status)
 {
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x;
     const Place at = place_of_row(g, b, row, status);
     if (at.page < 0) return;
-    const int words = g.dim / 8, items = 2 * g.heads * words;
+    const int items = 2 * g.heads * (D / 8);
+    const int pos = at.at & (KV4_BLOCK - 1);
+#pragma unroll 2
     for (int u = threadIdx.x; u < items; u += blockDim.x) {   // items is a multiple of 16: quads stay whole
-        const Item t = item_of(u, g.heads, words);
+        const Item<D> t(u, g.heads);
         float x[8];
-        load8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + (long long)t.head * g.dim + t.word * 8, x);
+        load8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + t.head * D + t.word * 8, x);
         float lo = x[0], hi = x[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
@@ -117,32 +120,33 @@ __global__ void kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k
             word |= (uint32_t)c << (4 * ((e >> 1) + 4 * (e & 1)));
         }
         uint8_t* blk = g.block(at.page, t.head, at.at);
-        const int pos = at.at & (KV4_BLOCK - 1);
-        *reinterpret_cast<uint32_t*>(blk + code_offset(t, g.dim, pos)) = word;
-        if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + scale_offset(t, g.dim, pos)) = __halves2half2(step, base);
+        *reinterpret_cast<uint32_t*>(blk + t.codes(pos)) = word;
+        if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + t.scales(pos)) = __halves2half2(step, base);
     }
 }
 
-template <typename T, bool VEC>
-__global__ void kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __restrict__ v, long long ldv, int* status)
+template <typename T, bool VEC, int D>
+__global__ void __launch_bounds__(512)
+kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __restrict__ v, long long ldv, int* status)
 {
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x;
     const Place at = place_of_row(g, b, row, status);
-    const int words = g.dim / 8, items = 2 * g.heads * words;
+    const int items = 2 * g.heads * (D / 8);
+    const int pos = at.at & (KV4_BLOCK - 1);
+#pragma unroll 2
     for (int u = threadIdx.x; u < items; u += blockDim.x) {
-        const Item t = item_of(u, g.heads, words);
+        const Item<D> t(u, g.heads);
         float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (at.page >= 0) {
             const uint8_t* blk = g.block(at.page, t.head, at.at);
-            const int pos = at.at & (KV4_BLOCK - 1);
-            const uint32_t word = *reinterpret_cast<const uint32_t*>(blk + code_offset(t, g.dim, pos));
-            const float2 sm = __half22float2(*reinterpret_cast<const __half2*>(blk + scale_offset(t, g.dim, pos)));
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(blk + t.codes(pos));
+            const float2 sm = __half22float2(*reinterpret_cast<const __half2*>(blk + t.scales(pos)));
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((word >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u), sm.x, sm.y);
         }
-        store8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + (long long)t.head * g.dim + t.word * 8, x);
+        store8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + t.head * D + t.word * 8, x);
     }
 }
 
@@ -223,13 +227,18 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
         PdlLaunch l((unsigned)n_rows, t, 0, st);
         e = cudaLaunchKernelEx(&l.cfg, kernel, h->g, b, kp, ldk, vp, ldv, h->dev_status);
     };
-    if (dtype == TSVD_F32) {
-        if (vec) go(kv4_append_kernel<float, true>, (const float*)k, (const float*)v);
-        else go(kv4_append_kernel<float, false>, (const float*)k, (const float*)v);
-    } else {
-        if (vec) go(kv4_append_kernel<__nv_bfloat16, true>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
-        else go(kv4_append_kernel<__nv_bfloat16, false>, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
-    }
+    auto by_type = [&](auto* kp, auto* vp) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
+        if (h->g.dim == 128) {
+            if (vec) go(kv4_append_kernel<T, true, 128>, kp, vp);
+            else go(kv4_append_kernel<T, false, 128>, kp, vp);
+        } else {
+            if (vec) go(kv4_append_kernel<T, true, 64>, kp, vp);
+            else go(kv4_append_kernel<T, false, 64>, kp, vp);
+        }
+    };
+    if (dtype == TSVD_F32) by_type((const float*)k, (const float*)v);
+    else by_type((const __nv_bfloat16*)k, (const __nv_bfloat16*)v);
     TSVD_CUDA_OK(e);
     tsvd_count_launch();
     return TSVD_OK;
@@ -257,13 +266,18 @@ extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, voi
         PdlLaunch l((unsigned)n_rows, t, 0, st);
         e = cudaLaunchKernelEx(&l.cfg, kernel, h->g, b, kp, ldk, vp, ldv, h->dev_status);
     };
-    if (dtype == TSVD_F32) {
-        if (vec) go(kv4_read_kernel<float, true>, (float*)k, (float*)v);
-        else go(kv4_read_kernel<float, false>, (float*)k, (float*)v);
-    } else {
-        if (vec) go(kv4_read_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
-        else go(kv4_read_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
-    }
+    auto by_type = [&](auto* kp, auto* vp) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
+        if (h->g.dim == 128) {
+            if (vec) go(kv4_read_kernel<T, true, 128>, kp, vp);
+            else go(kv4_read_kernel<T, false, 128>, kp, vp);
+        } else {
+            if (vec) go(kv4_read_kernel<T, true, 64>, kp, vp);
+            else go(kv4_read_kernel<T, false, 64>, kp, vp);
+        }
+    };
+    if (dtype == TSVD_F32) by_type((float*)k, (float*)v);
+    else by_type((__nv_bfloat16*)k, (__nv_bfloat16*)v);
     TSVD_CUDA_OK(e);
     tsvd_count_launch();
     return TSVD_OK;

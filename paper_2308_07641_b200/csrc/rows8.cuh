@@ -171,6 +171,8 @@ cudaError_t by_width(const void* x, int rows, int cols, long long ldx, const flo
     if (units <= 32) return launch<T, VEC, 32, 1>(x, rows, cols, ldx, given, out, scale, st);
     if (units <= 64) return launch<T, VEC, 32, 2>(x, rows, cols, ldx, given, out, scale, st);
     if (units <= 128) return launch<T, VEC, 128, 1>(x, rows, cols, ldx, given, out, scale, st);
+    // Many rows: all of them resident at once (16 blocks of 128 threads an SM) instead of in two rounds.
+    if (units <= 256 && rows >= 148 * 8) return launch<T, VEC, 128, 2>(x, rows, cols, ldx, given, out, scale, st);
     if (units <= 256) return launch<T, VEC, 256, 1>(x, rows, cols, ldx, given, out, scale, st);
     if (units <= 512) return launch<T, VEC, 256, 2>(x, rows, cols, ldx, given, out, scale, st);
     if (units <= 1024) return launch<T, VEC, 256, 4>(x, rows, cols, ldx, given, out, scale, st);
