@@ -101,7 +101,7 @@ typedef struct tsvd_kv4_s* tsvd_kv4_t; /* opaque; owns device memory on one GPU 
  * append and read; such a position is not written (append), reads as zeros (read) and is not seen (attend).  An unused
  * slot of a batch (seq_len 0 with a row) is therefore fine in attend, which gives it zeros.
  * Calls on one handle must be ordered on one stream (or otherwise serialised).
- * Synchronous.  Errors: E_NULL, E_SHAPE, E_TOOBIG (n_pages * page_tokens above 2^31 - 1), E_NOMEM, E_CUDA.
+ * Synchronous.  Errors: E_NULL, E_SHAPE, E_TOOBIG (n_pages * page_tokens above 2^31 - 1, page_tokens above 2^24), E_NOMEM, E_CUDA.
  */
 tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_tokens, long long n_pages, tsvd_kv4_t* out);
 

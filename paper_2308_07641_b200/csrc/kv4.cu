@@ -83,7 +83,23 @@ struct Item {
     __device__ __forceinline__ int scales(int at) const { return (is_v ? 18 * D : 8 * D) + at * (D / 8) + (word >> 2) * 4; }
 };
 
-// A block takes a row; the rows of a call go into different positions, so no two blocks write the same bytes.
+// Smallest and largest of three.
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float y;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
+// A block takes a row; the rows of a call go into different positions, so no two blocks write the same bytes.  A thread takes
+// sixteen numbers, half a group.  The kernel is bound by its instructions, the half-rate integer and comparison ones above
+// all, so the codes are put together as floats: four codes are an exact fp32 integer below 2^16.
 template <typename T, bool VEC, int D>
 __global__ void __launch_bounds__(512)
 kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv, int* status)
@@ -91,37 +107,53 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk,
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x;
-    const Place at = place_of_row(g, b, row, status);
+    __shared__ Place place_s;
+    if (threadIdx.x < 32) {
+        const Place p = place_of_row(g, b, row, status);
+        if (threadIdx.x == 0) place_s = p;
+    }
+    __syncthreads();
+    const Place at = place_s;
     if (at.page < 0) return;
-    const int items = 2 * g.heads * (D / 8);
-    const int pos = at.at & (KV4_BLOCK - 1);
-#pragma unroll 2
-    for (int u = threadIdx.x; u < items; u += blockDim.x) {   // items is a multiple of 16: quads stay whole
-        const Item<D> t(u, g.heads);
-        float x[8];
-        load8<T, VEC>((t.is_v ? v + row * ldv : k + row * ldk) + t.head * D + t.word * 8, x);
-        float lo = x[0], hi = x[0];
+    const int items = g.heads * (D / 8), pos = at.at & (KV4_BLOCK - 1);
+    for (int u0 = threadIdx.x & ~31; u0 < items; u0 += blockDim.x) {
+        const bool in = u0 + (int)(threadIdx.x & 31) < items;  // (whole warps take part in the exchange)
+        const int u = in ? u0 + (int)(threadIdx.x & 31) : items - 1;
+        const Item<D> t(2 * u, g.heads), t1(2 * u + 1, g.heads);
+        const T* src = (t.is_v ? v + row * ldv : k + row * ldk) + t.head * D + t.word * 8;
+        float x[16];
+        load8<T, VEC>(src, reinterpret_cast<float (&)[8]>(x[0]));
+        load8<T, VEC>(src + 8, reinterpret_cast<float (&)[8]>(x[8]));
+        float lo = fminf(x[0], x[1]), hi = fmaxf(x[0], x[1]);
 #pragma unroll
-        for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
-        const unsigned quad = 0xfu << (threadIdx.x & 28);
-        lo = fminf(lo, __shfl_xor_sync(quad, lo, 1));
-        hi = fmaxf(hi, __shfl_xor_sync(quad, hi, 1));
-        lo = fmaxf(fminf(lo, __shfl_xor_sync(quad, lo, 2)), -kMost);
-        hi = fminf(fmaxf(hi, __shfl_xor_sync(quad, hi, 2)), kMost);
-        lo = fminf(lo, kMost);
-        hi = fmaxf(hi, -kMost);
+        for (int i = 2; i < 16; i += 2) { lo = min3(lo, x[i], x[i + 1]); hi = max3(hi, x[i], x[i + 1]); }
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, 1));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, 1));
+        lo = fminf(fmaxf(lo, -kMost), kMost);
+        hi = fmaxf(fminf(hi, kMost), -kMost);
         const __half step = __float2half_rn(__fdiv_rn(hi - lo, 15.0f)), base = __float2half_rn(lo);
         const float s = __half2float(step), m = __half2float(base);
         const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
-        uint32_t word = 0;
+        uint32_t word[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int c = min(15, max(0, __float2int_rn(__fmul_rn(__fsub_rn(x[e], m), inv))));
-            word |= (uint32_t)c << (4 * ((e >> 1) + 4 * (e & 1)));
+        for (int w = 0; w < 2; ++w) {
+            // nibble (e >> 1) + 4 (e & 1) holds number e: the even numbers are the lower half of the word
+            float half[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int e = 7; e >= 0; --e) {
+                const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(x[8 * w + e], m), inv), 0.0f), 15.0f);
+                const float n = __fsub_rn(__fadd_rn(c, 12582912.0f), 12582912.0f);      // rounded to even
+                half[e & 1] = fmaf(half[e & 1], 16.0f, n);
+            }
+            // 2^23 + integer: the integer is in the low bits
+            word[w] = __byte_perm(__float_as_uint(half[0] + 8388608.0f), __float_as_uint(half[1] + 8388608.0f), 0x5410);
         }
         uint8_t* blk = g.block(at.page, t.head, at.at);
-        *reinterpret_cast<uint32_t*>(blk + t.codes(pos)) = word;
-        if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + t.scales(pos)) = __halves2half2(step, base);
+        if (in) {
+            *reinterpret_cast<uint32_t*>(blk + t.codes(pos)) = word[0];
+            *reinterpret_cast<uint32_t*>(blk + t1.codes(pos)) = word[1];
+            if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + t.scales(pos)) = __halves2half2(step, base);
+        }
     }
 }
 
@@ -132,7 +164,13 @@ kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __re
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x;
-    const Place at = place_of_row(g, b, row, status);
+    __shared__ Place place_s;
+    if (threadIdx.x < 32) {
+        const Place p = place_of_row(g, b, row, status);
+        if (threadIdx.x == 0) place_s = p;
+    }
+    __syncthreads();
+    const Place at = place_s;
     const int items = 2 * g.heads * (D / 8);
     const int pos = at.at & (KV4_BLOCK - 1);
 #pragma unroll 2
@@ -150,9 +188,9 @@ kv4_read_kernel(Kv4Geom g, Kv4Batch b, T* __restrict__ k, long long ldk, T* __re
     }
 }
 
-unsigned row_threads(const Kv4Geom& g)
+unsigned row_threads(const Kv4Geom& g, int numbers)   // a thread
 {
-    const int items = 2 * g.heads * (g.dim / 8);
+    const int items = 2 * g.heads * (g.dim / numbers);
     return (unsigned)(items >= 512 ? 512 : (items + 31) / 32 * 32);
 }
 
@@ -175,7 +213,7 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     *out = nullptr;
     if (n_kv_heads < 1 || (head_dim != 64 && head_dim != 128) || page_tokens < 1 || page_tokens % KV4_BLOCK || n_pages < 1)
         return TSVD_E_SHAPE;
-    if (n_pages > 0x7fffffffLL / page_tokens || n_kv_heads > 65535) return TSVD_E_TOOBIG;
+    if (n_pages > 0x7fffffffLL / page_tokens || page_tokens > (1 << 24) || n_kv_heads > 65535) return TSVD_E_TOOBIG;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return TSVD_E_CUDA; }
     tsvd_kv4_s* h = new (std::nothrow) tsvd_kv4_s();
@@ -185,7 +223,10 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     h->g.dim = head_dim;
     h->g.page_tokens = page_tokens;
     h->g.n_pages = (int)n_pages;
-    h->pool_bytes = (size_t)n_pages * h->g.page_bytes();
+    h->g.block_bytes = 20u * (unsigned)head_dim;
+    h->g.head_bytes = (unsigned)page_tokens / KV4_BLOCK * h->g.block_bytes;
+    h->g.page_bytes = (size_t)n_kv_heads * h->g.head_bytes;
+    h->pool_bytes = (size_t)n_pages * h->g.page_bytes;
     cudaError_t e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaMalloc(&h->g.pool, h->pool_bytes);
     if (e == cudaSuccess) e = cudaMemset(h->g.pool, 0, h->pool_bytes);
@@ -221,7 +262,7 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
     const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
-    const unsigned t = row_threads(h->g);
+    const unsigned t = row_threads(h->g, 16);
     cudaError_t e = cudaSuccess;
     auto go = [&](auto kernel, auto* kp, auto* vp) {
         PdlLaunch l((unsigned)n_rows, t, 0, st);
@@ -260,7 +301,7 @@ extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, voi
     const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
-    const unsigned t = row_threads(h->g);
+    const unsigned t = row_threads(h->g, 8);
     cudaError_t e = cudaSuccess;
     auto go = [&](auto kernel, auto* kp, auto* vp) {
         PdlLaunch l((unsigned)n_rows, t, 0, st);

@@ -54,12 +54,12 @@ struct Kv4Geom {
     uint8_t* pool;
     int heads, dim, page_tokens;
     int n_pages;
-    __host__ __device__ size_t block_bytes() const { return (size_t)20 * dim; }
-    __host__ __device__ size_t page_bytes() const { return (size_t)heads * (page_tokens / KV4_BLOCK) * block_bytes(); }
+    unsigned block_bytes, head_bytes;   // of a block of 16 positions; of one head's blocks in a page
+    size_t page_bytes;
     // the block that holds position `at` of page `page`, for one head
     __host__ __device__ uint8_t* block(int page, int head, int at) const
     {
-        return pool + (size_t)page * page_bytes() + ((size_t)head * (page_tokens / KV4_BLOCK) + at / KV4_BLOCK) * block_bytes();
+        return pool + (size_t)page * page_bytes + (size_t)head * head_bytes + ((unsigned)at / KV4_BLOCK) * block_bytes;
     }
 };
 
