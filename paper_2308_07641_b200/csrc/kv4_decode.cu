@@ -12,12 +12,13 @@
 // instead, which saves that last step.
 //
 // Arithmetic.  mma.sync m16n8k16 in fp16 with fp32 sums, the cached side as the 16-row operand, the query rows as the
-// 8-column one.  Scores use the codes as they are: a mask and an or make fp16 pairs 1024 + code, or 1024 + 16 code for the
-// odd nibbles, whose q is divided by 16 beforehand; 1024 sum q comes off through the accumulator's start value, and step and
-// base of the group are applied to the fp32 sum: s (q.code) + b (sum q).  So scores carry no rounding of k at all.  q enters
-// as fp16 after division by a power of two per row (exact up to 2^-24 of the row's largest).  Values become fp16 numbers
-// code * step + base (one rounding); probabilities fp16, relative to a reference that moves only when a score passes the
-// one it was set by by more than 5 (in units of log2): no exchange between lanes otherwise.
+// 8-column one.  Scores use the codes as they are: two masks leave pairs of them in the low bits of a word, which is what fp16
+// calls code * 2^-24, or 16 code * 2^-24 for the odd nibbles, whose q is divided by 16 beforehand; the group's step is applied
+// to the fp32 sum.  The bases' part, sum over groups of base * (sum of q), is one more small product with the sums of q in
+// two fp16 terms.  So scores carry no rounding of k at all.  q enters as fp16 after division by a power of two per row (exact
+// up to 2^-34 of the row's largest).  Values become fp16 numbers code * step + base (one rounding); probabilities fp16,
+// relative to a reference that moves only when a score passes the one it was set by by more than 5 (in units of log2): no
+// exchange between lanes otherwise.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -31,7 +32,9 @@ constexpr int DEC_MAX_STAGES = 6;
 constexpr int DEC_QUEUE = 8;             // items that the copies may be ahead: more than DEC_MAX_STAGES
 constexpr int DEC_APART = 6;             // units a warp up to which items get a block each: a step over scratch costs as much
 constexpr int DEC_STATIC = 13 * 1024;    // room for what the kernel declares
-constexpr int DEC_WARPS = 8;             // two on each quarter of an SM: up to 255 registers a thread
+// Warps of a block: 12 of up to 168 registers a thread for eight rows (8 of 255: 46 -> 42 us for 100003 positions), 8 for sixteen
+// rows, whose sums need more.
+template <int NT> constexpr int kWarps = NT == 1 ? 12 : 8;
 constexpr int DEC_UNIT = 2 * KV4_BLOCK;  // positions of a unit
 
 // Probabilities are 2^(score - reference): 2^10 where the reference was set, up to 2^15 before it moves, so that fp16
@@ -70,6 +73,12 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(b0));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -111,9 +120,9 @@ __device__ __forceinline__ Seq load_seq(const DecParams& p, int s)
     if (s >= p.b.n_seq) return q;
     q.first = kv4_first_row(p.b, s);
     q.all = kv4_first_row(p.b, s + 1) - q.first;
-    q.rows = min(min(q.all, p.max_q), p.b.n_rows - q.first);
-    if (q.rows <= 0 || q.first < 0) { q.rows = 0; return q; }
     q.len = p.b.seq_len[s];
+    q.rows = min(min(q.all, p.max_q), p.b.n_rows - q.first);
+    if (q.rows <= 0 || q.first < 0) { q.rows = q.units = 0; return q; }
     const long long room = (long long)p.b.max_pages * p.g.page_tokens;
     const long long seen = q.len < 0 ? 0 : min((long long)q.len, room);
     if (q.len > room) atomicOr(p.status, KV4_DEV_INDEX);
@@ -136,25 +145,40 @@ struct Item {
     long long u0;              // where the item begins in the call's list of units
 };
 
+// How the call's units are shared out to the blocks.
+struct Runs {
+    long long total;
+    int blocks, share;         // share: of a block, where items lie apart
+    __device__ __forceinline__ long long first_of(int b) const
+    {
+        if (share) return (long long)share * b;
+        if (b >= blocks) return total;
+        return total < (1LL << 31) / 1024 ? (long long)((unsigned)total * (unsigned)b / (unsigned)blocks) : total * b / blocks;   // (blocks <= 1024)
+    }
+    __device__ __forceinline__ int block_of(long long u) const
+    {
+        return share ? (int)(u / share) : (int)(((u + 1) * blocks - 1) / total);
+    }
+};
+
 // The run behind a warp's copies (what changes with every unit is in registers).
 struct Feed {
     int s, item, page_at;
     Seq q;
-    long long item_u0, u1;
+    long long item_u0, run_u0, u1;
 };
 
 template <int D, int NT>
-__global__ void __launch_bounds__(DEC_WARPS * 32, 1)
+__global__ void __launch_bounds__(kWarps<NT> * 32, 1)
 kv4_decode_kernel(const DecParams p)
 {
-    constexpr int WARPS = DEC_WARPS;
+    constexpr int WARPS = kWarps<NT>;
     constexpr int ROWS = 8 * NT, W = D / KV4_GROUP, BLOCK = 20 * D, UNIT = 2 * BLOCK;
     constexpr int VW = D / 64;   // words of value codes per thread and key
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 127) & ~(uintptr_t)127);
     float* heads_kept = reinterpret_cast<float*>(ring + (size_t)WARPS * p.stages * UNIT);   // [warps][keep_cols][D]
     __shared__ uint64_t full[WARPS][DEC_MAX_STAGES];
-    __shared__ uint8_t there[WARPS][DEC_MAX_STAGES];
     __shared__ Item queue[WARPS][DEC_QUEUE];
     __shared__ Feed feeds[WARPS];
     // What a warp keeps of an item that began before its run (0; the numbers in heads_kept) or ends after it (1; the numbers
@@ -190,20 +214,26 @@ kv4_decode_kernel(const DecParams p)
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     total_items = __reduce_add_sync(0xffffffffu, total_items);
     most = __reduce_max_sync(0xffffffffu, most);
+    // Block b has the units from share * b on where items lie apart, else from total * b / blocks on; warps likewise in it.
     const bool apart = total_items <= (int)gridDim.x && most <= DEC_APART * WARPS;
-    const long long runs = (long long)gridDim.x * WARPS;
-    const long long run = apart ? (most + WARPS - 1) / WARPS : max((total + runs - 1) / runs, 2LL), share = run * WARPS;
-    if (apart) total = share * total_items;                    // a block's share for each item, whatever its length
+    const int share = apart ? (most + WARPS - 1) / WARPS * WARPS : 0;
+    if (apart) total = (long long)share * total_items;         // a block's share for each item, whatever its length
+    // (no more blocks than have units for all their warps: a block without units would be waited for)
+    const Runs runs{total, apart ? (int)gridDim.x : (int)min((long long)gridDim.x, max(1LL, total / WARPS)), share};
     Feed& f = feeds[warp];
     {
-        const long long u0 = run * ((long long)blockIdx.x * WARPS + warp), u1 = min(u0 + run, total);
+        const long long c0 = runs.first_of(blockIdx.x), c1 = min(runs.first_of(blockIdx.x + 1), total);
+        const unsigned n = c1 > c0 ? (unsigned)(c1 - c0) : 0;
+        // the first n % WARPS warps have one more: where there are fewer units than warps, the last ones have none
+        const unsigned each = n / WARPS, over = n % WARPS;
+        const long long u0 = c0 + each * (unsigned)warp + min((unsigned)warp, over), u1 = u0 + each + ((unsigned)warp < over);
         long long before = 0;
         if (p.b.n_seq > 32) mine = load_seq<ROWS>(p, lane);
         if (u0 < u1)
             for (int s0 = 0; s0 < p.b.n_seq; mine = load_seq<ROWS>(p, s0 + lane)) {
-                const int span = apart ? (int)share : mine.units;
-                const long long n = (long long)mine.items * span;
-                long long scan = n;
+                const int span = apart ? share : mine.units;
+                const long long have = (long long)mine.items * span;
+                long long scan = have;
                 for (int o = 1; o < 32; o <<= 1) {
                     const long long v = __shfl_up_sync(0xffffffffu, scan, o);
                     if (lane >= o) scan += v;
@@ -211,7 +241,7 @@ kv4_decode_kernel(const DecParams p)
                 const unsigned holds = __ballot_sync(0xffffffffu, before + scan > u0);
                 if (holds) {
                     if (lane == __ffs(holds) - 1) {
-                        const unsigned in = (unsigned)(u0 - before - (scan - n));
+                        const unsigned in = (unsigned)(u0 - before - (scan - have));
                         f.s = s0 + lane;
                         f.item = (int)(in / (unsigned)span) - 1;          // the step to the first item adds one
                         f.q = mine;
@@ -225,6 +255,7 @@ kv4_decode_kernel(const DecParams p)
         __syncwarp();
         if (lane == 0) {
             f.u1 = u1;
+            f.run_u0 = u0;
             if (u0 >= u1) { f.u1 = f.item_u0 = 0; f.q.units = 0; }   // nothing to do
         }
         __syncwarp();
@@ -234,6 +265,7 @@ kv4_decode_kernel(const DecParams p)
     const uint8_t* ptr = nullptr;        // the next block, null where its page number is out of range
     int in_page = 0, in_item = 0;        // blocks left in the page, units left in the warp's share of the item
     int next_page = 0, pushed = 0;       // a page number is asked for one page ahead
+    uint32_t there = 0;                  // two bits a slot: which of its blocks are in range
     auto ask_page = [&](int at) {        // -2: no such position
         return at < p.b.max_pages && (long long)at * p.g.page_tokens < f.q.len ? p.b.table[(long long)f.s * p.b.max_pages + at] : -2;
     };
@@ -253,7 +285,7 @@ kv4_decode_kernel(const DecParams p)
     auto next_item = [&]() -> bool {     // false: the run is done
         __syncwarp();
         if (lane == 0) {
-            const int span = apart ? (int)share : f.q.units;
+            const int span = apart ? share : f.q.units;
             f.item_u0 += span;
             if (f.item_u0 < f.u1 && ++f.item == f.q.items) {
                 f.item = 0;
@@ -262,7 +294,7 @@ kv4_decode_kernel(const DecParams p)
             }
         }
         __syncwarp();
-        const long long run_u0 = run * ((long long)blockIdx.x * WARPS + warp), item_u0 = f.item_u0, u1 = f.u1;
+        const long long run_u0 = f.run_u0, item_u0 = f.item_u0, u1 = f.u1;
         const int unit0 = (int)max(0LL, run_u0 - item_u0), unit1 = (int)min((long long)f.q.units, u1 - item_u0);
         if (item_u0 >= u1 || unit0 >= unit1) return false;     // (unit0 >= unit1: an item apart, shorter than the block's share)
         const int blk = (f.q.unit0 + unit0) * 2;
@@ -305,9 +337,9 @@ kv4_decode_kernel(const DecParams p)
         }
         ptr = b ? b + BLOCK : nullptr;
         --in_item;
+        there = (there & ~(3u << (2 * st))) | (uint32_t)((a ? 1 : 0) | (b ? 2 : 0)) << (2 * st);
         if (lane == 0) {
             uint8_t* to = ring + (size_t)(warp * p.stages + st) * UNIT;
-            there[warp][st] = (a ? 1 : 0) | (b ? 2 : 0);
             mbar_arrive_expect_tx(&full[warp][st], UNIT);
             if (joined && a) {
                 bulk_g2s(to, a, UNIT, &full[warp][st]);
@@ -328,7 +360,8 @@ kv4_decode_kernel(const DecParams p)
 
         // ---- the item's query rows ----
         uint32_t qf[NT][2 * W][2];           // [..][MMA step][word]: column r
-        float off[NT][W][2], qsum[NT][W][2], cmul[NT][2];   // columns 2 j, 2 j + 1
+        uint32_t qs[NT];                     // column r: the sum of q over group j, in two fp16 terms
+        float cmul[NT][2];                   // columns 2 j, 2 j + 1
         int lo[NT][2], hi[NT][2];            // positions [lo, hi) that those columns see
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -350,37 +383,33 @@ kv4_decode_kernel(const DecParams p)
             }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // divide by the power of two at or below the row's largest (2^-60 at least)
+            // divide by the power of two at or below the row's largest (2^-60 at least), times 2^10
             const int e = min(max((int)(__float_as_uint(top) >> 23), 67), 253) - 127;
-            const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-            float so[W], ss[W];
+            const float down = __uint_as_float((uint32_t)(137 - e) << 23);
+            float ss[W];
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                so[w] = ss[w] = 0.0f;
+                ss[w] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {      // pairs (2 i, 2 i + 1): odd i hold q / 16
-                    const float f = (i & 1) ? down * 0.0625f : down, back = (i & 1) ? 16.0f : 1.0f;
+                    const float f = (i & 1) ? down * 0.0625f : down, back = (i & 1) ? 0x1p-6f : 0x1p-10f;
                     const uint32_t pr = h2(v[w][2 * i] * f, v[w][2 * i + 1] * f);
                     qf[t][2 * w + (i >> 1)][i & 1] = pr;
                     const float2 as = halves(pr);
-                    so[w] += 1024.0f * (as.x + as.y);
-                    ss[w] += back * (as.x + as.y);
+                    ss[w] = fmaf(back, as.x + as.y, ss[w]);
                 }
-                so[w] += __shfl_xor_sync(0xffffffffu, so[w], 1);
-                so[w] += __shfl_xor_sync(0xffffffffu, so[w], 2);
                 ss[w] += __shfl_xor_sync(0xffffffffu, ss[w], 1);
                 ss[w] += __shfl_xor_sync(0xffffffffu, ss[w], 2);
             }
+            float mine_s = 0.0f;                   // group j's
+#pragma unroll
+            for (int w = 0; w < W; ++w) mine_s = j == w ? ss[w] : mine_s;
+            const float hi_s = __half2float(__float2half_rn(mine_s));
+            qs[t] = h2(hi_s, mine_s - hi_s);
             const float up = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int from = 4 * (2 * j + k);
-#pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    off[t][w][k] = -__shfl_sync(0xffffffffu, so[w], from);
-                    qsum[t][w][k] = __shfl_sync(0xffffffffu, ss[w], from);
-                }
-                cmul[t][k] = p.c * __shfl_sync(0xffffffffu, up, from);
+                cmul[t][k] = p.c * __shfl_sync(0xffffffffu, up, 4 * (2 * j + k));
                 const int col = it.row0 + 8 * t + 2 * j + k;
                 const int pos = it.pos0 + col / p.group;
                 // (a column without a row: its q is 0, nothing is hidden and nothing written)
@@ -412,7 +441,7 @@ kv4_decode_kernel(const DecParams p)
         for (int u = it.unit0; u < it.unit1; ++u) {
             if (!(ok = mbar_wait(&full[warp][stage], phase, ctl))) break;
             const uint8_t* unit = ring + (size_t)(warp * p.stages + stage) * UNIT;
-            const int at = it.at0 + u * DEC_UNIT, here = there[warp][stage];
+            const int at = it.at0 + u * DEC_UNIT, here = (int)(there >> (2 * stage) & 3u);
             // rows r and r + 8 of a block's score tile are its positions kr and kr + 8
             const int kr = (r >> 1) + 4 * (r & 1);
             float sc[2][NT][4];
@@ -420,29 +449,35 @@ kv4_decode_kernel(const DecParams p)
             for (int h = 0; h < 2; ++h) {
                 const uint8_t* blk = unit + h * BLOCK;
                 Words<W> kw[2], ks[2];
+                uint32_t kb[2];                    // (step, base) of group j
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     kw[x] = *reinterpret_cast<const Words<W>*>(blk + (kr + 8 * x) * (D / 2) + j * 4 * W);
                     ks[x] = *reinterpret_cast<const Words<W>*>(blk + 8 * D + (kr + 8 * x) * (D / 8));
+                    kb[x] = *reinterpret_cast<const uint32_t*>(blk + 8 * D + (kr + 8 * x) * (D / 8) + (j & (W - 1)) * 4);
                 }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) sc[h][t][0] = sc[h][t][1] = sc[h][t][2] = sc[h][t][3] = 0.0f;
+                float part[NT][4];
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const uint32_t x0 = kw[0].w[w], x1 = kw[1].w[w], y0 = x0 >> 8, y1 = x1 >> 8;
-                    const uint32_t a[8] = {lop_or(x0, 0x000f000fu), lop_or(x1, 0x000f000fu), lop_or(x0, 0x00f000f0u), lop_or(x1, 0x00f000f0u),
-                                           lop_or(y0, 0x000f000fu), lop_or(y1, 0x000f000fu), lop_or(y0, 0x00f000f0u), lop_or(y1, 0x00f000f0u)};
-                    const float2 s0 = halves(ks[0].w[w]), s1 = halves(ks[1].w[w]);
+                    const uint32_t a[8] = {x0 & 0x000f000fu, x1 & 0x000f000fu, x0 & 0x00f000f0u, x1 & 0x00f000f0u,
+                                           y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
+                    const float s0 = halves(ks[0].w[w]).x, s1 = halves(ks[1].w[w]).x;
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        float d[4] = {off[t][w][0], off[t][w][1], off[t][w][0], off[t][w][1]};
+                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                         mma_f16(d, a[0], a[1], a[2], a[3], qf[t][2 * w][0], qf[t][2 * w][1]);
                         mma_f16(d, a[4], a[5], a[6], a[7], qf[t][2 * w + 1][0], qf[t][2 * w + 1][1]);
-                        sc[h][t][0] = fmaf(s0.y, qsum[t][w][0], fmaf(s0.x, d[0], sc[h][t][0]));
-                        sc[h][t][1] = fmaf(s0.y, qsum[t][w][1], fmaf(s0.x, d[1], sc[h][t][1]));
-                        sc[h][t][2] = fmaf(s1.y, qsum[t][w][0], fmaf(s1.x, d[2], sc[h][t][2]));
-                        sc[h][t][3] = fmaf(s1.y, qsum[t][w][1], fmaf(s1.x, d[3], sc[h][t][3]));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) part[t][k] = w ? fmaf(k < 2 ? s0 : s1, d[k], part[t][k]) : (k < 2 ? s0 : s1) * d[k];
                     }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    mma_f16_k8(d, __byte_perm(kb[0], 0, 0x3232), __byte_perm(kb[1], 0, 0x3232), qs[t]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sc[h][t][k] = fmaf(part[t][k], 16384.0f, d[k]);      // 2^(24 - 10)
                 }
             }
             if (at < all_lo || at + DEC_UNIT > all_hi || here != 3) {
@@ -628,7 +663,7 @@ kv4_decode_kernel(const DecParams p)
             }
         }
         if (!whole) {
-            const int b_first = (int)(it.u0 / share), b_last = (int)((it.u0 + it.units - 1) / share);
+            const int b_first = runs.block_of(it.u0), b_last = runs.block_of(it.u0 + it.units - 1);
             __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) {
@@ -640,21 +675,28 @@ kv4_decode_kernel(const DecParams p)
             }
             __syncthreads();
             if (last_s) {
+                // the parts' weights, then the numbers, all loads side by side (a part's reference and sum)
+                const int parts = b_last - b_first + 1;
+                float2* weight = reinterpret_cast<float2*>(heads_kept + (size_t)WARPS * p.keep_cols * D);
+                for (int i = threadIdx.x; i < parts * cols; i += THREADS) {
+                    const int b = i / cols, col = i - b * cols;
+                    const float* src = p.parts + ((size_t)(b_first + b) * 2 + (b == 0 ? 1 : 0)) * PART + ROWS * D + col;
+                    weight[i] = make_float2(__ldcg(src), __ldcg(src + ROWS));
+                }
+                __syncthreads();
                 for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
                     const int col = i / (D / 4), d = i % (D / 4) * 4;
                     float top = kNone, l = 0.0f;
+                    for (int b = 0; b < parts; ++b) top = fmaxf(top, weight[b * cols + col].x);
                     float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-                    for (int b = b_first; b <= b_last; ++b) {
-                        const float* src = p.parts + ((size_t)b * 2 + (b == b_first ? 1 : 0)) * PART;
-                        const float t = __ldcg(src + ROWS * D + col), ls = __ldcg(src + ROWS * (D + 1) + col);
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(src + col * D + d));
-                        const float nt = fmaxf(top, t);
-                        const float fa = ex2(top - nt), fb = ex2(t - nt);
-                        v.x = v.x * fa + x.x * fb; v.y = v.y * fa + x.y * fb;
-                        v.z = v.z * fa + x.z * fb; v.w = v.w * fa + x.w * fb;
-                        l = l * fa + ls * fb;
-                        top = nt;
+                    const float* src = p.parts + (size_t)b_first * 2 * PART + col * D + d;
+#pragma unroll 16
+                    for (int b = 0; b < parts; ++b) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)(2 * b + (b == 0 ? 1 : 0)) * PART));
+                        const float2 w = weight[b * cols + col];
+                        const float f = ex2(w.x - top);
+                        v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+                        l = fmaf(w.y, f, l);
                     }
                     write(col, d, v, l);
                 }
@@ -667,11 +709,11 @@ template <int D, int NT>
 tsvd_status_t launch(DecParams p, long long items, long long units_most, cudaStream_t st)
 {
     constexpr size_t kRoom = 227 * 1024 - DEC_STATIC;          // beside what the kernel declares itself
-    const size_t kept = sizeof(float) * DEC_WARPS * p.keep_cols * D;
-    const size_t unit = (size_t)DEC_WARPS * 40 * D;
+    const size_t kept = sizeof(float) * kWarps<NT> * p.keep_cols * D + sizeof(float2) * p.sms * p.keep_cols;
+    const size_t unit = (size_t)kWarps<NT> * 40 * D;
     p.stages = (int)std::min<size_t>(DEC_MAX_STAGES, (kRoom - 128 - kept) / unit);
-    const long long blocks = std::min((long long)p.sms, std::max(items, (units_most + DEC_WARPS - 1) / DEC_WARPS));
-    PdlLaunch l((unsigned)blocks, DEC_WARPS * 32, 128 + kept + p.stages * unit, st);
+    const long long blocks = std::min((long long)p.sms, std::max(items, (units_most + kWarps<NT> - 1) / kWarps<NT>));
+    PdlLaunch l((unsigned)blocks, kWarps<NT> * 32, 128 + kept + p.stages * unit, st);
     TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_decode_kernel<D, NT>, p));
     tsvd_count_launch();
     return TSVD_OK;
