@@ -186,7 +186,6 @@ kv4_decode_kernel(const DecParams p)
     __shared__ float kept_ref[2][WARPS][ROWS], kept_sum[2][WARPS][ROWS];
     __shared__ Item kept[2][WARPS];
     __shared__ int ctl_[2];
-    __shared__ unsigned last_s;
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
 
@@ -349,6 +348,21 @@ kv4_decode_kernel(const DecParams p)
             }
         }
     };
+    // An item's query rows: column r of each group of eight, numbers 32 w + 8 j .. + 7.
+    auto ask_q = [&](const Item& it, uint4 (&x)[NT][W]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = it.row0 + 8 * t + r;
+            const __nv_bfloat16* src = nullptr;
+            if (row < it.n_rows) src = p.q + (long long)(it.first_row + row / p.group) * p.ldq + (long long)(it.head * p.group + row % p.group) * D;
+#pragma unroll
+            for (int w = 0; w < W; ++w) x[t][w] = src ? *reinterpret_cast<const uint4*>(src + 32 * w + 8 * j) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    // (the first item's before any copy: behind the copies of all warps they took 3 us)
+    uint4 qx[NT][W];
+    more = next_item();
+    if (more) ask_q(queue[warp][0], qx);
     for (int i = 0; i < p.stages; ++i) feed(i);
     __syncwarp();
 
@@ -359,20 +373,18 @@ kv4_decode_kernel(const DecParams p)
         const Item it = queue[warp][popped % DEC_QUEUE];
 
         // ---- the item's query rows ----
+        if (popped > 0) ask_q(it, qx);
         uint32_t qf[NT][2 * W][2];           // [..][MMA step][word]: column r
         uint32_t qs[NT];                     // column r: the sum of q over group j, in two fp16 terms
         float cmul[NT][2];                   // columns 2 j, 2 j + 1
         int lo[NT][2], hi[NT][2];            // positions [lo, hi) that those columns see
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int row = it.row0 + 8 * t + r;
-            const __nv_bfloat16* src = nullptr;
-            if (row < it.n_rows) src = p.q + (long long)(it.first_row + row / p.group) * p.ldq + (long long)(it.head * p.group + row % p.group) * D;
             float v[W][8];
             float top = 0.0f;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                uint4 x = src ? *reinterpret_cast<const uint4*>(src + 32 * w + 8 * j) : make_uint4(0, 0, 0, 0);
+                const uint4 x = qx[t][w];
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -619,12 +631,25 @@ kv4_decode_kernel(const DecParams p)
     // ================= the block's parts: chains of warps that share an item =================
     __syncthreads();
     constexpr int THREADS = WARPS * 32, PART = ROWS * (D + 2);
-    // In the order of the units: warp 0's part of an item from before, then each warp's item that ends after it, with the
-    // parts of the warps that follow.
-    for (int a = -1; a < WARPS; ++a) {
-        const int from = a < 0 ? 0 : a;
-        const Item it = kept[a < 0 ? 0 : 1][from];
-        if (it.units == 0) continue;
+    // In the order of the units: warp 0's part of an item from before (-1), then each warp's item that ends after it (its
+    // number), with the parts of the warps that follow.  At most two of them lack other blocks' parts: the first and the last.
+    struct Open { int chain, b_first, b_last; };
+    __shared__ Open open_s[2];
+    __shared__ unsigned last_s[2];
+    const unsigned chains = __ballot_sync(0xffffffffu, lane <= WARPS && kept[lane ? 1 : 0][lane ? min(lane, WARPS) - 1 : 0].units != 0);
+    if (chains == 0) return;
+    auto write = [&](const Item& it, int col, int d, float4 v, float l) {
+        const int row = it.row0 + col;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+        *reinterpret_cast<uint2*>(p.out + (long long)(it.first_row + row / p.group) * p.ldo + (long long)(it.head * p.group + row % p.group) * D + d) =
+            make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
+    };
+    int open = 0;
+    for (unsigned rest = chains; rest; rest &= rest - 1) {
+        const int a = __ffs(rest) - 2, from = max(a, 0);
+        const bool starts = a >= 0;
+        const Item& it = kept[starts][from];
         int to = from;                                         // the last warp of the chain
         bool ends = it.unit1 == it.units;
         while (!ends && to + 1 < WARPS && kept[0][to + 1].units != 0) {
@@ -632,15 +657,7 @@ kv4_decode_kernel(const DecParams p)
             ends = kept[0][to].unit1 == kept[0][to].units;
         }
         const int cols = min(ROWS, it.n_rows - it.row0);
-        const bool starts = a >= 0, whole = starts && ends;
-        auto write = [&](int col, int d, float4 v, float l) {
-            const int row = it.row0 + col;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-            __nv_bfloat162 x = __floats2bfloat162_rn(v.x * inv, v.y * inv), y = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-            *reinterpret_cast<uint2*>(p.out + (long long)(it.first_row + row / p.group) * p.ldo +
-                                      (long long)(it.head * p.group + row % p.group) * D + d) =
-                make_uint2(*reinterpret_cast<uint32_t*>(&x), *reinterpret_cast<uint32_t*>(&y));
-        };
+        const bool whole = starts && ends;
         float* part = p.parts + ((size_t)blockIdx.x * 2 + (starts ? 1 : 0)) * PART;
         for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
             const int col = i / (D / 4), d = i % (D / 4) * 4;
@@ -656,51 +673,57 @@ kv4_decode_kernel(const DecParams p)
                 l = fmaf(kept_sum[own][w][col], f, l);
             }
             if (whole) {
-                write(col, d, v, l);
+                write(it, col, d, v, l);
             } else {
                 __stcg(reinterpret_cast<float4*>(part + col * D + d), v);
                 if (d == 0) { __stcg(part + ROWS * D + col, top); __stcg(part + ROWS * (D + 1) + col, l); }
             }
         }
         if (!whole) {
-            const int b_first = runs.block_of(it.u0), b_last = runs.block_of(it.u0 + it.units - 1);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const unsigned n = (unsigned)(b_last - b_first + 1);
-                const unsigned seen = atomicAdd(&p.tickets[b_first], 1u);
-                last_s = seen + 1 == n;
-                if (seen + 1 == n) p.tickets[b_first] = 0;
-                __threadfence();
-            }
-            __syncthreads();
-            if (last_s) {
-                // the parts' weights, then the numbers, all loads side by side (a part's reference and sum)
-                const int parts = b_last - b_first + 1;
-                float2* weight = reinterpret_cast<float2*>(heads_kept + (size_t)WARPS * p.keep_cols * D);
-                for (int i = threadIdx.x; i < parts * cols; i += THREADS) {
-                    const int b = i / cols, col = i - b * cols;
-                    const float* src = p.parts + ((size_t)(b_first + b) * 2 + (b == 0 ? 1 : 0)) * PART + ROWS * D + col;
-                    weight[i] = make_float2(__ldcg(src), __ldcg(src + ROWS));
-                }
-                __syncthreads();
-                for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
-                    const int col = i / (D / 4), d = i % (D / 4) * 4;
-                    float top = kNone, l = 0.0f;
-                    for (int b = 0; b < parts; ++b) top = fmaxf(top, weight[b * cols + col].x);
-                    float4 v = make_float4(0, 0, 0, 0);
-                    const float* src = p.parts + (size_t)b_first * 2 * PART + col * D + d;
+            if (threadIdx.x == 0) open_s[open] = Open{a, runs.block_of(it.u0), runs.block_of(it.u0 + it.units - 1)};
+            ++open;
+        }
+    }
+    if (open == 0) return;
+    __threadfence();
+    __syncthreads();
+    if ((int)threadIdx.x < open) {
+        const Open o = open_s[threadIdx.x];
+        const unsigned seen = atomicAdd(&p.tickets[o.b_first], 1u) + 1, n = (unsigned)(o.b_last - o.b_first + 1);
+        last_s[threadIdx.x] = seen == n;
+        if (seen == n) p.tickets[o.b_first] = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    for (int k = 0; k < open; ++k) {
+        if (!last_s[k]) continue;
+        // this block's part was the last: the parts' weights (reference and sum), then their numbers, all loads side by side
+        const Open o = open_s[k];
+        const Item& it = kept[o.chain >= 0][max(o.chain, 0)];
+        const int cols = min(ROWS, it.n_rows - it.row0), parts = o.b_last - o.b_first + 1;
+        float2* weight = reinterpret_cast<float2*>(heads_kept + (size_t)WARPS * p.keep_cols * D);
+        if (k) __syncthreads();
+        for (int i = threadIdx.x; i < parts * cols; i += THREADS) {
+            const int b = i / cols, col = i - b * cols;
+            const float* src = p.parts + ((size_t)(o.b_first + b) * 2 + (b == 0 ? 1 : 0)) * PART + ROWS * D + col;
+            weight[i] = make_float2(__ldcg(src), __ldcg(src + ROWS));
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
+            const int col = i / (D / 4), d = i % (D / 4) * 4;
+            float top = kNone, l = 0.0f;
+            for (int b = 0; b < parts; ++b) top = fmaxf(top, weight[b * cols + col].x);
+            float4 v = make_float4(0, 0, 0, 0);
+            const float* src = p.parts + (size_t)o.b_first * 2 * PART + col * D + d;
 #pragma unroll 16
-                    for (int b = 0; b < parts; ++b) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)(2 * b + (b == 0 ? 1 : 0)) * PART));
-                        const float2 w = weight[b * cols + col];
-                        const float f = ex2(w.x - top);
-                        v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-                        l = fmaf(w.y, f, l);
-                    }
-                    write(col, d, v, l);
-                }
+            for (int b = 0; b < parts; ++b) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)(2 * b + (b == 0 ? 1 : 0)) * PART));
+                const float2 w = weight[b * cols + col];
+                const float f = ex2(w.x - top);
+                v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+                l = fmaf(w.y, f, l);
             }
+            write(it, col, d, v, l);
         }
     }
 }
