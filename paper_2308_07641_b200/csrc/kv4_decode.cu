@@ -697,33 +697,67 @@ kv4_decode_kernel(const DecParams p)
     __syncthreads();
     for (int k = 0; k < open; ++k) {
         if (!last_s[k]) continue;
-        // this block's part was the last: the parts' weights (reference and sum), then their numbers, all loads side by side
+        // this block's part was the last
         const Open o = open_s[k];
         const Item& it = kept[o.chain >= 0][max(o.chain, 0)];
         const int cols = min(ROWS, it.n_rows - it.row0), parts = o.b_last - o.b_first + 1;
-        float2* weight = reinterpret_cast<float2*>(heads_kept + (size_t)WARPS * p.keep_cols * D);
+        // Each number's parts are dealt to `deal` threads, which load eight at a time, references and sums beside them, and meet
+        // in the (idle) ring: what counts here is how many loads follow one another, 1 to 2 us each.
+        const int numbers = cols * (D / 4), deal = max(1, THREADS / numbers);
+        float4* met = reinterpret_cast<float4*>(ring);
+        float2* met_tl = reinterpret_cast<float2*>(met + deal * numbers);
         if (k) __syncthreads();
-        for (int i = threadIdx.x; i < parts * cols; i += THREADS) {
-            const int b = i / cols, col = i - b * cols;
-            const float* src = p.parts + ((size_t)(o.b_first + b) * 2 + (b == 0 ? 1 : 0)) * PART + ROWS * D + col;
-            weight[i] = make_float2(__ldcg(src), __ldcg(src + ROWS));
+        for (int i = threadIdx.x; i < deal * numbers; i += THREADS) {
+            const int g = i / numbers, n = i - g * numbers, col = n / (D / 4), d = n % (D / 4) * 4;
+            float top = kNone, l = 0.0f;
+            float4 v = make_float4(0, 0, 0, 0);
+            const float* src = p.parts + (size_t)o.b_first * 2 * PART;
+            for (int b0 = g; b0 < parts; b0 += 8 * deal) {
+                float4 x[8];
+                float t[8], ls[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int b = b0 + e * deal;
+                    const float* at = src + (size_t)(2 * b + (b == 0 ? 1 : 0)) * PART;
+                    x[e] = make_float4(0, 0, 0, 0);
+                    t[e] = kNone;
+                    ls[e] = 0.0f;
+                    if (b < parts) {
+                        x[e] = __ldcg(reinterpret_cast<const float4*>(at + col * D + d));
+                        t[e] = __ldcg(at + ROWS * D + col);
+                        ls[e] = __ldcg(at + ROWS * (D + 1) + col);
+                    }
+                }
+                float high = top;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) high = fmaxf(high, t[e]);
+                const float keep = ex2(top - high);
+                top = high;
+                v.x *= keep; v.y *= keep; v.z *= keep; v.w *= keep;
+                l *= keep;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float f = ex2(t[e] - top);
+                    v.x = fmaf(x[e].x, f, v.x); v.y = fmaf(x[e].y, f, v.y); v.z = fmaf(x[e].z, f, v.z); v.w = fmaf(x[e].w, f, v.w);
+                    l = fmaf(ls[e], f, l);
+                }
+            }
+            met[i] = v;
+            met_tl[i] = make_float2(top, l);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < cols * (D / 4); i += THREADS) {
-            const int col = i / (D / 4), d = i % (D / 4) * 4;
+        for (int n = threadIdx.x; n < numbers; n += THREADS) {
             float top = kNone, l = 0.0f;
-            for (int b = 0; b < parts; ++b) top = fmaxf(top, weight[b * cols + col].x);
+            for (int g = 0; g < deal; ++g) top = fmaxf(top, met_tl[g * numbers + n].x);
             float4 v = make_float4(0, 0, 0, 0);
-            const float* src = p.parts + (size_t)o.b_first * 2 * PART + col * D + d;
-#pragma unroll 16
-            for (int b = 0; b < parts; ++b) {
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(src + (size_t)(2 * b + (b == 0 ? 1 : 0)) * PART));
-                const float2 w = weight[b * cols + col];
-                const float f = ex2(w.x - top);
+            for (int g = 0; g < deal; ++g) {
+                const float4 x = met[g * numbers + n];
+                const float2 tl = met_tl[g * numbers + n];
+                const float f = ex2(tl.x - top);
                 v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-                l = fmaf(w.y, f, l);
+                l = fmaf(tl.y, f, l);
             }
-            write(it, col, d, v, l);
+            write(it, n / (D / 4), n % (D / 4) * 4, v, l);
         }
     }
 }
@@ -732,7 +766,7 @@ template <int D, int NT>
 tsvd_status_t launch(DecParams p, long long items, long long units_most, cudaStream_t st)
 {
     constexpr size_t kRoom = 227 * 1024 - DEC_STATIC;          // beside what the kernel declares itself
-    const size_t kept = sizeof(float) * kWarps<NT> * p.keep_cols * D + sizeof(float2) * p.sms * p.keep_cols;
+    const size_t kept = sizeof(float) * kWarps<NT> * p.keep_cols * D;
     const size_t unit = (size_t)kWarps<NT> * 40 * D;
     p.stages = (int)std::min<size_t>(DEC_MAX_STAGES, (kRoom - 128 - kept) / unit);
     const long long blocks = std::min((long long)p.sms, std::max(items, (units_most + kWarps<NT> - 1) / kWarps<NT>));
