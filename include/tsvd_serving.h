@@ -20,13 +20,13 @@ extern "C" {
 
 /*
  * tsvd_quantize -- 8-bit integers with one scale per row:
- *     a_b = max_n |x_bn|,   scale_b = a_b / 127,   q_bn = rint(x_bn * (127 / a_b))
- * in fp32 (both divisions correctly rounded, rint to even), so -127 <= q <= 127.
+ *     a_b = max_n |x_bn|,   scale_b = a_b * (1 / 127),   q_bn = rint(x_bn * ((1 / a_b) * 127))
+ * in fp32 (every reciprocal and product rounded to nearest, rint to even), so -127 <= q <= 127.
  *
  *   x      device, TSVD_F32 or TSVD_BF16, row b at x + b*ldx (elements, ldx >= cols)
  *   q      device, row b at q + b*ldq (ldq >= cols); bytes between cols and ldq are not written
  *   scale  device, float [rows]
- * A row whose largest magnitude is 0, or so small (below 2^-100) that 127 / a_b would overflow, becomes q = 0.
+ * A row whose largest magnitude is 0, or so small (below 2^-100) that 1 / a_b might overflow, becomes q = 0.
  * A row that holds a NaN or an infinity gets a scale that is not finite (and unspecified q), so that what is
  * computed from it is not finite either.  rows = 0 does nothing (and looks at no pointer).  Any alignment that the types allow; 16-byte
  * aligned rows are read 16 bytes at a time.
@@ -86,7 +86,7 @@ typedef struct tsvd_kv4_s* tsvd_kv4_t; /* opaque; owns device memory on one GPU 
  * head_dim numbers.  head_dim is 64 or 128, page_tokens a multiple of 16.
  *
  * What is kept of a key or value: per position, head and group of 32 consecutive numbers
- *     step = fp16((hi - lo) / 15),  base = fp16(lo),  code = clamp(rint((x - base) * (1 / step)), 0, 15)
+ *     step = fp16((hi - lo) * (1 / 15)),  base = fp16(lo),  code = clamp(rint((x - base) * (1 / step)), 0, 15)
  * with lo and hi the group's smallest and largest number (clamped to +-65000), arithmetic in fp32; step = 0 makes
  * code = 0.  It stands for code * step + base.  5 bits a number in all.
  *

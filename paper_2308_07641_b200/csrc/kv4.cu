@@ -1,7 +1,7 @@
 // Keys and values in 4 bits: the pool of pages, append, read, and the entry point of the attention.
 //
-// Per position, head and group of 32 numbers: step = fp16((hi - lo) / 15), base = fp16(lo),
-// code = clamp(rint((x - base) / step), 0, 15).
+// Per position, head and group of 32 numbers: step = fp16((hi - lo) * (1 / 15)), base = fp16(lo),
+// code = clamp(rint((x - base) * (1 / step)), 0, 15).
 #include <new>
 #include <type_traits>
 
@@ -131,7 +131,7 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk,
         hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, 1));
         lo = fminf(fmaxf(lo, -kMost), kMost);
         hi = fmaxf(fminf(hi, kMost), -kMost);
-        const __half step = __float2half_rn(__fdiv_rn(hi - lo, 15.0f)), base = __float2half_rn(lo);
+        const __half step = __float2half_rn(__fmul_rn(hi - lo, 1.0f / 15.0f)), base = __float2half_rn(lo);
         const float s = __half2float(step), m = __half2float(base);
         const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
         uint32_t word[2];

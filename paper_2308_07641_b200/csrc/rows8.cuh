@@ -1,6 +1,6 @@
 // Rows into 8-bit integers, shared by tsvd_quantize (row-major result) and the 8-bit layer (tensor-core order).
 //
-//     a = max |x|,  scale = a / 127,  q = rint(x * (127 / a))
+//     a = max |x|,  scale = a * (1 / 127),  q = rint(x * ((1 / a) * 127))     each reciprocal and product rounded to fp32
 //
 // The largest magnitude of a row is needed before its first result, so a row's values stay in registers between the two
 // steps: a thread holds units of 16 columns (one 16-byte store of results).
@@ -11,9 +11,10 @@
 namespace rows8 {
 
 constexpr float kSmallest = 7.888609e-31f;   // 2^-100: below it 127 / a is no longer safely finite
+constexpr float kPart = 1.0f / 127.0f;
 
 // 0 for a row without values of any size; where a is not finite the scale says so
-__device__ __forceinline__ float inverse_step(float a) { return a >= kSmallest ? __fdiv_rn(127.0f, a) : 0.0f; }
+__device__ __forceinline__ float inverse_step(float a) { return a >= kSmallest ? __fmul_rn(__frcp_rn(a), 127.0f) : 0.0f; }
 __device__ __forceinline__ int quantised(float x, float inv) { return __float2int_rn(__fmul_rn(x, inv)); }
 
 // Magnitudes compared as integers: a NaN (its bits exceed infinity's) wins over everything.
@@ -144,7 +145,7 @@ quantize_kernel(const T* __restrict__ x, int rows, int cols, long long ldx, cons
         a = __uint_as_float(m);
         inv = inverse_step(a);
     }
-    if (t == 0) scale[row] = kInt ? (given ? given[row] : 1.0f) : __fdiv_rn(a, 127.0f);
+    if (t == 0) scale[row] = kInt ? (given ? given[row] : 1.0f) : __fmul_rn(a, kPart);
     if constexpr (NU > 0) {
 #pragma unroll
         for (int i = 0; i < NU; ++i) {

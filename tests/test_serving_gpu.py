@@ -47,8 +47,9 @@ def _plain_quantize(x):
     x = x.float().cpu().numpy()
     a = np.abs(x).max(axis=1) if x.shape[1] else np.zeros(x.shape[0], np.float32)
     inv = np.zeros_like(a)
-    np.divide(np.float32(127), a, out=inv, where=a >= np.float32(2.0 ** -100))
-    return np.rint(x * inv[:, None]).astype(np.int8), (a / np.float32(127)).astype(np.float32)
+    np.divide(np.float32(1), a, out=inv, where=a >= np.float32(2.0 ** -100))
+    inv = inv * np.float32(127)
+    return np.rint(x * inv[:, None]).astype(np.int8), a * (np.float32(1) / np.float32(127))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -263,7 +264,7 @@ def _plain_cached(x):
     g = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
     most = np.float32(65000)
     lo, hi = np.clip(g.min(-1), -most, most), np.clip(g.max(-1), -most, most)
-    step, base = ((hi - lo) / np.float32(15)).astype(np.float16), lo.astype(np.float16)
+    step, base = ((hi - lo) * (np.float32(1) / np.float32(15))).astype(np.float16), lo.astype(np.float16)
     s = step.astype(np.float32)
     inv = np.zeros_like(s)
     np.divide(np.float32(1), s, out=inv, where=s > 0)
