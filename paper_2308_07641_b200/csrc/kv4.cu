@@ -233,7 +233,8 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     if (e == cudaSuccess) e = cudaMalloc(&h->dev_status, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(h->dev_status, 0, sizeof(int));
     const size_t tickets = kv4_decode_tickets(h->sms) * sizeof(unsigned);
-    if (e == cudaSuccess) e = cudaMalloc(&h->parts, kv4_decode_parts_bytes(h->sms, head_dim));
+    const size_t parts = kv4_decode_parts_bytes(h->sms, head_dim), parts2 = kv4_prefill_parts_bytes(h->sms, head_dim);
+    if (e == cudaSuccess) e = cudaMalloc(&h->parts, parts > parts2 ? parts : parts2);
     if (e == cudaSuccess) e = cudaMalloc(&h->tickets, tickets);
     if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, tickets);
     if (e == cudaSuccess && (kv4_decode_prepare() != TSVD_OK || kv4_prefill_prepare() != TSVD_OK)) e = cudaErrorUnknown;

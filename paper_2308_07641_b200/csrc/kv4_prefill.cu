@@ -47,6 +47,8 @@ struct PreParams {
     float c;
     float sign;              // of the scale: goes into q
     int window, causal;
+    int splits;              // blocks that share a pair's positions; above 1 they leave their parts in `parts`
+    float* parts;            // [block][2 * PRE_ROWS][D] sums, [2 * PRE_ROWS] (reference, sum)
     int* status;
 };
 
@@ -215,7 +217,8 @@ kv4_prefill_kernel(const PreParams p)
     pdl_launch_dependents();
     pdl_wait();
     const int per = p.g.heads * p.b.n_seq;
-    const int pair = p.tiles - 1 - (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
+    const int job = (int)blockIdx.x / p.splits, split = (int)blockIdx.x - job * p.splits;
+    const int pair = p.tiles - 1 - job / per, rest = job % per;
     const int head = rest % p.g.heads, s = rest / p.g.heads;
     const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
     const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
@@ -240,8 +243,21 @@ kv4_prefill_kernel(const PreParams p)
         }
     }
     const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
-    const int j_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]), j_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
-    const int k_lo = j_lo / 2, k_hi = (j_hi + 1) / 2;       // tiles
+    const int j_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]);
+    int j_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
+    int k_lo = j_lo / 2, k_hi = (j_hi + 1) / 2;             // tiles
+    if (p.splits > 1) {
+        const int n = k_hi - k_lo, k0 = k_lo;
+        k_lo = k0 + (int)((long long)n * split / p.splits);
+        k_hi = k0 + (int)((long long)n * (split + 1) / p.splits);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            t_lo[x] = max(t_lo[x], 2 * k_lo);
+            t_hi[x] = max(min(t_hi[x], 2 * k_hi), t_lo[x]);
+        }
+        j_hi = max(t_hi[0], t_hi[1]);
+        if (t_hi[0] == t_lo[0] && t_hi[1] == t_lo[1]) k_hi = k_lo;
+    }
 
     if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before_sync();
@@ -371,7 +387,37 @@ kv4_prefill_kernel(const PreParams p)
         }
         if (ok && b > a) ok = mbar_wait(&o_done[x][(b - 1) & 1], (pho >> ((b - 1) & 1) & 1) ^ 1, ctl);
         tc_fence_after_sync();
-        if (ok) {
+        if (ok && p.splits > 1) {
+            // Its part, unnormalised, through the tile's own Q as below, half of the numbers at a time.
+            constexpr int LANES = D / 8, ROWS = 32 / LANES;
+            uint8_t* mine = own + wrow * (2 * D);
+            float* part = p.parts + (size_t)blockIdx.x * (2 * PRE_ROWS * (D + 2)) + (size_t)(x * PRE_ROWS + wrow) * D;
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                for (int c0 = 0; c0 < D / 2; c0 += 32) {
+                    uint32_t v[32] = {};
+                    if (b > a) {
+                        tmem_ld32(t_o + (uint32_t)(half * (D / 2) + c0), v);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<uint4*>(mine + lane * (2 * D) + ((((c0 + i) >> 2) ^ (lane & (LANES - 1))) << 4)) =
+                            make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < LANES; ++i) {
+                    const int rl = i * ROWS + lane / LANES, u = lane % LANES;
+                    *reinterpret_cast<uint4*>(part + rl * D + half * (D / 2) + 4 * u) =
+                        *reinterpret_cast<const uint4*>(mine + rl * (2 * D) + ((u ^ (rl & (LANES - 1))) << 4));
+                }
+                __syncwarp();
+            }
+            reinterpret_cast<float2*>(p.parts + (size_t)blockIdx.x * (2 * PRE_ROWS * (D + 2)) + 2 * PRE_ROWS * D)[x * PRE_ROWS + r] =
+                make_float2(b > a ? ref : kNone, sum);
+        } else if (ok) {
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
             // Through the tile's own Q, which the products are done with: the warp's 32 rows, 16 bytes of a row at unit
             // u ^ row, then D / 8 lanes a row.
@@ -577,18 +623,81 @@ kv4_prefill_kernel(const PreParams p)
     if (warp == 12) tmem_dealloc(tmem, 512);
 }
 
+// The parts of a pair's rows, in their order: D / 4 lanes a row, eight parts' loads side by side.
+constexpr int JOIN_ROWS = 32;            // rows of a block
+template <int D>
+__global__ void __launch_bounds__(256)
+kv4_join_kernel(const PreParams p)
+{
+    constexpr int LANES = D / 4, PART = 2 * PRE_ROWS * (D + 2);
+    pdl_launch_dependents();
+    pdl_wait();
+    const int per = p.g.heads * p.b.n_seq, blocks_per_job = 2 * PRE_ROWS / JOIN_ROWS;
+    const int job = (int)blockIdx.x / blocks_per_job, row_in0 = ((int)blockIdx.x - job * blocks_per_job) * JOIN_ROWS;
+    const int pair = p.tiles - 1 - job / per, rest = job % per, head = rest % p.g.heads, s = rest / p.g.heads;
+    const int first = kv4_first_row(p.b, s), all = kv4_first_row(p.b, s + 1) - first;
+    const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
+    const int d = (int)(threadIdx.x % LANES) * 4;
+    for (int r = (int)(threadIdx.x / LANES); r < JOIN_ROWS; r += 256 / LANES) {
+        const int row_in = row_in0 + r, row = pair * 2 * PRE_ROWS + row_in;
+        if (row >= n_rows) return;
+        const float* src = p.parts + (size_t)job * p.splits * PART;
+        float top = kNone, l = 0.0f;
+        float4 v = make_float4(0, 0, 0, 0);
+        for (int b0 = 0; b0 < p.splits; b0 += 8) {
+            float4 y[8];
+            float2 tl[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = make_float4(0, 0, 0, 0);
+                tl[e] = make_float2(kNone, 0.0f);
+                if (b0 + e < p.splits) {
+                    const float* at = src + (size_t)(b0 + e) * PART;
+                    y[e] = __ldcg(reinterpret_cast<const float4*>(at + row_in * D + d));
+                    tl[e] = __ldcg(reinterpret_cast<const float2*>(at + 2 * PRE_ROWS * D) + row_in);
+                }
+            }
+            float high = top;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) high = fmaxf(high, tl[e].x);
+            const float keep = ex2(top - high);
+            top = high;
+            v.x *= keep; v.y *= keep; v.z *= keep; v.w *= keep;
+            l *= keep;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float f = ex2(tl[e].x - top);
+                v.x = fmaf(y[e].x, f, v.x); v.y = fmaf(y[e].y, f, v.y); v.z = fmaf(y[e].z, f, v.z); v.w = fmaf(y[e].w, f, v.w);
+                l = fmaf(tl[e].y, f, l);
+            }
+        }
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const __nv_bfloat162 y0 = __floats2bfloat162_rn(v.x * inv, v.y * inv), y1 = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+        const int token = row / p.group;
+        *reinterpret_cast<uint2*>(p.out + (long long)(first + token) * p.ldo + (long long)(head * p.group + row - token * p.group) * D + d) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+    }
+}
+
 template <int D>
 tsvd_status_t launch(const PreParams& p, cudaStream_t st)
 {
-    const long long blocks = (long long)p.tiles * p.g.heads * p.b.n_seq;
+    const long long blocks = (long long)p.tiles * p.g.heads * p.b.n_seq * p.splits;
     if (blocks > 0x7fffffffLL) return TSVD_E_TOOBIG;
     PdlLaunch l((unsigned)blocks, PRE_THREADS, Layout<D>::kBytes + 1024, st);
     TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_prefill_kernel<D>, p));
     tsvd_count_launch();
+    if (p.splits > 1) {
+        PdlLaunch j((unsigned)(blocks / p.splits * (2 * PRE_ROWS / JOIN_ROWS)), 256, 0, st);
+        TSVD_CUDA_OK(cudaLaunchKernelEx(&j.cfg, kv4_join_kernel<D>, p));
+        tsvd_count_launch();
+    }
     return TSVD_OK;
 }
 
 }  // namespace
+
+size_t kv4_prefill_parts_bytes(int sms, int dim) { return sizeof(float) * (size_t)sms * 2 * PRE_ROWS * (dim + 2); }
 
 tsvd_status_t kv4_prefill_prepare()
 {
@@ -615,5 +724,12 @@ tsvd_status_t kv4_attend_prefill(const AttendArgs& a)
     p.window = a.window;
     p.causal = a.causal;
     p.status = a.h->dev_status;
+    p.parts = a.h->parts;
+    // Fewer pairs than half the SMs: blocks share a pair's positions, at least four tiles each (a tile takes about 2 us, the
+    // step over scratch about 4).
+    const long long jobs = (long long)p.tiles * p.g.heads * p.b.n_seq;
+    long long seen = a.max_kv;
+    if (a.window) seen = std::min<long long>(seen, (long long)a.window + 2 * PRE_ROWS / p.group + 1);
+    p.splits = (int)std::max(1LL, std::min(a.h->sms / jobs, seen / (4 * PRE_KEYS)));
     return p.g.dim == 128 ? launch<128>(p, a.stream) : launch<64>(p, a.stream);
 }

@@ -128,5 +128,6 @@ tsvd_status_t kv4_attend_decode(const AttendArgs& a);   // kv4_decode.cu: few ro
 tsvd_status_t kv4_decode_prepare();                     // once for the current device
 tsvd_status_t kv4_attend_prefill(const AttendArgs& a);  // kv4_prefill.cu: many rows, bf16
 tsvd_status_t kv4_prefill_prepare();
+size_t kv4_prefill_parts_bytes(int sms, int dim);
 size_t kv4_decode_parts_bytes(int sms, int dim);        // its scratch
 size_t kv4_decode_tickets(int sms);

@@ -431,6 +431,8 @@ ROWS = [
     ([64], [64], 2, 2, 64, 16), ([130], [130], 3, 3, 128, 16), ([127, 129, 300], [127, 129, 33], 4, 2, 64, 32),
     ([500, 0, 77], [300, 0, 77], 6, 2, 128, 48), ([1100], [257], 8, 1, 128, 64), ([900], [900], 2, 1, 64, 128), ([260, 1, 256], [256, 1, 1], 4, 4, 128, 256),
     ([33, 600], [33, 40], 5, 1, 64, 16), ([2048], [1024], 2, 2, 128, 64), ([1500, 1499], [129, 700], 12, 3, 64, 64),
+    # few rows behind a long context: blocks share the positions
+    ([4000], [40], 2, 2, 128, 64), ([3001, 700], [65, 1], 8, 1, 64, 32), ([5000, 90, 0, 1300], [130, 90, 0, 33], 4, 2, 128, 16),
 ]
 
 
