@@ -357,7 +357,14 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     a.causal = flags & TSVD_FLAG_CAUSAL;
     a.stream = (cudaStream_t)stream;
     if (dtype == TSVD_F32 || (flags & TSVD_FLAG_PATH_SIMPLE)) return kv4_attend_simple(a);
-    return (long long)a.max_q * (n_heads / h->g.heads) <= 32 ? kv4_attend_decode(a) : kv4_attend_prefill(a);
+    // Up to 16 rows a key/value head are one item of the kernel for few rows: 34 us against 40 (16 rows, 32 heads) and 60 against
+    // 94 (32 sequences of 8 heads) behind 8000 and 3000 positions.  At 17 to 32 rows it reads the cache twice, 45 against 42
+    // and 100 against 94; but with more than four heads and sequences an SM the other one's start and end, of about 9 us a
+    // block, weigh more: 42 against 74 us for 32 sequences of 32 heads and 88 positions, 142 against 165 for 1024 positions.
+    // Beyond 32 rows: 60 against 42 at 48 rows, 32 heads and 8000 positions.
+    const long long rows = (long long)a.max_q * (n_heads / h->g.heads);
+    const bool few = rows <= 16 || (rows <= 32 && (long long)n_seq * h->g.heads > 4LL * h->sms);
+    return few ? kv4_attend_decode(a) : kv4_attend_prefill(a);
 }
 
 extern "C" tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages, size_t* pool_bytes)

@@ -252,7 +252,7 @@ kv4_prefill_kernel(const PreParams p)
         k_hi = k0 + (int)((long long)n * (split + 1) / p.splits);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            t_lo[x] = max(t_lo[x], 2 * k_lo);
+            t_lo[x] = min(max(t_lo[x], 2 * k_lo), 2 * k_hi);
             t_hi[x] = max(min(t_hi[x], 2 * k_hi), t_lo[x]);
         }
         j_hi = max(t_hi[0], t_hi[1]);

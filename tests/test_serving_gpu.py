@@ -433,6 +433,9 @@ ROWS = [
     ([33, 600], [33, 40], 5, 1, 64, 16), ([2048], [1024], 2, 2, 128, 64), ([1500, 1499], [129, 700], 12, 3, 64, 64),
     # few rows behind a long context: blocks share the positions
     ([4000], [40], 2, 2, 128, 64), ([3001, 700], [65, 1], 8, 1, 64, 32), ([5000, 90, 0, 1300], [130, 90, 0, 33], 4, 2, 128, 16),
+    # many sequences of unlike lengths, some without a row or a position
+    ([(37 * i) % 301 for i in range(16)], [min((37 * i) % 301, (53 * i) % 190) for i in range(16)], 4, 4, 64, 16),
+    ([(61 * i) % 700 for i in range(10)], [min((61 * i) % 700, (89 * i) % 400) for i in range(10)], 16, 4, 128, 32),
 ]
 
 
