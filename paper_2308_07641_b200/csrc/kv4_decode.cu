@@ -19,6 +19,12 @@
 // up to 2^-34 of the row's largest).  Values become fp16 numbers code * step + base (one rounding); probabilities fp16,
 // relative to a reference that moves only when a score passes the one it was set by by more than 5 (in units of log2): no
 // exchange between lanes otherwise.
+//
+// Measured: 32 sequences of 32 heads on 8, 174 MB of cache, 56 us = 3.1 TB/s (floor 27); one sequence of 100003 positions, 128 MB,
+// 40 us = 3.2 TB/s (floor 20); one short sequence of 12 heads 8.8 us.  What bounds the long ones is instructions and their
+// latency, not the copies: issue slots 48% busy with three warps a scheduler, 1057 clocks a unit and scheduler, of which turning the
+// values' codes into fp16 is the largest share; some 4 us pass before the first unit and 4 to 8 after the last (the parts'
+// exchange).  Warps that only convert, feeding others, were slower (they were the bottleneck), as were 16 warps (80 us).
 #include <algorithm>
 
 #include "serving.cuh"
@@ -30,7 +36,9 @@ using namespace ptx;
 
 constexpr int DEC_MAX_STAGES = 6;
 constexpr int DEC_QUEUE = 8;             // items that the copies may be ahead: more than DEC_MAX_STAGES
-constexpr int DEC_APART = 6;             // units a warp up to which items get a block each: a step over scratch costs as much
+// Units a warp up to which items get a block each: a step over scratch costs as much.  8 sequences of 8 heads: 600 positions 11.1
+// us apart, 15.5 in equal runs; 1500 positions 15.9 and 17.7; 3000 25.5 and 22.1; 2 sequences, 4000: 32 and 16.
+constexpr int DEC_APART = 6;
 constexpr int DEC_STATIC = 13 * 1024;    // room for what the kernel declares
 // Warps of a block: 12 of up to 168 registers a thread for eight rows (8 of 255: 46 -> 42 us for 100003 positions), 8 for sixteen
 // rows, whose sums need more.
