@@ -45,6 +45,7 @@ typedef struct tsvd_i8_s* tsvd_i8_t; /* opaque; owns device memory on one GPU */
  * tsvd_i8_pack -- keep the weights of a linear layer in 8 bits:  W [M,N] row-major, one scale per output channel.
  *   W        int8, row m at W + m*ldw (ldw >= N); w_scale float [M]; bias float [M] or NULL.
  *            Host or device pointers; copied.  tsvd_quantize on the rows of a float matrix makes W and w_scale.
+ *            Device sources must be ready: the copies wait for no stream of the caller's (the torch front does).
  * The copy is cut into the 128 x 128 tiles that the tensor-core kernels read.
  * Synchronous.  Errors: E_NULL, E_SHAPE, E_TOOBIG (N above TSVD_I8_MAX_N: a sum of N products of two 8-bit values
  * must fit 32 bits), E_DTYPE (flags is not 0), E_NOMEM, E_CUDA.
