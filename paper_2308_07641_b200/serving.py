@@ -40,14 +40,16 @@ def _stream(x) -> int:
 
 
 def _rows(x, what: str):
-    """A CUDA tensor [rows, cols] with contiguous rows; returns (rows, cols, row stride)."""
+    """A CUDA tensor [rows, cols] with contiguous rows; returns (rows, cols, row stride).  The stride of a single row says
+    nothing and is taken as cols; any other is handed on as it is, and the library refuses one below cols (rows that overlap,
+    as expand and unfold make them)."""
     if not x.is_cuda or x.dim() != 2:
         raise TSVDError(binding.TSVD_E_SHAPE, what)
     rows, cols = x.shape
     ld, one = x.stride()
     if one != 1 and cols > 1:
         raise TSVDError(binding.TSVD_E_SHAPE, what)
-    return rows, cols, ld if ld > cols else cols
+    return rows, cols, ld if rows > 1 else cols
 
 
 def quantize(x):
@@ -95,7 +97,7 @@ class Int8Linear:
         self.M, self.N = w8.shape
         if w8.is_cuda or w_scale.is_cuda or (bias is not None and bias.is_cuda):
             torch.cuda.current_stream().synchronize()      # the copy runs on another stream
-        self.handle = binding.tsvd_i8_pack(w8.data_ptr(), max(w8.stride(0), self.N), w_scale.data_ptr(),
+        self.handle = binding.tsvd_i8_pack(w8.data_ptr(), w8.stride(0) if self.M > 1 else self.N, w_scale.data_ptr(),
                                            bias.data_ptr() if bias is not None else 0, self.M, self.N)
 
     def reserve(self, B_max: int, x_dtype: str) -> None:
@@ -156,14 +158,15 @@ class KV4Cache:
         self.n_kv_heads, self.head_dim, self.n_pages, self.page_tokens = n_kv_heads, head_dim, n_pages, page_tokens
 
     def _heads(self, x, what: str):
-        """A CUDA tensor [rows, heads, head_dim] whose rows lie in one piece; returns (rows, heads, row stride)."""
+        """A CUDA tensor [rows, heads, head_dim] whose rows lie in one piece; returns (rows, heads, row stride), the stride
+        as in _rows."""
         if not x.is_cuda or x.dim() != 3:
             raise TSVDError(binding.TSVD_E_SHAPE, what)
         rows, heads, dim = x.shape
         ld, per_head, one = x.stride()
         if dim != self.head_dim or one != 1 or (heads > 1 and per_head != dim):
             raise TSVDError(binding.TSVD_E_SHAPE, what)
-        return rows, heads, ld if ld > heads * dim else heads * dim
+        return rows, heads, ld if rows > 1 else heads * dim
 
     def _batch(self, page_table, seq_len, q_start, rows: int, what: str):
         if not _CODES:
