@@ -5,7 +5,8 @@
  * The paper converts linear layers of BERT-base and OPT-6.7B and runs them inside those models; a layer that is
  * not converted, and the attention between two converted ones, have no counterpart in it.  These calls follow
  * tsvd.h: plain C, pointers and sizes, a status from every call, arguments checked on the host before any launch,
- * all work asynchronous on the given stream unless stated otherwise, no CPU implementation behind them.
+ * all work asynchronous on the given stream unless stated otherwise, no CPU implementation behind them.  Work runs on
+ * the current device, where stream and pointers have to belong; a handle of another device is refused with TSVD_E_CUDA.
  */
 #ifndef TSVD_SERVING_H
 #define TSVD_SERVING_H

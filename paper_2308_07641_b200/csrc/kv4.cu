@@ -264,6 +264,7 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
     if (!k || !v) return TSVD_E_NULL;
     const size_t size = dtype == TSVD_F32 ? 4 : 2;
     if (((uintptr_t)k | (uintptr_t)v) & (size - 1)) return TSVD_E_ALIGN;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
@@ -303,6 +304,7 @@ extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, voi
     if (!k || !v) return TSVD_E_NULL;
     const size_t size = dtype == TSVD_F32 ? 4 : 2;
     if (((uintptr_t)k | (uintptr_t)v) & (size - 1)) return TSVD_E_ALIGN;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
     const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size);
     cudaStream_t st = (cudaStream_t)stream;
@@ -344,6 +346,7 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     if (n_rows == 0) return TSVD_OK;
     if (!q || !out) return TSVD_E_NULL;
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ldq % 8 || ldo % 8) return TSVD_E_ALIGN;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     AttendArgs a{};
     a.h = h;
     a.b = Kv4Batch{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
@@ -385,6 +388,7 @@ extern "C" tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_
 extern "C" tsvd_status_t tsvd_kv4_last_status(tsvd_kv4_t h)
 {
     if (!h) return TSVD_E_NULL;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     int word = 0;
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));

@@ -187,6 +187,7 @@ extern "C" tsvd_status_t tsvd_i8_reserve(tsvd_i8_t h, int B_max, tsvd_dtype_t dt
     if (!h) return TSVD_E_NULL;
     if (B_max < 1) return TSVD_E_SHAPE;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16 && dtype != TSVD_I8) return TSVD_E_DTYPE;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     return i8_grow(h, B_max);
 }
 
@@ -203,6 +204,7 @@ extern "C" tsvd_status_t tsvd_i8_forward(tsvd_i8_t h, const void* x, long long l
     const bool y_bf16 = flags ? flags == TSVD_FLAG_OUT_BF16 : dtype == TSVD_BF16;
     if (misaligned(x, dtype == TSVD_F32 ? 4 : dtype == TSVD_BF16 ? 2 : 1) || misaligned(y, y_bf16 ? 2 : 4) || misaligned(x_scale, 4))
         return TSVD_E_ALIGN;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     const tsvd_status_t grown = i8_grow(h, B);
     if (grown != TSVD_OK) return grown;
     const int groups = (B + 7) / 8;
@@ -225,6 +227,7 @@ extern "C" tsvd_status_t tsvd_i8_info(tsvd_i8_t h, int* M, int* N, size_t* packe
 extern "C" tsvd_status_t tsvd_i8_last_status(tsvd_i8_t h)
 {
     if (!h) return TSVD_E_NULL;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     int word = 0;
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));

@@ -108,6 +108,14 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 #endif
 
+// A handle's memory lies on one device; its calls launch on the current one.
+inline tsvd_status_t on_current_device(int device)
+{
+    int now = 0;
+    TSVD_CUDA_OK(cudaGetDevice(&now));
+    return now == device ? TSVD_OK : TSVD_E_CUDA;
+}
+
 struct AttendArgs {
     tsvd_kv4_s* h;
     Kv4Batch b;

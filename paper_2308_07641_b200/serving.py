@@ -12,14 +12,14 @@ from .binding import DTYPES, TSVD_BF16, TSVD_F32, TSVD_I8, TSVDError
 # torch is loaded with the first call: the package's other parts do without it.  These calls last microseconds, so the front
 # looks up as little as it can: the raw stream (a Stream object costs 2 us to make), the library's functions directly.
 _CODES: dict = {}          # torch dtype -> the library's number
-_empty = _raw_stream = _i32 = _f32 = _i8 = _bf16 = None
+_empty = _raw_stream = _device = _i32 = _f32 = _i8 = _bf16 = None
 
 
 def _load() -> None:
-    global _empty, _raw_stream, _i32, _f32, _i8, _bf16
+    global _empty, _raw_stream, _device, _i32, _f32, _i8, _bf16
     import torch
-    from torch._C import _cuda_getCurrentRawStream
-    _empty, _raw_stream = torch.empty_strided, _cuda_getCurrentRawStream
+    from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
+    _empty, _raw_stream, _device = torch.empty_strided, _cuda_getCurrentRawStream, _cuda_getDevice
     _i32, _f32, _i8, _bf16 = torch.int32, torch.float32, torch.int8, torch.bfloat16
     _CODES.update({torch.float32: TSVD_F32, torch.bfloat16: TSVD_BF16, torch.int8: TSVD_I8})
 
@@ -34,9 +34,16 @@ def _code(dtype, what: str) -> int:
     return code
 
 
-def _stream(x) -> int:
-    """torch's current stream on x's device."""
-    return _raw_stream(x.get_device())
+def _stream(what: str, x, *others) -> int:
+    """torch's current stream, after a check that all tensors (or None) of a call lie on the current device: the library
+    launches there, whatever the pointers."""
+    index = x.get_device()
+    if index != _device():
+        raise TSVDError(binding.TSVD_E_CUDA, what)
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise TSVDError(binding.TSVD_E_CUDA if t.is_cuda else binding.TSVD_E_SHAPE, what)
+    return _raw_stream(index)
 
 
 def _rows(x, what: str):
@@ -57,10 +64,11 @@ def quantize(x):
     (q int8 [rows, cols], its rows 16-byte aligned; scale float32 [rows]); x is about q * scale[:, None]."""
     rows, cols, ldx = _rows(x, "quantize")
     code, device = _code(x.dtype, "quantize"), x.device
+    stream = _stream("quantize", x)
     ldq = (cols + 15) & ~15
     q = _empty((rows, cols), (ldq, 1), dtype=_i8, device=device)
     scale = _empty((rows,), (1,), dtype=_f32, device=device)
-    err = binding.lib().tsvd_quantize(x.data_ptr(), code, rows, cols, ldx, q.data_ptr(), ldq, scale.data_ptr(), _stream(x))
+    err = binding.lib().tsvd_quantize(x.data_ptr(), code, rows, cols, ldx, q.data_ptr(), ldq, scale.data_ptr(), stream)
     if err:
         raise TSVDError(err, "tsvd_quantize")
     return q, scale
@@ -75,8 +83,9 @@ def dequantize(q, scale, dtype=None):
         raise TSVDError(binding.TSVD_E_SHAPE, "dequantize")
     dtype = dtype or _f32
     code = _code(dtype, "dequantize")
+    stream = _stream("dequantize", q, scale)
     y = _empty((rows, cols), (cols, 1), dtype=dtype, device=q.device)
-    err = binding.lib().tsvd_dequantize(q.data_ptr(), ldq, scale.data_ptr(), rows, cols, y.data_ptr(), code, cols, _stream(q))
+    err = binding.lib().tsvd_dequantize(q.data_ptr(), ldq, scale.data_ptr(), rows, cols, y.data_ptr(), code, cols, stream)
     if err:
         raise TSVDError(err, "tsvd_dequantize")
     return y
@@ -95,8 +104,8 @@ class Int8Linear:
                 bias is not None and (bias.shape != w_scale.shape or not bias.is_contiguous())):
             raise TSVDError(binding.TSVD_E_SHAPE, "Int8Linear")
         self.M, self.N = w8.shape
-        if w8.is_cuda or w_scale.is_cuda or (bias is not None and bias.is_cuda):
-            torch.cuda.current_stream().synchronize()      # the copy runs on another stream
+        for device in {t.device for t in (w8, w_scale, bias) if t is not None and t.is_cuda}:
+            torch.cuda.current_stream(device).synchronize()      # the copy runs on another stream
         self.handle = binding.tsvd_i8_pack(w8.data_ptr(), w8.stride(0) if self.M > 1 else self.N, w_scale.data_ptr(),
                                            bias.data_ptr() if bias is not None else 0, self.M, self.N)
 
@@ -115,6 +124,7 @@ class Int8Linear:
                 raise TSVDError(binding.TSVD_E_SHAPE, "Int8Linear.forward")
             if x_scale.dtype != _f32:
                 raise TSVDError(binding.TSVD_E_DTYPE, "Int8Linear.forward")
+        stream = _stream("Int8Linear.forward", x, x_scale, out)
         want = _bf16 if (flags & binding.TSVD_FLAG_OUT_BF16 or (dt == TSVD_BF16 and not flags & binding.TSVD_FLAG_OUT_F32)) else _f32
         ldy = self.M
         if out is None:
@@ -124,7 +134,7 @@ class Int8Linear:
         else:
             ldy = _rows(out, "Int8Linear.forward")[2]
         err = binding.lib().tsvd_i8_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else None,
-                                            out.data_ptr(), ldy, B, dt, flags, _stream(x))
+                                            out.data_ptr(), ldy, B, dt, flags, stream)
         if err:
             raise TSVDError(err, "tsvd_i8_forward")
         return out
@@ -195,7 +205,7 @@ class KV4Cache:
             raise TSVDError(binding.TSVD_E_SHAPE, "KV4Cache.append")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.append")
         err = binding.lib().tsvd_kv4_append(self.handle, k.data_ptr(), ldk, v.data_ptr(), ldv, _code(k.dtype, "KV4Cache.append"), *batch,
-                                            _stream(k))
+                                            _stream("KV4Cache.append", k, v, page_table, seq_len, q_start))
         if err:
             raise TSVDError(err, "tsvd_kv4_append")
 
@@ -204,10 +214,11 @@ class KV4Cache:
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.read")
         dtype, device, ld = dtype or _f32, seq_len.device, self.n_kv_heads * self.head_dim
         code = _code(dtype, "KV4Cache.read")
+        stream = _stream("KV4Cache.read", seq_len, page_table, q_start)
         shape, strides = (rows, self.n_kv_heads, self.head_dim), (ld, self.head_dim, 1)
         k = _empty(shape, strides, dtype=dtype, device=device)
         v = _empty(shape, strides, dtype=dtype, device=device)
-        err = binding.lib().tsvd_kv4_read(self.handle, k.data_ptr(), ld, v.data_ptr(), ld, code, *batch, _stream(seq_len))
+        err = binding.lib().tsvd_kv4_read(self.handle, k.data_ptr(), ld, v.data_ptr(), ld, code, *batch, stream)
         if err:
             raise TSVDError(err, "tsvd_kv4_read")
         return k, v
@@ -219,6 +230,7 @@ class KV4Cache:
         of one sequence, where the caller knows them.  Returns a tensor like q."""
         rows, n_heads, ldq = self._heads(q, "KV4Cache.attend")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.attend")
+        stream = _stream("KV4Cache.attend", q, out, page_table, seq_len, q_start)
         if max_q is None:
             max_q = 1 if q_start is None else max(1, rows)
         if out is None:
@@ -233,7 +245,7 @@ class KV4Cache:
         if causal:
             flags |= binding.TSVD_FLAG_CAUSAL
         err = binding.lib().tsvd_kv4_attend(self.handle, q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads,
-                                            _code(q.dtype, "KV4Cache.attend"), *batch, max_q, max_kv or 0, scale, window, flags, _stream(q))
+                                            _code(q.dtype, "KV4Cache.attend"), *batch, max_q, max_kv or 0, scale, window, flags, stream)
         if err:
             raise TSVDError(err, "tsvd_kv4_attend")
         return out

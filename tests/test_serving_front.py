@@ -27,6 +27,7 @@ def front(monkeypatch):
     from paper_2308_07641_b200 import binding, serving
     serving._load()
     monkeypatch.setattr(serving, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(serving, "_device", lambda: 0, raising=False)
 
     def empty(shape, strides, dtype=None, device=None):
         return OnCard(torch.empty_strided(shape, strides, dtype=dtype))
@@ -109,3 +110,40 @@ def test_a_single_row_has_any_stride(front):
     assert serving._rows(OnCard(torch.zeros(40).as_strided((1, 8), (3, 1))), "") == (1, 8, 8)
     assert serving._rows(OnCard(torch.zeros(4, 10)[:, :8]), "") == (4, 8, 10)
     assert _cache(serving)._heads(OnCard(torch.zeros(200).as_strided((1, 2, 64), (7, 64, 1))), "") == (1, 2, 128)
+
+
+def test_tensors_of_another_device(front, monkeypatch):
+    """The library launches on the current device: tensors of another one, or of two, are refused before any call of it."""
+    import types
+    binding, serving = front
+    monkeypatch.setattr(serving, "_device", lambda: 0)
+
+    def called(*a):
+        raise AssertionError("the library was called")
+
+    monkeypatch.setattr(binding, "lib", lambda: types.SimpleNamespace(
+        tsvd_strerror=lambda status: b"", **{f: called for f in ("tsvd_quantize", "tsvd_dequantize", "tsvd_i8_forward", "tsvd_kv4_append", "tsvd_kv4_read", "tsvd_kv4_attend")}))
+    x, far = OnCard(torch.zeros(3, 8)), OnCard(torch.zeros(3, 8), 1)
+    q, qfar = OnCard(torch.zeros(3, 8, dtype=torch.int8)), OnCard(torch.zeros(3, 8, dtype=torch.int8), 1)
+    s, sfar = OnCard(torch.ones(3)), OnCard(torch.ones(3), 1)
+    E = binding.TSVD_E_CUDA
+    assert _status(binding, serving.quantize, far) == E
+    assert _status(binding, serving.dequantize, qfar, sfar) == E
+    assert _status(binding, serving.dequantize, q, sfar) == E
+    layer = serving.Int8Linear.__new__(serving.Int8Linear)
+    layer.M, layer.N, layer.handle, layer.close = 8, 8, 1, lambda: None
+    assert _status(binding, layer, far) == E
+    assert _status(binding, layer, q, sfar) == E
+    assert _status(binding, layer, x, out=far) == E
+    assert _status(binding, layer, x, out=torch.zeros(3, 8)) == binding.TSVD_E_SHAPE        # on the host
+    cache = _cache(serving)
+    at = lambda d: (OnCard(torch.zeros(3, 2, 64), d), OnCard(torch.zeros(3, 2, dtype=torch.int32), d),  # noqa: E731
+                    OnCard(torch.ones(3, dtype=torch.int32), d), OnCard(torch.arange(4, dtype=torch.int32), d))
+    (k, table, n, start), (kf, tf, nf, sf) = at(0), at(1)
+    for a in ((kf, kf, tf, nf, sf), (kf, k, table, n), (k, kf, table, n), (k, k, tf, n), (k, k, table, nf), (k, k, table, n, sf)):
+        assert _status(binding, cache.append, *a) == E
+    for a in ((3, tf, nf), (3, tf, n), (3, table, nf), (3, table, n, sf)):
+        assert _status(binding, cache.read, *a) == E
+    for a in ((kf, tf, nf, sf), (kf, table, n), (k, tf, n), (k, table, nf), (k, table, n, sf)):
+        assert _status(binding, cache.attend, *a) == E
+    assert _status(binding, cache.attend, k, table, n, out=kf) == E
