@@ -221,6 +221,12 @@ kv4_prefill_kernel(const PreParams p)
         ctl[1] = kWaitLimitDefault;
         fence_mbar_init();
     }
+    // Tensor memory before the kernel after this one may start (see PdlLaunch).
+    if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;                        // S or P of tile x, buffer h: column 128 x + 64 h; O: column 256 + 128 x
     // ---- which rows: pairs of tiles with the most positions first ----
     pdl_launch_dependents();
     pdl_wait();
@@ -232,7 +238,10 @@ kv4_prefill_kernel(const PreParams p)
     const int n_rows = max(0, first < 0 ? 0 : min(min(all, p.max_q), p.b.n_rows - first)) * p.group;
     const int row_base = pair * 2 * PRE_ROWS;
     const int len = p.b.seq_len[s];
-    if (row_base >= n_rows) return;
+    if (row_base >= n_rows) {
+        if (warp == 12) tmem_dealloc(tmem, 512);
+        return;
+    }
     const long long room = (long long)p.b.max_pages * p.g.page_tokens;
     if (len > room && threadIdx.x == 0) atomicOr(p.status, KV4_DEV_INDEX);
     const int len_in = (int)max(0LL, min((long long)len, room));
@@ -266,12 +275,6 @@ kv4_prefill_kernel(const PreParams p)
         j_hi = max(t_hi[0], t_hi[1]);
         if (t_hi[0] == t_lo[0] && t_hi[1] == t_lo[1]) k_hi = k_lo;
     }
-
-    if (warp == 12) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    const uint32_t tmem = tmem_slot;                        // S or P of tile x, buffer h: column 128 x + 64 h; O: column 256 + 128 x
 
     if (warp < 8) {
         // ================= rows: one a thread =================

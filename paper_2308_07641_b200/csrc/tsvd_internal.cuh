@@ -135,6 +135,11 @@ constexpr int TSVD_DEV_BOUNDS = 4;    // checked builds (-DTSVD_CHECK_BOUNDS): a
 // pdl_wait() returns once that kernel has completed and its writes are visible.  A kernel calls
 // pdl_launch_dependents() to let the kernel after it start likewise.  Without the launch
 // attribute (or with nothing before or after it) both calls do nothing.
+//
+// Allocating tensor memory waits, without a limit, for whatever kernel on the SM holds it.  So a kernel calls
+// pdl_launch_dependents() only after its own allocation: a kernel that holds columns in its pdl_wait() then waits only for
+// kernels whose blocks all have theirs.  The other way round, a block could hold the columns that the kernel it waits for
+// still has to get.
 struct PdlLaunch {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];

@@ -1,0 +1,35 @@
+"""What keeps kernels from waiting for each other's tensor memory, read off the sources: an allocation has no time limit, so that it
+ends is a matter of construction and not of a run."""
+import glob
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2308_07641_b200", "csrc")
+
+
+def _kernels():
+    """(file, name, body) of every __global__ function."""
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cuh"))):
+        text = re.sub(r"//[^\n]*", "", open(path).read())
+        for m in re.finditer(r"__global__[^{;]*?(\w+)\s*\(([^{;]*)\)\s*\{", text):
+            depth, i = 1, m.end()
+            while depth:
+                depth += {"{": 1, "}": -1}.get(text[i], 0)
+                i += 1
+            yield os.path.basename(path), m.group(1), text[m.end():i]
+
+
+def test_tensor_memory_is_allocated_before_the_next_kernel_may_start():
+    """Else a later kernel of the stream can hold the columns, waiting for one that still has to get them."""
+    seen = set()
+    for path, name, body in _kernels():
+        if "tmem_alloc(" not in body:
+            continue
+        seen.add(path)
+        assert body.count("tmem_alloc(") == 1, name
+        for call in ("pdl_launch_dependents()", "pdl_wait()"):
+            first = body.find(call)
+            assert first < 0 or body.index("tmem_alloc(") < first, f"{path}: {name} calls {call} before it has its tensor memory"
+        # every way out gives it back
+        assert body.count("tmem_dealloc(") == 1 + len(re.findall(r"\breturn\s*;", body[body.index("tmem_alloc("):])), f"{path}: {name}"
+    assert {"kv4_prefill.cu", "i8_mma.cu", "midbatch.cu", "tensor.cu"} <= seen
