@@ -42,6 +42,7 @@ struct I8Params {
     int row_tiles, tok_tiles, NT;
     int band;                // row tiles of a band: a band's tiles are walked token tile by token tile
     int stages;
+    int columns;             // of tensor memory: one accumulator for a cluster's block, two for the others
     int* status;
 };
 
@@ -87,7 +88,8 @@ __device__ __forceinline__ bool any_of_128(bool x)
 }
 
 // CL = 1: persistent, a block walks over tiles (row tile fastest), two accumulators.
-// CL > 1: one tile for each cluster of CL blocks, which share its contraction and meet through distributed shared memory.
+// CL > 1: one tile for each cluster of CL blocks, which share its contraction and meet through distributed shared memory;
+// one block an SM (TSVD_ALONE_SMEM), because they hold tensor memory while they wait for one another.
 template <int CL>
 __global__ void __launch_bounds__(I8_THREADS, 1)
 i8_mma_kernel(const I8Params p)
@@ -112,7 +114,7 @@ i8_mma_kernel(const I8Params p)
         ctl[1] = kWaitLimitDefault;
         fence_mbar_init();
     }
-    if (warp == 5) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+    if (warp == 5) { tmem_alloc(&tmem_slot, (uint32_t)p.columns); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -290,7 +292,7 @@ i8_mma_kernel(const I8Params p)
     __syncthreads();
     tc_fence_after_sync();
     if (threadIdx.x == 0 && ctl[0]) atomicOr(p.status, TSVD_DEV_TIMEOUT);
-    if (warp == 5) tmem_dealloc(tmem, 512);
+    if (warp == 5) tmem_dealloc(tmem, (uint32_t)p.columns);
 }
 
 template <int CL>
@@ -305,7 +307,10 @@ tsvd_status_t launch(I8Params p, int blocks, cudaStream_t st)
         p.stages = std::min(p.stages, std::max(longest, 1));
         ring = std::max(p.stages * stage, (size_t)p.NT * 512);
     }
-    const size_t smem = ring + 1024;
+    p.columns = 512;
+    if (CL > 1)
+        for (p.columns = 32; p.columns < p.NT; p.columns *= 2) { }
+    const size_t smem = CL > 1 ? std::max(ring + 1024, TSVD_ALONE_SMEM) : ring + 1024;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(I8_THREADS);
@@ -355,7 +360,7 @@ tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_sc
         const long long tok = (B + nt - 1) / nt, tiles = tok * p.row_tiles;
         const long long block = std::max(2 * nt, (16384 + 128 * nt) / 56);
         for (int c = 1; c <= 8; c *= 2) {
-            if (c > 1 && (tiles * c > sms || p.KB < c)) break;
+            if (c > 1 && (tiles > h->clusters[c] || p.KB < c)) break;
             const long long cost = ((tiles * c + sms - 1) / sms) * ((p.KB + c - 1) / c) * block + 8 * nt + (c > 1 ? 2500 : 0);
             if (best < 0 || cost < best) { best = cost; p.NT = nt; p.tok_tiles = (int)tok; cl = c; }
         }
@@ -370,12 +375,32 @@ tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_sc
     }
 }
 
-tsvd_status_t i8_product_prepare()
+// How many clusters of CL blocks, one block an SM, the device runs at a time.
+template <int CL>
+static cudaError_t most_clusters(int* most)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(CL);
+    cfg.blockDim = dim3(I8_THREADS);
+    cfg.dynamicSmemBytes = I8_SMEM_LIMIT - 1024;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(most, i8_mma_kernel<CL>, &cfg);
+}
+
+tsvd_status_t i8_product_prepare(tsvd_i8_s* h)
 {
     const int most = I8_SMEM_LIMIT - 1024;
     TSVD_CUDA_OK(cudaFuncSetAttribute(i8_mma_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     TSVD_CUDA_OK(cudaFuncSetAttribute(i8_mma_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     TSVD_CUDA_OK(cudaFuncSetAttribute(i8_mma_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     TSVD_CUDA_OK(cudaFuncSetAttribute(i8_mma_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    TSVD_CUDA_OK(most_clusters<2>(&h->clusters[2]));
+    TSVD_CUDA_OK(most_clusters<4>(&h->clusters[4]));
+    TSVD_CUDA_OK(most_clusters<8>(&h->clusters[8]));
     return TSVD_OK;
 }

@@ -159,7 +159,7 @@ extern "C" tsvd_status_t tsvd_i8_pack(const int8_t* W, long long ldw, const floa
     h->row_tiles = (M + 127) / 128;
     h->col_blocks = (N + 127) / 128;
     tsvd_status_t st = i8_fill(h, W, ldw, w_scale, bias);
-    if (st == TSVD_OK) st = i8_product_prepare();
+    if (st == TSVD_OK) st = i8_product_prepare(h);
     if (st != TSVD_OK) { i8_free(h); return st; }
     *out = h;
     return TSVD_OK;

@@ -26,6 +26,7 @@ struct tsvd_i8_s {
     int sms = 0;
     int M = 0, N = 0;
     int row_tiles = 0, col_blocks = 0;   // 128 each
+    int clusters[9] = {};                // [2, 4, 8]: clusters of so many blocks that run at a time
     int8_t* W = nullptr;                 // device, row_tiles * col_blocks * 16 KiB
     float* w_scale = nullptr;            // device, [row_tiles * 128], zero padded
     float* bias = nullptr;               // device, the same, or null
@@ -36,7 +37,7 @@ struct tsvd_i8_s {
 
 // i8_mma.cu: the product of B tokens in tensor-core order (x, then their scales) with the handle's weights
 tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, cudaStream_t st);
-tsvd_status_t i8_product_prepare();   // once for the current device, before the first product
+tsvd_status_t i8_product_prepare(tsvd_i8_s* h);   // once for a handle, on its device, before its first product
 
 // ---- the 4-bit cache ------------------------------------------------------------------------------------------------
 // A page is [kv head][block of 16 positions], a block 20 * head_dim bytes:

@@ -140,6 +140,13 @@ constexpr int TSVD_DEV_BOUNDS = 4;    // checked builds (-DTSVD_CHECK_BOUNDS): a
 // pdl_launch_dependents() only after its own allocation: a kernel that holds columns in its pdl_wait() then waits only for
 // kernels whose blocks all have theirs.  The other way round, a block could hold the columns that the kernel it waits for
 // still has to get.
+//
+// Blocks of a cluster that wait for one another while they hold tensor memory: were two such blocks to share an SM, each of
+// two clusters (of one launch, or of two streams) could hold the columns that the other one waits for.  Their launches ask
+// for more than half of an SM's shared memory, so that no two of them ever do.
+constexpr size_t TSVD_SM_SMEM = 228 * 1024;
+constexpr size_t TSVD_ALONE_SMEM = 116 * 1024;
+static_assert(2 * TSVD_ALONE_SMEM > TSVD_SM_SMEM, "two blocks of cluster kernels would fit one SM");
 struct PdlLaunch {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];

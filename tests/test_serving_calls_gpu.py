@@ -3,6 +3,8 @@ import ctypes
 
 import pytest
 
+from tests.test_serving_gpu import Batch, _check_layer, _gen
+
 pytestmark = pytest.mark.gpu
 
 
@@ -44,3 +46,64 @@ def test_a_handle_of_another_device_is_refused():
         call()
     torch.cuda.synchronize()
     assert layer.status() == 0 and cache.status() == 0
+
+
+def test_layers_on_two_streams():
+    """Products whose contraction clusters share (few tokens, 18 row tiles, and smaller ones), side by side on two streams."""
+    import torch
+    from paper_2308_07641_b200 import Int8Linear
+    sizes = [(2304, 4096, 1), (4096, 2048, 32), (640, 4096, 33), (1001, 770, 197)]
+    layers, inputs = [], []
+    for M, N, B in sizes:
+        g = _gen(M + B)
+        w8 = torch.randint(-127, 128, (M, N), generator=g, device="cuda", dtype=torch.int8)
+        ws = torch.rand(M, generator=g, device="cuda") * 0.01 + 1e-4
+        x8 = torch.randint(-127, 128, (B, N), generator=g, device="cuda", dtype=torch.int8)
+        xs = torch.rand(B, generator=g, device="cuda") + 0.5
+        pair = [Int8Linear(w8, ws) for _ in range(2)]
+        for layer in pair:
+            layer.reserve(B, "i8")
+        layers.append(pair)
+        inputs.append((x8, xs, w8, ws))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = {}
+    for _ in range(10):
+        for i, (x8, xs, _, _) in enumerate(inputs):
+            for k, stream in enumerate(streams):
+                with torch.cuda.stream(stream):
+                    outs[i, k] = layers[(i + k) % len(sizes)][k](*inputs[(i + k) % len(sizes)][:2])
+    torch.cuda.synchronize()
+    for (i, k), y in outs.items():
+        x8, xs, w8, ws = inputs[(i + k) % len(sizes)]
+        _check_layer(y, x8, xs, w8, ws, None)
+    assert all(layer.status() == 0 for pair in layers for layer in pair)
+
+
+@pytest.mark.parametrize("D,new", [(64, 200), (128, 200), (64, 1)])
+def test_append_attend_and_layer_in_a_chain(D, new):
+    """Every kernel may start before the one ahead of it has ended; results are those of calls that wait for each other."""
+    import torch
+    from paper_2308_07641_b200 import Int8Linear, quantize
+    H = 2048 // D
+    b = Batch([new + 300, new + 77, new], H, D, 64, seed=D)
+    rows = 3 * new
+    g = _gen(D)
+    layer = Int8Linear(*quantize(torch.randn(4096, 2048, generator=g, device="cuda")))
+    layer.reserve(32, "bf16")
+    q, k, v = (torch.randn(rows, H, D, generator=g, device="cuda").bfloat16() for _ in range(3))
+    start = torch.arange(4, dtype=torch.int32, device="cuda") * new
+
+    def chain(wait):
+        b.cache.append(k, v, b.table, b.seq_len, start)
+        wait()
+        a = b.cache.attend(q, b.table, b.seq_len, start, max_q=new)
+        wait()
+        return layer(a.view(rows, 2048)[:32])
+
+    want = chain(torch.cuda.synchronize)
+    torch.cuda.synchronize()
+    outs = [chain(lambda: None) for _ in range(20)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in outs)
+    assert layer.status() == 0 and b.cache.status() == 0

@@ -4,6 +4,8 @@ import glob
 import os
 import re
 
+import pytest
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2308_07641_b200", "csrc")
 
 
@@ -33,3 +35,16 @@ def test_tensor_memory_is_allocated_before_the_next_kernel_may_start():
         # every way out gives it back
         assert body.count("tmem_dealloc(") == 1 + len(re.findall(r"\breturn\s*;", body[body.index("tmem_alloc("):])), f"{path}: {name}"
     assert {"kv4_prefill.cu", "i8_mma.cu", "midbatch.cu", "tensor.cu"} <= seen
+
+
+@pytest.mark.parametrize("path", ["i8_mma.cu"])
+def test_cluster_kernels_with_tensor_memory_have_an_sm_to_themselves(path):
+    """Their blocks wait for one another while they hold columns: two on an SM, of different clusters, could each wait for what
+    the other one holds.  More than half of an SM's shared memory keeps them apart (a static_assert says that it is)."""
+    both = [name for p, name, body in _kernels() if p == path and "tmem_alloc(" in body and "cluster_sync_all()" in body]
+    assert both
+    text = open(os.path.join(CSRC, path)).read()
+    assert re.search(r"std::max(<size_t>)?\([^;]*TSVD_ALONE_SMEM\)", text), "the launch does not ask for the shared memory"
+    head = open(os.path.join(CSRC, "tsvd_internal.cuh")).read()
+    alone, sm = (eval(re.search(r"constexpr size_t " + n + r" = ([\d *]+);", head).group(1)) for n in ("TSVD_ALONE_SMEM", "TSVD_SM_SMEM"))
+    assert 2 * alone > sm == 228 * 1024
