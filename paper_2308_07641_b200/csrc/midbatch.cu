@@ -14,8 +14,11 @@
 //   - and sends its partial results, as float (the exact integers for int8 activations in the V-stage),
 //     to the CTA that owns the row through distributed shared memory; after one cluster barrier the
 //     owner adds the parts in a fixed order and applies S, or the bias, and the output rounding.
+// A CTA holds tensor memory while it waits for its cluster, so each has an SM to itself (TSVD_ALONE_SMEM).
 // No global atomics, no scratch besides t = S*(V x); deterministic.  Results agree with the other
 // kernel families within the tolerance, not bit for bit (the per-slab scales).
+#include <algorithm>
+
 #include "digits.cuh"
 #include "sm100_ptx.cuh"
 #include "tsvd_internal.cuh"
@@ -390,7 +393,7 @@ cudaError_t launch_mid_cl(const MidParams& p, int R_pad, cudaStream_t stream)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(R_pad / 128 * CL));
     cfg.blockDim = dim3(MID_THREADS);
-    cfg.dynamicSmemBytes = mid_smem_bytes(p.KB, ND * TOK, TOK, CL);
+    cfg.dynamicSmemBytes = std::max(mid_smem_bytes(p.KB, ND * TOK, TOK, CL), TSVD_ALONE_SMEM);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

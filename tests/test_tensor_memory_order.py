@@ -37,7 +37,7 @@ def test_tensor_memory_is_allocated_before_the_next_kernel_may_start():
     assert {"kv4_prefill.cu", "i8_mma.cu", "midbatch.cu", "tensor.cu"} <= seen
 
 
-@pytest.mark.parametrize("path", ["i8_mma.cu"])
+@pytest.mark.parametrize("path", ["i8_mma.cu", "midbatch.cu"])
 def test_cluster_kernels_with_tensor_memory_have_an_sm_to_themselves(path):
     """Their blocks wait for one another while they hold columns: two on an SM, of different clusters, could each wait for what
     the other one holds.  More than half of an SM's shared memory keeps them apart (a static_assert says that it is)."""
