@@ -22,8 +22,9 @@
 // persistent blocks whose copies run ahead into the next pair (57: the row loop needs more registers and a step takes 2300).
 // With one row tile alone the codes bound it, 2 us per 128 positions: both groups of row warps on one tile gained nothing.
 //
-// Arithmetic: q as fp16 after division by a power of two for 32 rows together (exact down to 2^-24 of their largest number,
-// which is far below what a score can show; the power goes into the factor c), keys and values as fp16 (one rounding), probabilities as fp16, sums in fp32.
+// Arithmetic: q as fp16 after division by a power of two per row (a bf16 number is exact down to 2^-17 of the row's largest and
+// off by at most 2^-25 of that below; the power goes into the row's factor c), keys and values as fp16 (one rounding),
+// probabilities as fp16, sums in fp32.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -287,7 +288,8 @@ kv4_prefill_kernel(const PreParams p)
         __syncwarp();
         uint8_t* own = smem + L::kQ + x * L::kTile;
         float cm;
-        {   // Q: the warp's 32 rows, D / 8 lanes a row, divided by the power of two at or below their largest number (2^-60 at least)
+        {   // Q: the warp's 32 rows, D / 8 lanes a row, each row divided by the power of two at or below its largest number (2^-60
+            // at least)
             constexpr int LANES = D / 8, ROWS = 32 / LANES;
             const int u = lane % LANES;
             uint4 v[LANES];
@@ -297,21 +299,37 @@ kv4_prefill_kernel(const PreParams p)
                 v[i] = make_uint4(0, 0, 0, 0);
                 if (from.x >= 0) v[i] = *reinterpret_cast<const uint4*>(p.q + from.x * p.ldq + from.y + 8 * u);
             }
-            uint32_t top = 0;                               // magnitudes compared as 16-bit integers, two at a time
+            // The largest magnitudes as 16-bit integers, two rows (those of i and i + 1) a word; the lanes of a row halve the
+            // words they hold as they exchange them, so that lane u ends with the row of i = u.
+            uint32_t top[LANES / 2];
 #pragma unroll
-            for (int i = 0; i < LANES; ++i)
-                top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu)), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
-            top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-            const int e = min(max((int)(top >> 7), 67), 253) - 127;
-            const float down = p.sign * __uint_as_float((uint32_t)(127 - e) << 23);
-            cm = p.c * __uint_as_float((uint32_t)(127 + e) << 23);
+            for (int i = 0; i < LANES; ++i) {
+                const uint32_t m = __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
+                if (i & 1) top[i / 2] = __vmaxu2(__byte_perm(top[i / 2], m, 0x5410), __byte_perm(top[i / 2], m, 0x7632));
+                else top[i / 2] = m;
+            }
+#pragma unroll
+            for (int n = LANES / 4; n >= 1; n /= 2) {        // n words stay
+                const bool upper = u & (2 * n);
+#pragma unroll
+                for (int k = 0; k < n; ++k) {
+                    const uint32_t keep = upper ? top[k + n] : top[k], give = upper ? top[k] : top[k + n];
+                    top[k] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, 2 * n));
+                }
+            }
+            top[0] = __vmaxu2(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
+            const int e = min(max((int)((u & 1 ? top[0] >> 16 : top[0] & 0xffffu) >> 7), 67), 253);
+            const uint32_t down = (__float_as_uint(p.sign) & 0x80000000u) | (uint32_t)(254 - e) << 23;     // +-2^(127 - e)
+            // the thread's own row is that of i = (lane / ROWS), in group lane % ROWS of the lanes
+            cm = p.c * __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, e, lane % ROWS * LANES + lane / ROWS) << 23);
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                 const int rr = wrow + i * ROWS + lane / LANES;
+                const float f = __uint_as_float(__shfl_sync(0xffffffffu, down, i, LANES));
                 uint32_t h[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * down, __uint_as_float(w[k] & 0xffff0000u) * down);
+                for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
                 *reinterpret_cast<uint4*>(own + (u >> 3) * 16384 + rr * 128 + (((u & 7) ^ (rr & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
             fence_proxy_async_smem();

@@ -1,9 +1,11 @@
 """The serving operators where a call meets its surroundings: devices, streams, launches in a chain, rows of unlike size."""
 import ctypes
+import math
 
+import numpy as np
 import pytest
 
-from tests.test_serving_gpu import Batch, _check_layer, _gen
+from tests.test_serving_gpu import U, U8, U16, Batch, _check_layer, _gen
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +109,37 @@ def test_append_attend_and_layer_in_a_chain(D, new):
     torch.cuda.synchronize()
     assert all(torch.equal(y, want) for y in outs)
     assert layer.status() == 0 and b.cache.status() == 0
+
+
+@pytest.mark.parametrize("lens,new,H,Hkv,D", [([300, 77], [150, 40], 4, 4, 128), ([500, 90], [70, 70], 16, 4, 64), ([2500], [40], 8, 8, 128),
+                                              ([300, 50], [1, 1], 16, 2, 128)])
+def test_rows_of_unlike_size(lens, new, H, Hkv, D):
+    """A row's result does not depend on the rows beside it, whichever kernel takes them: neighbours 2^18 to 2^30 times larger,
+    infinite or NaN leave it within the tolerance of its own arithmetic (that of test_serving_gpu), and the kernel for many rows
+    changes no bit of it.  (Tokens and heads alike are rows.)"""
+    import torch
+    b = Batch(lens, Hkv, D, 64, seed=D + H)
+    n = sum(new)
+    g = _gen(n)
+    sizes = torch.tensor([1.0, 2.0 ** -18, 2.0 ** -22, 2.0 ** -26, 2.0 ** -30], device="cuda")
+    mul = sizes[torch.randint(0, 5, (n, H, 1), generator=g, device="cuda")] * 2.0 ** 18
+    b.check(H, new, qmul=mul, max_q=max(new))
+    b.check(H, new, qmul=mul, max_q=max(new), scale=-0.1, causal=False)
+    q = torch.randn(n, H, D, generator=g, device="cuda").bfloat16()
+    start = torch.tensor([0] + [sum(new[:i + 1]) for i in range(len(new))], dtype=torch.int32, device="cuda")
+    kw = dict(max_q=max(new), max_kv=max(lens))
+    alone = b.cache.attend(q, b.table, b.seq_len, start, **kw)
+    want, size, reach = b.plain(q, new, True, 0, 1 / math.sqrt(D))
+    tol = (2 * U16 * reach[..., None] + 3 * U16 + 2 * max(lens) * U) * size + U8 * np.abs(want)
+    own = torch.rand(n, H, generator=g, device="cuda") < 0.5
+    at = own.cpu().numpy()
+    for bad in (2.0 ** 18, 2.0 ** 30, 1e38, float("inf"), float("nan")):
+        every, one = torch.where(own[..., None], q, q * bad), q.clone()
+        one[..., 3] = torch.where(own, q[..., 3], bad)       # one number of a row is enough
+        for other in (every, one):
+            got = b.cache.attend(other, b.table, b.seq_len, start, **kw)
+            assert (np.abs(got.double().cpu().numpy() - want)[at] <= tol[at]).all(), bad
+            if max(new) * (H // Hkv) > 16:
+                assert torch.equal(got[own], alone[own]), bad
+    torch.cuda.synchronize()
+    assert b.cache.status() == 0
