@@ -241,6 +241,7 @@ extern "C" tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_
     if (e == cudaSuccess) e = cudaMalloc(&h->parts, parts > parts2 ? parts : parts2);
     if (e == cudaSuccess) e = cudaMalloc(&h->tickets, tickets);
     if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, tickets);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // (a memset returns before its end, and other streams do not wait for it)
     if (e == cudaSuccess && (kv4_decode_prepare() != TSVD_OK || kv4_prefill_prepare() != TSVD_OK)) e = cudaErrorUnknown;
     if (e != cudaSuccess) {
         tsvd_kv4_destroy(h);
@@ -393,6 +394,7 @@ extern "C" tsvd_status_t tsvd_kv4_last_status(tsvd_kv4_t h)
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));
     if (word & KV4_DEV_TIMEOUT) TSVD_CUDA_OK(cudaMemset(h->tickets, 0, kv4_decode_tickets(h->sms) * sizeof(unsigned)));
+    if (word) TSVD_CUDA_OK(cudaStreamSynchronize(nullptr));
     return (word & KV4_DEV_TIMEOUT) ? TSVD_E_TIMEOUT : (word & KV4_DEV_INDEX) ? TSVD_E_INDEX : TSVD_OK;
 }
 

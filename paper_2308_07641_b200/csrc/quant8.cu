@@ -231,6 +231,7 @@ extern "C" tsvd_status_t tsvd_i8_last_status(tsvd_i8_t h)
     int word = 0;
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));
+    if (word) TSVD_CUDA_OK(cudaStreamSynchronize(nullptr));      // other streams do not wait for the memset
     return (word & TSVD_DEV_TIMEOUT) ? TSVD_E_TIMEOUT : TSVD_OK;
 }
 

@@ -5,7 +5,7 @@ import math
 import numpy as np
 import pytest
 
-from tests.test_serving_gpu import U, U8, U16, Batch, _check_layer, _gen
+from tests.test_serving_gpu import U, U8, U16, Batch, _check_layer, _gen, _plain_cached
 
 pytestmark = pytest.mark.gpu
 
@@ -143,3 +143,26 @@ def test_rows_of_unlike_size(lens, new, H, Hkv, D):
                 assert torch.equal(got[own], alone[own]), bad
     torch.cuda.synchronize()
     assert b.cache.status() == 0
+
+
+def test_a_new_cache_on_another_stream():
+    """A pool is zeroed before its creation returns: what a stream that waits for nothing puts into it at once stays there.  (6 GB,
+    a millisecond of zeros; the appended positions lie at its end.)"""
+    import torch
+    from paper_2308_07641_b200 import KV4Cache
+    Hkv, D, page = 32, 128, 64
+    n_pages = (6 << 30) // (Hkv * page * D * 5 // 4)
+    side = torch.cuda.Stream()
+    x = torch.randn(100, Hkv, D, generator=_gen(3), device="cuda").bfloat16()
+    table = torch.tensor([[n_pages - 1, n_pages - 2]], dtype=torch.int32, device="cuda")
+    n, start = torch.tensor([100], dtype=torch.int32, device="cuda"), torch.tensor([0, 100], dtype=torch.int32, device="cuda")
+    want = _plain_cached(x)
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            cache = KV4Cache(Hkv, D, n_pages, page)
+            cache.append(x, x, table, n, start)
+        torch.cuda.synchronize()
+        k, v = cache.read(100, table, n, start)
+        assert np.array_equal(k.double().cpu().numpy(), want) and np.array_equal(v.double().cpu().numpy(), want)
+        cache.close()
