@@ -97,7 +97,8 @@ typedef struct tsvd_kv4_s* tsvd_kv4_t; /* opaque; owns device memory on one GPU 
  *   seq_len     device, int32 [n_seq]: positions of sequence s in the cache, the call's new ones included
  *   q_start     device, int32 [n_seq + 1]: the call's rows q_start[s] .. q_start[s+1]-1 are the last positions of
  *               sequence s, in order; NULL: one row per sequence
- *   n_rows      q_start[n_seq] (n_seq where q_start is NULL)
+ *   n_rows      q_start[n_seq] (n_seq where q_start is NULL); rows below q_start[0], or beyond q_start[n_seq] where n_rows
+ *               is larger, belong to no sequence: they are not written (append, attend) and read as zeros (read)
  * All three are read on the device: a captured graph serves them as they change.  A page number outside the pool or a
  * sequence longer than its pages makes tsvd_kv4_last_status report TSVD_E_INDEX, and so does a row before position 0 in
  * append and read; such a position is not written (append), reads as zeros (read) and is not seen (attend).  An unused

@@ -17,7 +17,7 @@ __device__ __forceinline__ Place place_of_row(const Kv4Geom& g, const Kv4Batch& 
 {
     Place p{-1, 0};
     const int s = kv4_seq_of_row(b, row);
-    if (s >= b.n_seq) return p;                       // behind the last sequence: not a row
+    if (s >= b.n_seq || row < kv4_first_row(b, s)) return p;   // behind the last sequence or before the first: not a row
     const int end = b.q_start ? b.q_start[s + 1] : row + 1;
     const long long pos = (long long)b.seq_len[s] - (end - row);
     if (pos >= 0 && pos < (long long)b.max_pages * g.page_tokens) {

@@ -49,7 +49,7 @@ kv4_attend_simple_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ q, long lo
     const int s = kv4_seq_of_row(b, row);
     if (s >= b.n_seq) return;                 // behind the last sequence: not a row
     const int first = kv4_first_row(b, s), last = b.q_start ? b.q_start[s + 1] : row + 1;
-    if (row - first >= max_q) return;
+    if (row < first || row - first >= max_q) return;
     const long long room = (long long)b.max_pages * g.page_tokens;
     const int len = b.seq_len[s];
     const long long len_in = len < room ? (len < 0 ? 0 : len) : room;

@@ -166,3 +166,36 @@ def test_a_new_cache_on_another_stream():
         k, v = cache.read(100, table, n, start)
         assert np.array_equal(k.double().cpu().numpy(), want) and np.array_equal(v.double().cpu().numpy(), want)
         cache.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_no_sequence(dtype):
+    """q_start may be a piece of a longer one: rows before its first number and behind its last are nobody's."""
+    import torch
+    Hkv, D = 2, 64
+    b = Batch([90, 200], Hkv, D, 16, seed=7, dtype=dtype)
+    kind = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    for new in (1, 30):
+        n = 2 * new + 10
+        start = torch.tensor([6, 6 + new, 6 + 2 * new], dtype=torch.int32, device="cuda")
+        mine = slice(6, 6 + 2 * new)
+        whole = torch.tensor([0, 90, 290], dtype=torch.int32, device="cuda")
+        before = b.cache.read(290, b.table, b.seq_len, whole)
+        k, v = (torch.randn(n, Hkv, D, generator=_gen(new + i), device="cuda").to(kind) for i in range(2))
+        b.cache.append(k, v, b.table, b.seq_len, start)
+        after = b.cache.read(290, b.table, b.seq_len, whole)
+        new_at = torch.zeros(290, dtype=torch.bool, device="cuda")
+        new_at[90 - new:90] = True
+        new_at[290 - new:] = True
+        for old, now, x in zip(before, after, (k, v)):
+            assert torch.equal(old[~new_at], now[~new_at])
+            assert np.array_equal(now[new_at].double().cpu().numpy(), _plain_cached(x[mine]))
+        for got, now in zip(b.cache.read(n, b.table, b.seq_len, start), after):
+            assert torch.equal(got[mine], now[new_at]) and (got[:6] == 0).all() and (got[6 + 2 * new:] == 0).all()
+        q = torch.randn(n, 4, D, generator=_gen(9), device="cuda").to(kind)
+        out = torch.full_like(q, 7.0)
+        b.cache.attend(q, b.table, b.seq_len, start, max_q=new, out=out)
+        want = b.cache.attend(q[mine], b.table, b.seq_len, start - 6, max_q=new)
+        assert torch.equal(out[mine], want) and (out[:6] == 7).all() and (out[6 + 2 * new:] == 7).all()
+        torch.cuda.synchronize()
+        assert b.cache.status() == 0
