@@ -22,9 +22,9 @@
 // persistent blocks whose copies run ahead into the next pair (57: the row loop needs more registers and a step takes 2300).
 // With one row tile alone the codes bound it, 2 us per 128 positions: both groups of row warps on one tile gained nothing.
 //
-// Arithmetic: q as fp16 after division by a power of two per row (a bf16 number is exact down to 2^-17 of the row's largest and
-// off by at most 2^-25 of that below; the power goes into the row's factor c), keys and values as fp16 (one rounding),
-// probabilities as fp16, sums in fp32.
+// Arithmetic: q as fp16 times a power of two for each row that brings its largest number to 2^15 (a bf16 number is then exact
+// down to 2^-32 of it; the power goes into the row's factor c), keys and values as fp16 (one rounding), probabilities as fp16,
+// sums in fp32.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -175,6 +175,21 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         : "memory");
 }
 
+// Sixteen bytes, or zeros.  Volatile: a row's loads go out together, one behind the other (left to the compiler, the prompt took
+// 58 us in place of 53).
+__device__ __forceinline__ uint4 ld_or_zero(const void* at, bool there)
+{
+    uint4 v;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %5, 0;\n\t"
+        "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+        "@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+        : "l"(at), "r"((uint32_t)there)
+        : "memory");
+    return v;
+}
 template <int WORDS>
 struct alignas(4 * WORDS) Words { uint32_t w[WORDS]; };
 
@@ -288,49 +303,38 @@ kv4_prefill_kernel(const PreParams p)
         __syncwarp();
         uint8_t* own = smem + L::kQ + x * L::kTile;
         float cm;
-        {   // Q: the warp's 32 rows, D / 8 lanes a row, each row divided by the power of two at or below its largest number (2^-60
-            // at least)
+        {   // Q: the warp's 32 rows, read by D / 8 lanes a row; then each thread has its own row, and scales it by the power of two
+            // that brings its largest number (2^-60 at least) to 2^15.
             constexpr int LANES = D / 8, ROWS = 32 / LANES;
             const int u = lane % LANES;
             uint4 v[LANES];
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
                 const int2 from = row_at[x][wrow + i * ROWS + lane / LANES];
-                v[i] = make_uint4(0, 0, 0, 0);
-                if (from.x >= 0) v[i] = *reinterpret_cast<const uint4*>(p.q + from.x * p.ldq + from.y + 8 * u);
+                v[i] = ld_or_zero(p.q + max(from.x, 0) * p.ldq + from.y + 8 * u, from.x >= 0);
             }
-            // The largest magnitudes as 16-bit integers, two rows (those of i and i + 1) a word; the lanes of a row halve the
-            // words they hold as they exchange them, so that lane u ends with the row of i = u.
-            uint32_t top[LANES / 2];
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
-                const uint32_t m = __vmaxu2(__vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
-                if (i & 1) top[i / 2] = __vmaxu2(__byte_perm(top[i / 2], m, 0x5410), __byte_perm(top[i / 2], m, 0x7632));
-                else top[i / 2] = m;
+                const int rr = wrow + i * ROWS + lane / LANES;
+                *reinterpret_cast<uint4*>(own + (u >> 3) * 16384 + rr * 128 + (((u & 7) ^ (rr & 7)) << 4)) = v[i];
             }
+            __syncwarp();
+            uint32_t top = 0;                               // magnitudes compared as 16-bit integers, two at a time
 #pragma unroll
-            for (int n = LANES / 4; n >= 1; n /= 2) {        // n words stay
-                const bool upper = u & (2 * n);
-#pragma unroll
-                for (int k = 0; k < n; ++k) {
-                    const uint32_t keep = upper ? top[k + n] : top[k], give = upper ? top[k] : top[k + n];
-                    top[k] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, 2 * n));
-                }
+            for (int i = 0; i < LANES; ++i) {
+                v[i] = *reinterpret_cast<const uint4*>(own + (i >> 3) * 16384 + r * 128 + (((i & 7) ^ (r & 7)) << 4));
+                top = __vmaxu2(__vmaxu2(top, __vmaxu2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu)), __vmaxu2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
             }
-            top[0] = __vmaxu2(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
-            const int e = min(max((int)((u & 1 ? top[0] >> 16 : top[0] & 0xffffu) >> 7), 67), 253);
-            const uint32_t down = (__float_as_uint(p.sign) & 0x80000000u) | (uint32_t)(254 - e) << 23;     // +-2^(127 - e)
-            // the thread's own row is that of i = (lane / ROWS), in group lane % ROWS of the lanes
-            cm = p.c * __uint_as_float((uint32_t)__shfl_sync(0xffffffffu, e, lane % ROWS * LANES + lane / ROWS) << 23);
+            const int e = min(max((int)(max(top & 0xffffu, top >> 16) >> 7), 67), 254) - 127;
+            const float by = p.sign * __uint_as_float((uint32_t)(127 + 15 - e) << 23);
+            cm = p.c * __uint_as_float((uint32_t)(127 - 15 + e) << 23);
 #pragma unroll
             for (int i = 0; i < LANES; ++i) {
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                const int rr = wrow + i * ROWS + lane / LANES;
-                const float f = __uint_as_float(__shfl_sync(0xffffffffu, down, i, LANES));
                 uint32_t h[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
-                *reinterpret_cast<uint4*>(own + (u >> 3) * 16384 + rr * 128 + (((u & 7) ^ (rr & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                for (int k = 0; k < 4; ++k) h[k] = h2(__uint_as_float(w[k] << 16) * by, __uint_as_float(w[k] & 0xffff0000u) * by);
+                *reinterpret_cast<uint4*>(own + (i >> 3) * 16384 + r * 128 + (((i & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
             fence_proxy_async_smem();
             __syncwarp();
