@@ -459,7 +459,7 @@ kv4_decode_kernel(const DecParams p)
 
         // ---- its units ----
         for (int u = it.unit0; u < it.unit1; ++u) {
-            if (!(ok = mbar_wait(&full[warp][stage], phase, ctl))) break;
+            if (!(ok = mbar_wait_warp(&full[warp][stage], phase, ctl))) break;
             const uint8_t* unit = ring + (size_t)(warp * p.stages + stage) * UNIT;
             const int at = it.at0 + u * DEC_UNIT, here = (int)(there >> (2 * stage) & 3u);
             // rows r and r + 8 of a block's score tile are its positions kr and kr + 8

@@ -349,7 +349,7 @@ kv4_prefill_kernel(const PreParams p)
         const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
         for (int k = a; k < b; ++k) {
             const int h = k & 1, at = k * PRE_STEP;
-            if (!(ok = mbar_wait(&s_full[x][h], phs >> h & 1, ctl))) break;
+            if (!(ok = mbar_wait_warp(&s_full[x][h], phs >> h & 1, ctl))) break;
             phs ^= 1u << h;
             tc_fence_after_sync();
             const uint32_t t_s = t_lane + 128u * x + 64u * h;
@@ -383,7 +383,7 @@ kv4_prefill_kernel(const PreParams p)
                 ref = to;
                 sum *= keep;
                 if (k > a) {
-                    if (!(ok = mbar_wait(&o_done[x][h ^ 1], (pho >> (h ^ 1) & 1) ^ 1, ctl))) break;   // the product of the step before
+                    if (!(ok = mbar_wait_warp(&o_done[x][h ^ 1], (pho >> (h ^ 1) & 1) ^ 1, ctl))) break;   // the product of the step before
                     tc_fence_after_sync();
 #pragma unroll 1
                     for (int c0 = 0; c0 < D; c0 += 16) {
@@ -418,7 +418,7 @@ kv4_prefill_kernel(const PreParams p)
             if (lane == 0) mbar_arrive(&p_full[x][h]);
             pho ^= 1u << h;
         }
-        if (ok && b > a) ok = mbar_wait(&o_done[x][(b - 1) & 1], (pho >> ((b - 1) & 1) & 1) ^ 1, ctl);
+        if (ok && b > a) ok = mbar_wait_warp(&o_done[x][(b - 1) & 1], (pho >> ((b - 1) & 1) & 1) ^ 1, ctl);
         tc_fence_after_sync();
         if (ok && p.splits > 1) {
             // Its part, unnormalised, through the tile's own Q as below, half of the numbers at a time.
@@ -494,7 +494,7 @@ kv4_prefill_kernel(const PreParams p)
         for (int k = k_lo; k < k_hi && ok; ++k) {
             const int buf = (k - k_lo) & 1;
             // keys: lane (position, j) has one word of every group; positions in the order 0 4 1 5 ... keep the stores apart
-            if (!(ok = mbar_wait(&stg_full[st], sph, ctl) && mbar_wait(&k_empty[buf], ph[buf] ^ 1, ctl))) break;
+            if (!(ok = mbar_wait_warp(&stg_full[st], sph, ctl) && mbar_wait_warp(&k_empty[buf], ph[buf] ^ 1, ctl))) break;
             const uint8_t* src = smem + L::kStg + st * L::kPacked;
             uint8_t* dst = smem + L::kK + buf * L::kTile;
             const int kr = (idx >> 1) + 4 * (idx & 1);
@@ -519,7 +519,7 @@ kv4_prefill_kernel(const PreParams p)
             if (lane == 0) { mbar_arrive(&k_full[buf]); mbar_arrive(&stg_empty[st]); }
             if (++st == L::kStages) { st = 0; sph ^= 1; }
             // values: lane (position, j) has D / 4 consecutive numbers; the upper two quarters start elsewhere
-            if (!(ok = mbar_wait(&stg_full[st], sph, ctl) && mbar_wait(&v_empty[buf], ph[buf] ^ 1, ctl))) break;
+            if (!(ok = mbar_wait_warp(&stg_full[st], sph, ctl) && mbar_wait_warp(&v_empty[buf], ph[buf] ^ 1, ctl))) break;
             src = smem + L::kStg + st * L::kPacked;
             dst = smem + L::kV + buf * L::kTile;
             const int turn = W == 4 ? j & 2 : 0;             // the words of a lane in the order n ^ turn
@@ -631,14 +631,13 @@ kv4_prefill_kernel(const PreParams p)
             const uint32_t gone = __ballot_sync(0xffffffffu, src == nullptr) & 0xffu;
             if (!src) src = p.g.pool;
             for (int half = 0; half < 2 && ok; ++half) {
-                ok = mbar_wait(&stg_empty[st], ph ^ 1, ctl);
+                ok = mbar_wait_warp(&stg_empty[st], ph ^ 1, ctl);
                 if (ok && half == 0 && lane == 0) hidden[k % PRE_HIDE] = (uint8_t)gone;
                 __syncwarp();
                 if (ok && lane < 8) {
                     mbar_arrive_expect_tx(&stg_full[st], 10 * D);
                     bulk_g2s(smem + L::kStg + st * L::kPacked + lane * (10 * D), src + half * (10 * D), 10 * D, &stg_full[st]);
                 }
-                ok = __all_sync(0xffffffffu, ok);
                 if (ok && ++st == L::kStages) { st = 0; ph ^= 1; }
             }
         }

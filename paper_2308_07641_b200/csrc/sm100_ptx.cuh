@@ -113,6 +113,13 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     }
 }
 
+// The same for a whole warp, whose lanes get one answer: where a phase ends as the limit does, some lanes see the one and some
+// the other, and those that carry on would wait for those that left at the next warp-wide step.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* ctl)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctl));
+}
+
 // ---- async proxy ------------------------------------------------------------------------
 // Make generic-proxy shared-memory writes visible to the async proxy (MMA operand reads).
 __device__ __forceinline__ void fence_proxy_async_smem()
