@@ -199,3 +199,57 @@ def test_rows_of_no_sequence(dtype):
         assert torch.equal(out[mine], want) and (out[:6] == 7).all() and (out[6 + 2 * new:] == 7).all()
         torch.cuda.synchronize()
         assert b.cache.status() == 0
+
+
+@pytest.mark.parametrize("D,H,new", [(64, 16, 17), (128, 16, 24), (64, 16, 32), (128, 64, 5), (64, 64, 6), (64, 64, 8), (128, 64, 8)])
+def test_many_short_sequences_of_several_rows(D, H, new):
+    """17 to 32 rows a key/value head in more heads and sequences than four an SM: several items for one sequence and head in
+    the kernel for few rows.  Lengths from none; sequences with fewer rows than the most, or none."""
+    Hkv = 16
+    lens = [(53 * i) % 211 for i in range(39)] + [700]
+    rows = [min(n, new if i % 3 else (7 * i) % (new + 1)) for i, n in enumerate(lens)]
+    rows[1] = min(lens[1], new)
+    assert max(rows) == new and 16 < new * (H // Hkv) <= 32 and len(lens) * Hkv > 4 * 148
+    b = Batch(lens, Hkv, D, 32, seed=D + H + new)
+    b.check(H, rows, max_q=new)
+    b.check(H, rows, max_q=new, max_kv=max(lens), window=70)
+    b.check(H, rows, max_q=new, window=9)
+    b.check(H, rows, max_q=new, causal=False, scale=-0.3)
+
+
+@pytest.mark.parametrize("H,Hkv,D", [(8, 2, 64), (4, 4, 128)])
+def test_a_prompt_among_single_tokens(H, Hkv, D):
+    """One prompt beside 31 sequences of one token behind some 4000 positions, one of them long: the most rows of a sequence
+    choose the kernel for all."""
+    lens = [512] + [3900 + 13 * i for i in range(30)] + [20000]
+    new = [512] + [1] * 31
+    b = Batch(lens, Hkv, D, 64, seed=H)
+    b.check(H, new, max_q=512)
+    b.check(H, new, max_q=512, max_kv=20000, window=1000)
+
+
+@pytest.mark.parametrize("D,H,new,qmul", [(64, 8, 1, 40.0), (128, 4, 1, 40.0), (128, 8, 3, 40.0), (128, 4, 1, 4.0), (64, 12, 2, 12.0)])
+def test_scores_of_few_rows_carry_no_rounding_of_keys(D, H, new, qmul):
+    """The kernel for few rows multiplies q (exact in fp16) with the codes and adds in fp32: a score is off by at most
+    (4 D + 8) u of scale sum |q| (|base| + 15 step) -- fp32 sums of D products of which the tensor cores cut each, the sums of q in
+    two fp16 terms, two products and one sum more -- in the place of u16 scale sum |q k|.  The rest as in test_serving_gpu."""
+    import torch
+    Hkv = 2
+    b = Batch([777, 130], Hkv, D, 64, seed=D)
+    rows = 2 * new
+    q = (torch.randn(rows, H, D, generator=_gen(11), device="cuda") * qmul).bfloat16()
+    start = torch.tensor([0, new, rows], dtype=torch.int32, device="cuda")
+    out = b.cache.attend(q, b.table, b.seq_len, start, max_q=new, causal=False).double().cpu().numpy()
+    scale = 1 / math.sqrt(D)
+    want, size, _ = b.plain(q, [new, new], False, 0, scale)
+    per_group = np.abs(q.double().cpu().numpy()).reshape(rows, H, D // 32, 32).sum(-1)
+    amp = []
+    for s, k in enumerate(b.k):
+        g = k.reshape(*k.shape[:-1], D // 32, 32)
+        lo, hi = g.min(-1), g.max(-1)
+        reach = np.repeat(np.abs(lo) + (hi - lo) * (1 + 2.0 ** -9), H // Hkv, axis=1)             # [positions, heads, groups]
+        amp.append(np.einsum("ihg,jhg->ihj", per_group[s * new:(s + 1) * new], reach).max(-1) * scale)
+    d = (4 * D + 8) * U * np.concatenate(amp)[..., None]
+    tol = (2 * d + 3 * U16 + 2 * 777 * U) * size + U8 * np.abs(want)
+    err = np.abs(out - want) / tol
+    assert err.max() <= 1, f"worst {err.max():.3g} of the tolerance"
