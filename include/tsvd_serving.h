@@ -63,7 +63,8 @@ tsvd_status_t tsvd_i8_pack(const int8_t* W, long long ldw, const float* w_scale,
  *            TSVD_F32, TSVD_BF16: quantised inside the call exactly as tsvd_quantize does; x_scale must be NULL
  *   y        device, row b at y + b*ldy (ldy >= M): fp32 for TSVD_F32 and TSVD_I8, bf16 for TSVD_BF16;
  *            TSVD_FLAG_OUT_F32 makes it fp32, TSVD_FLAG_OUT_BF16 bf16
- *   flags    one of those two, or 0
+ *   flags    one of those two, or 0; TSVD_FLAG_TEST_STALL (tsvd.h) as well: the tokens never reach the product, its waits run
+ *            out after some milliseconds, y is unspecified and tsvd_i8_last_status reports TSVD_E_TIMEOUT
  * The sum is exact (32-bit integers); it is rounded once to fp32, multiplied by scale_b and by w_scale_m, the bias
  * added in fp32, and rounded once more where y is bf16.  B = 0 does nothing.
  * Calls on one handle share its scratch and must be ordered, as with tsvd_forward; the scratch grows (with one
@@ -140,7 +141,9 @@ tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, void* v, long 
  *   max_q    at least the rows of any sequence; rows beyond it are not computed
  *   max_kv   at least any seq_len; 0: max_pages * page_tokens.  A tighter bound spreads the work better and
  *            changes no result
- *   flags    TSVD_FLAG_CAUSAL, TSVD_FLAG_PATH_SIMPLE (CUDA-core kernel in fp32), or both
+ *   flags    TSVD_FLAG_CAUSAL, TSVD_FLAG_PATH_SIMPLE (CUDA-core kernel in fp32), TSVD_FLAG_TEST_STALL (bf16 on the tensor
+ *            cores: the cached positions never arrive, the waits run out after some milliseconds, out is unspecified and
+ *            tsvd_kv4_last_status reports TSVD_E_TIMEOUT), or several
  * bf16: products of tensor-core precision (q, keys and values as the cache holds them in bf16 or fp16, probabilities in
  * fp16), sums in fp32, one rounding of the result.  fp32: fp32 throughout.
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN (q or out not 16-byte aligned, ldq or ldo not a multiple of 8 elements),
@@ -155,7 +158,8 @@ tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long ldq, void* 
 tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages,
                             size_t* pool_bytes);
 /* Device status since the last read (synchronise first): TSVD_E_TIMEOUT if a bounded wait gave up, else TSVD_E_INDEX if a
- * page number or length was out of range, else TSVD_OK. */
+ * page number or length was out of range, else TSVD_OK.  After TSVD_E_TIMEOUT the results of every tsvd_kv4_attend since the
+ * read before are unspecified; this read makes the handle fit for the next one. */
 tsvd_status_t tsvd_kv4_last_status(tsvd_kv4_t h);
 void tsvd_kv4_destroy(tsvd_kv4_t h);
 

@@ -42,6 +42,7 @@ struct I8Params {
     int row_tiles, tok_tiles, NT;
     int band;                // row tiles of a band: a band's tiles are walked token tile by token tile
     int stages;
+    int test_stall;          // test hook: the tokens are never copied, so the waits must give up
     int columns;             // of tensor memory: one accumulator for a cluster's block, two for the others
     int* status;
 };
@@ -111,7 +112,7 @@ i8_mma_kernel(const I8Params p)
         for (int s = 0; s < p.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], 4); }
         ctl[0] = 0;
-        ctl[1] = kWaitLimitDefault;
+        ctl[1] = p.test_stall ? kWaitLimitStall : kWaitLimitDefault;
         fence_mbar_init();
     }
     if (warp == 5) { tmem_alloc(&tmem_slot, (uint32_t)p.columns); tmem_relinquish(); }
@@ -135,7 +136,7 @@ i8_mma_kernel(const I8Params p)
                     bulk_g2s(smem + (size_t)ahead * stage_bytes, p.W + ((size_t)rt0 * p.KB + kb) * 16384, 16384u, &full[ahead]);
                 }
             pdl_wait();
-            bool ok = true;
+            bool ok = !p.test_stall;
             for (int tile = first; tile < tiles && ok; tile += step) {
                 int rt, t0;
                 tile_at(p, tile, rt, t0);
@@ -157,8 +158,7 @@ i8_mma_kernel(const I8Params p)
             // No copy may be in flight when the block ends.  The contraction waits for every stage; where a wait gave up,
             // the copies of each stage's last use are waited for here (again with a limit).
             if (ctl[0])
-                for (int i = 0; i < p.stages; ++i)
-                    for (int n = 0; n < 4096 && !mbar_try_wait_64(&full[i], i < s ? ph : ph ^ 1); ++n) { }
+                for (int i = 0; i < p.stages; ++i) mbar_drain(&full[i], i < s ? ph : ph ^ 1);
         }
     } else if (warp == 5) {
         if (elect_one()) {
@@ -331,9 +331,10 @@ tsvd_status_t launch(I8Params p, int blocks, cudaStream_t st)
 
 }  // namespace
 
-tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, cudaStream_t st)
+tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, bool test_stall, cudaStream_t st)
 {
     I8Params p{};
+    p.test_stall = test_stall;
     p.W = h->W;
     p.x = x;
     p.x_scale = x_scale;

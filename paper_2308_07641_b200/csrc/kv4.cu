@@ -343,7 +343,7 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     const long long width = (long long)n_heads * h->g.dim;
     if (ldq < width || ldo < width || max_q < 1 || max_kv < 0 || window < 0 || !(scale == scale)) return TSVD_E_SHAPE;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
-    if (flags & ~(TSVD_FLAG_CAUSAL | TSVD_FLAG_PATH_SIMPLE)) return TSVD_E_DTYPE;
+    if (flags & ~(TSVD_FLAG_CAUSAL | TSVD_FLAG_PATH_SIMPLE | TSVD_FLAG_TEST_STALL)) return TSVD_E_DTYPE;
     if (n_rows == 0) return TSVD_OK;
     if (!q || !out) return TSVD_E_NULL;
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ldq % 8 || ldo % 8) return TSVD_E_ALIGN;
@@ -363,6 +363,7 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     a.scale = scale;
     a.window = window;
     a.causal = flags & TSVD_FLAG_CAUSAL;
+    a.test_stall = flags & TSVD_FLAG_TEST_STALL;
     a.stream = (cudaStream_t)stream;
     if (dtype == TSVD_F32 || (flags & TSVD_FLAG_PATH_SIMPLE)) return kv4_attend_simple(a);
     // Up to 16 rows a key/value head are one item of the kernel for few rows: 34 us against 40 (16 rows, 32 heads) and 60 against

@@ -61,6 +61,7 @@ struct DecParams {
     int max_q;
     float c;             // scale * log2(e)
     int window, causal;
+    int test_stall;      // test hook: no unit is ever copied, so the waits must give up
     int stages;          // units of a warp's ring
     int keep_cols;       // query rows of an item that can hold anything: what is kept of a part
     float* parts;        // [grid][2][rows][D + 2]
@@ -197,7 +198,7 @@ kv4_decode_kernel(const DecParams p)
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
 
-    if (threadIdx.x == 0) { ctl[0] = 0; ctl[1] = kWaitLimitDefault; }
+    if (threadIdx.x == 0) { ctl[0] = 0; ctl[1] = p.test_stall ? kWaitLimitStall : kWaitLimitDefault; }
     if (threadIdx.x < WARPS) {
         for (int i = 0; i < p.stages; ++i) mbar_init(&full[threadIdx.x][i], 1);
         kept[0][threadIdx.x].units = kept[1][threadIdx.x].units = 0;
@@ -345,7 +346,7 @@ kv4_decode_kernel(const DecParams p)
         ptr = b ? b + BLOCK : nullptr;
         --in_item;
         there = (there & ~(3u << (2 * st))) | (uint32_t)((a ? 1 : 0) | (b ? 2 : 0)) << (2 * st);
-        if (lane == 0) {
+        if (lane == 0 && !p.test_stall) {
             uint8_t* to = ring + (size_t)(warp * p.stages + st) * UNIT;
             mbar_arrive_expect_tx(&full[warp][st], UNIT);
             if (joined && a) {
@@ -632,8 +633,7 @@ kv4_decode_kernel(const DecParams p)
     if (!ok) {
         // a wait gave up: the warp's copies in flight are waited for (with a limit)
         if (lane == 0) atomicOr(p.status, KV4_DEV_TIMEOUT);
-        for (int i = 0; i < p.stages; ++i)
-            for (int n = 0; n < 4096 && !mbar_try_wait_64(&full[warp][i], i < stage ? phase ^ 1 : phase); ++n) { }
+        for (int i = 0; i < p.stages; ++i) mbar_drain(&full[warp][i], i < stage ? phase ^ 1 : phase);
     }
 
     // ================= the block's parts: chains of warps that share an item =================
@@ -816,6 +816,7 @@ tsvd_status_t kv4_attend_decode(const AttendArgs& a)
     p.c = fabsf(a.scale) < 1e-18f ? 1e-18f : a.scale * 1.4426950408889634f;
     p.window = a.window;
     p.causal = a.causal;
+    p.test_stall = a.test_stall;
     p.parts = a.h->parts;
     p.tickets = a.h->tickets;
     p.status = a.h->dev_status;

@@ -56,6 +56,7 @@ struct PreParams {
     float c;
     float sign;              // of the scale: goes into q
     int window, causal;
+    int test_stall;          // test hook: no position is ever copied, so the waits must give up
     int splits;              // blocks that share a pair's positions; above 1 they leave their parts in `parts`
     float* parts;            // [block][2 * PRE_ROWS][D] sums, [2 * PRE_ROWS] (reference, sum)
     int* status;
@@ -234,7 +235,7 @@ kv4_prefill_kernel(const PreParams p)
         mbar_init(&q_full, 8);
         mbar_init(&drained, 1);
         ctl[0] = 0;
-        ctl[1] = kWaitLimitDefault;
+        ctl[1] = p.test_stall ? kWaitLimitStall : kWaitLimitDefault;
         fence_mbar_init();
     }
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
@@ -610,7 +611,7 @@ kv4_prefill_kernel(const PreParams p)
             }
             // every product has ended before the block does
             umma_commit(&drained);
-            for (int n = 0; n < (1 << 16) && !mbar_try_wait_64(&drained, 0); ++n) { }
+            mbar_drain(&drained, 0);
         }
         __syncwarp();
       } else if (warp == 13) {
@@ -618,7 +619,7 @@ kv4_prefill_kernel(const PreParams p)
         const int per_page = p.g.page_tokens / KV4_BLOCK;
         int st = 0;
         uint32_t ph = 0;
-        bool ok = true;
+        bool ok = !p.test_stall;
         for (int k = k_lo; k < k_hi && ok; ++k) {
             const int blk = k * (PRE_KEYS / KV4_BLOCK) + (lane & 7);
             const uint8_t* src = nullptr;
@@ -643,8 +644,7 @@ kv4_prefill_kernel(const PreParams p)
         }
         // where a wait gave up, copies in flight are waited for (with a limit)
         if (ctl[0])
-            for (int i = 0; i < L::kStages; ++i)
-                for (int n = 0; n < 4096 && !mbar_try_wait_64(&stg_full[i], i < st ? ph : ph ^ 1); ++n) { }
+            for (int i = 0; i < L::kStages; ++i) mbar_drain(&stg_full[i], i < st ? ph : ph ^ 1);
         __syncwarp();
       }
     }
@@ -755,6 +755,7 @@ tsvd_status_t kv4_attend_prefill(const AttendArgs& a)
     p.sign = a.scale < 0.0f ? -1.0f : 1.0f;
     p.window = a.window;
     p.causal = a.causal;
+    p.test_stall = a.test_stall;
     p.status = a.h->dev_status;
     p.parts = a.h->parts;
     // Fewer pairs than half the SMs: blocks share a pair's positions, at least four tiles each (a tile takes about 2 us, the

@@ -197,11 +197,12 @@ extern "C" tsvd_status_t tsvd_i8_forward(tsvd_i8_t h, const void* x, long long l
     if (!h) return TSVD_E_NULL;
     if (B < 0 || ldx < h->N || ldy < h->M) return TSVD_E_SHAPE;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16 && dtype != TSVD_I8) return TSVD_E_DTYPE;
-    if ((flags & ~(TSVD_FLAG_OUT_F32 | TSVD_FLAG_OUT_BF16)) || flags == (TSVD_FLAG_OUT_F32 | TSVD_FLAG_OUT_BF16)) return TSVD_E_DTYPE;
+    const unsigned as = flags & (TSVD_FLAG_OUT_F32 | TSVD_FLAG_OUT_BF16);
+    if ((flags & ~(as | TSVD_FLAG_TEST_STALL)) || as == (TSVD_FLAG_OUT_F32 | TSVD_FLAG_OUT_BF16)) return TSVD_E_DTYPE;
     if (x_scale && dtype != TSVD_I8) return TSVD_E_DTYPE;
     if (B == 0) return TSVD_OK;
     if (!x || !y) return TSVD_E_NULL;
-    const bool y_bf16 = flags ? flags == TSVD_FLAG_OUT_BF16 : dtype == TSVD_BF16;
+    const bool y_bf16 = as ? as == TSVD_FLAG_OUT_BF16 : dtype == TSVD_BF16;
     if (misaligned(x, dtype == TSVD_F32 ? 4 : dtype == TSVD_BF16 ? 2 : 1) || misaligned(y, y_bf16 ? 2 : 4) || misaligned(x_scale, 4))
         return TSVD_E_ALIGN;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
@@ -212,7 +213,7 @@ extern "C" tsvd_status_t tsvd_i8_forward(tsvd_i8_t h, const void* x, long long l
     const rows8::Tiles out{h->ws, groups};
     TSVD_CUDA_OK(rows8::quantize(x, dtype, B, h->N, ldx, x_scale, out, xs, (cudaStream_t)stream));
     tsvd_count_launch();
-    return i8_product(h, h->ws, xs, B, y, ldy, y_bf16, (cudaStream_t)stream);
+    return i8_product(h, h->ws, xs, B, y, ldy, y_bf16, flags & TSVD_FLAG_TEST_STALL, (cudaStream_t)stream);
 }
 
 extern "C" tsvd_status_t tsvd_i8_info(tsvd_i8_t h, int* M, int* N, size_t* packed_bytes)

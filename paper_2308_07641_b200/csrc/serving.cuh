@@ -36,7 +36,8 @@ struct tsvd_i8_s {
 };
 
 // i8_mma.cu: the product of B tokens in tensor-core order (x, then their scales) with the handle's weights
-tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, cudaStream_t st);
+tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_scale, int B, void* y, long long ldy, bool y_bf16, bool test_stall,
+                         cudaStream_t st);
 tsvd_status_t i8_product_prepare(tsvd_i8_s* h);   // once for a handle, on its device, before its first product
 
 // ---- the 4-bit cache ------------------------------------------------------------------------------------------------
@@ -130,6 +131,7 @@ struct AttendArgs {
     float scale;
     int window;
     bool causal;
+    bool test_stall;       // TSVD_FLAG_TEST_STALL
     cudaStream_t stream;
 };
 tsvd_status_t kv4_attend_simple(const AttendArgs& a);   // kv4_simple.cu

@@ -75,6 +75,7 @@ __device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity)
 // up it sets the flag and returns false; the caller carries on to the kernel's normal exit so
 // that tensor memory is released.
 constexpr int kWaitLimitDefault = 4096;  // 2^32 clocks, about two seconds
+constexpr int kWaitLimitStall = 16;      // for calls with TSVD_FLAG_TEST_STALL: some 8 ms
 // Up to 64 tries in one tight loop (two tries per trip: the polling warps share their schedulers'
 // issue slots with the warps that do the work, so a try has to cost as few instructions as possible).
 __device__ __forceinline__ bool mbar_try_wait_64(uint64_t* bar, uint32_t parity)
@@ -118,6 +119,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* ctl)
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctl));
+}
+
+// Before a block ends: lets a copy in flight land, or products end, for some 8 ms at most (a barrier that nothing is under way
+// to is left then).
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity)
+{
+    const long long t0 = clock64();
+    while (!mbar_try_wait_64(bar, parity) && clock64() - t0 <= 16LL << 20) { }
 }
 
 // ---- async proxy ------------------------------------------------------------------------

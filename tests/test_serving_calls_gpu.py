@@ -253,3 +253,44 @@ def test_scores_of_few_rows_carry_no_rounding_of_keys(D, H, new, qmul):
     tol = (2 * d + 3 * U16 + 2 * 777 * U) * size + U8 * np.abs(want)
     err = np.abs(out - want) / tol
     assert err.max() <= 1, f"worst {err.max():.3g} of the tolerance"
+
+
+def _stalled(call, status):
+    """A call whose input is withheld ends by itself, says TSVD_E_TIMEOUT once, and leaves what follows as it was."""
+    import time
+
+    import torch
+    from paper_2308_07641_b200 import binding
+    want = call(0)
+    torch.cuda.synchronize()
+    assert status() == 0
+    t0 = time.perf_counter()
+    call(binding.TSVD_FLAG_TEST_STALL)
+    torch.cuda.synchronize()
+    assert time.perf_counter() - t0 < 5.0
+    assert status() == binding.TSVD_E_TIMEOUT and status() == 0
+    for _ in range(2):
+        assert torch.equal(call(0), want)
+    torch.cuda.synchronize()
+    assert status() == 0
+
+
+@pytest.mark.parametrize("B,N,M", [(1, 4096, 640), (40, 300, 200), (600, 512, 40000)])
+def test_layer_waits_give_up(B, N, M):
+    """A few tokens (clusters), a single block's contraction, and blocks that walk over several tiles."""
+    import torch
+    from paper_2308_07641_b200 import Int8Linear, quantize
+    layer = Int8Linear(*quantize(torch.randn(M, N, generator=_gen(M), device="cuda")))
+    x = torch.randn(B, N, generator=_gen(B), device="cuda").bfloat16()
+    _stalled(lambda flags: layer(x, flags=flags), layer.status)
+
+
+@pytest.mark.parametrize("lens,new,H,Hkv,D", [([50], [1], 2, 2, 64), ([9000, 70], [1, 1], 8, 2, 128), ([400, 300], [3, 3], 16, 4, 64),
+                                              ([600], [300], 4, 2, 128), ([3000], [40], 4, 4, 64)])
+def test_attention_waits_give_up(lens, new, H, Hkv, D):
+    """Blocks apart, parts that blocks add up, items of sixteen rows; many rows, and with positions shared by blocks."""
+    import torch
+    b = Batch(lens, Hkv, D, 64, seed=H)
+    q = torch.randn(sum(new), H, D, generator=_gen(5), device="cuda").bfloat16()
+    start = torch.tensor([0] + [sum(new[:i + 1]) for i in range(len(new))], dtype=torch.int32, device="cuda")
+    _stalled(lambda flags: b.cache.attend(q, b.table, b.seq_len, start, max_q=max(new), flags=flags), b.cache.status)
