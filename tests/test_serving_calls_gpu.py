@@ -294,3 +294,42 @@ def test_attention_waits_give_up(lens, new, H, Hkv, D):
     q = torch.randn(sum(new), H, D, generator=_gen(5), device="cuda").bfloat16()
     start = torch.tensor([0] + [sum(new[:i + 1]) for i in range(len(new))], dtype=torch.int32, device="cuda")
     _stalled(lambda flags: b.cache.attend(q, b.table, b.seq_len, start, max_q=max(new), flags=flags), b.cache.status)
+
+
+def test_binding_entry_points():
+    """The one-to-one functions of `binding`, with raw pointers on the default stream, against the torch front."""
+    import torch
+    from paper_2308_07641_b200 import Int8Linear, KV4Cache, binding, dequantize, quantize
+    g = _gen(21)
+    x = torch.randn(9, 200, generator=g, device="cuda")
+    q, scale = quantize(x)
+    y = dequantize(q, scale)
+    q2, scale2, y2 = torch.zeros_like(q), torch.zeros_like(scale), torch.zeros_like(y)
+    layer = Int8Linear(q, scale)
+    out = layer(x)
+    out2 = torch.zeros_like(out)
+    cache, other = KV4Cache(2, 64, 4, 16), KV4Cache(2, 64, 4, 16)
+    k, v = (torch.randn(3, 2, 64, generator=g, device="cuda") for _ in range(2))
+    a = torch.randn(3, 4, 64, generator=g, device="cuda").bfloat16()
+    table = torch.arange(3, dtype=torch.int32, device="cuda").view(3, 1)
+    n, start = torch.ones(3, dtype=torch.int32, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")
+    cache.append(k, v, table, n, start)
+    rk, rv = cache.read(3, table, n, start)
+    want = cache.attend(a, table, n, start, max_q=1)
+    rk2, rv2, got = torch.zeros_like(rk), torch.zeros_like(rv), torch.zeros_like(want)
+    torch.cuda.synchronize()
+    F32, BF16, stream = binding.TSVD_F32, binding.TSVD_BF16, torch.cuda.current_stream().cuda_stream
+    binding.tsvd_quantize(x.data_ptr(), F32, 9, 200, 200, q2.data_ptr(), q2.stride(0), scale2.data_ptr(), stream)
+    binding.tsvd_dequantize(q.data_ptr(), q.stride(0), scale.data_ptr(), 9, 200, y2.data_ptr(), F32, 200, stream)
+    binding.tsvd_i8_forward(layer.handle, x.data_ptr(), 200, 0, out2.data_ptr(), 9, 9, F32, 0, stream)
+    batch = (table.data_ptr(), 1, n.data_ptr(), start.data_ptr(), 3, 3)
+    binding.tsvd_kv4_append(other.handle, k.data_ptr(), 128, v.data_ptr(), 128, F32, *batch, stream)
+    binding.tsvd_kv4_read(other.handle, rk2.data_ptr(), 128, rv2.data_ptr(), 128, F32, *batch, stream)
+    binding.tsvd_kv4_attend(other.handle, a.data_ptr(), 256, got.data_ptr(), 256, 4, BF16, *batch, 1, 0, 0.125, 0, binding.TSVD_FLAG_CAUSAL,
+                            stream)
+    torch.cuda.synchronize()
+    for mine, theirs in ((q2, q), (scale2, scale), (y2, y), (out2, out), (rk2, rk), (rv2, rv), (got, want)):
+        assert torch.equal(mine, theirs)
+    assert binding.tsvd_i8_info(layer.handle)["M"] == 9 and binding.tsvd_i8_info(layer.handle)["N"] == 200
+    assert binding.tsvd_kv4_info(cache.handle) == {"n_kv_heads": 2, "head_dim": 64, "page_tokens": 16, "n_pages": 4, "pool_bytes": 4 * 2 * 20 * 64}
+    assert binding.tsvd_i8_last_status(layer.handle) == 0 and binding.tsvd_kv4_last_status(other.handle) == 0
