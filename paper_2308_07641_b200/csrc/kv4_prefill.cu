@@ -350,7 +350,7 @@ kv4_prefill_kernel(const PreParams p)
         const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
         for (int k = a; k < b; ++k) {
             const int h = k & 1, at = k * PRE_STEP;
-            if (!(ok = mbar_wait_warp(&s_full[x][h], phs >> h & 1, ctl))) break;
+            ok = mbar_wait(&s_full[x][h], phs >> h & 1, ctl);   // (the warp agrees on it where it looks at `over`)
             phs ^= 1u << h;
             tc_fence_after_sync();
             const uint32_t t_s = t_lane + 128u * x + 64u * h;
@@ -379,7 +379,8 @@ kv4_prefill_kernel(const PreParams p)
             }
             const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]) * cm;
             const bool over = top > ref + kMove;
-            if (__any_sync(0xffffffffu, over)) {
+            if (__any_sync(0xffffffffu, over || !ok)) {
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
                 const float to = over ? top - kSet : ref, keep = ex2(ref - to);    // 0 before the first score
                 ref = to;
                 sum *= keep;

@@ -9,7 +9,8 @@ from tests.test_tensor_memory_order import _kernels
 @pytest.mark.parametrize("path", ["kv4_decode.cu", "kv4_prefill.cu"])
 def test_a_warp_agrees_on_a_wait_that_gives_up(path):
     """Where a phase ends as the limit does, the lanes of a warp may see different answers; those that go on would wait for the
-    others for ever.  So a warp waits with mbar_wait_warp, and only one elected lane with mbar_wait."""
+    others for ever.  So a warp waits with mbar_wait_warp, and with mbar_wait only one elected lane, or lanes that compare their
+    answers (`ok`) before any leaves."""
     found = 0
     for p, name, body in _kernels():
         if p != path:
@@ -22,6 +23,10 @@ def test_a_warp_agrees_on_a_wait_that_gives_up(path):
                 i += 1
             elected.append((m.end(), i))
         for m in re.finditer(r"\bmbar_wait\(", body):
-            assert any(a < m.start() < b for a, b in elected), f"{name}: {body[m.start():m.start() + 60]}"
+            if any(a < m.start() < b for a, b in elected):
+                continue
+            rest = body[body.rindex("\n", 0, m.start()):]
+            assert rest.lstrip().startswith("ok = mbar_wait("), f"{name}: {rest[:60]}"
+            assert "break" not in rest[:rest.index("__all_sync(0xffffffffu, ok)")], name
         found += len(re.findall(r"\bmbar_wait_warp\(", body))
     assert found
