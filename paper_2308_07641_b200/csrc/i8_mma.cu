@@ -209,7 +209,7 @@ i8_mma_kernel(const I8Params p)
                     tmem_ld16(src + (uint32_t)j0, r);
                     float xs[16];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(xs + 4 * j) = __ldg(reinterpret_cast<const float4*>(p.x_scale + t0 + j0) + j);
+                    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(xs + 4 * j) = reinterpret_cast<const float4*>(p.x_scale + t0 + j0)[j];
                     tmem_ld_wait();
                     uint8_t* chunk = out_stage + flip * 16 * 128 * 4;
 #pragma unroll
@@ -284,7 +284,7 @@ i8_mma_kernel(const I8Params p)
                 int sum = 0;
 #pragma unroll
                 for (int k = 0; k < CL; ++k) sum += slots[k * p.NT * OWN + i];
-                if (m < p.M) store_y(p, t0 + j, m, sum, __ldg(p.x_scale + t0 + j), p.w_scale[m], p.bias ? p.bias[m] : 0.0f);
+                if (m < p.M) store_y(p, t0 + j, m, sum, p.x_scale[t0 + j], p.w_scale[m], p.bias ? p.bias[m] : 0.0f);
             }
         }
     }

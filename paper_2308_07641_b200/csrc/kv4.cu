@@ -104,7 +104,7 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 // 2.1 us, a launch.
 template <typename T, bool VEC, int D>
 __global__ void __launch_bounds__(512)
-kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ k, long long ldk, const T* __restrict__ v, long long ldv, int* status)
+kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* k, long long ldk, const T* v, long long ldv, int* status)
 {
     pdl_launch_dependents();
     pdl_wait();

@@ -11,7 +11,7 @@ namespace {
 // Bound by its stores: 2048 x 4096 to fp32, 42 MB, 6.2 us with q in L2 (the copy bandwidth gives 6.5 from DRAM); 333 x 1001 2.9.
 template <typename T>
 __global__ void __launch_bounds__(256)
-dequantize_rows_kernel(const int8_t* __restrict__ q, long long ldq, const float* __restrict__ scale, int rows, int cols, T* __restrict__ y,
+dequantize_rows_kernel(const int8_t* q, long long ldq, const float* scale, int rows, int cols, T* __restrict__ y,
                        long long ldy, int per_row_log, bool wide)
 {
     constexpr int N = 16 / (int)sizeof(T);
@@ -27,8 +27,8 @@ dequantize_rows_kernel(const int8_t* __restrict__ q, long long ldq, const float*
     for (int c = (int)(threadIdx.x & ((1u << per_row_log) - 1)) * N; c < cols; c += step) {
         if (wide && c + N <= cols) {
             alignas(16) int8_t b[N];
-            if constexpr (N == 4) *reinterpret_cast<uint32_t*>(b) = __ldg(reinterpret_cast<const uint32_t*>(src + c));
-            else *reinterpret_cast<uint2*>(b) = __ldg(reinterpret_cast<const uint2*>(src + c));
+            if constexpr (N == 4) *reinterpret_cast<uint32_t*>(b) = *reinterpret_cast<const uint32_t*>(src + c);
+            else *reinterpret_cast<uint2*>(b) = *reinterpret_cast<const uint2*>(src + c);
             alignas(16) T t[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) t[e] = from_f32<T>((float)b[e] * s);

@@ -34,7 +34,7 @@ struct Unit {
         if (VEC && c + 16 <= cols) {
             alignas(16) T t[16];
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(row + c) + i);
+            for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(t)[i] = reinterpret_cast<const uint4*>(row + c)[i];
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = to_f32(t[i]);
         } else {
@@ -64,7 +64,7 @@ struct Unit<int8_t, true> {
     uint4 u;
     __device__ __forceinline__ void load(const int8_t* row, int c, int cols)
     {
-        if (c + 16 <= cols) { u = __ldg(reinterpret_cast<const uint4*>(row + c)); return; }
+        if (c + 16 <= cols) { u = *reinterpret_cast<const uint4*>(row + c); return; }
         alignas(16) int8_t t[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) t[i] = c + i < cols ? row[c + i] : (int8_t)0;
@@ -115,7 +115,7 @@ struct Tiles {
 // registers; NU = 0: rows of any length, read twice.
 template <typename T, bool VEC, int TPR, int NU, typename OUT>
 __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
-quantize_kernel(const T* __restrict__ x, int rows, int cols, long long ldx, const float* __restrict__ given, OUT out, float* __restrict__ scale)
+quantize_kernel(const T* x, int rows, int cols, long long ldx, const float* given, OUT out, float* scale)
 {
     __shared__ uint32_t slots[TPR == 32 ? 1 : TPR / 32];
     pdl_launch_dependents();

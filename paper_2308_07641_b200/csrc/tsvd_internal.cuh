@@ -136,6 +136,10 @@ constexpr int TSVD_DEV_BOUNDS = 4;    // checked builds (-DTSVD_CHECK_BOUNDS): a
 // pdl_launch_dependents() to let the kernel after it start likewise.  Without the launch
 // attribute (or with nothing before or after it) both calls do nothing.
 //
+// What the kernel ahead writes changes while its dependent already runs: the dependent reads it by ordinary loads behind
+// pdl_wait(), not by __ldg or a const __restrict__ parameter, which promise that the data never change while it runs and let
+// the loads move ahead of the wait.
+//
 // Allocating tensor memory waits, without a limit, for whatever kernel on the SM holds it.  So a kernel calls
 // pdl_launch_dependents() only after its own allocation: a kernel that holds columns in its pdl_wait() then waits only for
 // kernels whose blocks all have theirs.  The other way round, a block could hold the columns that the kernel it waits for

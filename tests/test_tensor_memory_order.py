@@ -48,3 +48,17 @@ def test_cluster_kernels_with_tensor_memory_have_an_sm_to_themselves(path):
     head = open(os.path.join(CSRC, "tsvd_internal.cuh")).read()
     alone, sm = (eval(re.search(r"constexpr size_t " + n + r" = ([\d *]+);", head).group(1)) for n in ("TSVD_ALONE_SMEM", "TSVD_SM_SMEM"))
     assert 2 * alone > sm == 228 * 1024
+
+
+def test_dependents_do_not_promise_that_their_inputs_stay():
+    """A kernel that starts before the one ahead of it has ended must not read that one's results as data that never change
+    (__ldg, const __restrict__): such loads may move ahead of its wait.  The serving kernels have none."""
+    seen = set()
+    for path in ("quant8.cu", "rows8.cuh", "i8_mma.cu", "kv4.cu", "kv4_decode.cu", "kv4_prefill.cu"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
+        assert "__ldg(" not in text and "ld.global.nc" not in text, path
+        for m in re.finditer(r"__global__[^{;]*?(\w+)\s*\(([^{;]*)\)\s*\{", text):
+            if "pdl_wait()" in text[m.end():m.end() + 4000]:
+                seen.add(path)
+                assert not re.search(r"const\s+[\w<>]+\s*\*\s*__restrict__", m.group(2)), f"{path}: {m.group(1)}"
+    assert len(seen) == 6
