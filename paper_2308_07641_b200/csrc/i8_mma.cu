@@ -4,12 +4,14 @@
 // each), N = a tile of up to 256 tokens (one accumulator column each), K = 32 bytes.  Both operands lie in global memory in
 // the order the instruction reads (serving.cuh), so a stage of 128 contraction bytes is two contiguous bulk copies.
 //
-// Many tokens: a persistent grid, one 128 x 256 tile an SM at a time, two accumulators, so that a tile's results leave (through
-// shared memory, a token's 128 channels together) while the next one's products run.  12288 x 4096 weights, 2048 tokens: the
-// product 79 us = 2.6 POP/s (0.78 of twice the measured bf16 rate; 86 us once the power limit holds), tensor pipe 69% of the
-// active cycles.  What bounds it is what an SM can take in: a stage of 48 KB feeds 512 clocks of products and arrives at about
-// 61 bytes a clock, 800 clocks a stage.  Two row tiles a block for one token tile take in a quarter less and were slower
-// (88 -> 93 us: no second pair of accumulators to overlap the results with).
+// Many tokens: a persistent grid, one tile of 128 channels by up to 256 tokens an SM at a time, two accumulators, so that a
+// tile's results leave (through shared memory, a token's 128 channels together) while the next one's products run.
+// 12288 x 4096 weights, 2048 tokens: tiles of 240 tokens (six rounds of 864 tiles, as 256 would take), the call 87 us with the
+// 6 to 9 of the quantisation, product some 80 = 2.6 POP/s (0.78 of twice the measured bf16 rate); 101 us when run for seconds,
+// the power limit then holds the SMs at 1582 MHz.  Tensor pipe 71% of the active cycles: a stage of 46 KB feeds 480 clocks of
+// products, and the 1.26 GB that the SMs take in come at 15.7 TB/s.  Two row tiles a block for one token tile take in a quarter
+// less and were slower (88 -> 93 us: no second pair of accumulators to overlap the results with); pairs of SMs on one tile
+// (cta_group::2) would take in a third less and were not built.
 // Few tokens: bound by streaming the weights, and by the latency of a launch, a round trip and the results; the contraction is
 // split over a cluster whose blocks add their parts through distributed shared memory.  One token, 4096 x 4096: 5.8 us with
 // the quantisation before it; the 16.8 MB take 2.6 at the copy bandwidth.

@@ -166,7 +166,7 @@ template <typename T, bool VEC, int TPR, int NU, typename OUT>
 cudaError_t launch(const void* x, int rows, int cols, long long ldx, const float* given, const OUT& out, float* scale, cudaStream_t st)
 {
     // A warp a row: blocks of one warp spread few rows over the SMs (333 x 1001 fp32 2.5 us, with eight 3.9; 1500 x 512 2.0 and
-    // 2.3), but at most 32 of them fit an SM (8192 x 512 9.1 us, with eight 4.5).
+    // 2.3), but at most 32 of them fit an SM (8192 x 512 9.1 us, with eight 4.5).  148: the SMs of the one GPU that this is built for.
     const unsigned warps = rows >= 148 * 16 ? 8 : 1;
     PdlLaunch l(TPR == 32 ? ((unsigned)rows + warps - 1) / warps : (unsigned)rows, TPR == 32 ? warps * 32 : TPR, 0, st);
     return cudaLaunchKernelEx(&l.cfg, quantize_kernel<T, VEC, TPR, NU, OUT>, (const T*)x, rows, cols, ldx, given, out, scale);

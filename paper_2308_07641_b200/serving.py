@@ -227,7 +227,8 @@ class KV4Cache:
                flags: int = 0):
         """Attention of q [rows, n_heads, head_dim] (bfloat16 or float32) over the cached keys and values; the rows are the
         last positions of their sequences (append their keys first).  max_q, max_kv: bounds on the rows and the positions
-        of one sequence, where the caller knows them.  Returns a tensor like q."""
+        of one sequence, where the caller knows them; with q_start and without max_q a sequence may have all the rows, and
+        the call takes the kernel for that (single tokens take far longer in it).  Returns a tensor like q."""
         rows, n_heads, ldq = self._heads(q, "KV4Cache.attend")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.attend")
         stream = _stream("KV4Cache.attend", q, out, page_table, seq_len, q_start)
