@@ -14,7 +14,8 @@
 // (cta_group::2) would take in a third less and were not built.
 // Few tokens: bound by streaming the weights, and by the latency of a launch, a round trip and the results; the contraction is
 // split over a cluster whose blocks add their parts through distributed shared memory.  One token, 4096 x 4096: 5.8 us with
-// the quantisation before it; the 16.8 MB take 2.6 at the copy bandwidth.
+// the quantisation before it and the weights in L2, 7.2 with the weights from DRAM, where the 16.8 MB take 2.6 at the copy
+// bandwidth.
 #include <algorithm>
 
 #include "serving.cuh"
@@ -354,7 +355,8 @@ tsvd_status_t i8_product(const tsvd_i8_s* h, const uint8_t* x, const float* x_sc
     p.status = h->dev_status;
     // Token tile and split of the contraction, by an estimate in SM clocks: a block of 128 columns costs its MMAs (2 clocks
     // a token) or its copies (about 56 bytes a clock), whichever is longer; a tile's end about 8 clocks a token; a cluster's
-    // two barriers and exchange about 2500.  One token, 4096 x 4096: 5.8 us, without clusters 9.7, with tiles of 256
+    // two barriers and exchange about 2500.  No more clusters than run at a time: eighteen of eight for 2304 channels, one token,
+    // took 9.0 us in two rounds where eighteen of four take 5.6.  One token, 4096 x 4096: 5.8 us, without clusters 9.7, with tiles of 256
     // tokens 6.8; 197 tokens, 1001 x 770: 7.0, without clusters the same, with tiles of 256 tokens 11.7.
     const int sms = h->sms;
     long long best = -1;
