@@ -56,19 +56,35 @@ __device__ __forceinline__ int tsvd_round_bits(float v, float qscale)
 template <int ND>
 __device__ __forceinline__ void digits_of_16(const int (&q)[16], uint32_t (&dig)[ND][4]) { digits_of<ND, 4>(q, dig); }
 
+// Sixteen or eight bytes behind pdl_wait(): the kernel ahead may have written them, so not a read-only load (__ldg), which may
+// move ahead of the wait; volatile keeps this one behind it, and unlike a plain load it may pass the kernel's own stores (int8
+// tokens of cfg5 46.5 us with plain loads, 45.8 with these).
+__device__ __forceinline__ uint4 ld16_behind_wait(const void* p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 ld8_behind_wait(const void* p)
+{
+    uint2 v;
+    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+
 // Load 8 consecutive values of a row as floats (one or two vector loads when the chunk is whole
 // and the row 16-byte aligned, guarded scalar loads otherwise).
 template <typename IN_T>
-__device__ __forceinline__ void load8(const IN_T* __restrict__ row, int c0, int C, bool vec_ok, float (&v)[8])
+__device__ __forceinline__ void load8(const IN_T* row, int c0, int C, bool vec_ok, float (&v)[8])
 {
     if (vec_ok && c0 + 8 <= C) {
         if constexpr (sizeof(IN_T) == 4) {
-            const float4 f0 = __ldg(reinterpret_cast<const float4*>(row + c0));
-            const float4 f1 = __ldg(reinterpret_cast<const float4*>(row + c0) + 1);
-            v[0] = f0.x; v[1] = f0.y; v[2] = f0.z; v[3] = f0.w;
-            v[4] = f1.x; v[5] = f1.y; v[6] = f1.z; v[7] = f1.w;
+            const uint4 u0 = ld16_behind_wait(row + c0), u1 = ld16_behind_wait(row + c0 + 4);
+            const uint32_t w[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
         } else if constexpr (sizeof(IN_T) == 2) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(row + c0));
+            const uint4 u = ld16_behind_wait(row + c0);
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {   // bf16 -> fp32 is a 16-bit shift
@@ -76,7 +92,7 @@ __device__ __forceinline__ void load8(const IN_T* __restrict__ row, int c0, int 
                 v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
             }
         } else {
-            const uint2 u = __ldg(reinterpret_cast<const uint2*>(row + c0));
+            const uint2 u = ld8_behind_wait(row + c0);
             const uint32_t w[2] = {u.x, u.y};
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (float)(int)(int8_t)((w[j >> 2] >> (8 * (j & 3))) & 0xFF);
@@ -90,21 +106,22 @@ __device__ __forceinline__ void load8(const IN_T* __restrict__ row, int c0, int 
 // Load 16 consecutive values of a row as floats (vector loads when the chunk is whole and
 // 16-byte aligned, guarded scalar loads otherwise).
 template <typename IN_T>
-__device__ __forceinline__ void load16(const IN_T* __restrict__ row, int c0, int C, bool vec_ok, float (&v)[16])
+__device__ __forceinline__ void load16(const IN_T* row, int c0, int C, bool vec_ok, float (&v)[16])
 {
     if (vec_ok && c0 + 16 <= C) {
         if constexpr (sizeof(IN_T) == 4) {
             const float4* p4 = reinterpret_cast<const float4*>(row + c0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float4 f = __ldg(p4 + i);
-                v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
+                const uint4 u = ld16_behind_wait(p4 + i);
+                v[4 * i] = __uint_as_float(u.x); v[4 * i + 1] = __uint_as_float(u.y);
+                v[4 * i + 2] = __uint_as_float(u.z); v[4 * i + 3] = __uint_as_float(u.w);
             }
         } else if constexpr (sizeof(IN_T) == 2) {
             const uint4* p4 = reinterpret_cast<const uint4*>(row + c0);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint4 u = __ldg(p4 + i);
+                const uint4 u = ld16_behind_wait(p4 + i);
                 const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {   // bf16 -> fp32 is a 16-bit shift
@@ -113,7 +130,7 @@ __device__ __forceinline__ void load16(const IN_T* __restrict__ row, int c0, int
                 }
             }
         } else {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(row + c0));
+            const uint4 u = ld16_behind_wait(row + c0);
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[j] = (float)(int)(int8_t)((w[j >> 2] >> (8 * (j & 3))) & 0xFF);

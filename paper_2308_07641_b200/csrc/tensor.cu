@@ -80,8 +80,8 @@ constexpr int GEMM_SMEM_BYTES = NB * B_SLOT_BYTES + NP * P_SLOT_BYTES +
 // values are their own single digit and the scale is 1.
 template <typename IN_T, int ND, int TPT, int TOK, int CH>
 __global__ void __launch_bounds__(256, 4)   // <= 64 registers: a batch of 4096 tokens is then one wave
-digitise_kernel(const IN_T* __restrict__ in, int ld_in, int B, int B_pad, int C, int KB,
-                const unsigned* __restrict__ amax_bits, int8_t* __restrict__ D, float* __restrict__ scale_out,
+digitise_kernel(const IN_T* in, int ld_in, int B, int B_pad, int C, int KB,
+                const unsigned* amax_bits, int8_t* __restrict__ D, float* __restrict__ scale_out,
                 int* __restrict__ zero_buf, int zero_per_token, int zero_total, int* __restrict__ status,
                 unsigned long long* __restrict__ stamp, const PatchGather pg)
 {
@@ -259,11 +259,11 @@ __device__ __forceinline__ void raw_zero(RawChunk16<IN_T>& r)
     for (int i = 0; i < (int)sizeof(IN_T); ++i) r.u[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 template <typename IN_T>
-__device__ __forceinline__ void raw_load(const IN_T* __restrict__ p, RawChunk16<IN_T>& r)
+__device__ __forceinline__ void raw_load(const IN_T* p, RawChunk16<IN_T>& r)
 {
     const uint4* p4 = reinterpret_cast<const uint4*>(p);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(IN_T); ++i) r.u[i] = __ldg(p4 + i);
+    for (int i = 0; i < (int)sizeof(IN_T); ++i) r.u[i] = ld16_behind_wait(p4 + i);
 }
 template <typename IN_T>
 __device__ __forceinline__ void raw_unpack(const RawChunk16<IN_T>& r, float (&v)[16])
@@ -293,7 +293,7 @@ __device__ __forceinline__ void raw_unpack(const RawChunk16<IN_T>& r, float (&v)
 
 template <typename IN_T, int ND, int TOK>
 __global__ void __launch_bounds__(256, 4)
-digitise_stream_kernel(const IN_T* __restrict__ in, int ld_in, int B, int B_pad, int C, int KB,
+digitise_stream_kernel(const IN_T* in, int ld_in, int B, int B_pad, int C, int KB,
                        int8_t* __restrict__ D, float* __restrict__ scale_out, int* __restrict__ zero_buf,
                        int zero_per_token, int zero_total, int* __restrict__ status,
                        unsigned long long* __restrict__ stamp, const PatchGather pg)
@@ -776,10 +776,10 @@ ternary_mma_kernel(const GemmParams p)
                 // array is padded to whole tiles), while the tensor-memory loads are in flight
                 float sc[8];
                 if constexpr (EPI != EPI_ACC) {
-                    const float4 s0 = __ldg(reinterpret_cast<const float4*>(p.scale + b0));
-                    const float4 s1 = __ldg(reinterpret_cast<const float4*>(p.scale + b0 + 4));
-                    sc[0] = s0.x; sc[1] = s0.y; sc[2] = s0.z; sc[3] = s0.w;
-                    sc[4] = s1.x; sc[5] = s1.y; sc[6] = s1.z; sc[7] = s1.w;
+                    const uint4 s0 = ld16_behind_wait(p.scale + b0), s1 = ld16_behind_wait(p.scale + b0 + 4);
+                    const uint32_t sb[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sc[i] = __uint_as_float(sb[i]);
                 }
                 tmem_ld_wait();
                 const int n_live = min(8, p.B - b0);   // uniform across the warp
@@ -893,7 +893,7 @@ ternary_mma_kernel(const GemmParams p)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const bool live = b0 + i < p.B;              // uniform across the warp
-                        sc[i] = live ? __ldg(p.scale + b0 + i) : 0.f;
+                        sc[i] = live ? p.scale[b0 + i] : 0.f;
 #pragma unroll
                         for (int d = 0; d < ND; ++d)
                             a[i][d] = live ? __ldcg(p.acc + ((size_t)(b0 + i) * ND + d) * p.acc_ld + row) : 0;

@@ -62,3 +62,13 @@ def test_dependents_do_not_promise_that_their_inputs_stay():
                 seen.add(path)
                 assert not re.search(r"const\s+[\w<>]+\s*\*\s*__restrict__", m.group(2)), f"{path}: {m.group(1)}"
     assert len(seen) == 6
+
+
+def test_ternary_dependents_do_not_promise_it_either():
+    """The same for the ternary kernels: read-only loads only of what belongs to the handle and no kernel writes."""
+    for path in ("digits.cuh", "tensor.cu", "decode.cu", "index.cu", "midbatch.cu"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
+        for m in re.finditer(r"__ldg\(([^)]*)\)", text):
+            assert re.match(r"p\.(bias|row_ptr|entries)\b", m.group(1)), f"{path}: {m.group(0)}"
+        for m in re.finditer(r"const\s+(\w+)\s*\*\s*__restrict__\s+(\w+)", text):
+            raise AssertionError(f"{path}: {m.group(0)}")
