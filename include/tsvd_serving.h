@@ -136,7 +136,8 @@ tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, void* v, long 
  * A row that sees nothing (seq_len 0, for instance) gets zeros.  Append the new keys first.
  *
  *   q, out   device, TSVD_BF16 or TSVD_F32 both: head a of row i at q + i*ldq + a*head_dim (ldq >= n_heads*head_dim);
- *            out and ldo likewise.  A row's result depends on that row of q alone: an infinity or a NaN spoils its own.
+ *            out and ldo likewise.  Rows do not disturb each other: an infinity or a NaN in a row of q spoils that row's
+ *            result only.
  *   n_heads  a multiple of the cache's n_kv_heads
  *   max_q    at least the rows of any sequence; rows beyond it are not computed.  It chooses the kernel, for all sequences of
  *            the call: up to 16 rows a key/value head are far faster by the one for few rows
