@@ -40,6 +40,32 @@ tsvd_status_t tsvd_quantize(const void* x, tsvd_dtype_t dtype, long long rows, i
 tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const float* scale, long long rows, int cols, void* y,
                               tsvd_dtype_t dtype, long long ldy, void* stream);
 
+/*
+ * tsvd_rms_norm -- root-mean-square norm of rows, the residual added on the way, the result as numbers or in 8 bits:
+ *     h_bn = x_bn + residual_bn, rounded to x's type (x itself without a residual)
+ *     rho_b = 1 / sqrt(mean_n h_bn^2 + eps)
+ *     y:  y_bn = h_bn * rho_b * w_n, computed in fp32, rounded once to x's type
+ *     q:  t_bn = h_bn * w_n,  a_b = max_n |t_bn|,  q_bn = rint(t_bn * ((1 / a_b) * 127)),  scale_b = (a_b * (1 / 127)) * rho_b
+ * The sum of squares is taken in fp32, and once more in 64 bits for a row whose squares leave fp32's range.  q is
+ * elementwise in fp32 from h and w (every reciprocal and product rounded to nearest, rint to even) and does not depend on rho.
+ * It is what tsvd_i8_forward takes as TSVD_I8 rows with x_scale.
+ *
+ *   x         device, TSVD_F32 or TSVD_BF16, row b at x + b*ldx (elements, ldx >= cols)
+ *   residual  device, like x, or NULL; then h is NULL too
+ *   h         device, like x, receives the sum (the next layer's residual).  It may be x or the residual itself (the same
+ *             pointer and row stride), otherwise it must not overlap them
+ *   weight    device, [cols], TSVD_F32 or TSVD_BF16
+ *   eps       1e-12 or more
+ *   y         device, like x, or NULL; may be x itself, where there is no residual
+ *   q, scale  device, row b at q + b*ldq (ldq >= cols), scale float [rows]; NULL where y is given.  One of the two results.
+ * A row with a NaN or an infinity gets results that are not all finite (in 8 bits a scale that is not finite); no other row does.
+ * A row whose a_b is below 2^-100 becomes q = 0.  rows = 0 does nothing.
+ * Errors: E_NULL (also both results, or none), E_SHAPE, E_DTYPE, E_VALUE (eps), E_ALIGN, E_CUDA.
+ */
+tsvd_status_t tsvd_rms_norm(const void* x, tsvd_dtype_t dtype, long long rows, int cols, long long ldx, const void* residual,
+                            long long ldr, void* h, long long ldh, const void* weight, tsvd_dtype_t weight_dtype, float eps,
+                            void* y, long long ldy, int8_t* q, long long ldq, float* scale, void* stream);
+
 typedef struct tsvd_i8_s* tsvd_i8_t; /* opaque; owns device memory on one GPU */
 
 /*
@@ -79,6 +105,54 @@ tsvd_status_t tsvd_i8_info(tsvd_i8_t h, int* M, int* N, size_t* packed_bytes);
 /* TSVD_E_TIMEOUT if a bounded device-side wait gave up since the last read (synchronise first), else TSVD_OK. */
 tsvd_status_t tsvd_i8_last_status(tsvd_i8_t h);
 void tsvd_i8_destroy(tsvd_i8_t h);
+
+/* ---- low-rank adapters of many requests beside a shared projection ------------------------------------------- */
+
+typedef struct tsvd_adapters_s* tsvd_adapters_t; /* opaque; owns device memory on one GPU */
+
+/*
+ * tsvd_adapters_create -- room for n_slots adapters of a projection from N to M numbers:  A [rank, N], B [M, rank], a factor
+ * each, ranks up to max_rank (at most TSVD_ADAPTERS_MAX_RANK).  Every slot is empty at first.
+ * Synchronous.  Errors: E_NULL, E_SHAPE, E_TOOBIG (also N above 2^24, M above 2^21), E_NOMEM, E_CUDA.
+ */
+#define TSVD_ADAPTERS_MAX_RANK 128
+tsvd_status_t tsvd_adapters_create(int N, int M, int max_rank, int n_slots, tsvd_adapters_t* out);
+
+/*
+ * tsvd_adapters_set -- an adapter into a slot, in the stream's order: calls ahead on the stream use what the slot held before.
+ *   A  device, row r at A + r*lda (elements, lda >= N);  B  device, row m at B + m*ldb (ldb >= rank); TSVD_F32 or TSVD_BF16.
+ *      Copied, and kept in bf16: fp32 weights are rounded once here.
+ *   rank = 0 empties the slot (A and B are not looked at).
+ * Errors: E_NULL, E_INDEX (slot), E_SHAPE, E_DTYPE, E_ALIGN, E_CUDA.
+ */
+tsvd_status_t tsvd_adapters_set(tsvd_adapters_t h, int slot, const void* A, long long lda, const void* B, long long ldb,
+                                tsvd_dtype_t dtype, int rank, float scale, void* stream);
+
+/*
+ * tsvd_adapters_forward -- out_i = base_i + scale_s * B_s (A_s x_i)  for n_rows rows, s = slots[sequence of row i].
+ *   x         device, row i at x + i*ldx (ldx >= N): TSVD_F32, TSVD_BF16, or TSVD_I8 with x_scale device float [n_rows]
+ *             (NULL: all ones), as tsvd_i8_forward takes them
+ *   base      device, row i at base + i*ldb (ldb >= M), out_dtype: the shared projection's result; NULL: zeros
+ *   out       device, row i at out + i*ldo (ldo >= M), TSVD_F32 or TSVD_BF16.  May be base itself (same pointer and stride)
+ *   slots     device, int32 [n_seq]: the slot of each sequence; -1 or an empty slot: none, the row becomes base's.  A number
+ *             below -1 or from n_slots on counts as none and makes tsvd_adapters_last_status report TSVD_E_INDEX
+ *   q_start   device, int32 [n_seq + 1]: the rows q_start[s] .. q_start[s+1]-1 belong to sequence s; NULL: one row each.  Rows
+ *             below q_start[0] or from q_start[n_seq] on belong to none and are not written
+ * Weights are bf16; sums, A x and the result's addition fp32 (see adapters.cu); one rounding of the result.  Rows and
+ * adapters do not disturb each other: what is not finite in one stays there.
+ * Calls on one handle share its scratch and must be ordered; it grows on the first call with more rows unless
+ * tsvd_adapters_reserve has sized it (outgrown scratch lives as long as the handle: captured graphs stay valid).
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_NOMEM, E_CUDA.
+ */
+tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
+                                    const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
+                                    const int* slots, const int* q_start, int n_seq, int n_rows, void* stream);
+/* Scratch for calls of up to rows_max rows, so that none of them allocates. */
+tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max);
+tsvd_status_t tsvd_adapters_info(tsvd_adapters_t h, int* N, int* M, int* max_rank, int* n_slots, size_t* bytes);
+/* TSVD_E_INDEX if a slot number was out of range since the last read (synchronise first), else TSVD_OK. */
+tsvd_status_t tsvd_adapters_last_status(tsvd_adapters_t h);
+void tsvd_adapters_destroy(tsvd_adapters_t h);
 
 /* ---- keys and values in 4 bits ------------------------------------------------------------------------------- */
 
@@ -120,6 +194,35 @@ tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long ldk, const 
                               const int* page_table, int max_pages, const int* seq_len, const int* q_start, int n_seq,
                               int n_rows, void* stream);
 
+/*
+ * tsvd_kv4_append_rotated -- tsvd_kv4_append with the rotation by position on the way: row i stands at position
+ * P_i = seq_len[s] - (rows of s) + (i - q_start[s]); of every head of q and k the first `turned` numbers are rotated in pairs,
+ *     (u, v)  ->  (u * cos - v * sin,  v * cos + u * sin)      every product and sum rounded to fp32
+ * with cos = table[P_i * turned + p] and sin = table[P_i * turned + turned/2 + p] for pair p.  Keys then go into the cache from
+ * fp32, queries are rounded once to their type; the other numbers of a head, and v, are taken as they are.
+ *   q         device, like k: head a of row i at q + i*ldq + a*head_dim (ldq >= n_heads*head_dim); n_heads = 0: no queries
+ *   q_out     device, like q; must not overlap q, k or v
+ *   table     device, float [positions][turned], as tsvd_rotary_table makes it
+ *   turned    even, 2 .. head_dim
+ *   interleaved  0: pair p is the numbers (p, p + turned/2); else (2p, 2p + 1)
+ * A position behind the table makes tsvd_kv4_last_status report TSVD_E_INDEX, as does one before 0 or outside the pages; its
+ * keys and values are not written, and its row of q_out is zeros where the table has no such position.  Rows that belong to no
+ * sequence are not written.
+ * Errors: those of tsvd_kv4_append; E_VALUE (q_out is q).
+ */
+tsvd_status_t tsvd_kv4_append_rotated(tsvd_kv4_t h, const void* q, long long ldq, void* q_out, long long ldqo, int n_heads,
+                                      const void* k, long long ldk, const void* v, long long ldv, tsvd_dtype_t dtype,
+                                      const float* table, int positions, int turned, int interleaved, const int* page_table,
+                                      int max_pages, const int* seq_len, const int* q_start, int n_seq, int n_rows, void* stream);
+
+/*
+ * tsvd_rotary_table -- table[P * turned + p] = amplitude * cos(P * rates[p]), and sin at + turned/2, for P = 0 .. positions-1
+ * and p = 0 .. turned/2-1; angles in 64 bits, one rounding to fp32.
+ *   table  device, float [positions][turned];  rates  device, double [turned/2]
+ * Errors: E_NULL, E_SHAPE, E_ALIGN, E_CUDA.
+ */
+tsvd_status_t tsvd_rotary_table(float* table, int positions, int turned, const double* rates, float amplitude, void* stream);
+
 /* tsvd_kv4_read -- the inverse: what the cache holds for those rows, into k and v (the numbers the codes stand for, as
  * TSVD_F32 or TSVD_BF16).  Arguments and errors as tsvd_kv4_append. */
 tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, void* v, long long ldv, tsvd_dtype_t dtype,
@@ -156,6 +259,19 @@ tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long ldq, void* 
                               tsvd_dtype_t dtype, const int* page_table, int max_pages, const int* seq_len,
                               const int* q_start, int n_seq, int n_rows, int max_q, int max_kv, float scale, int window,
                               unsigned flags, void* stream);
+
+/*
+ * tsvd_kv4_attend_sinks -- the same with the first `sinks` positions of a sequence exempt from the window: a row sees j < seq_len[s] with
+ *     j <= P_i                                 with TSVD_FLAG_CAUSAL
+ *     j >  P_i - window  or  j < sinks         where window > 0
+ * Without a window, sinks changes nothing; sinks = 0 is tsvd_kv4_attend.  With both, pages that hold none of the positions that
+ * the rows see are not looked at: they may be handed out again, their numbers in page_table be anything.
+ * Errors: those of tsvd_kv4_attend; E_SHAPE (sinks below 0).
+ */
+tsvd_status_t tsvd_kv4_attend_sinks(tsvd_kv4_t h, const void* q, long long ldq, void* out, long long ldo, int n_heads,
+                                    tsvd_dtype_t dtype, const int* page_table, int max_pages, const int* seq_len,
+                                    const int* q_start, int n_seq, int n_rows, int max_q, int max_kv, float scale, int window,
+                                    int sinks, unsigned flags, void* stream);
 
 tsvd_status_t tsvd_kv4_info(tsvd_kv4_t h, int* n_kv_heads, int* head_dim, int* page_tokens, long long* n_pages,
                             size_t* pool_bytes);

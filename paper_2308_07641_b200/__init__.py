@@ -12,7 +12,7 @@ from . import binding
 from .binding import (DTYPES, TSVD_BF16, TSVD_F32, TSVD_I8, TSVD_FLAG_OUT_F32,  # noqa: F401
                       TSVD_FLAG_PATH_DECODE, TSVD_FLAG_PATH_SIMPLE, TSVD_FLAG_PATH_TENSOR,
                       TSVD_FLAG_WIDE_X, TSVDError)
-from .serving import Int8Linear, KV4Cache, dequantize, quantize  # noqa: F401
+from .serving import Int8Linear, KV4Cache, LowRankAdapters, dequantize, quantize, rms_norm, rms_norm_quantize, rotary_table  # noqa: F401
 
 
 def device_activations(x_np, x_dtype: str):

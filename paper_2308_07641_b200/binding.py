@@ -36,6 +36,7 @@ TSVD_FLAG_WIDE_X = 0x200         # bf16 activations as four digits (outliers up 
 TSVD_FLAG_OUT_BF16 = 0x2         # tsvd_i8_forward: bf16 results
 TSVD_FLAG_CAUSAL = 0x4           # tsvd_kv4_attend
 TSVD_I8_MAX_N = 131071
+TSVD_ADAPTERS_MAX_RANK = 128
 
 DTYPES = {"f32": TSVD_F32, "bf16": TSVD_BF16, "i8": TSVD_I8}
 
@@ -46,7 +47,10 @@ EXPORTS = ("tsvd_pack", "tsvd_forward", "tsvd_forward_ex", "tsvd_forward_host", 
            # include/tsvd_serving.h
            "tsvd_quantize", "tsvd_dequantize", "tsvd_i8_pack", "tsvd_i8_forward", "tsvd_i8_reserve", "tsvd_i8_info",
            "tsvd_i8_last_status", "tsvd_i8_destroy", "tsvd_kv4_create", "tsvd_kv4_append", "tsvd_kv4_read",
-           "tsvd_kv4_attend", "tsvd_kv4_info", "tsvd_kv4_last_status", "tsvd_kv4_destroy")
+           "tsvd_kv4_attend", "tsvd_kv4_info", "tsvd_kv4_last_status", "tsvd_kv4_destroy",
+           "tsvd_rms_norm", "tsvd_kv4_append_rotated", "tsvd_rotary_table", "tsvd_kv4_attend_sinks",
+           "tsvd_adapters_create", "tsvd_adapters_set", "tsvd_adapters_forward", "tsvd_adapters_reserve", "tsvd_adapters_info",
+           "tsvd_adapters_last_status", "tsvd_adapters_destroy")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -129,14 +133,28 @@ def lib() -> ctypes.CDLL:
         L.tsvd_kv4_append.argtypes = [vp, vp, ll, vp, ll, ci, vp, ci, vp, vp, ci, ci, vp]
         L.tsvd_kv4_read.argtypes = [vp, vp, ll, vp, ll, ci, vp, ci, vp, vp, ci, ci, vp]
         L.tsvd_kv4_attend.argtypes = [vp, vp, ll, vp, ll, ci, ci, vp, ci, vp, vp, ci, ci, ci, ci, ctypes.c_float, ci, cu, vp]
+        L.tsvd_rms_norm.argtypes = [vp, ci, ll, ci, ll, vp, ll, vp, ll, vp, ci, ctypes.c_float, vp, ll, vp, ll, vp, vp]
+        L.tsvd_kv4_append_rotated.argtypes = [vp, vp, ll, vp, ll, ci, vp, ll, vp, ll, ci, vp, ci, ci, ci, vp, ci, vp, vp, ci, ci, vp]
+        L.tsvd_rotary_table.argtypes = [vp, ci, ci, vp, ctypes.c_float, vp]
+        L.tsvd_kv4_attend_sinks.argtypes = [vp, vp, ll, vp, ll, ci, ci, vp, ci, vp, vp, ci, ci, ci, ci, ctypes.c_float, ci, ci, cu, vp]
+        L.tsvd_adapters_create.argtypes = [ci, ci, ci, ci, ctypes.POINTER(vp)]
+        L.tsvd_adapters_set.argtypes = [vp, ci, vp, ll, vp, ll, ci, ci, ctypes.c_float, vp]
+        L.tsvd_adapters_forward.argtypes = [vp, vp, ll, vp, ci, vp, ll, vp, ll, ci, vp, vp, ci, ci, vp]
+        L.tsvd_adapters_reserve.argtypes = [vp, ci]
+        L.tsvd_adapters_info.argtypes = [vp] + [ctypes.POINTER(ci)] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
+        L.tsvd_adapters_last_status.argtypes = [vp]
+        L.tsvd_adapters_destroy.argtypes = [vp]
         L.tsvd_kv4_info.argtypes = [vp] + [ctypes.POINTER(ci)] * 3 + [ctypes.POINTER(ll), ctypes.POINTER(ctypes.c_size_t)]
         L.tsvd_kv4_last_status.argtypes = [vp]
         L.tsvd_kv4_destroy.argtypes = [vp]
         for f in ("quantize", "dequantize", "i8_pack", "i8_forward", "i8_reserve", "i8_info", "i8_last_status", "kv4_create",
-                  "kv4_append", "kv4_read", "kv4_attend", "kv4_info", "kv4_last_status"):
+                  "kv4_append", "kv4_read", "kv4_attend", "kv4_info", "kv4_last_status", "rms_norm", "kv4_append_rotated", "rotary_table",
+                  "kv4_attend_sinks", "adapters_create", "adapters_set", "adapters_forward", "adapters_reserve", "adapters_info",
+                  "adapters_last_status"):
             getattr(L, "tsvd_" + f).restype = ci
         L.tsvd_i8_destroy.restype = None
         L.tsvd_kv4_destroy.restype = None
+        L.tsvd_adapters_destroy.restype = None
         L.tsvd_strerror.argtypes = [ci]
         L.tsvd_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -376,6 +394,70 @@ def tsvd_kv4_attend(h: int, q_ptr: int, ldq: int, out_ptr: int, ldo: int, n_head
     _check(lib().tsvd_kv4_attend(h, q_ptr, ldq, out_ptr, ldo, n_heads, dtype, table_ptr, max_pages, seq_len_ptr,
                                  q_start_ptr or None, n_seq, n_rows, max_q, max_kv, scale, window, flags, stream or None),
            "tsvd_kv4_attend")
+
+
+def tsvd_adapters_create(N: int, M: int, max_rank: int, n_slots: int) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().tsvd_adapters_create(N, M, max_rank, n_slots, ctypes.byref(h)), "tsvd_adapters_create")
+    return h.value
+
+
+def tsvd_adapters_set(h: int, slot: int, A_ptr: int, lda: int, B_ptr: int, ldb: int, dtype: int, rank: int, scale: float,
+                      stream: int = 0) -> None:
+    _check(lib().tsvd_adapters_set(h, slot, A_ptr or None, lda, B_ptr or None, ldb, dtype, rank, scale, stream or None), "tsvd_adapters_set")
+
+
+def tsvd_adapters_forward(h: int, x_ptr: int, ldx: int, x_scale_ptr: int, dtype: int, base_ptr: int, ldb: int, out_ptr: int, ldo: int,
+                          out_dtype: int, slots_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, stream: int = 0) -> None:
+    _check(lib().tsvd_adapters_forward(h, x_ptr, ldx, x_scale_ptr or None, dtype, base_ptr or None, ldb, out_ptr, ldo, out_dtype, slots_ptr,
+                                       q_start_ptr or None, n_seq, n_rows, stream or None), "tsvd_adapters_forward")
+
+
+def tsvd_adapters_reserve(h: int, rows_max: int) -> None:
+    _check(lib().tsvd_adapters_reserve(h, rows_max), "tsvd_adapters_reserve")
+
+
+def tsvd_adapters_info(h: int) -> dict:
+    N, M, r, n, b = ctypes.c_int(), ctypes.c_int(), ctypes.c_int(), ctypes.c_int(), ctypes.c_size_t()
+    _check(lib().tsvd_adapters_info(h, ctypes.byref(N), ctypes.byref(M), ctypes.byref(r), ctypes.byref(n), ctypes.byref(b)),
+           "tsvd_adapters_info")
+    return {"N": N.value, "M": M.value, "max_rank": r.value, "n_slots": n.value, "bytes": b.value}
+
+
+def tsvd_adapters_last_status(h: int) -> int:
+    return int(lib().tsvd_adapters_last_status(h))
+
+
+def tsvd_adapters_destroy(h: int) -> None:
+    if _lib is not None and h:
+        lib().tsvd_adapters_destroy(h)
+
+
+def tsvd_kv4_attend_sinks(h: int, q_ptr: int, ldq: int, out_ptr: int, ldo: int, n_heads: int, dtype: int, table_ptr: int,
+                          max_pages: int, seq_len_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, max_q: int, max_kv: int,
+                          scale: float, window: int, sinks: int, flags: int, stream: int = 0) -> None:
+    _check(lib().tsvd_kv4_attend_sinks(h, q_ptr, ldq, out_ptr, ldo, n_heads, dtype, table_ptr, max_pages, seq_len_ptr, q_start_ptr or None,
+                                       n_seq, n_rows, max_q, max_kv, scale, window, sinks, flags, stream or None), "tsvd_kv4_attend_sinks")
+
+
+def tsvd_kv4_append_rotated(h: int, q_ptr: int, ldq: int, q_out_ptr: int, ldqo: int, n_heads: int, k_ptr: int, ldk: int, v_ptr: int,
+                            ldv: int, dtype: int, rotary_ptr: int, positions: int, turned: int, interleaved: int, table_ptr: int,
+                            max_pages: int, seq_len_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, stream: int = 0) -> None:
+    _check(lib().tsvd_kv4_append_rotated(h, q_ptr or None, ldq, q_out_ptr or None, ldqo, n_heads, k_ptr, ldk, v_ptr, ldv, dtype, rotary_ptr,
+                                         positions, turned, interleaved, table_ptr, max_pages, seq_len_ptr, q_start_ptr or None, n_seq,
+                                         n_rows, stream or None), "tsvd_kv4_append_rotated")
+
+
+def tsvd_rotary_table(table_ptr: int, positions: int, turned: int, rates_ptr: int, amplitude: float = 1.0, stream: int = 0) -> None:
+    _check(lib().tsvd_rotary_table(table_ptr, positions, turned, rates_ptr, amplitude, stream or None), "tsvd_rotary_table")
+
+
+def tsvd_rms_norm(x_ptr: int, dtype: int, rows: int, cols: int, ldx: int, residual_ptr: int, ldr: int, h_ptr: int, ldh: int,
+                  weight_ptr: int, weight_dtype: int, eps: float, y_ptr: int, ldy: int, q_ptr: int, ldq: int, scale_ptr: int,
+                  stream: int = 0) -> None:
+    """One of y_ptr and (q_ptr, scale_ptr); 0: not asked for."""
+    _check(lib().tsvd_rms_norm(x_ptr, dtype, rows, cols, ldx, residual_ptr or None, ldr, h_ptr or None, ldh, weight_ptr, weight_dtype, eps,
+                               y_ptr or None, ldy, q_ptr or None, ldq, scale_ptr or None, stream or None), "tsvd_rms_norm")
 
 
 def tsvd_kv4_info(h: int) -> dict:

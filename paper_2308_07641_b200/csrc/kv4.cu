@@ -12,14 +12,20 @@ namespace {
 constexpr float kMost = 65000.0f;   // the largest magnitude kept: 15 steps above -kMost still are an fp16 number
 
 // Where row `row` of the batch lives: its page and place, or page = -1 (with the status bit) when that is out of range.
-struct Place { int page, at; };
+struct Place {
+    int page, at;
+    int pos;             // its position in the sequence: below 0 if that is before its start
+    bool row;            // it belongs to a sequence
+};
 __device__ __forceinline__ Place place_of_row(const Kv4Geom& g, const Kv4Batch& b, int row, int* status)
 {
-    Place p{-1, 0};
+    Place p{-1, 0, 0, false};
     const int s = kv4_seq_of_row(b, row);
     if (s >= b.n_seq || row < kv4_first_row(b, s)) return p;   // behind the last sequence or before the first: not a row
     const int end = b.q_start ? b.q_start[s + 1] : row + 1;
     const long long pos = (long long)b.seq_len[s] - (end - row);
+    p.row = true;
+    p.pos = (int)max(pos, -1LL);
     if (pos >= 0 && pos < (long long)b.max_pages * g.page_tokens) {
         const unsigned at = (unsigned)pos, n = at / (unsigned)g.page_tokens;
         const int page = b.table[(long long)s * b.max_pages + n];
@@ -97,6 +103,43 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return y;
 }
 
+// Sixteen numbers, half a group, into the cache; the lane beside holds the other half.  Whole warps; `in`: the lane has numbers.
+template <int D>
+__device__ __forceinline__ void keep16(const Kv4Geom& g, const Place& at, const Item<D>& t, const Item<D>& t1, const float (&x)[16], bool in)
+{
+    const int pos = at.at & (KV4_BLOCK - 1);
+    float lo = fminf(x[0], x[1]), hi = fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) { lo = min3(lo, x[i], x[i + 1]); hi = max3(hi, x[i], x[i + 1]); }
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, 1));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, 1));
+    lo = fminf(fmaxf(lo, -kMost), kMost);
+    hi = fmaxf(fminf(hi, kMost), -kMost);
+    const __half step = __float2half_rn(__fmul_rn(hi - lo, 1.0f / 15.0f)), base = __float2half_rn(lo);
+    const float s = __half2float(step), m = __half2float(base);
+    const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+    uint32_t word[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        // nibble (e >> 1) + 4 (e & 1) holds number e: the even numbers are the lower half of the word
+        float half[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 7; e >= 0; --e) {
+            const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(x[8 * w + e], m), inv), 0.0f), 15.0f);
+            const float n = __fsub_rn(__fadd_rn(c, 12582912.0f), 12582912.0f);      // rounded to even
+            half[e & 1] = fmaf(half[e & 1], 16.0f, n);
+        }
+        // 2^23 + integer: the integer is in the low bits
+        word[w] = __byte_perm(__float_as_uint(half[0] + 8388608.0f), __float_as_uint(half[1] + 8388608.0f), 0x5410);
+    }
+    uint8_t* blk = g.block(at.page, t.head, at.at);
+    if (in) {
+        *reinterpret_cast<uint32_t*>(blk + t.codes(pos)) = word[0];
+        *reinterpret_cast<uint32_t*>(blk + t1.codes(pos)) = word[1];
+        if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + t.scales(pos)) = __halves2half2(step, base);
+    }
+}
+
 // A block takes a row; the rows of a call go into different positions, so no two blocks write the same bytes.  A thread takes
 // sixteen numbers, half a group.  The kernel is bound by its instructions, the half-rate integer and comparison ones above
 // all, so the codes are put together as floats: four codes are an exact fp32 integer below 2^16.  Issue slots 64% busy; three
@@ -117,7 +160,7 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* k, long long ldk, const T* v, 
     __syncthreads();
     const Place at = place_s;
     if (at.page < 0) return;
-    const int items = g.heads * (D / 8), pos = at.at & (KV4_BLOCK - 1);
+    const int items = g.heads * (D / 8);
     for (int u0 = threadIdx.x & ~31; u0 < items; u0 += blockDim.x) {
         const bool in = u0 + (int)(threadIdx.x & 31) < items;  // (whole warps take part in the exchange)
         const int u = in ? u0 + (int)(threadIdx.x & 31) : items - 1;
@@ -126,36 +169,149 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* k, long long ldk, const T* v, 
         float x[16];
         load8<T, VEC>(src, reinterpret_cast<float (&)[8]>(x[0]));
         load8<T, VEC>(src + 8, reinterpret_cast<float (&)[8]>(x[8]));
-        float lo = fminf(x[0], x[1]), hi = fmaxf(x[0], x[1]);
+        keep16<D>(g, at, t, t1, x, in);
+    }
+}
+
+// ---- append with the rotation ---------------------------------------------------------------------------------------------
+// Pairs (u, v) of a head's first `turned` numbers become (u cos - v sin, v cos + u sin), every product and sum rounded to fp32,
+// and go on in fp32: keys into the cache's codes, queries rounded once to their type.  The table holds, for each position, the
+// cosines of its turned / 2 angles and then their sines, so nothing here knows how the angles were chosen, and far positions
+// are as exact as near ones.
+struct Turn {
+    const float* table;      // [positions][turned]
+    int turned, positions;
+    int interleaved;         // pairs (2 i, 2 i + 1); else (i, i + turned / 2)
+};
+
+// Numbers d0 .. d0 + 15 of a head that begins at `head`, turned.  FAST: sixteen numbers are turned all or none, have their
+// partners in one piece, and cosines and sines may be read 16 bytes at a time.
+template <typename T, bool VEC, bool FAST>
+__device__ __forceinline__ void turn16(const T* head, int d0, const Turn& t, const float* cosines, float (&x)[16])
+{
+    load8<T, VEC>(head + d0, reinterpret_cast<float (&)[8]>(x[0]));
+    load8<T, VEC>(head + d0 + 8, reinterpret_cast<float (&)[8]>(x[8]));
+    if (d0 >= t.turned) return;
+    const int half = t.turned >> 1;
+    const float* sines = cosines + half;
+    if (t.interleaved) {
+        float c[8], s[8];
+        if constexpr (FAST) {
+            load8<float, true>(cosines + (d0 >> 1), c);
+            load8<float, true>(sines + (d0 >> 1), s);
+        } else {
 #pragma unroll
-        for (int i = 2; i < 16; i += 2) { lo = min3(lo, x[i], x[i + 1]); hi = max3(hi, x[i], x[i + 1]); }
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, 1));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, 1));
-        lo = fminf(fmaxf(lo, -kMost), kMost);
-        hi = fmaxf(fminf(hi, kMost), -kMost);
-        const __half step = __float2half_rn(__fmul_rn(hi - lo, 1.0f / 15.0f)), base = __float2half_rn(lo);
-        const float s = __half2float(step), m = __half2float(base);
-        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
-        uint32_t word[2];
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            // nibble (e >> 1) + 4 (e & 1) holds number e: the even numbers are the lower half of the word
-            float half[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int e = 7; e >= 0; --e) {
-                const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(x[8 * w + e], m), inv), 0.0f), 15.0f);
-                const float n = __fsub_rn(__fadd_rn(c, 12582912.0f), 12582912.0f);      // rounded to even
-                half[e & 1] = fmaf(half[e & 1], 16.0f, n);
+            for (int i = 0; i < 8; ++i) {
+                const bool in = (d0 >> 1) + i < half;
+                c[i] = in ? cosines[(d0 >> 1) + i] : 1.0f;
+                s[i] = in ? sines[(d0 >> 1) + i] : 0.0f;
             }
-            // 2^23 + integer: the integer is in the low bits
-            word[w] = __byte_perm(__float_as_uint(half[0] + 8388608.0f), __float_as_uint(half[1] + 8388608.0f), 0x5410);
         }
-        uint8_t* blk = g.block(at.page, t.head, at.at);
-        if (in) {
-            *reinterpret_cast<uint32_t*>(blk + t.codes(pos)) = word[0];
-            *reinterpret_cast<uint32_t*>(blk + t1.codes(pos)) = word[1];
-            if ((t.word & 3) == 0) *reinterpret_cast<__half2*>(blk + t.scales(pos)) = __halves2half2(step, base);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float u = x[2 * i], v = x[2 * i + 1];
+            if (FAST || (d0 >> 1) + i < half) {
+                x[2 * i] = __fsub_rn(__fmul_rn(u, c[i]), __fmul_rn(v, s[i]));
+                x[2 * i + 1] = __fadd_rn(__fmul_rn(v, c[i]), __fmul_rn(u, s[i]));
+            }
         }
+        return;
+    }
+    if constexpr (FAST) {
+        const bool lower = d0 < half;
+        const int at = lower ? d0 : d0 - half;
+        const float sign = lower ? -1.0f : 1.0f;
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
+            float o[8], c[8], s[8];
+            load8<T, VEC>(head + (lower ? d0 + half : at) + h, o);
+            load8<float, true>(cosines + at + h, c);
+            load8<float, true>(sines + at + h, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[h + i] = __fadd_rn(__fmul_rn(x[h + i], c[i]), sign * __fmul_rn(o[i], s[i]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int d = d0 + i;
+            if (d < t.turned) {
+                const bool lower = d < half;
+                const int at = lower ? d : d - half;
+                const float o = to_f32(head[lower ? d + half : at]);
+                const float p = __fmul_rn(o, sines[at]);
+                x[i] = __fadd_rn(__fmul_rn(x[i], cosines[at]), lower ? -p : p);
+            }
+        }
+    }
+}
+
+template <typename T, bool VEC, int D, bool FAST>
+__global__ void __launch_bounds__(512)
+kv4_append_rotated_kernel(Kv4Geom g, Kv4Batch b, Turn turn, const T* q, long long ldq, T* q_out, long long ldqo, int n_heads, const T* k,
+                          long long ldk, const T* v, long long ldv, int* status)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.x;
+    __shared__ Place place_s;
+    if (threadIdx.x < 32) {
+        Place p = place_of_row(g, b, row, status);
+        if (p.page >= 0 && p.pos >= turn.positions) {
+            p.page = -1;
+            if (threadIdx.x == 0) atomicOr(status, KV4_DEV_INDEX);
+        }
+        if (threadIdx.x == 0) place_s = p;
+    }
+    __syncthreads();
+    const Place at = place_s;
+    if (!at.row) return;
+    const int lane = threadIdx.x & 31, items = g.heads * (D / 8), q_items = n_heads * (D / 16);
+    const int kv_warps = (items + 31) / 32, warps = kv_warps + (q_items + 31) / 32;
+    const bool known = at.pos >= 0 && at.pos < turn.positions;
+    const float* cosines = turn.table + (size_t)(known ? at.pos : 0) * turn.turned;
+    for (int w = threadIdx.x >> 5; w < warps; w += blockDim.x >> 5) {
+        float x[16];
+        if (w < kv_warps) {
+            if (at.page < 0) continue;
+            const bool in = w * 32 + lane < items;             // (whole warps take part in the exchange)
+            const int u = in ? w * 32 + lane : items - 1;
+            const Item<D> t(2 * u, g.heads), t1(2 * u + 1, g.heads);
+            if (t.is_v) {
+                const T* src = v + row * ldv + t.head * D + t.word * 8;
+                load8<T, VEC>(src, reinterpret_cast<float (&)[8]>(x[0]));
+                load8<T, VEC>(src + 8, reinterpret_cast<float (&)[8]>(x[8]));
+            } else {
+                turn16<T, VEC, FAST>(k + row * ldk + t.head * D, t.word * 8, turn, cosines, x);
+            }
+            keep16<D>(g, at, t, t1, x, in);
+        } else {
+            const int u = (w - kv_warps) * 32 + lane;
+            if (u >= q_items) continue;
+            const int head = u / (D / 16), d0 = u % (D / 16) * 16;
+            if (known) {
+                turn16<T, VEC, FAST>(q + row * ldq + head * D, d0, turn, cosines, x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+            }
+            T* to = q_out + row * ldqo + head * D + d0;
+            store8<T, VEC>(to, reinterpret_cast<float (&)[8]>(x[0]));
+            store8<T, VEC>(to + 8, reinterpret_cast<float (&)[8]>(x[8]));
+        }
+    }
+}
+
+// cos and sin of position * rate, in 64 bits, kept in fp32.
+__global__ void rotary_table_kernel(float* table, int positions, int half, const double* rates, float amplitude)
+{
+    const long long n = (long long)positions * half;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const long long pos = i / half;
+        const int at = (int)(i - pos * half);
+        double s, c;
+        sincos((double)pos * rates[at], &s, &c);
+        table[pos * 2 * half + at] = (float)(c * amplitude);
+        table[pos * 2 * half + half + at] = (float)(s * amplitude);
     }
 }
 
@@ -292,6 +448,70 @@ extern "C" tsvd_status_t tsvd_kv4_append(tsvd_kv4_t h, const void* k, long long 
     return TSVD_OK;
 }
 
+extern "C" tsvd_status_t tsvd_kv4_append_rotated(tsvd_kv4_t h, const void* q, long long ldq, void* q_out, long long ldqo, int n_heads,
+                                                 const void* k, long long ldk, const void* v, long long ldv, tsvd_dtype_t dtype,
+                                                 const float* table, int positions, int turned, int interleaved, const int* page_table,
+                                                 int max_pages, const int* seq_len, const int* q_start, int n_seq, int n_rows, void* stream)
+{
+    const tsvd_status_t ok = check_batch(h, page_table, max_pages, seq_len, n_seq, n_rows, q_start);
+    if (ok != TSVD_OK) return ok;
+    const long long width = (long long)h->g.heads * h->g.dim, q_width = (long long)n_heads * h->g.dim;
+    if (n_heads < 0 || n_heads > 65535 || ldk < width || ldv < width || (n_heads && (ldq < q_width || ldqo < q_width))) return TSVD_E_SHAPE;
+    if (positions < 1 || turned < 2 || turned % 2 || turned > h->g.dim) return TSVD_E_SHAPE;
+    if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
+    if (n_rows == 0) return TSVD_OK;
+    if (!k || !v || !table || (n_heads && (!q || !q_out))) return TSVD_E_NULL;
+    if (n_heads && q == q_out) return TSVD_E_VALUE;
+    const size_t size = dtype == TSVD_F32 ? 4 : 2;
+    if (((uintptr_t)k | (uintptr_t)v | (n_heads ? (uintptr_t)q | (uintptr_t)q_out : 0)) & (size - 1)) return TSVD_E_ALIGN;
+    if ((uintptr_t)table & 3) return TSVD_E_ALIGN;
+    if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
+    const Kv4Batch b{page_table, max_pages, seq_len, q_start, n_seq, n_rows};
+    const Turn turn{table, turned, positions, interleaved != 0};
+    const bool vec = aligned16(k, ldk, size) && aligned16(v, ldv, size) && (!n_heads || (aligned16(q, ldq, size) && aligned16(q_out, ldqo, size)));
+    // (neighbours: eight angles of an item; halves: sixteen)
+    const bool fast = ((uintptr_t)table & 15) == 0 && turned % (interleaved ? 16 : 32) == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    const long long items = (long long)(h->g.heads * (h->g.dim / 8) + 31) / 32 + ((long long)n_heads * (h->g.dim / 16) + 31) / 32;
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto kernel, auto* kp) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
+        PdlLaunch l((unsigned)n_rows, (unsigned)(items > 16 ? 16 : items) * 32, 0, st);
+        e = cudaLaunchKernelEx(&l.cfg, kernel, h->g, b, turn, (const T*)q, ldq, (T*)q_out, ldqo, n_heads, kp, ldk, (const T*)v, ldv, h->dev_status);
+    };
+    auto by_type = [&](auto* kp) {
+        using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
+        if (h->g.dim == 128) {
+            if (vec && fast) go(kv4_append_rotated_kernel<T, true, 128, true>, kp);
+            else if (vec) go(kv4_append_rotated_kernel<T, true, 128, false>, kp);
+            else if (fast) go(kv4_append_rotated_kernel<T, false, 128, true>, kp);
+            else go(kv4_append_rotated_kernel<T, false, 128, false>, kp);
+        } else {
+            if (vec && fast) go(kv4_append_rotated_kernel<T, true, 64, true>, kp);
+            else if (vec) go(kv4_append_rotated_kernel<T, true, 64, false>, kp);
+            else if (fast) go(kv4_append_rotated_kernel<T, false, 64, true>, kp);
+            else go(kv4_append_rotated_kernel<T, false, 64, false>, kp);
+        }
+    };
+    if (dtype == TSVD_F32) by_type((const float*)k);
+    else by_type((const __nv_bfloat16*)k);
+    TSVD_CUDA_OK(e);
+    tsvd_count_launch();
+    return TSVD_OK;
+}
+
+extern "C" tsvd_status_t tsvd_rotary_table(float* table, int positions, int turned, const double* rates, float amplitude, void* stream)
+{
+    if (positions < 1 || turned < 2 || turned % 2) return TSVD_E_SHAPE;
+    if (!table || !rates) return TSVD_E_NULL;
+    if (((uintptr_t)table & 3) || ((uintptr_t)rates & 7)) return TSVD_E_ALIGN;
+    const long long n = (long long)positions * (turned / 2), blocks = (n + 255) / 256;
+    rotary_table_kernel<<<(unsigned)(blocks > 148 * 8 ? 148 * 8 : blocks), 256, 0, (cudaStream_t)stream>>>(table, positions, turned / 2, rates, amplitude);
+    TSVD_CUDA_OK(cudaGetLastError());
+    tsvd_count_launch();
+    return TSVD_OK;
+}
+
 extern "C" tsvd_status_t tsvd_kv4_read(tsvd_kv4_t h, void* k, long long ldk, void* v, long long ldv, tsvd_dtype_t dtype,
                                        const int* page_table, int max_pages, const int* seq_len, const int* q_start, int n_seq,
                                        int n_rows, void* stream)
@@ -337,11 +557,20 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
                                          const int* q_start, int n_seq, int n_rows, int max_q, int max_kv, float scale, int window,
                                          unsigned flags, void* stream)
 {
+    return tsvd_kv4_attend_sinks(h, q, ldq, out, ldo, n_heads, dtype, page_table, max_pages, seq_len, q_start, n_seq, n_rows, max_q, max_kv,
+                                 scale, window, 0, flags, stream);
+}
+
+extern "C" tsvd_status_t tsvd_kv4_attend_sinks(tsvd_kv4_t h, const void* q, long long ldq, void* out, long long ldo, int n_heads,
+                                               tsvd_dtype_t dtype, const int* page_table, int max_pages, const int* seq_len,
+                                               const int* q_start, int n_seq, int n_rows, int max_q, int max_kv, float scale, int window,
+                                               int sinks, unsigned flags, void* stream)
+{
     const tsvd_status_t ok = check_batch(h, page_table, max_pages, seq_len, n_seq, n_rows, q_start);
     if (ok != TSVD_OK) return ok;
     if (n_heads < 1 || n_heads % h->g.heads || n_heads > 65535) return TSVD_E_SHAPE;
     const long long width = (long long)n_heads * h->g.dim;
-    if (ldq < width || ldo < width || max_q < 1 || max_kv < 0 || window < 0 || !(scale == scale)) return TSVD_E_SHAPE;
+    if (ldq < width || ldo < width || max_q < 1 || max_kv < 0 || window < 0 || sinks < 0 || !(scale == scale)) return TSVD_E_SHAPE;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (flags & ~(TSVD_FLAG_CAUSAL | TSVD_FLAG_PATH_SIMPLE | TSVD_FLAG_TEST_STALL)) return TSVD_E_DTYPE;
     if (n_rows == 0) return TSVD_OK;
@@ -362,6 +591,7 @@ extern "C" tsvd_status_t tsvd_kv4_attend(tsvd_kv4_t h, const void* q, long long 
     a.max_kv = (int)(max_kv && max_kv < room ? max_kv : room < 0x7fffffffLL ? room : 0x7fffffffLL);
     a.scale = scale;
     a.window = window;
+    a.sinks = window ? sinks : 0;
     a.causal = flags & TSVD_FLAG_CAUSAL;
     a.test_stall = flags & TSVD_FLAG_TEST_STALL;
     a.stream = (cudaStream_t)stream;

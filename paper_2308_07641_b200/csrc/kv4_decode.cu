@@ -64,6 +64,7 @@ struct DecParams {
     int max_q;
     float c;             // scale * log2(e)
     int window, causal;
+    int sinks;           // (with SINKS) first positions that the window does not hide
     int test_stall;      // test hook: no unit is ever copied, so the waits must give up
     int stages;          // units of a warp's ring
     int keep_cols;       // query rows of an item that can hold anything: what is kept of a part
@@ -123,12 +124,14 @@ struct alignas(4 * WORDS) Words { uint32_t w[WORDS]; };
 struct Seq {
     int rows, len, first, items, unit0, units;  // units of one item; unit0: its first, counted from position 0
     int all;                                    // its rows, those beyond max_q (which are not computed) included
+    int front;                                  // (SINKS) units 0 .. front-1 are the cache's first; unit u >= front is its unit0 + u
+    int lo;                                     // (SINKS) positions from `sinks` up to it are seen by no row
 };
 
-template <int ROWS>
+template <int ROWS, bool SINKS>
 __device__ __forceinline__ Seq load_seq(const DecParams& p, int s)
 {
-    Seq q{0, 0, 0, 0, 0, 0, 0};
+    Seq q{0, 0, 0, 0, 0, 0, 0, 0, 0};
     if (s >= p.b.n_seq) return q;
     q.first = kv4_first_row(p.b, s);
     q.all = kv4_first_row(p.b, s + 1) - q.first;
@@ -143,6 +146,18 @@ __device__ __forceinline__ Seq load_seq(const DecParams& p, int s)
     if (p.window) lo = max(0LL, pos0 - p.window + 1);
     if (p.causal) hi = min(hi, pos0 + q.rows);
     q.items = p.g.heads * ((q.rows * p.group + ROWS - 1) / ROWS);
+    if constexpr (SINKS) {
+        // what lies between the first positions and the window is left out, where that is a unit or more
+        const long long front = (min((long long)p.sinks, hi) + DEC_UNIT - 1) / DEC_UNIT, ends = (hi + DEC_UNIT - 1) / DEC_UNIT;
+        const long long from = min(lo / DEC_UNIT, ends);
+        if (front < from) {
+            q.front = (int)front;
+            q.unit0 = (int)(from - front);
+        }
+        q.units = max(1, (int)ends - q.unit0);
+        q.lo = (int)lo;
+        return q;
+    }
     q.unit0 = (int)(lo / DEC_UNIT);
     q.units = hi > lo ? (int)((hi + DEC_UNIT - 1) / DEC_UNIT) - q.unit0 : 1;   // an item that sees nothing still writes zeros
     return q;
@@ -154,6 +169,7 @@ struct Item {
     int head, row0;            // the pairs row0 .. are this item's
     int len, pos0;             // positions that can be seen at all; position of the sequence's first row
     int at0, unit0, unit1, units;    // position of its unit 0; units [unit0, unit1) of `units` are the warp's
+    int front;                 // (SINKS) units below it count from position 0
     long long u0;              // where the item begins in the call's list of units
 };
 
@@ -180,7 +196,7 @@ struct Feed {
     long long item_u0, run_u0, u1;
 };
 
-template <int D, int NT>
+template <int D, int NT, bool SINKS>
 __global__ void __launch_bounds__(kWarps<NT> * 32, 1)
 kv4_decode_kernel(const DecParams p)
 {
@@ -214,8 +230,8 @@ kv4_decode_kernel(const DecParams p)
     // ---- the warp's run of units ----
     long long total = 0;
     int total_items = 0, most = 0;
-    Seq mine = load_seq<ROWS>(p, lane);
-    for (int s0 = 0;; mine = load_seq<ROWS>(p, s0 + lane)) {
+    Seq mine = load_seq<ROWS, SINKS>(p, lane);
+    for (int s0 = 0;; mine = load_seq<ROWS, SINKS>(p, s0 + lane)) {
         total += (long long)mine.items * mine.units;
         total_items += mine.items;
         most = max(most, mine.units);
@@ -239,9 +255,9 @@ kv4_decode_kernel(const DecParams p)
         const unsigned each = n / WARPS, over = n % WARPS;
         const long long u0 = c0 + each * (unsigned)warp + min((unsigned)warp, over), u1 = u0 + each + ((unsigned)warp < over);
         long long before = 0;
-        if (p.b.n_seq > 32) mine = load_seq<ROWS>(p, lane);
+        if (p.b.n_seq > 32) mine = load_seq<ROWS, SINKS>(p, lane);
         if (u0 < u1)
-            for (int s0 = 0; s0 < p.b.n_seq; mine = load_seq<ROWS>(p, s0 + lane)) {
+            for (int s0 = 0; s0 < p.b.n_seq; mine = load_seq<ROWS, SINKS>(p, s0 + lane)) {
                 const int span = apart ? share : mine.units;
                 const long long have = (long long)mine.items * span;
                 long long scan = have;
@@ -276,8 +292,10 @@ kv4_decode_kernel(const DecParams p)
     const uint8_t* ptr = nullptr;        // the next block, null where its page number is out of range
     int in_page = 0, in_item = 0;        // blocks left in the page, units left in the warp's share of the item
     int next_page = 0, pushed = 0;       // a page number is asked for one page ahead
+    int to_front = -1;                   // (SINKS) units left before the step over what the window hides
     uint32_t there = 0;                  // two bits a slot: which of its blocks are in range
-    auto ask_page = [&](int at) {        // -2: no such position
+    auto ask_page = [&](int at) {        // -2: no such position, or (SINKS) none that is seen
+        if (SINKS && (long long)at * p.g.page_tokens >= p.sinks && (long long)(at + 1) * p.g.page_tokens <= f.q.lo) return -2;
         return at < p.b.max_pages && (long long)at * p.g.page_tokens < f.q.len ? p.b.table[(long long)f.s * p.b.max_pages + at] : -2;
     };
     auto open_page = [&](int page, int in) {
@@ -300,7 +318,7 @@ kv4_decode_kernel(const DecParams p)
             f.item_u0 += span;
             if (f.item_u0 < f.u1 && ++f.item == f.q.items) {
                 f.item = 0;
-                do f.q = load_seq<ROWS>(p, ++f.s); while (f.q.items == 0 && f.s < p.b.n_seq);
+                do f.q = load_seq<ROWS, SINKS>(p, ++f.s); while (f.q.items == 0 && f.s < p.b.n_seq);
                 if (f.q.items == 0) f.u1 = 0;                  // only if the lengths changed meanwhile
             }
         }
@@ -308,7 +326,7 @@ kv4_decode_kernel(const DecParams p)
         const long long run_u0 = f.run_u0, item_u0 = f.item_u0, u1 = f.u1;
         const int unit0 = (int)max(0LL, run_u0 - item_u0), unit1 = (int)min((long long)f.q.units, u1 - item_u0);
         if (item_u0 >= u1 || unit0 >= unit1) return false;     // (unit0 >= unit1: an item apart, shorter than the block's share)
-        const int blk = (f.q.unit0 + unit0) * 2;
+        const int blk = (SINKS && unit0 < f.q.front ? unit0 : f.q.unit0 + unit0) * 2;
         if (lane == 0) {
             Item& it = queue[warp][pushed % DEC_QUEUE];
             it.first_row = f.q.first;
@@ -321,12 +339,14 @@ kv4_decode_kernel(const DecParams p)
             it.unit0 = unit0;
             it.unit1 = unit1;
             it.units = f.q.units;
+            if constexpr (SINKS) it.front = f.q.front;
             it.u0 = item_u0;
             f.page_at = blk / per_page;
         }
         __syncwarp();
         ++pushed;
         in_item = unit1 - unit0;
+        if constexpr (SINKS) to_front = unit0 < f.q.front ? f.q.front - unit0 : -1;
         open_page(ask_page(blk / per_page), blk % per_page);
         return true;
     };
@@ -335,6 +355,13 @@ kv4_decode_kernel(const DecParams p)
     // finite) and hidden.
     auto feed = [&](int st) {
         if (!more || (in_item == 0 && !(more = next_item()))) return;
+        if (SINKS && to_front-- == 0) {
+            const int blk = (f.q.unit0 + f.q.front) * 2;
+            __syncwarp();
+            if (lane == 0) f.page_at = blk / per_page;
+            __syncwarp();
+            open_page(ask_page(blk / per_page), blk % per_page);
+        }
         if (in_page == 0) turn_page();
         const uint8_t *a = ptr, *b;
         const bool joined = in_page >= 2;
@@ -465,7 +492,7 @@ kv4_decode_kernel(const DecParams p)
         for (int u = it.unit0; u < it.unit1; ++u) {
             if (!(ok = mbar_wait_warp(&full[warp][stage], phase, ctl))) break;
             const uint8_t* unit = ring + (size_t)(warp * p.stages + stage) * UNIT;
-            const int at = it.at0 + u * DEC_UNIT, here = (int)(there >> (2 * stage) & 3u);
+            const int at = (SINKS && u < it.front ? 0 : it.at0) + u * DEC_UNIT, here = (int)(there >> (2 * stage) & 3u);
             // rows r and r + 8 of a block's score tile are its positions kr and kr + 8
             const int kr = (r >> 1) + 4 * (r & 1);
             float sc[2][NT][4];
@@ -504,7 +531,7 @@ kv4_decode_kernel(const DecParams p)
                     for (int k = 0; k < 4; ++k) sc[h][t][k] = fmaf(part[t][k], 16384.0f, d[k]);      // 2^(24 - 10)
                 }
             }
-            if (at < all_lo || at + DEC_UNIT > all_hi || here != 3) {
+            if ((at < all_lo && (!SINKS || at + DEC_UNIT > p.sinks)) || at + DEC_UNIT > all_hi || here != 3) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -513,7 +540,7 @@ kv4_decode_kernel(const DecParams p)
                         for (int k = 0; k < 4; ++k) {
                             const int pos = at + h * KV4_BLOCK + kr + (k & 2 ? 8 : 0);
                             // hidden whatever the scale's sign: the product below has to be -inf
-                            if (pos < lo[t][k & 1] || pos >= hi[t][k & 1] || !(here >> h & 1)) sc[h][t][k] = cmul[t][k & 1] < 0.0f ? INFINITY : -INFINITY;
+                            if ((pos < lo[t][k & 1] && (!SINKS || pos >= p.sinks)) || pos >= hi[t][k & 1] || !(here >> h & 1)) sc[h][t][k] = cmul[t][k & 1] < 0.0f ? INFINITY : -INFINITY;
                         }
             }
             float e[2][NT][4];
@@ -773,7 +800,7 @@ kv4_decode_kernel(const DecParams p)
     }
 }
 
-template <int D, int NT>
+template <int D, int NT, bool SINKS>
 tsvd_status_t launch(DecParams p, long long items, long long units_most, cudaStream_t st)
 {
     constexpr size_t kRoom = 227 * 1024 - DEC_STATIC;          // beside what the kernel declares itself
@@ -782,9 +809,16 @@ tsvd_status_t launch(DecParams p, long long items, long long units_most, cudaStr
     p.stages = (int)std::min<size_t>(DEC_MAX_STAGES, (kRoom - 128 - kept) / unit);
     const long long blocks = std::min((long long)p.sms, std::max(items, (units_most + kWarps<NT> - 1) / kWarps<NT>));
     PdlLaunch l((unsigned)blocks, kWarps<NT> * 32, 128 + kept + p.stages * unit, st);
-    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_decode_kernel<D, NT>, p));
+    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_decode_kernel<D, NT, SINKS>, p));
     tsvd_count_launch();
     return TSVD_OK;
+}
+
+template <bool SINKS>
+tsvd_status_t launch_dim(const DecParams& p, bool two, long long items, long long most, cudaStream_t st)
+{
+    if (p.g.dim == 128) return two ? launch<128, 2, SINKS>(p, items, most, st) : launch<128, 1, SINKS>(p, items, most, st);
+    return two ? launch<64, 2, SINKS>(p, items, most, st) : launch<64, 1, SINKS>(p, items, most, st);
 }
 
 constexpr int kRowsMost = 16;      // rows of an item: 8 or 16
@@ -797,10 +831,11 @@ size_t kv4_decode_tickets(int sms) { return (size_t)sms; }
 tsvd_status_t kv4_decode_prepare()
 {
     const int most = 227 * 1024 - DEC_STATIC;
-    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
-    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<64, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
-    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
-    TSVD_CUDA_OK((cudaFuncSetAttribute(kv4_decode_kernel<64, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
+    for (const void* kernel : {(const void*)kv4_decode_kernel<128, 1, false>, (const void*)kv4_decode_kernel<64, 1, false>,
+                               (const void*)kv4_decode_kernel<128, 2, false>, (const void*)kv4_decode_kernel<64, 2, false>,
+                               (const void*)kv4_decode_kernel<128, 1, true>, (const void*)kv4_decode_kernel<64, 1, true>,
+                               (const void*)kv4_decode_kernel<128, 2, true>, (const void*)kv4_decode_kernel<64, 2, true>})
+        TSVD_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     return TSVD_OK;
 }
 
@@ -818,6 +853,7 @@ tsvd_status_t kv4_attend_decode(const AttendArgs& a)
     // (a scale of 0 is a tiny one: hidden positions become -inf through the product with it)
     p.c = fabsf(a.scale) < 1e-18f ? 1e-18f : a.scale * 1.4426950408889634f;
     p.window = a.window;
+    p.sinks = a.sinks;
     p.causal = a.causal;
     p.test_stall = a.test_stall;
     p.parts = a.h->parts;
@@ -829,6 +865,5 @@ tsvd_status_t kv4_attend_decode(const AttendArgs& a)
     p.keep_cols = (int)std::min<long long>(rows, two ? 16 : 8);
     const long long items = (long long)a.b.n_seq * p.g.heads * ((rows + (two ? 15 : 7)) / (two ? 16 : 8));
     const long long most = items * (((long long)a.max_kv + DEC_UNIT - 1) / DEC_UNIT + 1);
-    if (p.g.dim == 128) return two ? launch<128, 2>(p, items, most, a.stream) : launch<128, 1>(p, items, most, a.stream);
-    return two ? launch<64, 2>(p, items, most, a.stream) : launch<64, 1>(p, items, most, a.stream);
+    return a.sinks ? launch_dim<true>(p, two, items, most, a.stream) : launch_dim<false>(p, two, items, most, a.stream);
 }

@@ -60,6 +60,7 @@ struct PreParams {
     float c;
     float sign;              // of the scale: goes into q
     int window, causal;
+    int sinks;               // (with SINKS) first positions that the window does not hide
     int test_stall;          // test hook: no position is ever copied, so the waits must give up
     int splits;              // blocks that share a pair's positions; above 1 they leave their parts in `parts`
     float* parts;            // [block][2 * PRE_ROWS][D] sums, [2 * PRE_ROWS] (reference, sum)
@@ -210,7 +211,7 @@ struct Layout {
     static constexpr int kBytes = kStg + kStages * kPacked;
 };
 
-template <int D>
+template <int D, bool SINKS>
 __global__ void __launch_bounds__(PRE_THREADS, 1)
 kv4_prefill_kernel(const PreParams p)
 {
@@ -275,9 +276,27 @@ kv4_prefill_kernel(const PreParams p)
         const int r0 = row_base + x * PRE_ROWS, r1 = min(r0 + PRE_ROWS, n_rows) - 1;
         t_lo[x] = t_hi[x] = 0;
         const int lo = token_lo(r0 / p.group), hi = token_hi(r1 / p.group);
-        if (r1 >= r0 && hi > lo) {
+        if (r1 >= r0 && hi > (SINKS ? 0 : lo)) {
             t_lo[x] = lo / PRE_STEP;
             t_hi[x] = (hi + PRE_STEP - 1) / PRE_STEP;
+        }
+    }
+    // With first positions that stay visible, the pair's tiles [0, front) and those from its window's first on are counted as one
+    // run: what is left out between them, `gap` tiles, is added where a tile becomes positions.  Both row tiles take the run from
+    // its start (the steps that only the other one's window holds are hidden row by row).
+    int front = 0, gap = 0;
+    if constexpr (SINKS) {
+        const int ends = max(t_hi[0], t_hi[1]);
+        int from = ends;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (t_hi[x] > 0) from = min(from, t_lo[x]);
+        front = (int)((min((long long)p.sinks, (long long)ends * PRE_STEP) + PRE_KEYS - 1) / PRE_KEYS);
+        gap = max(0, from / 2 - front);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            t_lo[x] = 0;
+            t_hi[x] = min(t_hi[x], max(2 * front, t_hi[x] - 2 * gap));
         }
     }
     const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
@@ -353,7 +372,7 @@ kv4_prefill_kernel(const PreParams p)
         bool ok = true;
         const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
         for (int k = a; k < b; ++k) {
-            const int h = k & 1, at = k * PRE_STEP;
+            const int h = k & 1, at = (SINKS && k >= 2 * front ? k + 2 * gap : k) * PRE_STEP;
             ok = mbar_wait(&s_full[x][h], phs >> h & 1, ctl);   // (the warp agrees on it where it looks at `over`)
             phs ^= 1u << h;
             tc_fence_after_sync();
@@ -362,7 +381,7 @@ kv4_prefill_kernel(const PreParams p)
             tmem_ld32(t_s, v[0]);
             tmem_ld32(t_s + 32, v[1]);
             const uint32_t hide = hidden[(k >> 1) % PRE_HIDE] >> (4 * h) & 15;
-            const bool edge = at < all_lo || at + PRE_STEP > all_hi || hide;
+            const bool edge = (at < all_lo && (!SINKS || at + PRE_STEP > p.sinks)) || at + PRE_STEP > all_hi || hide;
             tmem_ld_wait();
             if (edge) {
 #pragma unroll
@@ -370,7 +389,7 @@ kv4_prefill_kernel(const PreParams p)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const int pos = at + 32 * c + i;
-                        if (pos < lo || pos >= hi || (hide >> (2 * c + (i >> 4)) & 1)) v[c][i] = 0xff800000u;
+                        if ((pos < lo && (!SINKS || pos >= p.sinks)) || pos >= hi || (hide >> (2 * c + (i >> 4)) & 1)) v[c][i] = 0xff800000u;
                     }
             }
             float m[4];
@@ -626,9 +645,11 @@ kv4_prefill_kernel(const PreParams p)
         uint32_t ph = 0;
         bool ok = !p.test_stall;
         for (int k = k_lo; k < k_hi && ok; ++k) {
-            const int blk = k * (PRE_KEYS / KV4_BLOCK) + (lane & 7);
+            const int blk = (SINKS && k >= front ? k + gap : k) * (PRE_KEYS / KV4_BLOCK) + (lane & 7);
             const uint8_t* src = nullptr;
-            if ((long long)blk * KV4_BLOCK < len_in) {
+            // (with SINKS, blocks that no row of the pair sees may lie in pages that are gone)
+            const bool seen = !SINKS || blk * KV4_BLOCK < p.sinks || blk * KV4_BLOCK + KV4_BLOCK > token_lo(row_base / p.group);
+            if (seen && (long long)blk * KV4_BLOCK < len_in) {
                 const int page = p.b.table[(long long)s * p.b.max_pages + blk / per_page];
                 if (page >= 0 && page < p.g.n_pages) src = p.g.block(page, head, blk % per_page * KV4_BLOCK);
                 else if (lane < 8) atomicOr(p.status, KV4_DEV_INDEX);
@@ -716,13 +737,13 @@ kv4_join_kernel(const PreParams p)
     }
 }
 
-template <int D>
+template <int D, bool SINKS>
 tsvd_status_t launch(const PreParams& p, cudaStream_t st)
 {
     const long long blocks = (long long)p.tiles * p.g.heads * p.b.n_seq * p.splits;
     if (blocks > 0x7fffffffLL) return TSVD_E_TOOBIG;
     PdlLaunch l((unsigned)blocks, PRE_THREADS, Layout<D>::kBytes + 1024, st);
-    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_prefill_kernel<D>, p));
+    TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, kv4_prefill_kernel<D, SINKS>, p));
     tsvd_count_launch();
     if (p.splits > 1) {
         PdlLaunch j((unsigned)(blocks / p.splits * (2 * PRE_ROWS / JOIN_ROWS)), 256, 0, st);
@@ -738,8 +759,10 @@ size_t kv4_prefill_parts_bytes(int sms, int dim) { return sizeof(float) * (size_
 
 tsvd_status_t kv4_prefill_prepare()
 {
-    TSVD_CUDA_OK(cudaFuncSetAttribute(kv4_prefill_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<128>::kBytes + 1024));
-    TSVD_CUDA_OK(cudaFuncSetAttribute(kv4_prefill_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<64>::kBytes + 1024));
+    for (const void* kernel : {(const void*)kv4_prefill_kernel<128, false>, (const void*)kv4_prefill_kernel<128, true>})
+        TSVD_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<128>::kBytes + 1024));
+    for (const void* kernel : {(const void*)kv4_prefill_kernel<64, false>, (const void*)kv4_prefill_kernel<64, true>})
+        TSVD_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<64>::kBytes + 1024));
     return TSVD_OK;
 }
 
@@ -759,6 +782,7 @@ tsvd_status_t kv4_attend_prefill(const AttendArgs& a)
     p.c = std::max(fabsf(a.scale) * 1.4426950408889634f, 1e-18f);
     p.sign = a.scale < 0.0f ? -1.0f : 1.0f;
     p.window = a.window;
+    p.sinks = a.sinks;
     p.causal = a.causal;
     p.test_stall = a.test_stall;
     p.status = a.h->dev_status;
@@ -768,7 +792,8 @@ tsvd_status_t kv4_attend_prefill(const AttendArgs& a)
     // heads after 1000 (two blocks): 22.1 and 22.2.
     const long long jobs = (long long)p.tiles * p.g.heads * p.b.n_seq;
     long long seen = a.max_kv;
-    if (a.window) seen = std::min<long long>(seen, (long long)a.window + 2 * PRE_ROWS / p.group + 1);
+    if (a.window) seen = std::min<long long>(seen, (long long)a.window + 2 * PRE_ROWS / p.group + 1 + a.sinks);
     p.splits = (int)std::max(1LL, std::min(a.h->sms / jobs, seen / (4 * PRE_KEYS)));
-    return p.g.dim == 128 ? launch<128>(p, a.stream) : launch<64>(p, a.stream);
+    if (a.sinks) return p.g.dim == 128 ? launch<128, true>(p, a.stream) : launch<64, true>(p, a.stream);
+    return p.g.dim == 128 ? launch<128, false>(p, a.stream) : launch<64, false>(p, a.stream);
 }

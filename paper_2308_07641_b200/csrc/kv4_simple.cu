@@ -38,7 +38,7 @@ __device__ __forceinline__ float code_dot(const uint8_t* blk, int pos, const flo
 template <typename T, int D>
 __global__ void __launch_bounds__(SIMPLE_WARPS * 32)
 kv4_attend_simple_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ q, long long ldq, T* __restrict__ out, long long ldo, int group,
-                         int max_q, float scale, int window, int causal, int* status)
+                         int max_q, float scale, int window, int sinks, int causal, int* status)
 {
     constexpr int PER = D / 32;               // numbers of the head that a lane sums
     __shared__ float qs[D];
@@ -56,18 +56,21 @@ kv4_attend_simple_kernel(Kv4Geom g, Kv4Batch b, const T* __restrict__ q, long lo
     if (len > room && threadIdx.x == 0) atomicOr(status, KV4_DEV_INDEX);
     const long long pos = (long long)len - (last - row);
     const long long hi = causal ? (pos + 1 < len_in ? pos + 1 : len_in) : len_in;   // sees [lo, hi)
-    const long long lo = window && pos - window + 1 > 0 ? pos - window + 1 : 0;
+    const long long lo = window && pos - window + 1 > 0 ? pos - window + 1 : 0;   // and [0, sinks) below hi
+    // runs of 32 positions: those of the first positions, then from the window's on
+    const long long runs = (hi + 31) / 32, first_runs = ((sinks < hi ? sinks : hi) + 31) / 32;
+    const long long gap = lo / 32 > first_runs ? lo / 32 - first_runs : 0;
     for (int d = threadIdx.x; d < D; d += blockDim.x) qs[d] = to_f32(q[row * ldq + (long long)head * D + d]) * scale;
     __syncthreads();
 
     float top = -INFINITY, sum = 0.0f, acc[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
-    for (long long j0 = lo / 32 * 32 + warp * 32; j0 < hi; j0 += SIMPLE_WARPS * 32) {
-        const long long j = j0 + lane;
+    for (long long run = warp; run < first_runs || run + gap < runs; run += SIMPLE_WARPS) {
+        const long long j0 = (run < first_runs ? run : run + gap) * 32, j = j0 + lane;
         float score = -INFINITY;
         const uint8_t* blk = nullptr;
-        if (j >= lo && j < hi) {
+        if ((j >= lo || j < sinks) && j < hi) {
             const int page = b.table[(long long)s * b.max_pages + j / g.page_tokens];
             if (page >= 0 && page < g.n_pages) {
                 blk = g.block(page, kvh, (int)(j % g.page_tokens));
@@ -128,7 +131,7 @@ template <typename T, int D>
 void launch(const AttendArgs& a)
 {
     kv4_attend_simple_kernel<T, D><<<dim3((unsigned)a.b.n_rows, (unsigned)a.n_heads), SIMPLE_WARPS * 32, 0, a.stream>>>(
-        a.h->g, a.b, (const T*)a.q, a.ldq, (T*)a.out, a.ldo, a.n_heads / a.h->g.heads, a.max_q, a.scale, a.window, a.causal, a.h->dev_status);
+        a.h->g, a.b, (const T*)a.q, a.ldq, (T*)a.out, a.ldo, a.n_heads / a.h->g.heads, a.max_q, a.scale, a.window, a.sinks, a.causal, a.h->dev_status);
 }
 
 }  // namespace

@@ -130,6 +130,7 @@ struct AttendArgs {
     int max_q, max_kv;
     float scale;
     int window;
+    int sinks;             // first positions that the window does not hide; 0 without a window
     bool causal;
     bool test_stall;       // TSVD_FLAG_TEST_STALL
     cudaStream_t stream;

@@ -91,6 +91,76 @@ def dequantize(q, scale, dtype=None):
     return y
 
 
+def _norm(x, weight, eps: float, residual, what: str):
+    """What the two norms check alike: (rows, cols, ldx, dtype code, stream, residual's pointer and stride, h or None)."""
+    rows, cols, ldx = _rows(x, what)
+    code = _code(x.dtype, what)
+    _code(weight.dtype, what)
+    if weight.shape != (cols,) or not weight.is_contiguous() or not weight.is_cuda:
+        raise TSVDError(binding.TSVD_E_SHAPE, what)
+    r = ldr = 0
+    h = None
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise TSVDError(binding.TSVD_E_DTYPE if residual.dtype != x.dtype else binding.TSVD_E_SHAPE, what)
+        ldr = _rows(residual, what)[2]
+        r = residual.data_ptr()
+    stream = _stream(what, x, weight, residual)
+    if residual is not None:
+        h = _empty((rows, cols), (cols, 1), dtype=x.dtype, device=x.device)
+    return rows, cols, ldx, code, stream, r, ldr, h
+
+
+def rms_norm(x, weight, eps: float = 1e-6, residual=None):
+    """Root-mean-square norm of rows: x float32 or bfloat16 [rows, cols] (row stride >= cols), weight float32 or bfloat16 [cols].
+    With a residual (like x), h = x + residual is normalised, and the call returns (y, h); else y.  y and h like x."""
+    rows, cols, ldx, code, stream, r, ldr, h = _norm(x, weight, eps, residual, "rms_norm")
+    y = _empty((rows, cols), (cols, 1), dtype=x.dtype, device=x.device)
+    err = binding.lib().tsvd_rms_norm(x.data_ptr(), code, rows, cols, ldx, r or None, ldr, h.data_ptr() if r else None, cols, weight.data_ptr(),
+                                      _CODES[weight.dtype], eps, y.data_ptr(), cols, None, 0, None, stream)
+    if err:
+        raise TSVDError(err, "tsvd_rms_norm")
+    return y if h is None else (y, h)
+
+
+def rms_norm_quantize(x, weight, eps: float = 1e-6, residual=None):
+    """The same with the result in 8-bit rows, as quantize makes them: (q int8 [rows, cols], its rows 16-byte aligned, scale
+    float32 [rows]), and h behind them where there is a residual.  Int8Linear and LowRankAdapters take q with its scale."""
+    rows, cols, ldx, code, stream, r, ldr, h = _norm(x, weight, eps, residual, "rms_norm_quantize")
+    ldq, device = (cols + 15) & ~15, x.device
+    q = _empty((rows, cols), (ldq, 1), dtype=_i8, device=device)
+    scale = _empty((rows,), (1,), dtype=_f32, device=device)
+    err = binding.lib().tsvd_rms_norm(x.data_ptr(), code, rows, cols, ldx, r or None, ldr, h.data_ptr() if r else None, cols, weight.data_ptr(),
+                                      _CODES[weight.dtype], eps, None, 0, q.data_ptr(), ldq, scale.data_ptr(), stream)
+    if err:
+        raise TSVDError(err, "tsvd_rms_norm")
+    return (q, scale) if h is None else (q, scale, h)
+
+
+def rotary_table(positions: int, turned: int, base: float = 10000.0, rates=None, amplitude: float = 1.0, device=None):
+    """Cosines and sines for KV4Cache.append_rotated: float32 [positions, turned], for each position turned / 2 cosines and then as
+    many sines of position * rate, the angles in 64 bits.  rates: float64 [turned / 2]; without them base ** (-2 i / turned)."""
+    import torch
+    if not _CODES:
+        _load()
+    if positions < 1 or turned < 2 or turned % 2:
+        raise TSVDError(binding.TSVD_E_SHAPE, "rotary_table")
+    device = torch.device(device if device is not None else "cuda")
+    if rates is None:
+        rates = base ** (-torch.arange(0, turned, 2, dtype=torch.float64) / turned)
+    if rates.dtype != torch.float64:
+        raise TSVDError(binding.TSVD_E_DTYPE, "rotary_table")
+    if rates.shape != (turned // 2,):
+        raise TSVDError(binding.TSVD_E_SHAPE, "rotary_table")
+    rates = rates.to(device).contiguous()
+    table = _empty((positions, turned), (turned, 1), dtype=_f32, device=device)
+    stream = _stream("rotary_table", table, rates)
+    err = binding.lib().tsvd_rotary_table(table.data_ptr(), positions, turned, rates.data_ptr(), amplitude, stream)
+    if err:
+        raise TSVDError(err, "tsvd_rotary_table")
+    return table
+
+
 class Int8Linear:
     """y = x W^T + bias with W in 8 bits (one scale per output channel) and x in 8 bits (one scale per token)."""
 
@@ -156,6 +226,100 @@ class Int8Linear:
             pass
 
 
+class LowRankAdapters:
+    """Low-rank adapters of many requests beside one projection from N to M numbers (an Int8Linear, a TSVDLinear, any other):
+    row i of a batch gets scale * B (A x_i) of its sequence's adapter added.  Weights are kept in bfloat16."""
+
+    def __init__(self, N: int, M: int, max_rank: int, n_slots: int):
+        self.handle = binding.tsvd_adapters_create(N, M, max_rank, n_slots)
+        self.N, self.M, self.max_rank, self.n_slots = N, M, max_rank, n_slots
+
+    def set(self, slot: int, A, B, scale: float = 1.0) -> None:
+        """An adapter into a slot, on torch's current stream: A [rank, N], B [M, rank], CUDA tensors, both float32 or both
+        bfloat16."""
+        what = "LowRankAdapters.set"
+        if A.dtype != B.dtype or _code(A.dtype, what) == TSVD_I8:
+            raise TSVDError(binding.TSVD_E_DTYPE, what)
+        (rank, N, lda), (M, rank_b, ldb) = _rows(A, what), _rows(B, what)
+        if N != self.N or M != self.M or rank != rank_b or not 0 < rank <= self.max_rank:
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        stream = _stream(what, A, B)
+        err = binding.lib().tsvd_adapters_set(self.handle, slot, A.data_ptr(), lda, B.data_ptr(), ldb, _code(A.dtype, what), rank, scale, stream)
+        if err:
+            raise TSVDError(err, "tsvd_adapters_set")
+
+    def clear(self, slot: int) -> None:
+        """Empty a slot, on torch's current stream."""
+        if not _CODES:
+            _load()
+        err = binding.lib().tsvd_adapters_set(self.handle, slot, None, 0, None, 0, TSVD_BF16, 0, 0.0, _raw_stream(_device()))
+        if err:
+            raise TSVDError(err, "tsvd_adapters_set")
+
+    def reserve(self, rows_max: int) -> None:
+        binding.tsvd_adapters_reserve(self.handle, rows_max)
+
+    def forward(self, x, base, slots, q_start=None, x_scale=None, out=None):
+        """base + scale * B (A x) for every row: x [rows, N] float32, bfloat16, or int8 with x_scale float32 [rows] (None: ones),
+        base [rows, M] float32 or bfloat16 (None: zeros, float32 unless x is bfloat16), slots int32 [n_seq] (-1: no adapter),
+        q_start int32 [n_seq + 1] (None: one row per sequence); all CUDA tensors, rows with any stride.  out may be base.
+        Returns [rows, M] of base's type."""
+        what = "LowRankAdapters.forward"
+        rows, N, ldx = _rows(x, what)
+        code = _code(x.dtype, what)
+        if N != self.N:
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        if x_scale is not None:
+            if x_scale.shape != (rows,) or not x_scale.is_contiguous() or not x_scale.is_cuda:
+                raise TSVDError(binding.TSVD_E_SHAPE, what)
+            if x_scale.dtype != _f32:
+                raise TSVDError(binding.TSVD_E_DTYPE, what)
+        if slots.dtype != _i32 or (q_start is not None and q_start.dtype != _i32):
+            raise TSVDError(binding.TSVD_E_DTYPE, what)
+        if slots.dim() != 1 or not slots.is_cuda or not slots.is_contiguous():
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        n_seq, start = slots.shape[0], None
+        if q_start is not None:
+            if q_start.shape != (n_seq + 1,) or not q_start.is_cuda or not q_start.is_contiguous():
+                raise TSVDError(binding.TSVD_E_SHAPE, what)
+            start = q_start.data_ptr()
+        stream = _stream(what, x, base, slots, q_start, x_scale, out)
+        ldb, dtype = 0, _bf16 if code == TSVD_BF16 else _f32
+        if base is not None:
+            if base.shape != (rows, self.M):
+                raise TSVDError(binding.TSVD_E_SHAPE, what)
+            ldb, dtype = _rows(base, what)[2], base.dtype
+        ldo = self.M
+        if out is None:
+            out = _empty((rows, ldo), (ldo, 1), dtype=dtype, device=x.device)
+        elif out.dtype != dtype or out.shape != (rows, ldo):
+            raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != dtype else binding.TSVD_E_SHAPE, what)
+        else:
+            ldo = _rows(out, what)[2]
+        err = binding.lib().tsvd_adapters_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else None, code,
+                                                  base.data_ptr() if base is not None else None, ldb, out.data_ptr(), ldo,
+                                                  _code(dtype, what), slots.data_ptr(), start, n_seq, rows, stream)
+        if err:
+            raise TSVDError(err, "tsvd_adapters_forward")
+        return out
+
+    __call__ = forward
+
+    def status(self) -> int:
+        return binding.tsvd_adapters_last_status(self.handle)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            binding.tsvd_adapters_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class KV4Cache:
     """Keys and values in 4 bits, in pages; the caller hands out the pages.
 
@@ -209,6 +373,37 @@ class KV4Cache:
         if err:
             raise TSVDError(err, "tsvd_kv4_append")
 
+    def append_rotated(self, q, k, v, rotary, page_table, seq_len, q_start=None, interleaved: bool = False):
+        """append with the rotation by position: the first rotary.shape[1] numbers of every head of q and k are turned by the
+        angles of the row's position (rotary float32 [positions, turned], see rotary_table), in pairs (p, p + turned / 2), or
+        (2 p, 2 p + 1) where interleaved.  Keys go into the cache turned; q [rows, n_heads, head_dim], of the same type, is
+        returned turned, as a new tensor (None: no queries)."""
+        what = "KV4Cache.append_rotated"
+        if k.dtype != v.dtype or k.shape != v.shape or (q is not None and q.dtype != k.dtype):
+            raise TSVDError(binding.TSVD_E_DTYPE if k.dtype != v.dtype or k.shape == v.shape else binding.TSVD_E_SHAPE, what)
+        (rows, heads, ldk), (_, _, ldv) = self._heads(k, what), self._heads(v, what)
+        n_heads = ldq = 0
+        if q is not None:
+            q_rows, n_heads, ldq = self._heads(q, what)
+            if q_rows != rows:
+                raise TSVDError(binding.TSVD_E_SHAPE, what)
+        if heads != self.n_kv_heads or rotary.dim() != 2 or not rotary.is_cuda or not rotary.is_contiguous():
+            raise TSVDError(binding.TSVD_E_SHAPE, what)
+        batch = self._batch(page_table, seq_len, q_start, rows, what)
+        if rotary.dtype != _f32:
+            raise TSVDError(binding.TSVD_E_DTYPE, what)
+        code, stream = _code(k.dtype, what), _stream(what, k, v, q, rotary, page_table, seq_len, q_start)
+        ldo, out = n_heads * self.head_dim, None
+        if q is not None:
+            out = _empty((rows, n_heads, self.head_dim), (ldo, self.head_dim, 1), dtype=q.dtype, device=q.device)
+        positions, turned = rotary.shape
+        err = binding.lib().tsvd_kv4_append_rotated(self.handle, q.data_ptr() if n_heads else None, ldq, out.data_ptr() if n_heads else None, ldo,
+                                                    n_heads, k.data_ptr(), ldk, v.data_ptr(), ldv, code, rotary.data_ptr(), positions,
+                                                    turned, int(interleaved), *batch, stream)
+        if err:
+            raise TSVDError(err, "tsvd_kv4_append_rotated")
+        return out
+
     def read(self, rows: int, page_table, seq_len, q_start=None, dtype=None):
         """(k, v) [rows, n_kv_heads, head_dim] as the cache holds them: float32 (default) or bfloat16."""
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.read")
@@ -224,11 +419,12 @@ class KV4Cache:
         return k, v
 
     def attend(self, q, page_table, seq_len, q_start=None, max_q=None, max_kv=None, causal=True, window=0, scale=None, out=None,
-               flags: int = 0):
+               flags: int = 0, sinks: int = 0):
         """Attention of q [rows, n_heads, head_dim] (bfloat16 or float32) over the cached keys and values; the rows are the
         last positions of their sequences (append their keys first).  max_q, max_kv: bounds on the rows and the positions
         of one sequence, where the caller knows them; with q_start and without max_q a sequence may have all the rows, and
-        the call takes the kernel for that (single tokens take far longer in it).  Returns a tensor like q."""
+        the call takes the kernel for that (single tokens take far longer in it).  sinks: first positions of a sequence that a
+        window does not hide.  Returns a tensor like q."""
         rows, n_heads, ldq = self._heads(q, "KV4Cache.attend")
         batch = self._batch(page_table, seq_len, q_start, rows, "KV4Cache.attend")
         stream = _stream("KV4Cache.attend", q, out, page_table, seq_len, q_start)
@@ -245,8 +441,9 @@ class KV4Cache:
             scale = 1.0 / math.sqrt(self.head_dim)
         if causal:
             flags |= binding.TSVD_FLAG_CAUSAL
-        err = binding.lib().tsvd_kv4_attend(self.handle, q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads,
-                                            _code(q.dtype, "KV4Cache.attend"), *batch, max_q, max_kv or 0, scale, window, flags, stream)
+        err = binding.lib().tsvd_kv4_attend_sinks(self.handle, q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads,
+                                                  _code(q.dtype, "KV4Cache.attend"), *batch, max_q, max_kv or 0, scale, window, sinks, flags,
+                                                  stream)
         if err:
             raise TSVDError(err, "tsvd_kv4_attend")
         return out
