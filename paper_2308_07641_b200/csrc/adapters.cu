@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "serving.cuh"
+#include "sm100_ptx.cuh"
 
 struct tsvd_adapters_s {
     int device = 0;
@@ -31,6 +32,7 @@ struct tsvd_adapters_s {
     uint8_t* B = nullptr;            // [slot][block][its groups][4][32 lanes][16]
     int* ranks = nullptr;            // [slot], 0: empty
     float* scales = nullptr;         // [slot]
+    int few[9] = {};                 // [1, 2, 4, 8]: clusters of so many blocks of the kernel for few rows that run at a time
     float* z = nullptr;              // scratch: [split][row][16 * groups]
     size_t z_bytes = 0;
     std::vector<void*>* outgrown = nullptr;   // scratch that captured graphs may still use
@@ -156,10 +158,10 @@ __global__ void adapter_set_kernel(const T* A, long long lda, const T* B, long l
             const int lane = (int)(k & 31), quarter = (int)(k >> 5 & 3), n = lane >> 2, t = lane & 3;
             const long long piece = k >> 7;
             const int group = (int)(piece % groups), block = (int)(piece / groups);
-            // column n of product j is channel 16 (n / 2) + 2 j + n % 2: a lane's results are 16 channels in a row
-            const int ch = block * BLOCK + 16 * (n >> 1) + 4 * quarter + (n & 1), r = group * GROUP + 4 * t;
-            b_out[k] = make_uint4(pair_of(B, ldb, ch, r, M, rank), pair_of(B, ldb, ch, r + 2, M, rank),
-                                  pair_of(B, ldb, ch + 2, r, M, rank), pair_of(B, ldb, ch + 2, r + 2, M, rank));
+            // rows n and n + 8 of product q are channels 8 n + 2 q and the next: a lane's results are eight channels in a row
+            const int ch = block * BLOCK + 8 * n + 2 * quarter, r = group * GROUP + 4 * t;
+            b_out[k] = make_uint4(pair_of(B, ldb, ch, r, M, rank), pair_of(B, ldb, ch + 1, r, M, rank),
+                                  pair_of(B, ldb, ch, r + 2, M, rank), pair_of(B, ldb, ch + 1, r + 2, M, rank));
         }
     }
 }
@@ -222,6 +224,34 @@ template <> struct Terms<float> {
     }
 };
 
+// A lane's eight columns of a row into its place; zeros where the row or the columns end.
+template <typename T>
+__device__ __forceinline__ void copy_x(uint8_t* dst, const void* m, long long ldx, int row, int n_rows, int col, int left, int aligned, int lane)
+{
+    const bool there = row < n_rows && left > 0;
+    const T* x = (const T*)m + (there ? (long long)row * ldx + col : 0);
+    const int have = there ? min(left, 8) * (int)sizeof(T) : 0;
+    if (aligned) {
+        if constexpr (sizeof(T) == 1) {
+            copy8(dst + lane * 8, x, have);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kXBytes<T> / 16; ++i)
+                copy16(dst + i * 512 + lane * 16, have > 16 * i ? x + i * (16 / (int)sizeof(T)) : (const T*)m, max(0, min(16, have - 16 * i)));
+        }
+    } else {
+        alignas(16) T v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i * (int)sizeof(T) < have ? x[i] : T(0.0f);
+        if constexpr (sizeof(T) == 1) {
+            *reinterpret_cast<uint2*>(dst + lane * 8) = *reinterpret_cast<uint2*>(v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kXBytes<T> / 16; ++i) *reinterpret_cast<uint4*>(dst + i * 512 + lane * 16) = reinterpret_cast<uint4*>(v)[i];
+        }
+    }
+}
+
 // A block: 8 NT rows, a share of the columns; a warp every eighth chunk of 32 of them.  RG: groups of ranks at a time.
 template <typename T, int NT, int RG>
 __global__ void __launch_bounds__(DOWN_WARPS * 32)
@@ -271,30 +301,7 @@ adapter_down_kernel(const DownParams p)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 if (!(mask >> (8 * n) & 0xffu)) continue;
-                const int row = row0 + 8 * n + g;
-                const bool there = row < p.rows.n_rows && left > 0;
-                const T* x = (const T*)p.x + (there ? (long long)row * p.ldx + col : 0);
-                uint8_t* dst = to + RG * 1024 + n * 32 * kXBytes<T>;
-                const int have = there ? min(left, 8) * (int)sizeof(T) : 0;
-                if (p.aligned) {
-                    if constexpr (sizeof(T) == 1) {
-                        copy8(dst + lane * 8, x, have);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kXBytes<T> / 16; ++i)
-                            copy16(dst + i * 512 + lane * 16, have > 16 * i ? x + i * (16 / (int)sizeof(T)) : (const T*)p.x, max(0, min(16, have - 16 * i)));
-                    }
-                } else {
-                    alignas(16) T v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = i * (int)sizeof(T) < have ? x[i] : T(0.0f);
-                    if constexpr (sizeof(T) == 1) {
-                        *reinterpret_cast<uint2*>(dst + lane * 8) = *reinterpret_cast<uint2*>(v);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kXBytes<T> / 16; ++i) *reinterpret_cast<uint4*>(dst + i * 512 + lane * 16) = reinterpret_cast<uint4*>(v)[i];
-                    }
-                }
+                copy_x<T>(to + RG * 1024 + n * 32 * kXBytes<T>, p.x, p.ldx, row0 + 8 * n + g, p.rows.n_rows, col, left, p.aligned, lane);
             }
             fc += DOWN_WARPS;
             if (fc >= c1) {
@@ -391,77 +398,137 @@ struct UpParams {
     int in_place;            // out is base: rows without an adapter are as they should be
     int M, blocks, per_warp; // per_warp: blocks of 64 channels that a warp takes
     int tile_rows;           // rows of a block of threads: at most UP_ROWS
-    int stages;
     const uint8_t* B;
     size_t b_slot;
 };
 
 template <typename T> constexpr int kTerms = sizeof(T) == 2 ? 2 : 3;
 
-// Sixteen channels of a row, in the row's type.
+// Eight channels of a row, in the row's type.
 template <typename T> struct Piece {
-    static constexpr int U = (int)sizeof(T);         // 16-byte units
+    static constexpr int U = (int)sizeof(T) / 2;     // 16-byte units
     uint4 u[U];
-    __device__ __forceinline__ void zero()
+    __device__ __forceinline__ void load(const T* at, int left)                // number by number; zeros behind the row's end
     {
+        alignas(16) T v[8];
 #pragma unroll
-        for (int i = 0; i < U; ++i) u[i] = make_uint4(0, 0, 0, 0);
-    }
-    __device__ __forceinline__ void load(const T* at, int left, bool vec)
-    {
-        if (vec && left >= 16) {
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? at[i] : T(0.0f);
 #pragma unroll
-            for (int i = 0; i < U; ++i) u[i] = reinterpret_cast<const uint4*>(at)[i];
-        } else {
-            alignas(16) T v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = i < left ? at[i] : T(0.0f);
-#pragma unroll
-            for (int i = 0; i < U; ++i) u[i] = reinterpret_cast<uint4*>(v)[i];
-        }
+        for (int i = 0; i < U; ++i) u[i] = reinterpret_cast<uint4*>(v)[i];
     }
     __device__ __forceinline__ void store(T* at, int left, bool vec) const
     {
-        if (vec && left >= 16) {
+        if (vec && left >= 8) {
 #pragma unroll
             for (int i = 0; i < U; ++i) reinterpret_cast<uint4*>(at)[i] = u[i];
         } else {
-            alignas(16) T v[16];
+            alignas(16) T v[8];
 #pragma unroll
             for (int i = 0; i < U; ++i) reinterpret_cast<uint4*>(v)[i] = u[i];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 8; ++i)
                 if (i < left) at[i] = v[i];
         }
     }
-    // channels 2 j and 2 j + 1
-    __device__ __forceinline__ void add(int j, float a, float b)
+    // channels 2 q and 2 q + 1
+    __device__ __forceinline__ void add(int q, float a, float b)
     {
         if constexpr (sizeof(T) == 2) {
-            uint32_t& w = reinterpret_cast<uint32_t*>(u)[j];
+            uint32_t& w = reinterpret_cast<uint32_t*>(u)[q];
             w = rounded(__uint_as_float(w << 16) + a, __uint_as_float(w & 0xffff0000u) + b);
         } else {
             float* f = reinterpret_cast<float*>(u);
-            f[2 * j] += a;
-            f[2 * j + 1] += b;
+            f[2 * q] += a;
+            f[2 * q + 1] += b;
+        }
+    }
+};
+template <typename T> constexpr int kBaseBytes = 32 * 2 * 8 * (int)sizeof(T);    // of eight rows and 64 channels
+
+// Base of rows 2 t and 2 t + 1 of eight and this lane's eight channels, into a stage: where `mask` has the row.
+template <typename T>
+__device__ __forceinline__ void copy_base(uint8_t* dst, const UpParams& p, int row0, int ch, unsigned mask, int lane)
+{
+    const int t = lane & 3, left = p.M - ch;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!(mask >> (2 * t + h) & 1) || left <= 0) continue;
+        const T* src = (const T*)p.base + (long long)(row0 + 2 * t + h) * p.ldb + ch;
+        uint8_t* to = dst + h * (Piece<T>::U * 512) + lane * 16;
+        if (p.base && p.vec && left >= 8) {
+#pragma unroll
+            for (int i = 0; i < Piece<T>::U; ++i) copy16(to + i * 512, src + i * (16 / (int)sizeof(T)));
+        } else {
+            Piece<T> v;
+            v.load(src, p.base ? left : 0);
+#pragma unroll
+            for (int i = 0; i < Piece<T>::U; ++i) *reinterpret_cast<uint4*>(to + i * 512) = v.u[i];
+        }
+    }
+}
+
+// Base in a stage plus the product, to out; acc[q]: channels 2 q, 2 q + 1 (elements 0 and 2, 1 and 3) of rows 2 t, 2 t + 1.
+template <typename T>
+__device__ __forceinline__ void add_and_store(const uint8_t* from, const float (&acc)[4][4], const UpParams& p, int row0, int ch, unsigned mask, int lane)
+{
+    const int t = lane & 3, left = p.M - ch;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if ((mask >> (2 * t + h) & 1) && left > 0) {
+            Piece<T> v;
+#pragma unroll
+            for (int i = 0; i < Piece<T>::U; ++i) v.u[i] = *reinterpret_cast<const uint4*>(from + h * (Piece<T>::U * 512) + i * 512 + lane * 16);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v.add(q, acc[q][h], acc[q][2 + h]);
+            v.store((T*)p.out + (long long)(row0 + 2 * t + h) * p.ldo + ch, left, p.vec);
+        }
+}
+
+// z of eight rows and sixteen ranks as the product's second operand, a lane's rank quadruple of its row: TERMS pairs of words.
+template <int TERMS>
+struct ZTerms {
+    uint32_t w[TERMS][2];
+    __device__ __forceinline__ void make(float (&v)[4])
+    {
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) {
+            const bool last = k + 1 == TERMS;
+            w[k][0] = last ? rounded(v[0], v[1]) : cut(v[0], v[1]);
+            w[k][1] = last ? rounded(v[2], v[3]) : cut(v[2], v[3]);
+        }
+    }
+    __device__ __forceinline__ void put(uint8_t* at, int lane) const           // at: 32 * 8 * TERMS bytes
+    {
+        *reinterpret_cast<uint4*>(at + lane * 16) = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+        if constexpr (TERMS == 3) *reinterpret_cast<uint2*>(at + 512 + lane * 8) = make_uint2(w[2][0], w[2][1]);
+    }
+    __device__ __forceinline__ void get(const uint8_t* at, int lane)
+    {
+        const uint4 u = *reinterpret_cast<const uint4*>(at + lane * 16);
+        w[0][0] = u.x; w[0][1] = u.y; w[1][0] = u.z; w[1][1] = u.w;
+        if constexpr (TERMS == 3) {
+            const uint2 v = *reinterpret_cast<const uint2*>(at + 512 + lane * 8);
+            w[2][0] = v.x; w[2][1] = v.y;
         }
     }
 };
 
-// A warp: tiles of 16 rows by 64 channels, the rows of the block's tile for each of its channel blocks in turn.
-template <typename T>
-__global__ void __launch_bounds__(UP_WARPS * 32)
+constexpr int UP_STAGES = 6;
+
+// A warp: 64 channels, whose weights (of one adapter) it holds in registers, eight rows after another of the block's tile; then the
+// tile's next adapter; then its next 64 channels.  Weights and base are copied ahead into the warp's own shared memory.  G: groups
+// of ranks at most.
+template <typename T, int G>
+__global__ void __launch_bounds__(UP_WARPS * 32, G <= 4 ? 3 : 2)
 adapter_up_kernel(const UpParams p)
 {
-    constexpr int TERMS = kTerms<T>;
+    constexpr int TERMS = kTerms<T>, Z = 256 * TERMS;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int slot_s[UP_ROWS];
-    // what a channel block does: for each 16 rows the adapters they ask for, those that differ from the one before being fetched
-    __shared__ int use_slot[UP_ROWS], use_groups[UP_ROWS], use_first[UP_ROWS / 16 + 1], fetches_s;
-    __shared__ unsigned short use_mask[UP_ROWS];
-    __shared__ int fetch_slot[UP_ROWS], fetch_groups[UP_ROWS];
+    __shared__ int slot_s[UP_ROWS], entry_slot[UP_ROWS + 1], entry_groups[UP_ROWS + 1], steps_s;
+    // what is done for each 64 channels: (adapter, eight rows); behind the adapters the rows without one, whose base is copied
+    __shared__ unsigned char step_entry[2 * UP_ROWS], step_tile[2 * UP_ROWS], step_mask[2 * UP_ROWS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * p.tile_rows, tiles = (p.tile_rows + 15) / 16;
+    const int row0 = blockIdx.x * p.tile_rows, tiles = (p.tile_rows + 7) / 8;
     // Adapters, slots and base are there: the first kernel let this one start after its own wait.  z is behind this one's wait.
     {
         Rows mine = p.rows;
@@ -469,163 +536,415 @@ adapter_up_kernel(const UpParams p)
         find_slots<UP_ROWS, UP_WARPS>(mine, row0, slot_s);
     }
     if (warp == 0) {
-        int uses = 0, fetches = 0, last = kNoAdapter;
-        for (int m = 0; m < tiles; ++m) {
-            const int slot = lane < 16 ? slot_s[16 * m + lane] : kNoRow;
-            const unsigned same = __match_any_sync(0xffffffffu, slot);
-            const bool leads = slot >= 0 && lane == __ffs(same) - 1;
-            const unsigned leaders = __ballot_sync(0xffffffffu, leads);
-            const int n = __popc(leaders), e = __popc(leaders & ((1u << lane) - 1));
-            const int first_slot = __shfl_sync(0xffffffffu, slot, n ? __ffs(leaders) - 1 : 0);
-            const int kept = n && first_slot == last;        // the first of them is there already
-            if (leads) {
-                const int groups = (p.rows.ranks[slot] + GROUP - 1) / GROUP;
-                use_slot[uses + e] = slot;
-                use_groups[uses + e] = groups;
-                use_mask[uses + e] = (unsigned short)same;
-                if (e >= kept) {
-                    fetch_slot[fetches + e - kept] = slot;
-                    fetch_groups[fetches + e - kept] = groups;
-                }
+        int a = slot_s[lane], b = slot_s[32 + lane], entries = 0, steps = 0;
+        auto add = [&](int slot, unsigned in_a, unsigned in_b) {               // one adapter's rows
+            const unsigned in = lane < 4 ? in_a >> (8 * lane) & 0xffu : lane < 8 ? in_b >> (8 * (lane - 4)) & 0xffu : 0u;
+            const unsigned there = __ballot_sync(0xffffffffu, in != 0);
+            if (in) {
+                const int k = steps + __popc(there & ((1u << lane) - 1));
+                step_entry[k] = (unsigned char)entries;
+                step_tile[k] = (unsigned char)lane;
+                step_mask[k] = (unsigned char)in;
             }
-            if (n) last = __shfl_sync(0xffffffffu, slot, 31 - __clz(leaders));
-            if (lane == 0) use_first[m] = uses;
-            uses += n;
-            fetches += n - kept;
+            if (lane == 0) {
+                entry_slot[entries] = slot;
+                entry_groups[entries] = slot < 0 ? 0 : (p.rows.ranks[slot] + GROUP - 1) / GROUP;
+            }
+            steps += __popc(there);
+            ++entries;
+        };
+        unsigned rest_a = __ballot_sync(0xffffffffu, a >= 0), rest_b = __ballot_sync(0xffffffffu, b >= 0);
+        while (rest_a | rest_b) {
+            const int slot = rest_a ? __shfl_sync(0xffffffffu, a, __ffs(rest_a) - 1) : __shfl_sync(0xffffffffu, b, __ffs(rest_b) - 1);
+            const unsigned in_a = __ballot_sync(0xffffffffu, a == slot), in_b = __ballot_sync(0xffffffffu, b == slot);
+            add(slot, in_a, in_b);
+            rest_a &= ~in_a;
+            rest_b &= ~in_b;
         }
-        if (lane == 0) { use_first[tiles] = uses; fetches_s = fetches; }
+        const unsigned none_a = __ballot_sync(0xffffffffu, a == kNoAdapter), none_b = __ballot_sync(0xffffffffu, b == kNoAdapter);
+        if ((none_a | none_b) && !p.in_place) add(kNoAdapter, none_a, none_b);
+        if (lane == 0) steps_s = steps;
     }
     __syncthreads();
-    const int fetches = fetches_s;
-    const int b0 = (blockIdx.y * UP_WARPS + warp) * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
-    const int stage_bytes = p.groups * 2048;
-    uint8_t* ring = smem + (size_t)warp * p.stages * stage_bytes;
-    uint4* zs = reinterpret_cast<uint4*>(smem + (size_t)UP_WARPS * p.stages * stage_bytes);     // [tile][group][term][lane]
+    const int steps = steps_s, b0 = (blockIdx.y * UP_WARPS + warp) * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
+    uint8_t* zs = smem;                                                        // [tile][group][Z]
+    uint8_t* weights = smem + tiles * p.groups * Z + warp * (p.groups * 2048 + UP_STAGES * kBaseBytes<T>);
+    uint8_t* ring = weights + p.groups * 2048;
 
-    int fb = b0, ff = 0, fs = 0;
+    // ---- copies: base of the next (block, step); weights of the next (block, adapter) ----
+    int fb = b0, fk = 0, fs = 0;
     auto fetch = [&]() {
-        if (fb < b1 && ff < fetches) {
-            const int groups = fetch_groups[ff];
-            const uint8_t* from = p.B + (size_t)fetch_slot[ff] * p.b_slot + (size_t)fb * groups * 2048 + lane * 16;
-            uint8_t* to = ring + fs * stage_bytes + lane * 16;
-            for (int i = 0; i < groups; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) copy16(to + i * 2048 + k * 512, from + i * 2048 + k * 512);
-            if (++ff == fetches) { ff = 0; ++fb; }
+        if (fb < b1 && steps > 0) {
+            copy_base<T>(ring + fs * kBaseBytes<T>, p, row0 + 8 * step_tile[fk], fb * BLOCK + 8 * g, step_mask[fk], lane);
+            if (++fk == steps) { fk = 0; ++fb; }
         }
         copies_commit();
-        if (++fs == p.stages) fs = 0;
+        if (++fs == UP_STAGES) fs = 0;
     };
-    for (int i = 0; i < p.stages - 1; ++i) fetch();
-
-    // base of 16 rows, this lane's two rows and 16 channels
-    Piece<T> base[2];
-    auto ask = [&](int b, int m) {
-        const int ch = b * BLOCK + 16 * t;
+    int wb = b0, wk = 0;                                                       // the step at which the weights on their way are needed
+    auto fetch_weights = [&]() {                                               // (in the next group that is committed)
+        if (wb >= b1 || steps == 0) return;
+        const int e = step_entry[wk], groups = entry_groups[e];
+        if (groups) {
+            const uint8_t* from = p.B + (size_t)entry_slot[e] * p.b_slot + (size_t)wb * groups * 2048 + lane * 16;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = 16 * m + g + 8 * h;
-            base[h].zero();
-            if (p.base && slot_s[r] != kNoRow && ch < p.M)
-                base[h].load((const T*)p.base + (long long)(row0 + r) * p.ldb + ch, p.M - ch, p.vec);
+            for (int i = 0; i < 4 * G; ++i)
+                if (i < 4 * groups) copy16(weights + i * 512 + lane * 16, from + i * 512);
         }
     };
-    if (b0 < b1) ask(b0, 0);
+    auto next_weights = [&]() {                                                // behind the adapter at (wb, wk)
+        const int e = step_entry[wk];
+        while (wk < steps && step_entry[wk] == e) ++wk;
+        if (wk == steps) { wk = 0; ++wb; }
+    };
+    fetch_weights();
+    for (int i = 0; i < UP_STAGES - 1; ++i) fetch();
 
-    // ---- z: the splits' sum, scaled, as bf16 terms in the order of the product's first operand ----
+    // ---- z: the splits' sum, scaled, as bf16 terms in the order of the product's second operand ----
     pdl_wait();
     pdl_launch_dependents();
     const int rank_pad = p.groups * GROUP;
     for (int i = threadIdx.x; i < tiles * p.groups * 32; i += UP_WARPS * 32) {
-        const int ln = i & 31, group = (i >> 5) % p.groups, m = (i >> 5) / p.groups;
-        float v[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = 16 * m + (ln >> 2) + 8 * h, slot = slot_s[r], first = group * GROUP + 4 * (ln & 3);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[h][k] = 0.0f;
-            const int have = slot >= 0 ? p.rows.ranks[slot] - first : 0;     // z is written for the adapter's own ranks only
-            if (have > 0) {
-                const float* z = p.z + (size_t)(row0 + r) * rank_pad + first;
+        const int ln = i & 31, group = (i >> 5) % p.groups, tile = (i >> 5) / p.groups;
+        const int r = 8 * tile + (ln >> 2), slot = slot_s[r], first = group * GROUP + 4 * (ln & 3);
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int have = slot >= 0 ? p.rows.ranks[slot] - first : 0;           // z is written for the adapter's own ranks only
+        if (have > 0) {
+            const float* z = p.z + (size_t)(row0 + r) * rank_pad + first;
 #pragma unroll 8
-                for (int s = 0; s < p.splits; ++s) {
-                    const float4 u = __ldcg(reinterpret_cast<const float4*>(z + (size_t)s * p.rows.n_rows * rank_pad));
-                    v[h][0] += u.x; v[h][1] += u.y; v[h][2] += u.z; v[h][3] += u.w;
-                }
-                const float c = p.scales[slot] * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[h][k] = k < have ? v[h][k] * c : 0.0f;
+            for (int s = 0; s < p.splits; ++s) {
+                const float4 u = __ldcg(reinterpret_cast<const float4*>(z + (size_t)s * p.rows.n_rows * rank_pad));
+                v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
             }
-        }
-        uint4* to = zs + (size_t)((i >> 5) * TERMS) * 32 + ln;
+            const float c = p.scales[slot] * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
 #pragma unroll
-        for (int k = 0; k < TERMS; ++k) {
-            uint4 w;
-            if (k + 1 < TERMS) {
-                w.x = cut(v[0][0], v[0][1]); w.y = cut(v[1][0], v[1][1]);
-                w.z = cut(v[0][2], v[0][3]); w.w = cut(v[1][2], v[1][3]);
-            } else {
-                w.x = rounded(v[0][0], v[0][1]); w.y = rounded(v[1][0], v[1][1]);
-                w.z = rounded(v[0][2], v[0][3]); w.w = rounded(v[1][2], v[1][3]);
-            }
-            to[k * 32] = w;
+            for (int k = 0; k < 4; ++k) v[k] = k < have ? v[k] * c : 0.0f;
         }
+        ZTerms<TERMS> z;
+        z.make(v);
+        z.put(zs + (i >> 5) * Z, ln);
     }
     __syncthreads();
 
-    int stage = -1;
+    int stage = 0, since = UP_STAGES;                                          // since: groups committed after the weights'
+    uint4 w[4 * G];
     for (int b = b0; b < b1; ++b) {
-        int last = kNoAdapter;
-        for (int m = 0; m < tiles; ++m) {
-            for (int e = use_first[m]; e < use_first[m + 1]; ++e) {
-                const int groups = use_groups[e];
-                if (use_slot[e] != last) {           // its weights: the stage before is free
-                    last = use_slot[e];
-                    if (stage >= 0) fetch();
-                    if (++stage == p.stages) stage = 0;
-                    // (a stage's copies are one group, and stages - 2 groups may follow the one that is needed)
-                    if (p.stages == 2) copies_wait<0>();
-                    else if (p.stages == 3) copies_wait<1>();
-                    else if (p.stages == 4) copies_wait<2>();
-                    else copies_wait<6>();
+        int last = -1, groups = 0;
+        for (int k = 0; k < steps; ++k) {
+            // (a step's copies are one group, and UP_STAGES - 2 groups may follow the one that is needed)
+            copies_wait<UP_STAGES - 2>();
+            const int e = step_entry[k];
+            if (e != last) {
+                last = e;
+                groups = entry_groups[e];
+                if (since < UP_STAGES - 1) copies_wait<0>();
+#pragma unroll
+                for (int i = 0; i < 4 * G; ++i)
+                    if (i < 4 * groups) w[i] = *reinterpret_cast<const uint4*>(weights + i * 512 + lane * 16);
+                next_weights();
+                fetch_weights();
+                since = 0;
+            }
+            float acc[4][4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
+            const int tile = step_tile[k];
+            const uint8_t* z_at = zs + tile * p.groups * Z;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (i < groups) {
+                    ZTerms<TERMS> z;
+                    z.get(z_at + i * Z, lane);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = TERMS - 1; j >= 0; --j) mma_bf16(acc[q], w[4 * i + q], z.w[j][0], z.w[j][1]);
                 }
-                const uint8_t* from = ring + stage * stage_bytes + lane * 16;
-                float acc[8][4];
+            add_and_store<T>(ring + stage * kBaseBytes<T>, acc, p, row0 + 8 * tile, b * BLOCK + 8 * g, step_mask[k], lane);
+            fetch();
+            ++since;
+            if (++stage == UP_STAGES) stage = 0;
+        }
+    }
+    copies_wait<0>();
+}
+
+// ---- both in one launch, for few rows ---------------------------------------------------------------------------------------
+// A cluster of blocks takes up to eight rows.  The adapters that they ask for, one after another, are cut into equal runs of
+// chunks of columns for its warps, and then into runs of blocks of channels: a warp reads a few long pieces.  Its copies run through
+// both products, so that while the parts of z are added up and exchanged (each block writes its part to every block's shared
+// memory: one cluster barrier), the first weights of the second product are on their way.  Against two launches this saves a
+// launch, the way of z through memory, and the second search for the rows' adapters.
+
+constexpr int FEW_WARPS = 12, FEW_ROWS = 8, FEW_GROUPS = 4;      // (of more than 64 ranks shared memory holds too few stages)
+
+struct FewParams {
+    DownParams d;
+    UpParams u;
+    int cluster, rows;       // blocks; rows of a cluster
+};
+
+// A stage of a warp's ring: weights (of one adapter; chunks as a whole, blocks in groups of ranks), then x of the chunks, or base of
+// the block whose last groups they are.
+template <typename T, typename O>
+struct FewStage {
+    int groups, chunks, units, weights, bytes, stages;       // groups: most
+    __host__ __device__ explicit FewStage(int groups)
+        : groups(groups), chunks(groups == 1 ? 2 : 1), units(groups == 4 ? 2 : 1), weights(groups < 2 ? 2048 : groups * 1024),
+          bytes(weights + (chunks * 32 * kXBytes<T> > kBaseBytes<O> ? chunks * 32 * kXBytes<T> : kBaseBytes<O>)), stages(groups <= 2 ? 4 : groups == 4 && sizeof(O) == 4 ? 2 : 3) {}
+    __host__ __device__ int ring() const { return FEW_WARPS * stages * bytes; }
+    size_t smem(int cluster) const { return (size_t)ring() + (size_t)(FEW_WARPS + cluster) * FEW_ROWS * groups * GROUP * sizeof(float); }
+};
+
+template <typename T, typename O>
+__global__ void __launch_bounds__(FEW_WARPS * 32, 1)
+adapter_few_kernel(const FewParams p)
+{
+    constexpr int TERMS = kTerms<O>, Z = 256 * TERMS, MOST = FEW_ROWS + 1;
+    extern __shared__ __align__(16) uint8_t smem[];
+    // the adapters asked for, and behind them (slot kNoAdapter) the rows without one, whose base is copied
+    __shared__ int slot_s[FEW_ROWS], entry_slot[MOST], entry_groups[MOST], entries_s, all_s;
+    __shared__ unsigned entry_mask[MOST];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = p.cluster > 1 ? (int)ptx::cluster_ctarank() : 0, row0 = (int)(blockIdx.x / (unsigned)p.cluster) * p.rows;
+    const FewStage<T, O> st(p.d.groups);
+    const int rank_pad = st.groups * GROUP, numbers = FEW_ROWS * rank_pad;
+    uint8_t* ring = smem + (size_t)warp * st.stages * st.bytes;
+    float* parts = reinterpret_cast<float*>(smem + st.ring());           // [warp][row][rank_pad]
+    float* z_all = parts + FEW_WARPS * numbers;                          // [block of the cluster][row][rank_pad]
+    uint8_t* zs = reinterpret_cast<uint8_t*>(parts);                     // over the parts, once they are added up: [group][Z]
+    pdl_wait();
+    pdl_launch_dependents();
+    if (p.cluster > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");               // (its blocks have all begun)
+    {
+        Rows mine = p.d.rows;
+        mine.n_rows = min(mine.n_rows, row0 + p.rows);
+        find_slots<FEW_ROWS, FEW_WARPS>(mine, row0, slot_s);
+    }
+    if (warp == 0) {
+        const int slot = lane < FEW_ROWS ? slot_s[lane] : kNoRow;
+        const unsigned same = __match_any_sync(0xffffffffu, slot);
+        const bool leads = slot >= 0 && lane == __ffs(same) - 1;
+        const unsigned leaders = __ballot_sync(0xffffffffu, leads), none = __ballot_sync(0xffffffffu, slot == kNoAdapter);
+        const int n = __popc(leaders);
+        if (leads) {
+            const int e = __popc(leaders & ((1u << lane) - 1));
+            entry_slot[e] = slot;
+            entry_mask[e] = same;
+            entry_groups[e] = (p.d.rows.ranks[slot] + GROUP - 1) / GROUP;
+        }
+        if (lane == 0) {
+            entries_s = n;
+            all_s = n + (none && !p.u.in_place);
+            entry_slot[n] = kNoAdapter;
+            entry_groups[n] = 0;
+            entry_mask[n] = none;
+        }
+    }
+    __syncthreads();
+    const int entries = entries_s, all = all_s, of = p.cluster * FEW_WARPS, me = rank * FEW_WARPS + warp;
+
+    // A warp's run of (adapter, chunk) or (adapter, block), by weight: from (e, at) on, of `left` weight.
+    struct Run { int e, at, end, stop; };          // at, end: in adapter e; stop: weight where the run ends
+    auto weight_of = [&](int e, bool up) { return up ? entry_groups[e] + 1 : entry_groups[e]; };
+    auto enter = [&](Run& r, int before, bool up) {          // the run's part of adapter r.e, which begins at weight `before`
+        const int count = up ? p.u.blocks : p.d.chunks, w = weight_of(r.e, up);
+        r.end = min(count, (r.stop - before + w - 1) / w);
+    };
+    auto begin = [&](bool up) {
+        const int n = up ? all : entries, count = up ? p.u.blocks : p.d.chunks;
+        unsigned total = 0;                                  // (below 2^24, and `of` below 2^7)
+        for (int e = 0; e < n; ++e) total += (unsigned)(weight_of(e, up) * count);
+        const int start = (int)(total * (unsigned)me / (unsigned)of);
+        Run r{0, 0, 0, (int)(total * (unsigned)(me + 1) / (unsigned)of)};
+        int before = 0;
+        for (; r.e < n; ++r.e) {
+            const int w = weight_of(r.e, up);
+            r.at = max(0, (start - before + w - 1) / w);
+            enter(r, before, up);
+            if (r.at < r.end || before >= r.stop) break;
+            before += w * count;
+        }
+        if (r.e >= n || r.at >= r.end) r.e = n;
+        r.stop -= before;                                    // from here on counted from adapter e's begin
+        return r;
+    };
+    auto advance = [&](Run& r, bool up) {                    // behind r.end: the next adapter's part, or e = n
+        const int n = up ? all : entries, count = up ? p.u.blocks : p.d.chunks;
+        r.stop -= weight_of(r.e, up) * count;
+        ++r.e;
+        r.at = 0;
+        if (r.e >= n || r.stop <= 0) { r.e = n; return; }
+        enter(r, 0, up);
+    };
+
+    // ---- the copies ----
+    Run run = begin(false);
+    bool up = false;
+    int unit = 0, fs = 0;                                    // up: the groups of the block that are on their way
+    if (run.e == entries) { up = true; run = begin(true); }
+    auto fetch = [&]() {
+        uint8_t* to = ring + fs * st.bytes;
+        if (!up) {
+            const int groups = entry_groups[run.e], n = min(st.chunks, run.end - run.at);
+            const uint8_t* a = p.d.A + (size_t)entry_slot[run.e] * p.d.a_slot + (size_t)run.at * groups * 1024 + lane * 16;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+            for (int i = 0; i < 2 * FEW_GROUPS; ++i)
+                if (i < 2 * n * groups) copy16(to + i * 512 + lane * 16, a + i * 512);
+            if (entry_mask[run.e] >> g & 1)
+                for (int c = 0; c < n; ++c) {
+                    const int col = (run.at + c) * CHUNK + 8 * t;
+                    copy_x<T>(to + st.weights + c * 32 * kXBytes<T>, p.d.x, p.d.ldx, row0 + g, p.d.rows.n_rows, col, p.d.N - col, p.d.aligned, lane);
+                }
+            if ((run.at += n) >= run.end) {
+                advance(run, false);
+                if (run.e == entries) { up = true; run = begin(true); }
+            }
+        } else if (run.e < all) {
+            const int groups = entry_groups[run.e], n = min(st.units, groups - unit);
+            if (groups) {
+                const uint8_t* b = p.u.B + (size_t)entry_slot[run.e] * p.u.b_slot + ((size_t)run.at * groups + unit) * 2048 + lane * 16;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[j][k] = 0.0f;
-                for (int i = 0; i < groups; ++i) {
-                    uint4 z[TERMS];
+                for (int i = 0; i < 8; ++i)
+                    if (i < 4 * n) copy16(to + i * 512 + lane * 16, b + i * 512);
+            }
+            unit += n;
+            if (unit >= groups) {                            // with the block's last ones, base
+                copy_base<O>(to + st.weights, p.u, row0, run.at * BLOCK + 8 * g, entry_mask[run.e], lane);
+                unit = 0;
+                if (++run.at >= run.end) advance(run, true);
+            }
+        }
+        copies_commit();
+        if (++fs == st.stages) fs = 0;
+    };
+    // (a stage's copies are one group, and stages - 2 groups may follow the one that is needed)
+    auto arrived = [&]() {
+        if (st.stages == 4) copies_wait<2>();
+        else if (st.stages == 3) copies_wait<1>();
+        else copies_wait<0>();
+    };
+    int stage = 0;
+    auto done = [&]() {
+        fetch();
+        if (++stage == st.stages) stage = 0;
+    };
+    Run mine = run, mine_up = up ? run : begin(true);
+    const bool has_down = !up;
+    for (int i = 0; i < st.stages - 1; ++i) fetch();
+    for (int i = lane; i < numbers; i += 32) parts[warp * numbers + i] = 0.0f;
+    __syncwarp();
+
+    // ---- parts of z ----
+    if (has_down)
+        while (mine.e < entries) {
+            const int groups = entry_groups[mine.e];
+            const unsigned mask = entry_mask[mine.e];
+            float acc[FEW_GROUPS][4];
 #pragma unroll
-                    for (int k = 0; k < TERMS; ++k) z[k] = zs[(size_t)((m * p.groups + i) * TERMS + k) * 32 + lane];
+            for (int i = 0; i < FEW_GROUPS; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][k] = 0.0f;
+            while (mine.at < mine.end) {
+                const int n = min(st.chunks, mine.end - mine.at);
+                arrived();
+                const uint8_t* from = ring + stage * st.bytes;
+                for (int c = 0; c < n; ++c) {
+                    Terms<T> x{};
+                    if (mask >> g & 1) x.read(from + st.weights + c * 32 * kXBytes<T> + lane * (sizeof(T) == 1 ? 8 : 16));
+#pragma unroll
+                    for (int i = 0; i < FEW_GROUPS; ++i)
+                        if (i < groups) {
+                            const uint8_t* w = from + (c * groups + i) * 1024 + lane * 16;
+                            const uint4 a0 = *reinterpret_cast<const uint4*>(w), a1 = *reinterpret_cast<const uint4*>(w + 512);
+#pragma unroll
+                            for (int k = Terms<T>::n - 1; k >= 0; --k) {
+                                mma_bf16(acc[i], a0, x.w[k][0], x.w[k][1]);
+                                mma_bf16(acc[i], a1, x.w[k][2], x.w[k][3]);
+                            }
+                        }
+                }
+                mine.at += n;
+                done();
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = 2 * t + (k & 1);
+                if (mask >> row & 1)
+#pragma unroll
+                    for (int i = 0; i < FEW_GROUPS; ++i)
+                        if (i < groups) parts[warp * numbers + row * rank_pad + i * GROUP + g + (k & 2 ? 8 : 0)] = acc[i][k];
+            }
+            advance(mine, false);
+        }
+    __syncwarp();
+    if (p.cluster > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    __syncthreads();
+    for (int i = threadIdx.x; i < numbers; i += FEW_WARPS * 32) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) sum += parts[w * numbers + i];
+        if (p.cluster > 1) {
+            const uint32_t at = ptx::smem_u32(z_all + rank * numbers + i);
+            for (int c = 0; c < p.cluster; ++c)
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ptx::cluster_map_u32(at, (uint32_t)c)), "f"(sum) : "memory");
+        } else {
+            z_all[i] = sum;
+        }
+    }
+    if (p.cluster > 1) ptx::cluster_sync_all();
+    else __syncthreads();
+
+    // ---- z, scaled, as bf16 terms in the order of the product's second operand ----
+    for (int i = threadIdx.x; i < st.groups * 32; i += FEW_WARPS * 32) {
+        const int ln = i & 31, group = i >> 5, row = ln >> 2, slot = slot_s[row];
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (slot >= 0) {
+            for (int c = 0; c < p.cluster; ++c) {
+                const float4 u = *reinterpret_cast<const float4*>(z_all + c * numbers + row * rank_pad + group * GROUP + 4 * (ln & 3));
+                v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+            }
+            const float c = p.u.scales[slot] * (p.u.x_scale ? p.u.x_scale[row0 + row] : 1.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] *= c;
+        }
+        ZTerms<TERMS> z;
+        z.make(v);
+        z.put(zs + group * Z, ln);
+    }
+    __syncthreads();
+
+    while (mine_up.e < all) {
+        const int groups = entry_groups[mine_up.e];
+        const unsigned mask = entry_mask[mine_up.e];
+        for (; mine_up.at < mine_up.end; ++mine_up.at) {
+            float acc[4][4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[q][k] = 0.0f;
+            int i = 0;
+            do {
+                arrived();
+                const uint8_t* from = ring + stage * st.bytes;
+                const int n = min(st.units, groups - i);
+                for (int c = 0; c < n; ++c, ++i) {
+                    ZTerms<TERMS> z;
+                    z.get(zs + i * Z, lane);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const uint4 w = *reinterpret_cast<const uint4*>(from + i * 2048 + q * 512);
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + c * 2048 + q * 512 + lane * 16);
 #pragma unroll
-                        for (int k = TERMS - 1; k >= 0; --k) {
-                            mma_bf16(acc[2 * q], z[k], w.x, w.y);
-                            mma_bf16(acc[2 * q + 1], z[k], w.z, w.w);
-                        }
+                        for (int k = TERMS - 1; k >= 0; --k) mma_bf16(acc[q], w, z.w[k][0], z.w[k][1]);
                     }
                 }
-                const unsigned mask = use_mask[e];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (mask >> (g + 8 * h) & 1)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) base[h].add(j, acc[j][2 * h], acc[j][2 * h + 1]);
-            }
-            const int ch = b * BLOCK + 16 * t;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = 16 * m + g + 8 * h, slot = slot_s[r];
-                if (slot != kNoRow && ch < p.M && !(p.in_place && slot == kNoAdapter))
-                    base[h].store((T*)p.out + (long long)(row0 + r) * p.ldo + ch, p.M - ch, p.vec);
-            }
-            if (m + 1 < tiles) ask(b, m + 1);
-            else if (b + 1 < b1) ask(b + 1, 0);
+                if (i >= groups) add_and_store<O>(from + st.weights, acc, p.u, row0, mine_up.at * BLOCK + 8 * g, mask, lane);
+                done();
+            } while (i < groups);
         }
+        advance(mine_up, true);
     }
     copies_wait<0>();
 }
@@ -656,16 +975,6 @@ cudaError_t prepare_type()
     if (e == cudaSuccess) e = prepare_down<T, 2, 4>();
     return e;
 }
-cudaError_t prepare()
-{
-    cudaError_t e = prepare_type<float>();
-    if (e == cudaSuccess) e = prepare_type<__nv_bfloat16>();
-    if (e == cudaSuccess) e = prepare_type<int8_t>();
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_up_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_up_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    return e;
-}
-
 template <typename T, int NT, int RG>
 cudaError_t down(const DownParams& p, cudaStream_t st)
 {
@@ -680,6 +989,82 @@ cudaError_t down_type(const DownParams& p, bool wide, cudaStream_t st)
     const int rg = p.groups == 1 ? 1 : p.groups == 2 ? 2 : 4;
     if (wide) return rg == 1 ? down<T, 2, 1>(p, st) : rg == 2 ? down<T, 2, 2>(p, st) : down<T, 2, 4>(p, st);
     return rg == 1 ? down<T, 1, 1>(p, st) : rg == 2 ? down<T, 1, 2>(p, st) : down<T, 1, 4>(p, st);
+}
+
+template <typename T, typename O>
+cudaError_t prepare_few()
+{
+    return cudaFuncSetAttribute(adapter_few_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+}
+
+struct FewLaunch {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    FewLaunch(unsigned tiles, int cluster, size_t smem, cudaStream_t st)
+    {
+        cfg.gridDim = dim3(tiles * (unsigned)cluster);
+        cfg.blockDim = dim3(FEW_WARPS * 32);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster > 1 ? 2 : 1;
+    }
+};
+
+template <typename T>
+cudaError_t few(const FewParams& p, unsigned tiles, bool out_f32, cudaStream_t st)
+{
+    if (out_f32) {
+        FewLaunch l(tiles, p.cluster, FewStage<T, float>(p.d.groups).smem(p.cluster), st);
+        return cudaLaunchKernelEx(&l.cfg, adapter_few_kernel<T, float>, p);
+    }
+    FewLaunch l(tiles, p.cluster, FewStage<T, __nv_bfloat16>(p.d.groups).smem(p.cluster), st);
+    return cudaLaunchKernelEx(&l.cfg, adapter_few_kernel<T, __nv_bfloat16>, p);
+}
+
+cudaError_t prepare()
+{
+    cudaError_t e = prepare_type<float>();
+    if (e == cudaSuccess) e = prepare_type<__nv_bfloat16>();
+    if (e == cudaSuccess) e = prepare_type<int8_t>();
+    if (e == cudaSuccess) e = prepare_few<float, float>();
+    if (e == cudaSuccess) e = prepare_few<float, __nv_bfloat16>();
+    if (e == cudaSuccess) e = prepare_few<__nv_bfloat16, float>();
+    if (e == cudaSuccess) e = prepare_few<__nv_bfloat16, __nv_bfloat16>();
+    if (e == cudaSuccess) e = prepare_few<int8_t, float>();
+    if (e == cudaSuccess) e = prepare_few<int8_t, __nv_bfloat16>();
+    for (const void* kernel : {(const void*)adapter_up_kernel<float, 1>, (const void*)adapter_up_kernel<float, 2>, (const void*)adapter_up_kernel<float, 4>,
+                               (const void*)adapter_up_kernel<float, 8>, (const void*)adapter_up_kernel<__nv_bfloat16, 1>,
+                               (const void*)adapter_up_kernel<__nv_bfloat16, 2>, (const void*)adapter_up_kernel<__nv_bfloat16, 4>,
+                               (const void*)adapter_up_kernel<__nv_bfloat16, 8>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    return e;
+}
+
+template <typename T, int G>
+cudaError_t up(const UpParams& p, unsigned tiles, unsigned columns, cudaStream_t st)
+{
+    const size_t smem = (size_t)(p.tile_rows + 7) / 8 * p.groups * 256 * kTerms<T> + (size_t)UP_WARPS * (p.groups * 2048 + UP_STAGES * kBaseBytes<T>);
+    PdlLaunch l(tiles, UP_WARPS * 32, smem, st);
+    l.cfg.gridDim.y = columns;
+    return cudaLaunchKernelEx(&l.cfg, adapter_up_kernel<T, G>, p);
+}
+
+template <typename T>
+cudaError_t up_type(UpParams& p, int sms, cudaStream_t st)
+{
+    // Channel blocks a warp: so many that the blocks run in one round, three an SM (they read z again each).
+    const int tiles = (p.rows.n_rows + p.tile_rows - 1) / p.tile_rows;
+    auto columns = [&] { return (p.blocks + UP_WARPS * p.per_warp - 1) / (UP_WARPS * p.per_warp); };
+    p.per_warp = 1;
+    while ((long long)tiles * columns() > 3LL * sms && p.per_warp < p.blocks) ++p.per_warp;
+    const unsigned x = (unsigned)tiles, y = (unsigned)columns();
+    return p.groups == 1 ? up<T, 1>(p, x, y, st) : p.groups == 2 ? up<T, 2>(p, x, y, st) : p.groups <= 4 ? up<T, 4>(p, x, y, st) : up<T, 8>(p, x, y, st);
 }
 
 struct Shape {
@@ -697,7 +1082,28 @@ Shape shape_of(const tsvd_adapters_s* h, int rows)
     if (s.splits > MAX_SPLITS) s.splits = MAX_SPLITS;
     return s;
 }
-size_t z_bytes(const tsvd_adapters_s* h, int rows) { return (size_t)shape_of(h, rows).splits * rows * h->groups * GROUP * sizeof(float); }
+// How the kernel for few rows serves a call of so many, if it does (else cluster = 0): clusters of as many blocks as have a chunk
+// or a block of channels for each of their warps, eight at most, or half or a quarter of that where this lets more blocks run; as few
+// rows each as are served by the clusters that run at a time (a second round would cost what the other kernels' second launch does).
+struct Few { int cluster, rows; };
+Few few_of(const tsvd_adapters_s* h, int rows)
+{
+    if (h->groups > FEW_GROUPS) return {0, 0};
+    const int work = h->chunks > h->blocks ? h->chunks : h->blocks;
+    int most = 1;
+    while (most < 8 && most * FEW_WARPS < work) most *= 2;
+    Few best{0, 0};
+    int blocks = 0;
+    for (int c = most; c >= 1 && 4 * c >= most; c /= 2)
+        for (int r = 1; r <= FEW_ROWS; r *= 2) {
+            const int clusters = (rows + r - 1) / r;
+            if (clusters > h->few[c]) continue;
+            if (clusters * c > blocks) { best = {c, r}; blocks = clusters * c; }
+            break;
+        }
+    return best;
+}
+size_t z_bytes(const tsvd_adapters_s* h, int rows) { return few_of(h, rows).cluster ? 0 : (size_t)shape_of(h, rows).splits * rows * h->groups * GROUP * sizeof(float); }
 
 tsvd_status_t grow(tsvd_adapters_s* h, size_t need)
 {
@@ -767,6 +1173,14 @@ extern "C" tsvd_status_t tsvd_adapters_create(int N, int M, int max_rank, int n_
     if (e == cudaSuccess) e = cudaMemset(h->dev_status, 0, sizeof(int));
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e == cudaSuccess) e = prepare();
+    if (h->groups <= FEW_GROUPS)
+        for (int c = 1; c <= 8 && e == cudaSuccess; c *= 2) {
+            FewLaunch l((unsigned)(h->sms / 8 * 8), c, FewStage<float, float>(h->groups).smem(c), nullptr);
+            l.cfg.numAttrs = 0;
+            if (c > 1) { l.attr[0] = l.attr[1]; l.cfg.numAttrs = 1; }
+            h->few[c] = h->sms;
+            if (c > 1) e = cudaOccupancyMaxActiveClusters(&h->few[c], adapter_few_kernel<float, float>, &l.cfg);
+        }
     if (e != cudaSuccess) {
         release(h);
         return e == cudaErrorMemoryAllocation ? TSVD_E_NOMEM : TSVD_E_CUDA;
@@ -829,24 +1243,14 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     const size_t size = dtype == TSVD_F32 ? 4 : dtype == TSVD_BF16 ? 2 : 1, out_size = out_dtype == TSVD_F32 ? 4 : 2;
     if (off(x, size) || off(base, out_size) || off(out, out_size) || off(x_scale, 4) || off(slots, 4) || off(q_start, 4)) return TSVD_E_ALIGN;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
-    const tsvd_status_t grown = grow(h, z_bytes(h, n_rows));
-    if (grown != TSVD_OK) return grown;
     cudaStream_t st = (cudaStream_t)stream;
     const Rows rows{slots, q_start, n_seq, n_rows, h->n_slots, h->ranks, h->dev_status};
-    const Shape s = shape_of(h, n_rows);
     const size_t step = dtype == TSVD_I8 ? 8 : 16;
-    const DownParams d{rows, x, ldx, !off(x, step) && (n_rows == 1 || ldx * (long long)size % (long long)step == 0), h->N, h->chunks, s.splits, h->groups,
-                       h->A, h->a_slot, h->z};
-    if (dtype == TSVD_F32) TSVD_CUDA_OK(down_type<float>(d, s.wide, st));
-    else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_type<__nv_bfloat16>(d, s.wide, st));
-    else TSVD_CUDA_OK(down_type<int8_t>(d, s.wide, st));
-    tsvd_count_launch();
-
+    DownParams d{rows, x, ldx, !off(x, step) && (n_rows == 1 || ldx * (long long)size % (long long)step == 0), h->N, h->chunks, 0, h->groups,
+                 h->A, h->a_slot, nullptr};
     auto even = [&](const void* p, long long ld) { return !p || (!off(p, 16) && (n_rows == 1 || ld * (long long)out_size % 16 == 0)); };
     UpParams u{};
     u.rows = rows;
-    u.z = h->z;
-    u.splits = s.splits;
     u.groups = h->groups;
     u.scales = h->scales;
     u.x_scale = x_scale;
@@ -860,17 +1264,31 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     u.blocks = h->blocks;
     u.B = h->B;
     u.b_slot = h->b_slot;
+    if (const Few how = few_of(h, n_rows); how.cluster) {
+        const FewParams f{d, u, how.cluster, how.rows};
+        const unsigned tiles = (unsigned)((n_rows + how.rows - 1) / how.rows);
+        if (dtype == TSVD_F32) TSVD_CUDA_OK(few<float>(f, tiles, out_dtype == TSVD_F32, st));
+        else if (dtype == TSVD_BF16) TSVD_CUDA_OK(few<__nv_bfloat16>(f, tiles, out_dtype == TSVD_F32, st));
+        else TSVD_CUDA_OK(few<int8_t>(f, tiles, out_dtype == TSVD_F32, st));
+        tsvd_count_launch();
+        return TSVD_OK;
+    }
+    const tsvd_status_t grown = grow(h, z_bytes(h, n_rows));
+    if (grown != TSVD_OK) return grown;
+    const Shape s = shape_of(h, n_rows);
+    d.splits = u.splits = s.splits;
+    d.z = h->z;
+    u.z = h->z;
+    if (dtype == TSVD_F32) TSVD_CUDA_OK(down_type<float>(d, s.wide, st));
+    else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_type<__nv_bfloat16>(d, s.wide, st));
+    else TSVD_CUDA_OK(down_type<int8_t>(d, s.wide, st));
+    tsvd_count_launch();
+
+    // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
+    // with few rows there are few tiles.
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows > 256 ? 16 : 8;
-    const long long tiles = (n_rows + u.tile_rows - 1) / u.tile_rows;
-    // channel blocks a warp, so that there are about three blocks of threads an SM
-    u.per_warp = 1;
-    while (tiles * ((h->blocks + UP_WARPS * u.per_warp - 1) / (UP_WARPS * u.per_warp)) > 4LL * h->sms && u.per_warp < h->blocks) ++u.per_warp;
-    u.stages = h->groups == 1 ? (u.tile_rows == UP_ROWS ? 4 : 8) : h->groups == 2 ? 4 : 2;
-    const size_t smem = (size_t)UP_WARPS * u.stages * h->groups * 2048 + (size_t)((u.tile_rows + 15) / 16) * h->groups * (out_size == 2 ? 2 : 3) * 512;
-    PdlLaunch l((unsigned)tiles, UP_WARPS * 32, smem, st);
-    l.cfg.gridDim.y = (unsigned)((h->blocks + UP_WARPS * u.per_warp - 1) / (UP_WARPS * u.per_warp));
-    if (out_dtype == TSVD_F32) TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, adapter_up_kernel<float>, u));
-    else TSVD_CUDA_OK(cudaLaunchKernelEx(&l.cfg, adapter_up_kernel<__nv_bfloat16>, u));
+    if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_type<float>(u, h->sms, st));
+    else TSVD_CUDA_OK(up_type<__nv_bfloat16>(u, h->sms, st));
     tsvd_count_launch();
     return TSVD_OK;
 }
