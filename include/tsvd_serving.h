@@ -150,7 +150,8 @@ tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long 
 /* Scratch for calls of up to rows_max rows, so that none of them allocates. */
 tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max);
 tsvd_status_t tsvd_adapters_info(tsvd_adapters_t h, int* N, int* M, int* max_rank, int* n_slots, size_t* bytes);
-/* TSVD_E_INDEX if a slot number was out of range since the last read (synchronise first), else TSVD_OK. */
+/* Device status since the last read (synchronise first): TSVD_E_TIMEOUT if a bounded wait gave up (the results are then
+ * unspecified), else TSVD_E_INDEX if a slot number was out of range, else TSVD_OK. */
 tsvd_status_t tsvd_adapters_last_status(tsvd_adapters_t h);
 void tsvd_adapters_destroy(tsvd_adapters_t h);
 

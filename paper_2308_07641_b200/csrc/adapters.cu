@@ -29,11 +29,11 @@ struct tsvd_adapters_s {
     int chunks = 0, blocks = 0;      // of 32 columns of A, of 64 channels of B
     size_t a_slot = 0, b_slot = 0;   // bytes of a slot
     uint8_t* A = nullptr;            // [slot][chunk][its groups][2][32 lanes][16]
-    uint8_t* B = nullptr;            // [slot][block][its groups][4][32 lanes][16]
+    uint8_t* B = nullptr;            // [slot][block][its groups][2][64 rows][16]: see adapter_set_kernel
     int* ranks = nullptr;            // [slot], 0: empty
     float* scales = nullptr;         // [slot]
     int few[9] = {};                 // [1, 2, 4, 8]: clusters of so many blocks of the kernel for few rows that run at a time
-    float* z = nullptr;              // scratch: [split][row][16 * groups]
+    float* z = nullptr;              // scratch: [row][16 * groups]
     size_t z_bytes = 0;
     std::vector<void*>* outgrown = nullptr;   // scratch that captured graphs may still use
     int* dev_status = nullptr;
@@ -47,7 +47,7 @@ constexpr int BLOCK = 64;        // channels of B that a warp takes at a time
 constexpr int MAX_RANK = 128;
 constexpr int DOWN_WARPS = 8, UP_WARPS = 4;
 constexpr int UP_ROWS = 64;      // rows of a tile of the second kernel at most
-constexpr int MAX_SPLITS = 32;
+constexpr int MAX_SPLITS = 8;      // a cluster
 
 struct Rows {                    // which adapter a row has
     const int* slots;            // [n_seq]
@@ -155,13 +155,14 @@ __global__ void adapter_set_kernel(const T* A, long long lda, const T* B, long l
                                   pair_of(A, lda, r, c + 2, rank, N), pair_of(A, lda, r + 8, c + 2, rank, N));
         } else {
             const long long k = i - na;
-            const int lane = (int)(k & 31), quarter = (int)(k >> 5 & 3), n = lane >> 2, t = lane & 3;
+            const int row = (int)(k & 63), half = (int)(k >> 6 & 1);
             const long long piece = k >> 7;
             const int group = (int)(piece % groups), block = (int)(piece / groups);
-            // rows n and n + 8 of product q are channels 8 n + 2 q and the next: a lane's results are eight channels in a row
-            const int ch = block * BLOCK + 8 * n + 2 * quarter, r = group * GROUP + 4 * t;
-            b_out[k] = make_uint4(pair_of(B, ldb, ch, r, M, rank), pair_of(B, ldb, ch + 1, r, M, rank),
-                                  pair_of(B, ldb, ch, r + 2, M, rank), pair_of(B, ldb, ch + 1, r + 2, M, rank));
+            // Eight ranks of a row are 16 bytes, eight rows in a row what the tensor cores take as one matrix.  Row 8 j + n is channel
+            // 8 n + j: a lane (or a thread) gets its results as eight channels in a row.
+            const int ch = block * BLOCK + 8 * (row & 7) + (row >> 3), r = group * GROUP + 8 * half;
+            b_out[k] = make_uint4(pair_of(B, ldb, ch, r, M, rank), pair_of(B, ldb, ch, r + 2, M, rank), pair_of(B, ldb, ch, r + 4, M, rank),
+                                  pair_of(B, ldb, ch, r + 6, M, rank));
         }
     }
 }
@@ -181,7 +182,9 @@ struct DownParams {
 
 template <typename T> constexpr int kXBytes = 8 * (int)sizeof(T);    // of a lane: eight columns of a row
 template <typename T, int NT, int RG> constexpr int kDownStage = RG * 1024 + NT * 32 * kXBytes<T>;
-template <typename T, int NT, int RG> constexpr int kDownStages = 12 * 1024 / kDownStage<T, NT, RG> < 3 ? 3 : 12 * 1024 / kDownStage<T, NT, RG> > 8 ? 8 : 12 * 1024 / kDownStage<T, NT, RG>;
+// (as many as 16 KB a warp hold, 12 for few rows; with four groups and 32 rows the warps' parts take the rest)
+template <typename T, int NT, int RG> constexpr int kDownRoom = (NT == 1 ? 12 : RG == 4 ? 20 : 16) * 1024 / kDownStage<T, NT, RG>;
+template <typename T, int NT, int RG> constexpr int kDownStages = kDownRoom<T, NT, RG> < 2 ? 2 : kDownRoom<T, NT, RG> > 8 ? 8 : kDownRoom<T, NT, RG>;
 
 // Eight columns of a row as bf16 pairs: the terms of fp32 numbers one after another.
 template <typename T> struct Terms;
@@ -252,6 +255,8 @@ __device__ __forceinline__ void copy_x(uint8_t* dst, const void* m, long long ld
     }
 }
 
+constexpr int DOWN_GROUPS = 4;   // groups of ranks of a block at most (more are dealt to blocks of their own: the parts' place)
+
 // A block: 8 NT rows, a share of the columns; a warp every eighth chunk of 32 of them.  RG: groups of ranks at a time.
 template <typename T, int NT, int RG>
 __global__ void __launch_bounds__(DOWN_WARPS * 32)
@@ -265,18 +270,20 @@ adapter_down_kernel(const DownParams p)
     // What the kernel ahead has written is there before the next kernel starts: that one reads it ahead of its own wait.
     pdl_wait();
     pdl_launch_dependents();
-    const int row0 = blockIdx.x * ROWS, rank_pad = p.groups * GROUP;
+    const int row0 = blockIdx.x * ROWS, rank_pad = p.groups * GROUP, first_group = (int)blockIdx.z * DOWN_GROUPS;
+    const int here_pad = min(DOWN_GROUPS, p.groups - first_group) * GROUP;
     find_slots<ROWS, DOWN_WARPS>(p.rows, row0, slot_s);
     if (warp == 0) {
         const int slot = lane < ROWS ? slot_s[lane] : kNoRow;
         const unsigned same = __match_any_sync(0xffffffffu, slot);
-        const bool leads = slot >= 0 && lane == __ffs(same) - 1;
+        const int groups = slot >= 0 ? (p.rows.ranks[slot] + GROUP - 1) / GROUP : 0;
+        const bool leads = groups > first_group && lane == __ffs(same) - 1;
         const unsigned leaders = __ballot_sync(0xffffffffu, leads);
         if (leads) {
             const int e = __popc(leaders & ((1u << lane) - 1));
             entry_slot[e] = slot;
             entry_mask[e] = same;
-            entry_groups[e] = (p.rows.ranks[slot] + GROUP - 1) / GROUP;
+            entry_groups[e] = groups;
         }
         if (lane == 0) entries_s = __popc(leaders);
     }
@@ -284,43 +291,66 @@ adapter_down_kernel(const DownParams p)
     const int entries = entries_s;
     const int c0 = (int)((long long)p.chunks * blockIdx.y / p.splits), c1 = (int)((long long)p.chunks * (blockIdx.y + 1) / p.splits);
     uint8_t* ring = smem + (size_t)warp * STAGES * STAGE;
-    float* parts = reinterpret_cast<float*>(smem + (size_t)DOWN_WARPS * STAGES * STAGE);     // [warp][row][rank_pad]
+    float* parts = reinterpret_cast<float*>(smem + (size_t)DOWN_WARPS * STAGES * STAGE);     // [warp][row][here_pad]
 
     // ---- the next item (adapter, groups, chunk) into a stage ----
-    int fe = 0, fg = 0, fc = c0 + warp, fs = 0;
+    int fe = 0, fg = first_group, fc = c0 + warp, fs = 0, f_here = 0;
+    const uint8_t* fa = nullptr;
+    size_t f_step = 0;
+    unsigned f_mask = 0;
+    auto aim = [&]() {                       // at the first chunk of (adapter fe, groups from fg on)
+        const int groups = entry_groups[fe];
+        f_here = min(RG, min(groups, first_group + DOWN_GROUPS) - fg);
+        f_step = (size_t)groups * (DOWN_WARPS * 1024);
+        f_mask = entry_mask[fe];
+        fa = p.A + (size_t)entry_slot[fe] * p.a_slot + ((size_t)fc * groups + fg) * 1024 + lane * 16;
+    };
+    const T* xp = (const T*)p.x + (long long)(row0 + g) * p.ldx + 8 * t;
+    const long long ldx8 = 8 * p.ldx;
     auto fetch = [&]() {
         if (fe < entries && fc < c1) {
             uint8_t* to = ring + fs * STAGE;
-            const int groups = entry_groups[fe], here = min(RG, groups - fg);
-            const uint8_t* a = p.A + (size_t)entry_slot[fe] * p.a_slot + ((size_t)fc * groups + fg) * 1024 + lane * 16;
 #pragma unroll
             for (int i = 0; i < 2 * RG; ++i)
-                if (i < 2 * here) copy16(to + i * 512 + lane * 16, a + i * 512);
-            const unsigned mask = entry_mask[fe];
-            const int col = fc * CHUNK + 8 * t, left = p.N - col;
+                if (i < 2 * f_here) copy16(to + i * 512 + lane * 16, fa + i * 512);
+            const bool whole = p.aligned && (fc + 1) * CHUNK <= p.N && row0 + ROWS <= p.rows.n_rows;
+            const T* x = xp + fc * CHUNK;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (!(mask >> (8 * n) & 0xffu)) continue;
-                copy_x<T>(to + RG * 1024 + n * 32 * kXBytes<T>, p.x, p.ldx, row0 + 8 * n + g, p.rows.n_rows, col, left, p.aligned, lane);
+            for (int n = 0; n < NT; ++n, x += ldx8) {
+                if (NT > 1 && !(f_mask >> (8 * n) & 0xffu)) continue;
+                uint8_t* dst = to + RG * 1024 + n * 32 * kXBytes<T>;
+                if (whole) {
+                    if constexpr (sizeof(T) == 1) {
+                        copy8(dst + lane * 8, x, 8);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kXBytes<T> / 16; ++i) copy16(dst + i * 512 + lane * 16, x + i * (16 / (int)sizeof(T)));
+                    }
+                } else {
+                    copy_x<T>(dst, p.x, p.ldx, row0 + 8 * n + g, p.rows.n_rows, fc * CHUNK + 8 * t, p.N - fc * CHUNK - 8 * t, p.aligned, lane);
+                }
             }
             fc += DOWN_WARPS;
+            fa += f_step;
             if (fc >= c1) {
                 fc = c0 + warp;
                 fg += RG;
-                if (fg >= groups) { fg = 0; ++fe; }
+                if (fg >= min(entry_groups[fe], first_group + DOWN_GROUPS)) { fg = first_group; ++fe; }
+                if (fe < entries) aim();
             }
         }
         copies_commit();
         if (++fs == STAGES) fs = 0;
     };
+    if (entries > 0) aim();
     for (int i = 0; i < STAGES - 1; ++i) fetch();
 
     int stage = 0;
     if (c0 + warp < c1)
         for (int e = 0; e < entries; ++e) {
-            const int groups = entry_groups[e];
+            const int groups = min(entry_groups[e], first_group + DOWN_GROUPS);
             const unsigned mask = entry_mask[e];
-            for (int g0 = 0; g0 < groups; g0 += RG) {
+            for (int g0 = first_group; g0 < groups; g0 += RG) {
                 const int here = min(RG, groups - g0);
                 float acc[RG][NT][4];
 #pragma unroll
@@ -366,19 +396,45 @@ adapter_down_kernel(const DownParams p)
                         if (mask >> row & 1)
 #pragma unroll
                             for (int i = 0; i < RG; ++i)
-                                if (i < here) parts[(warp * ROWS + row) * rank_pad + (g0 + i) * GROUP + g + (k & 2 ? 8 : 0)] = acc[i][n][k];
+                                if (i < here) parts[(warp * ROWS + row) * here_pad + (g0 - first_group + i) * GROUP + g + (k & 2 ? 8 : 0)] = acc[i][n][k];
                     }
             }
         }
     copies_wait<0>();
     __syncthreads();
-    const int warps = min(DOWN_WARPS, c1 - c0);
-    for (int i = threadIdx.x; i < ROWS * rank_pad; i += DOWN_WARPS * 32) {
-        const int row = i / rank_pad, r = i - row * rank_pad, slot = slot_s[row];
+    // The blocks that share the contraction are a cluster: each adds its warps' parts, the first one gets them all (over its own
+    // warps' parts, which are read by then) and adds them in their order.
+    const int warps = min(DOWN_WARPS, c1 - c0), numbers = ROWS * here_pad;
+    float sums[(ROWS * DOWN_GROUPS * GROUP + DOWN_WARPS * 32 - 1) / (DOWN_WARPS * 32)];
+#pragma unroll
+    for (int j = 0; j < (int)(sizeof(sums) / sizeof(float)); ++j) {
+        const int i = (int)threadIdx.x + j * DOWN_WARPS * 32;
+        sums[j] = 0.0f;
+        if (i < numbers && slot_s[i / here_pad] >= 0)
+            for (int w = 0; w < warps; ++w) sums[j] += parts[w * numbers + i];
+    }
+    if (p.splits > 1) {
+        ptx::cluster_sync_all();
+        const uint32_t first = ptx::cluster_map_u32(ptx::smem_u32(parts + blockIdx.y * numbers), 0);
+#pragma unroll
+        for (int j = 0; j < (int)(sizeof(sums) / sizeof(float)); ++j) {
+            const int i = (int)threadIdx.x + j * DOWN_WARPS * 32;
+            if (i < numbers) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(first + 4u * (unsigned)i), "f"(sums[j]) : "memory");
+        }
+        ptx::cluster_sync_all();
+        if (blockIdx.y > 0) return;
+    }
+#pragma unroll
+    for (int j = 0; j < (int)(sizeof(sums) / sizeof(float)); ++j) {
+        const int i = (int)threadIdx.x + j * DOWN_WARPS * 32, row = i / here_pad, r = first_group * GROUP + i - row * here_pad;
+        if (i >= numbers) break;
+        const int slot = slot_s[row];
         if (slot < 0 || r >= p.rows.ranks[slot]) continue;
-        float sum = 0.0f;
-        for (int w = 0; w < warps; ++w) sum += parts[w * ROWS * rank_pad + i];
-        p.z[((size_t)blockIdx.y * p.rows.n_rows + row0 + row) * rank_pad + r] = sum;
+        if (p.splits > 1) {
+            sums[j] = 0.0f;
+            for (int k = 0; k < p.splits; ++k) sums[j] += parts[k * numbers + i];
+        }
+        p.z[(size_t)(row0 + row) * rank_pad + r] = sums[j];
     }
 }
 
@@ -387,7 +443,7 @@ adapter_down_kernel(const DownParams p)
 struct UpParams {
     Rows rows;
     const float* z;
-    int splits, groups;
+    int groups;
     const float* scales;     // [slot]
     const float* x_scale;    // [row] or null
     const void* base;        // null: zeros
@@ -416,73 +472,94 @@ template <typename T> struct Piece {
 #pragma unroll
         for (int i = 0; i < U; ++i) u[i] = reinterpret_cast<uint4*>(v)[i];
     }
-    __device__ __forceinline__ void store(T* at, int left, bool vec) const
+    __device__ __forceinline__ void store(T* at, int left) const
     {
-        if (vec && left >= 8) {
+        alignas(16) T v[8];
 #pragma unroll
-            for (int i = 0; i < U; ++i) reinterpret_cast<uint4*>(at)[i] = u[i];
-        } else {
-            alignas(16) T v[8];
+        for (int i = 0; i < U; ++i) reinterpret_cast<uint4*>(v)[i] = u[i];
 #pragma unroll
-            for (int i = 0; i < U; ++i) reinterpret_cast<uint4*>(v)[i] = u[i];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) at[i] = v[i];
-        }
-    }
-    // channels 2 q and 2 q + 1
-    __device__ __forceinline__ void add(int q, float a, float b)
-    {
-        if constexpr (sizeof(T) == 2) {
-            uint32_t& w = reinterpret_cast<uint32_t*>(u)[q];
-            w = rounded(__uint_as_float(w << 16) + a, __uint_as_float(w & 0xffff0000u) + b);
-        } else {
-            float* f = reinterpret_cast<float*>(u);
-            f[2 * q] += a;
-            f[2 * q + 1] += b;
-        }
+        for (int i = 0; i < 8; ++i)
+            if (i < left) at[i] = v[i];
     }
 };
-template <typename T> constexpr int kBaseBytes = 32 * 2 * 8 * (int)sizeof(T);    // of eight rows and 64 channels
+template <typename T> constexpr int kBaseBytes = 32 * 2 * 8 * (int)sizeof(T);    // base of eight rows and 64 channels
 
-// Base of rows 2 t and 2 t + 1 of eight and this lane's eight channels, into a stage: where `mask` has the row.
+// Base of rows 2 t and 2 t + 1 of eight and this lane's eight channels, into a stage: of the rows in `mask` (bits 0, 1).  at: the
+// first row's place; left: channels there; full (of the whole warp): all 64 channels, and rows on 16-byte boundaries.
 template <typename T>
-__device__ __forceinline__ void copy_base(uint8_t* dst, const UpParams& p, int row0, int ch, unsigned mask, int lane)
+__device__ __forceinline__ void copy_base(uint8_t* dst, const T* at, long long ld, unsigned mask, int left, bool full, int lane)
 {
-    const int t = lane & 3, left = p.M - ch;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        if (!(mask >> (2 * t + h) & 1) || left <= 0) continue;
-        const T* src = (const T*)p.base + (long long)(row0 + 2 * t + h) * p.ldb + ch;
+        const T* src = at + h * ld;
         uint8_t* to = dst + h * (Piece<T>::U * 512) + lane * 16;
-        if (p.base && p.vec && left >= 8) {
+        if (full) {
+            if (mask >> h & 1)
 #pragma unroll
-            for (int i = 0; i < Piece<T>::U; ++i) copy16(to + i * 512, src + i * (16 / (int)sizeof(T)));
-        } else {
+                for (int i = 0; i < Piece<T>::U; ++i) copy16(to + i * 512, src + i * (16 / (int)sizeof(T)));
+        } else if ((mask >> h & 1) && left > 0) {
             Piece<T> v;
-            v.load(src, p.base ? left : 0);
+            v.load(src, left);
 #pragma unroll
             for (int i = 0; i < Piece<T>::U; ++i) *reinterpret_cast<uint4*>(to + i * 512) = v.u[i];
         }
     }
 }
 
-// Base in a stage plus the product, to out; acc[q]: channels 2 q, 2 q + 1 (elements 0 and 2, 1 and 3) of rows 2 t, 2 t + 1.
+// The sums of a product of 64 channels and eight rows: acc[q] holds channels 2 q, 2 q + 1 (elements 0 and 2, 1 and 3) of this lane's
+// eight, of rows 2 t, 2 t + 1.  bf16: the tensor core adds to base; fp32, where its sums' last bits count, base is added afterwards.
 template <typename T>
-__device__ __forceinline__ void add_and_store(const uint8_t* from, const float (&acc)[4][4], const UpParams& p, int row0, int ch, unsigned mask, int lane)
-{
-    const int t = lane & 3, left = p.M - ch;
+struct Sums {
+    float acc[4][4];
+    uint4 base[sizeof(T) == 4 ? 4 : 1];
+    __device__ __forceinline__ void begin(const uint8_t* from, int lane)
+    {
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if ((mask >> (2 * t + h) & 1) && left > 0) {
-            Piece<T> v;
+            for (int h = 0; h < 2; ++h) {
+                const uint4 u = *reinterpret_cast<const uint4*>(from + h * 512 + lane * 16);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int i = 0; i < Piece<T>::U; ++i) v.u[i] = *reinterpret_cast<const uint4*>(from + h * (Piece<T>::U * 512) + i * 512 + lane * 16);
+                for (int q = 0; q < 4; ++q) { acc[q][h] = __uint_as_float(w[q] << 16); acc[q][2 + h] = __uint_as_float(w[q] & 0xffff0000u); }
+            }
+        } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v.add(q, acc[q][h], acc[q][2 + h]);
-            v.store((T*)p.out + (long long)(row0 + 2 * t + h) * p.ldo + ch, left, p.vec);
+            for (int i = 0; i < 4; ++i) base[i] = *reinterpret_cast<const uint4*>(from + i * 512 + lane * 16);
+            zero();
         }
-}
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[q][k] = 0.0f;
+    }
+    __device__ __forceinline__ void store(T* at, long long ld, unsigned mask, int left, bool full) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Piece<T> v;
+            if constexpr (sizeof(T) == 2) {
+                v.u[0] = make_uint4(rounded(acc[0][h], acc[0][2 + h]), rounded(acc[1][h], acc[1][2 + h]), rounded(acc[2][h], acc[2][2 + h]),
+                                    rounded(acc[3][h], acc[3][2 + h]));
+            } else {
+                const float* f = reinterpret_cast<const float*>(base + 2 * h);
+                float* y = reinterpret_cast<float*>(v.u);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { y[2 * q] = f[2 * q] + acc[q][h]; y[2 * q + 1] = f[2 * q + 1] + acc[q][2 + h]; }
+            }
+            T* to = at + h * ld;
+            if (full) {
+                if (mask >> h & 1)
+#pragma unroll
+                    for (int i = 0; i < Piece<T>::U; ++i) reinterpret_cast<uint4*>(to)[i] = v.u[i];
+            } else if (mask >> h & 1) {
+                v.store(to, left);
+            }
+        }
+    }
+};
 
 // z of eight rows and sixteen ranks as the product's second operand, a lane's rank quadruple of its row: TERMS pairs of words.
 template <int TERMS>
@@ -513,22 +590,32 @@ struct ZTerms {
     }
 };
 
-constexpr int UP_STAGES = 6;
+// Product q's first operand out of 16 ranks' weights of 64 channels: rows 16 q + g and + 8, this lane's rank quadruple.
+__device__ __forceinline__ uint4 b_rows(const uint8_t* at, int q, int lane)
+{
+    const uint8_t* from = at + (lane >> 1 & 1) * 1024 + (16 * q + (lane >> 2)) * 16 + (lane & 1) * 8;
+    const uint2 lo = *reinterpret_cast<const uint2*>(from), hi = *reinterpret_cast<const uint2*>(from + 128);
+    return make_uint4(lo.x, hi.x, lo.y, hi.y);
+}
 
-// A warp: 64 channels, whose weights (of one adapter) it holds in registers, eight rows after another of the block's tile; then the
+constexpr int UP_STAGES = 3;
+// Blocks of threads an SM: 102, 128, 168 or 255 registers a thread.
+template <typename T, int G> constexpr int kUpBlocks = G == 8 ? 2 : sizeof(T) == 2 ? (G == 4 ? 4 : 5) : G == 4 ? 3 : 4;
+
+// A warp: 64 channels, whose weights (of one adapter) it holds in registers, sixteen rows after another of the block's tile; then the
 // tile's next adapter; then its next 64 channels.  Weights and base are copied ahead into the warp's own shared memory.  G: groups
 // of ranks at most.
 template <typename T, int G>
-__global__ void __launch_bounds__(UP_WARPS * 32, G <= 4 ? 3 : 2)
+__global__ void __launch_bounds__(UP_WARPS * 32, kUpBlocks<T, G>)
 adapter_up_kernel(const UpParams p)
 {
     constexpr int TERMS = kTerms<T>, Z = 256 * TERMS;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int slot_s[UP_ROWS], entry_slot[UP_ROWS + 1], entry_groups[UP_ROWS + 1], steps_s;
-    // what is done for each 64 channels: (adapter, eight rows); behind the adapters the rows without one, whose base is copied
-    __shared__ unsigned char step_entry[2 * UP_ROWS], step_tile[2 * UP_ROWS], step_mask[2 * UP_ROWS];
+    // what is done for each 64 channels: (adapter, sixteen rows); behind the adapters the rows without one, whose base is copied
+    __shared__ unsigned step_s[2 * UP_ROWS];                                   // adapter | tile << 8 | rows << 16
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int row0 = blockIdx.x * p.tile_rows, tiles = (p.tile_rows + 7) / 8;
+    const int row0 = blockIdx.x * p.tile_rows, tiles = (p.tile_rows + 15) / 16;
     // Adapters, slots and base are there: the first kernel let this one start after its own wait.  z is behind this one's wait.
     {
         Rows mine = p.rows;
@@ -538,13 +625,11 @@ adapter_up_kernel(const UpParams p)
     if (warp == 0) {
         int a = slot_s[lane], b = slot_s[32 + lane], entries = 0, steps = 0;
         auto add = [&](int slot, unsigned in_a, unsigned in_b) {               // one adapter's rows
-            const unsigned in = lane < 4 ? in_a >> (8 * lane) & 0xffu : lane < 8 ? in_b >> (8 * (lane - 4)) & 0xffu : 0u;
+            const unsigned in = lane < 2 ? in_a >> (16 * lane) & 0xffffu : lane < 4 ? in_b >> (16 * (lane - 2)) & 0xffffu : 0u;
             const unsigned there = __ballot_sync(0xffffffffu, in != 0);
             if (in) {
                 const int k = steps + __popc(there & ((1u << lane) - 1));
-                step_entry[k] = (unsigned char)entries;
-                step_tile[k] = (unsigned char)lane;
-                step_mask[k] = (unsigned char)in;
+                step_s[k] = (unsigned)entries | (unsigned)lane << 8 | in << 16;
             }
             if (lane == 0) {
                 entry_slot[entries] = slot;
@@ -567,16 +652,27 @@ adapter_up_kernel(const UpParams p)
     }
     __syncthreads();
     const int steps = steps_s, b0 = (blockIdx.y * UP_WARPS + warp) * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
-    uint8_t* zs = smem;                                                        // [tile][group][Z]
-    uint8_t* weights = smem + tiles * p.groups * Z + warp * (p.groups * 2048 + UP_STAGES * kBaseBytes<T>);
+    uint8_t* zs = smem;                                                        // [eight rows][group][Z]
+    uint8_t* weights = smem + 2 * tiles * p.groups * Z + warp * (p.groups * 2048 + 2 * UP_STAGES * kBaseBytes<T>);
     uint8_t* ring = weights + p.groups * 2048;
 
     // ---- copies: base of the next (block, step); weights of the next (block, adapter) ----
+    const long long ldb8 = 8 * p.ldb, ldo8 = 8 * p.ldo;
+    auto rows16 = [](unsigned step, long long ld8) { return (step >> 8 & 1u ? 2 * ld8 : 0) + (step >> 9 & 1u ? 4 * ld8 : 0); };   // (tile 0 .. 3)
     int fb = b0, fk = 0, fs = 0;
+    const T* fbase = (const T*)p.base + (long long)(row0 + 2 * t) * p.ldb + b0 * BLOCK + 8 * g;
+    auto left_of = [&](int b) { return p.M - b * BLOCK - 8 * g; };
+    auto full_of = [&](int b) { return p.vec && (b + 1) * BLOCK <= p.M; };
     auto fetch = [&]() {
         if (fb < b1 && steps > 0) {
-            copy_base<T>(ring + fs * kBaseBytes<T>, p, row0 + 8 * step_tile[fk], fb * BLOCK + 8 * g, step_mask[fk], lane);
-            if (++fk == steps) { fk = 0; ++fb; }
+            const unsigned step = step_s[fk];
+            if (p.base) {
+                uint8_t* to = ring + fs * (2 * kBaseBytes<T>);
+                const T* from = fbase + rows16(step, ldb8);
+                copy_base<T>(to, from, p.ldb, step >> (16 + 2 * t), left_of(fb), full_of(fb), lane);
+                copy_base<T>(to + kBaseBytes<T>, from + ldb8, p.ldb, step >> (24 + 2 * t), left_of(fb), full_of(fb), lane);
+            }
+            if (++fk == steps) { fk = 0; ++fb; fbase += BLOCK; }
         }
         copies_commit();
         if (++fs == UP_STAGES) fs = 0;
@@ -584,7 +680,7 @@ adapter_up_kernel(const UpParams p)
     int wb = b0, wk = 0;                                                       // the step at which the weights on their way are needed
     auto fetch_weights = [&]() {                                               // (in the next group that is committed)
         if (wb >= b1 || steps == 0) return;
-        const int e = step_entry[wk], groups = entry_groups[e];
+        const int e = (int)(step_s[wk] & 0xffu), groups = entry_groups[e];
         if (groups) {
             const uint8_t* from = p.B + (size_t)entry_slot[e] * p.b_slot + (size_t)wb * groups * 2048 + lane * 16;
 #pragma unroll
@@ -593,29 +689,25 @@ adapter_up_kernel(const UpParams p)
         }
     };
     auto next_weights = [&]() {                                                // behind the adapter at (wb, wk)
-        const int e = step_entry[wk];
-        while (wk < steps && step_entry[wk] == e) ++wk;
+        const unsigned e = step_s[wk] & 0xffu;
+        while (wk < steps && (step_s[wk] & 0xffu) == e) ++wk;
         if (wk == steps) { wk = 0; ++wb; }
     };
     fetch_weights();
     for (int i = 0; i < UP_STAGES - 1; ++i) fetch();
 
-    // ---- z: the splits' sum, scaled, as bf16 terms in the order of the product's second operand ----
+    // ---- z, scaled, as bf16 terms in the order of the product's second operand ----
     pdl_wait();
     pdl_launch_dependents();
     const int rank_pad = p.groups * GROUP;
-    for (int i = threadIdx.x; i < tiles * p.groups * 32; i += UP_WARPS * 32) {
+    for (int i = threadIdx.x; i < 2 * tiles * p.groups * 32; i += UP_WARPS * 32) {
         const int ln = i & 31, group = (i >> 5) % p.groups, tile = (i >> 5) / p.groups;
         const int r = 8 * tile + (ln >> 2), slot = slot_s[r], first = group * GROUP + 4 * (ln & 3);
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         const int have = slot >= 0 ? p.rows.ranks[slot] - first : 0;           // z is written for the adapter's own ranks only
         if (have > 0) {
-            const float* z = p.z + (size_t)(row0 + r) * rank_pad + first;
-#pragma unroll 8
-            for (int s = 0; s < p.splits; ++s) {
-                const float4 u = __ldcg(reinterpret_cast<const float4*>(z + (size_t)s * p.rows.n_rows * rank_pad));
-                v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
-            }
+            const float4 u = __ldcg(reinterpret_cast<const float4*>(p.z + (size_t)(row0 + r) * rank_pad + first));
+            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
             const float c = p.scales[slot] * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = k < have ? v[k] * c : 0.0f;
@@ -628,47 +720,374 @@ adapter_up_kernel(const UpParams p)
 
     int stage = 0, since = UP_STAGES;                                          // since: groups committed after the weights'
     uint4 w[4 * G];
-    for (int b = b0; b < b1; ++b) {
+    T* out = (T*)p.out + (long long)(row0 + 2 * t) * p.ldo + b0 * BLOCK + 8 * g;
+    for (int b = b0; b < b1; ++b, out += BLOCK) {
         int last = -1, groups = 0;
+        const int left = left_of(b);
+        const bool full = full_of(b);
         for (int k = 0; k < steps; ++k) {
+            const unsigned step = step_s[k];
             // (a step's copies are one group, and UP_STAGES - 2 groups may follow the one that is needed)
             copies_wait<UP_STAGES - 2>();
-            const int e = step_entry[k];
-            if (e != last) {
-                last = e;
-                groups = entry_groups[e];
+            if ((int)(step & 0xffu) != last) {
+                last = (int)(step & 0xffu);
+                groups = entry_groups[last];
                 if (since < UP_STAGES - 1) copies_wait<0>();
+                __syncwarp();                                                  // (the other lanes' copies)
 #pragma unroll
                 for (int i = 0; i < 4 * G; ++i)
-                    if (i < 4 * groups) w[i] = *reinterpret_cast<const uint4*>(weights + i * 512 + lane * 16);
+                    w[i] = i < 4 * groups ? b_rows(weights + (i >> 2) * 2048, i & 3, lane) : make_uint4(0, 0, 0, 0);
+                __syncwarp();                                                  // (all have read)
                 next_weights();
                 fetch_weights();
                 since = 0;
             }
-            float acc[4][4];
+            Sums<T> sums[2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int n = 0; n < 2; ++n) {
+                if (p.base) sums[n].begin(ring + (2 * stage + n) * kBaseBytes<T>, lane);
+                else sums[n] = Sums<T>{};
+            }
+            const uint8_t* z_at = zs + 2 * (int)(step >> 8 & 0xffu) * p.groups * Z;
+            auto product = [&](int i) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[q][j] = 0.0f;
-            const int tile = step_tile[k];
-            const uint8_t* z_at = zs + tile * p.groups * Z;
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-                if (i < groups) {
+                for (int n = 0; n < 2; ++n) {
                     ZTerms<TERMS> z;
-                    z.get(z_at + i * Z, lane);
+                    z.get(z_at + (n * p.groups + i) * Z, lane);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int j = TERMS - 1; j >= 0; --j)
 #pragma unroll
-                        for (int j = TERMS - 1; j >= 0; --j) mma_bf16(acc[q], w[4 * i + q], z.w[j][0], z.w[j][1]);
+                        for (int q = 0; q < 4; ++q) mma_bf16(sums[n].acc[q], w[4 * i + q], z.w[j][0], z.w[j][1]);
                 }
-            add_and_store<T>(ring + stage * kBaseBytes<T>, acc, p, row0 + 8 * tile, b * BLOCK + 8 * g, step_mask[k], lane);
+            };
+            if (groups == G) {
+#pragma unroll
+                for (int i = 0; i < G; ++i) product(i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (i < groups) product(i);
+            }
+            T* to = out + rows16(step, ldo8);
+            sums[0].store(to, p.ldo, step >> (16 + 2 * t), left, full);
+            sums[1].store(to + ldo8, p.ldo, step >> (24 + 2 * t), left, full);
             fetch();
             ++since;
             if (++stage == UP_STAGES) stage = 0;
         }
     }
     copies_wait<0>();
+}
+
+// ---- the same for many rows, on tcgen05 --------------------------------------------------------------------------------------
+// A block: 128 rows, blocks of 64 channels one after another, of each the adapters that the rows ask for (a job).  D = Z B^T, 128 x 64,
+// in tensor memory, with the terms of z side by side along the contraction (128-byte swizzle, 64 ranks an atom) and the same
+// weights against each:
+//   warp 8     brings a job's weights into shared memory (in the order they lie in: one bulk copy), and issues its products
+//   warps 0-7  one row and 32 channels a thread: base, copied ahead into the warp's own place, plus D, by way of that place to out
+// Warp-level products of this size would set the pace: an m16n8k16 was measured to take some 28 clocks a scheduler here, a seventh of
+// which this form needs.
+
+constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32, MANY_D = 4, MANY_B = 3;   // accumulators of 64 columns; jobs whose weights are there or on their way
+
+// 32 lanes x 4 consecutive 32-bit columns.
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4])  // whole warp
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void umma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// kind::f16, both operands bf16 and K-major, fp32 sums
+__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// K-major without swizzle: eight rows of 16 bytes a matrix, the next eight rows 128 bytes on, the next eight ranks `apart`.
+__device__ __forceinline__ uint64_t umma_desc_k_plain(uint32_t smem_addr, uint32_t apart)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(apart >> 4) << 16;
+    d |= (uint64_t)(128u >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    return d;
+}
+
+// Shared memory (1024-aligned): Z [eight ranks of a term][128 rows][16 B] | B [MANY_B][groups][2 KB] | base [8 warps][stages][32 rows][32 channels],
+// the 16-byte unit u of row r turned by r (see unit_at)
+template <typename T>
+struct Many {
+    static constexpr int kPitch = BLOCK / 2 * (int)sizeof(T), kStage = 32 * kPitch, kStages = sizeof(T) == 2 ? 3 : 2;
+    // a row of 64 or 128 bytes: threads on neighbouring rows and the same unit, or on neighbouring units, meet no bank twice
+    __device__ static __forceinline__ int unit_at(int r, int u) { return r * kPitch + ((sizeof(T) == 2 ? u ^ (r >> 1 & 3) : u ^ (r & 7)) << 4); }
+    int groups;
+    __host__ __device__ int z_bytes() const { return kTerms<T> * groups * 2 * 2048; }
+    __host__ __device__ int b_bytes() const { return groups * 2048; }
+    __host__ __device__ int base() const { return z_bytes() + MANY_B * b_bytes(); }
+    __host__ __device__ size_t smem() const { return (size_t)base() + 8 * kStages * kStage + 1024; }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(MANY_THREADS, 2)
+adapter_many_kernel(const UpParams p)
+{
+    using namespace ptx;
+    using L = Many<T>;
+    constexpr int TERMS = kTerms<T>, E = 16 / (int)sizeof(T), LANES = 32 / E, PER = 32 / LANES;    // lanes of a row's 32 channels, rows at a time
+    const L lay{p.groups};
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    __shared__ uint64_t d_full[MANY_D], d_free[MANY_D], b_full[MANY_B], b_done[MANY_B], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int ctl_[2];
+    __shared__ int slot_s[MANY_ROWS], entry_slot[MANY_ROWS + 1], entries_s;
+    __shared__ unsigned char entry_groups[MANY_ROWS + 1];
+    __shared__ unsigned entry_mask[MANY_ROWS + 1][4];
+    volatile int* ctl = ctl_;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < MANY_D; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_free[i], 8); }
+        for (int i = 0; i < MANY_B; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_done[i], 1); }
+        mbar_init(&drained, 1);
+        ctl[0] = 0;
+        ctl[1] = kWaitLimitDefault;
+        fence_mbar_init();
+    }
+    // Tensor memory before the kernel after this one may start (see PdlLaunch).
+    if (warp == 8) { tmem_alloc(&tmem_slot, MANY_D * 64); tmem_relinquish(); }
+    const int row0 = blockIdx.x * MANY_ROWS;
+    // Adapters, slots and base are there: the first kernel let this one start after its own wait.  z is behind this one's wait.
+    find_slots<MANY_ROWS, MANY_THREADS / 32>(p.rows, row0, slot_s);
+    if (warp == 0) {
+        int slot[4], entries = 0;
+        unsigned rest[4], in[4] = {};
+        auto add = [&](int which) {
+            if (lane < 4) entry_mask[entries][lane] = lane == 0 ? in[0] : lane == 1 ? in[1] : lane == 2 ? in[2] : in[3];
+            if (lane == 0) {
+                entry_slot[entries] = which;
+                entry_groups[entries] = (unsigned char)(which < 0 ? 0 : (p.rows.ranks[which] + GROUP - 1) / GROUP);
+            }
+            ++entries;
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            slot[i] = slot_s[32 * i + lane];
+            rest[i] = __ballot_sync(0xffffffffu, slot[i] >= 0);
+        }
+        while (rest[0] | rest[1] | rest[2] | rest[3]) {
+            int which = 0;
+#pragma unroll
+            for (int i = 3; i >= 0; --i)
+                if (rest[i]) which = __shfl_sync(0xffffffffu, slot[i], __ffs(rest[i]) - 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                in[i] = __ballot_sync(0xffffffffu, slot[i] == which);
+                rest[i] &= ~in[i];
+            }
+            add(which);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) in[i] = __ballot_sync(0xffffffffu, slot[i] == kNoAdapter);
+        if ((in[0] | in[1] | in[2] | in[3]) && !p.in_place) add(kNoAdapter);     // rows without one: base is copied
+        if (lane == 0) entries_s = entries;
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    const int entries = entries_s, b0 = blockIdx.y * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
+
+    // ---- base of the next job into the warp's next stage: the rows in the adapter's mask, a row's 32 channels by LANES lanes ----
+    const int quarter = warp & 3, half = warp >> 2 & 1, mine0 = row0 + 32 * quarter;         // its rows (the tensor memory's lanes) and channels
+    uint8_t* place = smem + lay.base() + (warp & 7) * (L::kStages * L::kStage);
+    const int sub = lane / LANES, u = lane % LANES, ch_in = 32 * half + u * E;
+    int my_first = 0;            // the first adapter that the warp has rows of
+    while (my_first < entries && entry_mask[my_first][quarter] == 0) ++my_first;
+    int fb = b0, fe = my_first, fs = 0;
+    auto fetch = [&]() {
+        if (fb < b1 && my_first < entries) {
+            if (p.base) {
+                const unsigned mask = entry_mask[fe][quarter] >> sub;
+                const int ch = fb * BLOCK + ch_in, left = p.M - ch;
+                const T* from = (const T*)p.base + (long long)(mine0 + sub) * p.ldb + ch;
+                uint8_t* to = place + fs * L::kStage;
+                if (p.vec && (fb + 1) * BLOCK <= p.M) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
+                        if (mask >> i & 1) copy16(to + L::unit_at(i + sub, u), from);
+                } else {
+                    for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
+                        if (mask >> i & 1) {
+                            T* unit = reinterpret_cast<T*>(to + L::unit_at(i + sub, u));
+                            for (int e = 0; e < E; ++e) unit[e] = e < left ? from[e] : T(0.0f);
+                        }
+                }
+            }
+            do ++fe; while (fe < entries && entry_mask[fe][quarter] == 0);
+            if (fe == entries) { fe = my_first; ++fb; }
+        }
+        copies_commit();
+        if (++fs == L::kStages) fs = 0;
+    };
+    if (warp < 8)
+        for (int i = 0; i < L::kStages - 1; ++i) fetch();
+
+    // ---- z, scaled, as bf16 terms, each at its ranks behind those of the term before ----
+    pdl_launch_dependents();
+    pdl_wait();
+    // (four lanes take 32 ranks of a row, two its 16: between loads of whole lines and stores without conflicts)
+    const int rank_pad = p.groups * GROUP, eights = 2 * p.groups, wide = p.groups == 1 ? 2 : 4, across = (eights + wide - 1) / wide;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < MANY_ROWS * across * wide; i += MANY_THREADS) {
+        const int piece = i / (MANY_ROWS * wide), rest = i - piece * (MANY_ROWS * wide), r = rest / wide, eight = piece * wide + rest % wide;
+        if (eight >= eights) continue;
+        const int first = 8 * eight, slot = slot_s[r], have = slot >= 0 ? p.rows.ranks[slot] - first : 0;     // z is written for the adapter's own ranks only
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (have > 0) {
+            const float4* at = reinterpret_cast<const float4*>(p.z + (size_t)(row0 + r) * rank_pad + first);
+            const float4 lo = __ldcg(at), hi = __ldcg(at + 1);
+            const float c = p.scales[slot] * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
+            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k < have ? v[k] * c : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = k + 1 == TERMS ? rounded(v[2 * j], v[2 * j + 1]) : cut(v[2 * j], v[2 * j + 1]);
+            *reinterpret_cast<uint4*>(smem + (k * eights + eight) * 2048 + r * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    fence_proxy_async_smem();
+    __syncthreads();
+
+    bool ok = true;
+    if (warp == 8) {
+        // ================= weights and products =================
+        if (elect_one()) {
+            const int real = entries > 0 && entry_slot[entries - 1] == kNoAdapter ? entries - 1 : entries;
+            const uint64_t desc_z = umma_desc_k_plain(smem_u32(smem), 2048), desc_b = umma_desc_k_plain(smem_u32(smem + lay.z_bytes()), 1024);
+            constexpr uint32_t kDesc = idesc_bf16(MANY_ROWS, BLOCK);
+            int wb = b0, we = 0, wj = 0;                                       // the job whose weights are asked for next
+            auto ask = [&]() {
+                if (wb >= b1 || real == 0) return;
+                const int groups = entry_groups[we], buf = wj % MANY_B;
+                mbar_arrive_expect_tx(&b_full[buf], (uint32_t)groups * 2048);
+                bulk_g2s(smem + lay.z_bytes() + buf * lay.b_bytes(), p.B + (size_t)entry_slot[we] * p.b_slot + (size_t)wb * groups * 2048,
+                         (uint32_t)groups * 2048, &b_full[buf]);
+                ++wj;
+                if (++we == real) { we = 0; ++wb; }
+            };
+            for (int i = 0; i < MANY_B - 1; ++i) ask();
+            int job = 0;
+            for (int b = b0; b < b1 && ok; ++b)
+                for (int e = 0; e < real && ok; ++e, ++job) {
+                    const int buf = job % MANY_B, d = job % MANY_D, groups = entry_groups[e];
+                    // (the place of the job after next was the last one's)
+                    if (job > 0 && !(ok = mbar_wait(&b_done[(job - 1) % MANY_B], (uint32_t)((job - 1) / MANY_B & 1), ctl))) break;
+                    ask();
+                    if (!(ok = mbar_wait(&b_full[buf], (uint32_t)(job / MANY_B & 1), ctl))) break;
+                    if (!(ok = mbar_wait(&d_free[d], (uint32_t)(job / MANY_D & 1) ^ 1, ctl))) break;
+                    tc_fence_after_sync();
+                    const uint64_t weights = desc_b + (uint32_t)(buf * (lay.b_bytes() >> 4));
+                    for (int k = TERMS - 1; k >= 0; --k)
+                        for (int i = 0; i < groups; ++i)
+                            umma_bf16_ss(tmem + 64u * d, desc_z + (uint32_t)((k * p.groups + i) * (4096 >> 4)), weights + (uint32_t)(i * (2048 >> 4)), kDesc,
+                                         k != TERMS - 1 || i > 0);
+                    umma_commit(&b_done[buf]);
+                    umma_commit(&d_full[d]);
+                }
+            // every copy has landed and every product ended before the block does
+            if (!ok)
+                for (int i = 0; i < MANY_B; ++i)
+                    if (wj > i) mbar_drain(&b_full[i], (uint32_t)((wj - 1 - i) / MANY_B & 1));
+            umma_commit(&drained);
+            mbar_drain(&drained, 0);
+        }
+        __syncwarp();
+    } else {
+        // ================= rows: one a thread =================
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + 4u * half;
+        int job = 0, stage = 0;
+        for (int b = b0; b < b1 && ok; ++b)
+            for (int e = 0; e < entries && ok; ++e) {
+                const unsigned mask = entry_mask[e][quarter];
+                const bool real = entry_slot[e] != kNoAdapter;
+                uint32_t v[8][4] = {};                       // channel 8 n + j is column 8 j + n: [j][n % 4] of the half's n
+                if (real) {
+                    const int d = job % MANY_D;
+                    if (!(ok = mbar_wait_warp(&d_full[d], (uint32_t)(job / MANY_D & 1), ctl))) break;
+                    tc_fence_after_sync();
+                    if (mask) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) tmem_ld4(lanes + 64u * d + 8u * j, v[j]);
+                        tmem_ld_wait();
+                    }
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&d_free[d]);
+                    ++job;
+                }
+                if (mask == 0) continue;
+                uint8_t* here = place + stage * L::kStage;
+                copies_wait<L::kStages - 2>();
+                __syncwarp();
+                if (mask >> lane & 1) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+#pragma unroll
+                        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+                            uint4* unit = reinterpret_cast<uint4*>(here + L::unit_at(lane, n * ((int)sizeof(T) / 2) + h));
+                            uint4 x = p.base ? *unit : make_uint4(0, 0, 0, 0);
+                            uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if constexpr (sizeof(T) == 2)
+                                    w[k] = rounded(__uint_as_float(w[k] << 16) + __uint_as_float(v[2 * k][n]),
+                                                   __uint_as_float(w[k] & 0xffff0000u) + __uint_as_float(v[2 * k + 1][n]));
+                                else
+                                    w[k] = __float_as_uint(__uint_as_float(w[k]) + __uint_as_float(v[4 * h + k][n]));
+                            }
+                            *unit = x;
+                        }
+                    }
+                }
+                __syncwarp();
+                const int ch = b * BLOCK + ch_in, left = p.M - ch;
+                T* to = (T*)p.out + (long long)(mine0 + sub) * p.ldo + ch;
+                if (p.vec && (b + 1) * BLOCK <= p.M) {
+                    uint4 x[32 / PER];
+#pragma unroll
+                    for (int i = 0; i < 32; i += PER) x[i / PER] = *reinterpret_cast<const uint4*>(here + L::unit_at(i + sub, u));
+#pragma unroll
+                    for (int i = 0; i < 32; i += PER, to += PER * p.ldo)
+                        if (mask >> (i + sub) & 1) *reinterpret_cast<uint4*>(to) = x[i / PER];
+                } else {
+                    for (int i = 0; i < 32; i += PER, to += PER * p.ldo)
+                        if (mask >> (i + sub) & 1)
+                            for (int e = 0; e < E; ++e)
+                                if (e < left) to[e] = reinterpret_cast<const T*>(here + L::unit_at(i + sub, u))[e];
+                }
+                __syncwarp();
+                fetch();
+                if (++stage == L::kStages) stage = 0;
+            }
+        copies_wait<0>();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (threadIdx.x == 0 && ctl[0]) atomicOr(p.rows.status, KV4_DEV_TIMEOUT);
+    if (warp == 8) tmem_dealloc(tmem, MANY_D * 64);
 }
 
 // ---- both in one launch, for few rows ---------------------------------------------------------------------------------------
@@ -812,7 +1231,9 @@ adapter_few_kernel(const FewParams p)
             }
             unit += n;
             if (unit >= groups) {                            // with the block's last ones, base
-                copy_base<O>(to + st.weights, p.u, row0, run.at * BLOCK + 8 * g, entry_mask[run.e], lane);
+                if (p.u.base)
+                    copy_base<O>(to + st.weights, (const O*)p.u.base + (long long)(row0 + 2 * t) * p.u.ldb + run.at * BLOCK + 8 * g, p.u.ldb,
+                                 entry_mask[run.e] >> (2 * t), p.u.M - run.at * BLOCK - 8 * g, p.u.vec && (run.at + 1) * BLOCK <= p.u.M, lane);
                 unit = 0;
                 if (++run.at >= run.end) advance(run, true);
             }
@@ -920,27 +1341,44 @@ adapter_few_kernel(const FewParams p)
         const int groups = entry_groups[mine_up.e];
         const unsigned mask = entry_mask[mine_up.e];
         for (; mine_up.at < mine_up.end; ++mine_up.at) {
-            float acc[4][4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[q][k] = 0.0f;
+            Sums<O> sums;
+            sums.zero();
             int i = 0;
             do {
                 arrived();
+                __syncwarp();                                    // (weights are the other lanes' copies too)
                 const uint8_t* from = ring + stage * st.bytes;
                 const int n = min(st.units, groups - i);
+                if (i + n >= groups && p.u.base) {               // (the block's last stage brings base: what is there already is kept beside it)
+                    if constexpr (sizeof(O) == 4) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sums.base[k] = *reinterpret_cast<const uint4*>(from + st.weights + k * 512 + lane * 16);
+                    } else {
+                        Sums<O> b;
+                        b.begin(from + st.weights, lane);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) sums.acc[q][k] += b.acc[q][k];
+                    }
+                } else if (sizeof(O) == 4) {
+#pragma unroll
+                    for (int k = 0; k < (int)sizeof(O); ++k) sums.base[k < (int)(sizeof(sums.base) / 16) ? k : 0] = make_uint4(0, 0, 0, 0);
+                }
                 for (int c = 0; c < n; ++c, ++i) {
                     ZTerms<TERMS> z;
                     z.get(zs + i * Z, lane);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const uint4 w = *reinterpret_cast<const uint4*>(from + c * 2048 + q * 512 + lane * 16);
+                        const uint4 w = b_rows(from + c * 2048, q, lane);
 #pragma unroll
-                        for (int k = TERMS - 1; k >= 0; --k) mma_bf16(acc[q], w, z.w[k][0], z.w[k][1]);
+                        for (int k = TERMS - 1; k >= 0; --k) mma_bf16(sums.acc[q], w, z.w[k][0], z.w[k][1]);
                     }
                 }
-                if (i >= groups) add_and_store<O>(from + st.weights, acc, p.u, row0, mine_up.at * BLOCK + 8 * g, mask, lane);
+                if (i >= groups) {
+                    sums.store((O*)p.u.out + (long long)(row0 + 2 * t) * p.u.ldo + mine_up.at * BLOCK + 8 * g, p.u.ldo, mask >> (2 * t),
+                               p.u.M - mine_up.at * BLOCK - 8 * g, p.u.vec && (mine_up.at + 1) * BLOCK <= p.u.M);
+                }
                 done();
             } while (i < groups);
         }
@@ -956,7 +1394,7 @@ bool off(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; 
 template <typename T, int NT, int RG>
 size_t down_smem(int groups)
 {
-    return (size_t)DOWN_WARPS * (kDownStages<T, NT, RG> * kDownStage<T, NT, RG> + 8 * NT * groups * GROUP * sizeof(float));
+    return (size_t)DOWN_WARPS * (kDownStages<T, NT, RG> * kDownStage<T, NT, RG> + 8 * NT * (groups < DOWN_GROUPS ? groups : DOWN_GROUPS) * GROUP * sizeof(float));
 }
 
 template <typename T, int NT, int RG>
@@ -970,16 +1408,23 @@ cudaError_t prepare_type()
     cudaError_t e = prepare_down<T, 1, 1>();
     if (e == cudaSuccess) e = prepare_down<T, 1, 2>();
     if (e == cudaSuccess) e = prepare_down<T, 1, 4>();
-    if (e == cudaSuccess) e = prepare_down<T, 2, 1>();
-    if (e == cudaSuccess) e = prepare_down<T, 2, 2>();
-    if (e == cudaSuccess) e = prepare_down<T, 2, 4>();
+    if (e == cudaSuccess) e = prepare_down<T, 4, 1>();
+    if (e == cudaSuccess) e = prepare_down<T, 4, 2>();
+    if (e == cudaSuccess) e = prepare_down<T, 4, 4>();
     return e;
 }
 template <typename T, int NT, int RG>
 cudaError_t down(const DownParams& p, cudaStream_t st)
 {
     PdlLaunch l((unsigned)((p.rows.n_rows + 8 * NT - 1) / (8 * NT)), DOWN_WARPS * 32, down_smem<T, NT, RG>(p.groups), st);
+    cudaLaunchAttribute attr[2] = {l.attr[0], {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.y = (unsigned)p.splits;
+    l.cfg.attrs = attr;
+    l.cfg.numAttrs = p.splits > 1 ? 2 : 1;
     l.cfg.gridDim.y = (unsigned)p.splits;
+    l.cfg.gridDim.z = (unsigned)(p.groups + DOWN_GROUPS - 1) / DOWN_GROUPS;
     return cudaLaunchKernelEx(&l.cfg, adapter_down_kernel<T, NT, RG>, p);
 }
 
@@ -987,7 +1432,7 @@ template <typename T>
 cudaError_t down_type(const DownParams& p, bool wide, cudaStream_t st)
 {
     const int rg = p.groups == 1 ? 1 : p.groups == 2 ? 2 : 4;
-    if (wide) return rg == 1 ? down<T, 2, 1>(p, st) : rg == 2 ? down<T, 2, 2>(p, st) : down<T, 2, 4>(p, st);
+    if (wide) return rg == 1 ? down<T, 4, 1>(p, st) : rg == 2 ? down<T, 4, 2>(p, st) : down<T, 4, 4>(p, st);
     return rg == 1 ? down<T, 1, 1>(p, st) : rg == 2 ? down<T, 1, 2>(p, st) : down<T, 1, 4>(p, st);
 }
 
@@ -1041,15 +1486,16 @@ cudaError_t prepare()
     for (const void* kernel : {(const void*)adapter_up_kernel<float, 1>, (const void*)adapter_up_kernel<float, 2>, (const void*)adapter_up_kernel<float, 4>,
                                (const void*)adapter_up_kernel<float, 8>, (const void*)adapter_up_kernel<__nv_bfloat16, 1>,
                                (const void*)adapter_up_kernel<__nv_bfloat16, 2>, (const void*)adapter_up_kernel<__nv_bfloat16, 4>,
-                               (const void*)adapter_up_kernel<__nv_bfloat16, 8>})
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+                               (const void*)adapter_up_kernel<__nv_bfloat16, 8>, (const void*)adapter_many_kernel<float>,
+                               (const void*)adapter_many_kernel<__nv_bfloat16>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
     return e;
 }
 
 template <typename T, int G>
 cudaError_t up(const UpParams& p, unsigned tiles, unsigned columns, cudaStream_t st)
 {
-    const size_t smem = (size_t)(p.tile_rows + 7) / 8 * p.groups * 256 * kTerms<T> + (size_t)UP_WARPS * (p.groups * 2048 + UP_STAGES * kBaseBytes<T>);
+    const size_t smem = (size_t)(p.tile_rows + 15) / 16 * 2 * p.groups * 256 * kTerms<T> + (size_t)UP_WARPS * (p.groups * 2048 + 2 * UP_STAGES * kBaseBytes<T>);
     PdlLaunch l(tiles, UP_WARPS * 32, smem, st);
     l.cfg.gridDim.y = columns;
     return cudaLaunchKernelEx(&l.cfg, adapter_up_kernel<T, G>, p);
@@ -1058,26 +1504,40 @@ cudaError_t up(const UpParams& p, unsigned tiles, unsigned columns, cudaStream_t
 template <typename T>
 cudaError_t up_type(UpParams& p, int sms, cudaStream_t st)
 {
-    // Channel blocks a warp: so many that the blocks run in one round, three an SM (they read z again each).
+    // Channel blocks a warp: so many that the blocks run in one round, three or four an SM (they read z again each).
+    const int at_once = (p.groups <= 2 ? 4 : 3) * sms;
     const int tiles = (p.rows.n_rows + p.tile_rows - 1) / p.tile_rows;
     auto columns = [&] { return (p.blocks + UP_WARPS * p.per_warp - 1) / (UP_WARPS * p.per_warp); };
     p.per_warp = 1;
-    while ((long long)tiles * columns() > 3LL * sms && p.per_warp < p.blocks) ++p.per_warp;
+    while ((long long)tiles * columns() > at_once && p.per_warp < p.blocks) ++p.per_warp;
     const unsigned x = (unsigned)tiles, y = (unsigned)columns();
     return p.groups == 1 ? up<T, 1>(p, x, y, st) : p.groups == 2 ? up<T, 2>(p, x, y, st) : p.groups <= 4 ? up<T, 4>(p, x, y, st) : up<T, 8>(p, x, y, st);
 }
 
+template <typename T>
+cudaError_t many(UpParams& p, int sms, cudaStream_t st)
+{
+    // Blocks of channels of a block of threads: so many that all run in one round.
+    const Many<T> lay{p.groups};
+    const int tiles = (p.rows.n_rows + MANY_ROWS - 1) / MANY_ROWS, at_once = (lay.smem() <= 109 * 1024 ? 2 : 1) * sms;
+    p.per_warp = (int)(((long long)p.blocks * tiles + at_once - 1) / at_once);
+    while ((long long)tiles * ((p.blocks + p.per_warp - 1) / p.per_warp) > at_once && p.per_warp < p.blocks) ++p.per_warp;
+    PdlLaunch l((unsigned)tiles, MANY_THREADS, lay.smem(), st);
+    l.cfg.gridDim.y = (unsigned)((p.blocks + p.per_warp - 1) / p.per_warp);
+    return cudaLaunchKernelEx(&l.cfg, adapter_many_kernel<T>, p);
+}
+
 struct Shape {
-    bool wide;           // the first kernel's tiles have 16 rows, else 8
+    bool wide;           // the first kernel's tiles have 32 rows, else 8
     int splits;          // blocks that share a contraction
 };
 Shape shape_of(const tsvd_adapters_s* h, int rows)
 {
     Shape s;
-    s.wide = rows >= 1024;
-    const int tiles = (rows + (s.wide ? 15 : 7)) / (s.wide ? 16 : 8);
-    // two blocks an SM, a chunk for every warp
-    const int want = (2 * h->sms + tiles - 1) / tiles, most = (h->chunks + DOWN_WARPS - 1) / DOWN_WARPS;
+    s.wide = rows >= 256;
+    const int tiles = (rows + (s.wide ? 31 : 7)) / (s.wide ? 32 : 8);
+    // wide: one block an SM, in one round; else two; a chunk for every warp
+    const int want = s.wide ? (h->sms > tiles ? h->sms / tiles : 1) : (2 * h->sms + tiles - 1) / tiles, most = (h->chunks + DOWN_WARPS - 1) / DOWN_WARPS;
     s.splits = want < most ? want : most;
     if (s.splits > MAX_SPLITS) s.splits = MAX_SPLITS;
     return s;
@@ -1085,6 +1545,7 @@ Shape shape_of(const tsvd_adapters_s* h, int rows)
 // How the kernel for few rows serves a call of so many, if it does (else cluster = 0): clusters of as many blocks as have a chunk
 // or a block of channels for each of their warps, eight at most, or half or a quarter of that where this lets more blocks run; as few
 // rows each as are served by the clusters that run at a time (a second round would cost what the other kernels' second launch does).
+constexpr int MANY_FROM = 512, MANY_EACH = 64;
 struct Few { int cluster, rows; };
 Few few_of(const tsvd_adapters_s* h, int rows)
 {
@@ -1103,7 +1564,7 @@ Few few_of(const tsvd_adapters_s* h, int rows)
         }
     return best;
 }
-size_t z_bytes(const tsvd_adapters_s* h, int rows) { return few_of(h, rows).cluster ? 0 : (size_t)shape_of(h, rows).splits * rows * h->groups * GROUP * sizeof(float); }
+size_t z_bytes(const tsvd_adapters_s* h, int rows) { return few_of(h, rows).cluster ? 0 : (size_t)rows * h->groups * GROUP * sizeof(float); }
 
 tsvd_status_t grow(tsvd_adapters_s* h, size_t need)
 {
@@ -1219,14 +1680,8 @@ extern "C" tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max)
     if (!h) return TSVD_E_NULL;
     if (rows_max < 1) return TSVD_E_SHAPE;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
-    // (fewer rows may be cut into more splits: the most that any number of rows up to rows_max takes)
-    size_t need = z_bytes(h, rows_max);
-    for (int rows = 8; rows < rows_max; rows += 8) {
-        const size_t n = z_bytes(h, rows);
-        if (n > need) need = n;
-        if (shape_of(h, rows).splits == 1 && rows >= 1024) break;
-    }
-    return grow(h, need);
+    const size_t need = (size_t)rows_max * h->groups * GROUP * sizeof(float);
+    return few_of(h, rows_max).cluster ? TSVD_OK : grow(h, need);
 }
 
 extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
@@ -1276,7 +1731,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     const tsvd_status_t grown = grow(h, z_bytes(h, n_rows));
     if (grown != TSVD_OK) return grown;
     const Shape s = shape_of(h, n_rows);
-    d.splits = u.splits = s.splits;
+    d.splits = s.splits;
     d.z = h->z;
     u.z = h->z;
     if (dtype == TSVD_F32) TSVD_CUDA_OK(down_type<float>(d, s.wide, st));
@@ -1287,7 +1742,12 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
     // with few rows there are few tiles.
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows > 256 ? 16 : 8;
-    if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_type<float>(u, h->sms, st));
+    // tcgen05 from 512 rows on, where a tile of 128 holds few adapters, as far as the number of sequences tells (each is a job of its
+    // own for the whole tile): 2048 rows of four sequences, ranks of 64, 12288 channels 26 us against 62; 1000 rows of fifty 42 against 26.
+    if (n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH) {
+        if (out_dtype == TSVD_F32) TSVD_CUDA_OK(many<float>(u, h->sms, st));
+        else TSVD_CUDA_OK(many<__nv_bfloat16>(u, h->sms, st));
+    } else if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_type<float>(u, h->sms, st));
     else TSVD_CUDA_OK(up_type<__nv_bfloat16>(u, h->sms, st));
     tsvd_count_launch();
     return TSVD_OK;
@@ -1312,7 +1772,7 @@ extern "C" tsvd_status_t tsvd_adapters_last_status(tsvd_adapters_t h)
     TSVD_CUDA_OK(cudaMemcpy(&word, h->dev_status, sizeof(int), cudaMemcpyDeviceToHost));
     if (word) TSVD_CUDA_OK(cudaMemset(h->dev_status, 0, sizeof(int)));
     if (word) TSVD_CUDA_OK(cudaStreamSynchronize(nullptr));      // other streams do not wait for the memset
-    return word ? TSVD_E_INDEX : TSVD_OK;
+    return (word & KV4_DEV_TIMEOUT) ? TSVD_E_TIMEOUT : word ? TSVD_E_INDEX : TSVD_OK;
 }
 
 extern "C" void tsvd_adapters_destroy(tsvd_adapters_t h)
