@@ -245,7 +245,28 @@ __device__ __forceinline__ void turn16(const T* head, int d0, const Turn& t, con
     }
 }
 
-template <typename T, bool VEC, int D, bool FAST>
+// Numbers d0 .. d0 + 15 and their partners half a rotation on, turned: one reading of either, of cosines and of sines.
+template <typename T, bool VEC>
+__device__ __forceinline__ void turn_both(const T* head, int d0, int half, const float* cosines, float (&x)[16], float (&y)[16])
+{
+#pragma unroll
+    for (int h = 0; h < 16; h += 8) {
+        float u[8], v[8], c[8], s[8];
+        load8<T, VEC>(head + d0 + h, u);
+        load8<T, VEC>(head + d0 + half + h, v);
+        load8<float, true>(cosines + d0 + h, c);
+        load8<float, true>(cosines + half + d0 + h, s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[h + i] = __fsub_rn(__fmul_rn(u[i], c[i]), __fmul_rn(v[i], s[i]));
+            y[h + i] = __fadd_rn(__fmul_rn(v[i], c[i]), __fmul_rn(u[i], s[i]));
+        }
+    }
+}
+
+// A block takes a row, a warp 32 items of its keys, values or queries.  FAST: see turn16.  WHOLE: as FAST, and all of a head is turned,
+// half against half: a thread takes sixteen numbers of either half, so that nothing is read twice.
+template <typename T, bool VEC, int D, bool FAST, bool WHOLE>
 __global__ void __launch_bounds__(512)
 kv4_append_rotated_kernel(Kv4Geom g, Kv4Batch b, Turn turn, const T* q, long long ldq, T* q_out, long long ldqo, int n_heads, const T* k,
                           long long ldk, const T* v, long long ldv, int* status)
@@ -265,38 +286,50 @@ kv4_append_rotated_kernel(Kv4Geom g, Kv4Batch b, Turn turn, const T* q, long lon
     __syncthreads();
     const Place at = place_s;
     if (!at.row) return;
-    const int lane = threadIdx.x & 31, items = g.heads * (D / 8), q_items = n_heads * (D / 16);
-    const int kv_warps = (items + 31) / 32, warps = kv_warps + (q_items + 31) / 32;
+    const int lane = threadIdx.x & 31;
     const bool known = at.pos >= 0 && at.pos < turn.positions;
     const float* cosines = turn.table + (size_t)(known ? at.pos : 0) * turn.turned;
+    constexpr int BOTH = WHOLE ? 32 : 16;                      // numbers of an item of keys or queries
+    const int k_items = g.heads * (D / BOTH), v_items = g.heads * (D / 16), q_items = n_heads * (D / BOTH);
+    const int k_warps = (k_items + 31) / 32, v_warps = (v_items + 31) / 32, warps = k_warps + v_warps + (q_items + 31) / 32;
     for (int w = threadIdx.x >> 5; w < warps; w += blockDim.x >> 5) {
-        float x[16];
-        if (w < kv_warps) {
+        float x[16], y[16];
+        if (w < k_warps + v_warps) {
             if (at.page < 0) continue;
-            const bool in = w * 32 + lane < items;             // (whole warps take part in the exchange)
-            const int u = in ? w * 32 + lane : items - 1;
-            const Item<D> t(2 * u, g.heads), t1(2 * u + 1, g.heads);
-            if (t.is_v) {
-                const T* src = v + row * ldv + t.head * D + t.word * 8;
+            const bool is_v = w >= k_warps;
+            const int u0 = (is_v ? w - k_warps : w) * 32 + lane, items = is_v ? v_items : k_items;
+            const bool in = u0 < items;                        // (whole warps take part in the exchange)
+            const int u = in ? u0 : items - 1;
+            if (is_v) {
+                const Item<D> t(2 * (v_items + u), g.heads), t1(2 * (v_items + u) + 1, g.heads);
+                const T* src = v + row * ldv + u * 16;
                 load8<T, VEC>(src, reinterpret_cast<float (&)[8]>(x[0]));
                 load8<T, VEC>(src + 8, reinterpret_cast<float (&)[8]>(x[8]));
+                keep16<D>(g, at, t, t1, x, in);
             } else {
-                turn16<T, VEC, FAST>(k + row * ldk + t.head * D, t.word * 8, turn, cosines, x);
+                const int head = u / (D / BOTH), d0 = u % (D / BOTH) * 16, first = head * (D / 8) + d0 / 8;
+                if constexpr (WHOLE) turn_both<T, VEC>(k + row * ldk + head * D, d0, D / 2, cosines, x, y);
+                else turn16<T, VEC, FAST>(k + row * ldk + head * D, d0, turn, cosines, x);
+                keep16<D>(g, at, Item<D>(first, g.heads), Item<D>(first + 1, g.heads), x, in);
+                if constexpr (WHOLE) keep16<D>(g, at, Item<D>(first + D / 16, g.heads), Item<D>(first + D / 16 + 1, g.heads), y, in);
             }
-            keep16<D>(g, at, t, t1, x, in);
         } else {
-            const int u = (w - kv_warps) * 32 + lane;
+            const int u = (w - k_warps - v_warps) * 32 + lane;
             if (u >= q_items) continue;
-            const int head = u / (D / 16), d0 = u % (D / 16) * 16;
-            if (known) {
-                turn16<T, VEC, FAST>(q + row * ldq + head * D, d0, turn, cosines, x);
-            } else {
+            const int head = u / (D / BOTH), d0 = u % (D / BOTH) * 16;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+            for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+            if (known) {
+                if constexpr (WHOLE) turn_both<T, VEC>(q + row * ldq + head * D, d0, D / 2, cosines, x, y);
+                else turn16<T, VEC, FAST>(q + row * ldq + head * D, d0, turn, cosines, x);
             }
             T* to = q_out + row * ldqo + head * D + d0;
             store8<T, VEC>(to, reinterpret_cast<float (&)[8]>(x[0]));
             store8<T, VEC>(to + 8, reinterpret_cast<float (&)[8]>(x[8]));
+            if constexpr (WHOLE) {
+                store8<T, VEC>(to + D / 2, reinterpret_cast<float (&)[8]>(y[0]));
+                store8<T, VEC>(to + D / 2 + 8, reinterpret_cast<float (&)[8]>(y[8]));
+            }
         }
     }
 }
@@ -472,7 +505,9 @@ extern "C" tsvd_status_t tsvd_kv4_append_rotated(tsvd_kv4_t h, const void* q, lo
     // (neighbours: eight angles of an item; halves: sixteen)
     const bool fast = ((uintptr_t)table & 15) == 0 && turned % (interleaved ? 16 : 32) == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    const long long items = (long long)(h->g.heads * (h->g.dim / 8) + 31) / 32 + ((long long)n_heads * (h->g.dim / 16) + 31) / 32;
+    const bool whole = vec && fast && !interleaved && turned == h->g.dim;
+    const int both = whole ? 32 : 16;
+    const long long items = (h->g.heads * (h->g.dim / both) + 31) / 32 + (h->g.heads * (h->g.dim / 16) + 31) / 32 + (n_heads * (h->g.dim / both) + 31) / 32;
     cudaError_t e = cudaSuccess;
     auto go = [&](auto kernel, auto* kp) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
@@ -482,15 +517,17 @@ extern "C" tsvd_status_t tsvd_kv4_append_rotated(tsvd_kv4_t h, const void* q, lo
     auto by_type = [&](auto* kp) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(kp)>>;
         if (h->g.dim == 128) {
-            if (vec && fast) go(kv4_append_rotated_kernel<T, true, 128, true>, kp);
-            else if (vec) go(kv4_append_rotated_kernel<T, true, 128, false>, kp);
-            else if (fast) go(kv4_append_rotated_kernel<T, false, 128, true>, kp);
-            else go(kv4_append_rotated_kernel<T, false, 128, false>, kp);
+            if (whole) go(kv4_append_rotated_kernel<T, true, 128, true, true>, kp);
+            else if (vec && fast) go(kv4_append_rotated_kernel<T, true, 128, true, false>, kp);
+            else if (vec) go(kv4_append_rotated_kernel<T, true, 128, false, false>, kp);
+            else if (fast) go(kv4_append_rotated_kernel<T, false, 128, true, false>, kp);
+            else go(kv4_append_rotated_kernel<T, false, 128, false, false>, kp);
         } else {
-            if (vec && fast) go(kv4_append_rotated_kernel<T, true, 64, true>, kp);
-            else if (vec) go(kv4_append_rotated_kernel<T, true, 64, false>, kp);
-            else if (fast) go(kv4_append_rotated_kernel<T, false, 64, true>, kp);
-            else go(kv4_append_rotated_kernel<T, false, 64, false>, kp);
+            if (whole) go(kv4_append_rotated_kernel<T, true, 64, true, true>, kp);
+            else if (vec && fast) go(kv4_append_rotated_kernel<T, true, 64, true, false>, kp);
+            else if (vec) go(kv4_append_rotated_kernel<T, true, 64, false, false>, kp);
+            else if (fast) go(kv4_append_rotated_kernel<T, false, 64, true, false>, kp);
+            else go(kv4_append_rotated_kernel<T, false, 64, false, false>, kp);
         }
     };
     if (dtype == TSVD_F32) by_type((const float*)k);

@@ -282,9 +282,10 @@ kv4_prefill_kernel(const PreParams p)
         }
     }
     // With first positions that stay visible, the pair's tiles [0, front) and those from its window's first on are counted as one
-    // run: what is left out between them, `gap` tiles, is added where a tile becomes positions.  Both row tiles take the run from
-    // its start (the steps that only the other one's window holds are hidden row by row).
-    int front = 0, gap = 0;
+    // run: what is left out between them, `gap` tiles, is added where a tile becomes positions.  Steps from 2 front up to skip[x] of
+    // that run are hidden from row tile x (the other one's window begins earlier): it leaves them out, an even number of them, so
+    // that its steps go on taking turns at the two score buffers.
+    int front = 0, gap = 0, skip[2] = {0, 0};
     if constexpr (SINKS) {
         const int ends = max(t_hi[0], t_hi[1]);
         int from = ends;
@@ -295,10 +296,12 @@ kv4_prefill_kernel(const PreParams p)
         gap = max(0, from / 2 - front);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+            skip[x] = t_hi[x] > 0 ? max(2 * front, min((t_lo[x] & ~1) - 2 * gap, t_hi[x] - 2 * gap & ~1)) : 2 * front;
             t_lo[x] = 0;
             t_hi[x] = min(t_hi[x], max(2 * front, t_hi[x] - 2 * gap));
         }
     }
+    auto left_out = [&](int x, int k) { return SINKS && k >= 2 * front && k < (x ? skip[1] : skip[0]); };
     const bool one = t_hi[1] == t_lo[1], none = t_hi[0] == t_lo[0];
     const int j_lo = none ? t_lo[1] : one ? t_lo[0] : min(t_lo[0], t_lo[1]);
     int j_hi = none ? t_hi[1] : one ? t_hi[0] : max(t_hi[0], t_hi[1]);
@@ -314,6 +317,14 @@ kv4_prefill_kernel(const PreParams p)
         }
         j_hi = max(t_hi[0], t_hi[1]);
         if (t_hi[0] == t_lo[0] && t_hi[1] == t_lo[1]) k_hi = k_lo;
+    }
+    if constexpr (SINKS) {
+        // a share's steps neither begin nor end with ones that are left out
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (left_out(x, t_lo[x])) t_lo[x] = min(skip[x], t_hi[x]);
+            if (t_hi[x] > t_lo[x] && left_out(x, t_hi[x] - 1)) t_hi[x] = max(2 * front, t_lo[x]);
+        }
     }
 
     if (warp < 8) {
@@ -372,6 +383,7 @@ kv4_prefill_kernel(const PreParams p)
         bool ok = true;
         const int a = x ? t_lo[1] : t_lo[0], b = x ? t_hi[1] : t_hi[0];
         for (int k = a; k < b; ++k) {
+            if (SINKS && left_out(x, k)) k = x ? skip[1] : skip[0];
             const int h = k & 1, at = (SINKS && k >= 2 * front ? k + 2 * gap : k) * PRE_STEP;
             ok = mbar_wait(&s_full[x][h], phs >> h & 1, ctl);   // (the warp agrees on it where it looks at `over`)
             phs ^= 1u << h;
@@ -617,14 +629,14 @@ kv4_prefill_kernel(const PreParams p)
                     tc_fence_after_sync();
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
-                        if (n >= t_lo[x] && n < t_hi[x]) scores(x, n);
+                        if (n >= t_lo[x] && n < t_hi[x] && !left_out(x, n)) scores(x, n);
                     if (n & 1) umma_commit(&k_empty[((n >> 1) - k_lo) & 1]);
                 }
                 if (j < 2 * k_lo) continue;
                 if (!(j & 1) && !(ok = mbar_wait(&v_full[((j >> 1) - k_lo) & 1], (uint32_t)((j >> 1) - k_lo) >> 1 & 1, ctl))) break;
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                    if (j >= t_lo[x] && j < t_hi[x]) {
+                    if (j >= t_lo[x] && j < t_hi[x] && !left_out(x, j)) {
                         if (!(ok = mbar_wait(&p_full[x][j & 1], pph[x] >> (j & 1) & 1, ctl))) break;
                         pph[x] ^= 1u << (j & 1);
                         tc_fence_after_sync();
