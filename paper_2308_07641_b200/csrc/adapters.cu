@@ -100,6 +100,15 @@ __device__ __forceinline__ void copy16(void* to, const void* from, int bytes = 1
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
 }
+// (shared addresses of 32 bits, and sixteen bytes for certain: the offsets of a run of copies go into the instructions)
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ void copy8(void* to, const void* from, int bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
@@ -310,9 +319,10 @@ adapter_down_kernel(const DownParams p)
     auto fetch = [&]() {
         if (fe < entries && fc < c1) {
             uint8_t* to = ring + fs * STAGE;
+            const uint32_t to32 = ptx::smem_u32(to) + lane * 16;
 #pragma unroll
             for (int i = 0; i < 2 * RG; ++i)
-                if (i < 2 * f_here) copy16(to + i * 512 + lane * 16, fa + i * 512);
+                if (i < 2 * f_here) copy16(to32 + i * 512, fa + i * 512);
             const bool whole = p.aligned && (fc + 1) * CHUNK <= p.N && row0 + ROWS <= p.rows.n_rows;
             const T* x = xp + fc * CHUNK;
 #pragma unroll
@@ -321,10 +331,10 @@ adapter_down_kernel(const DownParams p)
                 uint8_t* dst = to + RG * 1024 + n * 32 * kXBytes<T>;
                 if (whole) {
                     if constexpr (sizeof(T) == 1) {
-                        copy8(dst + lane * 8, x, 8);
+                        copy8(to32 - lane * 8 + RG * 1024 + n * 32 * kXBytes<T>, x);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < kXBytes<T> / 16; ++i) copy16(dst + i * 512 + lane * 16, x + i * (16 / (int)sizeof(T)));
+                        for (int i = 0; i < kXBytes<T> / 16; ++i) copy16(to32 + RG * 1024 + n * 32 * kXBytes<T> + i * 512, x + i * (16 / (int)sizeof(T)));
                     }
                 } else {
                     copy_x<T>(dst, p.x, p.ldx, row0 + 8 * n + g, p.rows.n_rows, fc * CHUNK + 8 * t, p.N - fc * CHUNK - 8 * t, p.aligned, lane);
@@ -491,12 +501,13 @@ __device__ __forceinline__ void copy_base(uint8_t* dst, const T* at, long long l
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+        const uint32_t to32 = ptx::smem_u32(dst) + lane * 16;
         const T* src = at + h * ld;
         uint8_t* to = dst + h * (Piece<T>::U * 512) + lane * 16;
         if (full) {
             if (mask >> h & 1)
 #pragma unroll
-                for (int i = 0; i < Piece<T>::U; ++i) copy16(to + i * 512, src + i * (16 / (int)sizeof(T)));
+                for (int i = 0; i < Piece<T>::U; ++i) copy16(to32 + (h * Piece<T>::U + i) * 512, src + i * (16 / (int)sizeof(T)));
         } else if ((mask >> h & 1) && left > 0) {
             Piece<T> v;
             v.load(src, left);
@@ -685,7 +696,7 @@ adapter_up_kernel(const UpParams p)
             const uint8_t* from = p.B + (size_t)entry_slot[e] * p.b_slot + (size_t)wb * groups * 2048 + lane * 16;
 #pragma unroll
             for (int i = 0; i < 4 * G; ++i)
-                if (i < 4 * groups) copy16(weights + i * 512 + lane * 16, from + i * 512);
+                if (i < 4 * groups) copy16(ptx::smem_u32(weights) + lane * 16 + i * 512, from + i * 512);
         }
     };
     auto next_weights = [&]() {                                                // behind the adapter at (wb, wk)
@@ -922,7 +933,7 @@ adapter_many_kernel(const UpParams p)
                 if (p.vec && (fb + 1) * BLOCK <= p.M) {
 #pragma unroll
                     for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
-                        if (mask >> i & 1) copy16(to + L::unit_at(i + sub, u), from);
+                        if (mask >> i & 1) copy16(smem_u32(to) + L::unit_at(i + sub, u), from);
                 } else {
                     for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
                         if (mask >> i & 1) {
@@ -1106,18 +1117,16 @@ struct FewParams {
 };
 
 // A stage of a warp's ring: weights (of one adapter; chunks as a whole, blocks in groups of ranks), then x of the chunks, or base of
-// the block whose last groups they are.
-template <typename T, typename O>
+// the block whose last groups they are.  G: groups of ranks at most.
+template <typename T, typename O, int G>
 struct FewStage {
-    int groups, chunks, units, weights, bytes, stages;       // groups: most
-    __host__ __device__ explicit FewStage(int groups)
-        : groups(groups), chunks(groups == 1 ? 2 : 1), units(groups == 4 ? 2 : 1), weights(groups < 2 ? 2048 : groups * 1024),
-          bytes(weights + (chunks * 32 * kXBytes<T> > kBaseBytes<O> ? chunks * 32 * kXBytes<T> : kBaseBytes<O>)), stages(groups <= 2 ? 4 : groups == 4 && sizeof(O) == 4 ? 2 : 3) {}
-    __host__ __device__ int ring() const { return FEW_WARPS * stages * bytes; }
-    size_t smem(int cluster) const { return (size_t)ring() + (size_t)(FEW_WARPS + cluster) * FEW_ROWS * groups * GROUP * sizeof(float); }
+    static constexpr int chunks = G == 1 ? 2 : 1, units = G == 4 ? 2 : 1, weights = G == 1 ? 2048 : G * 1024;
+    static constexpr int bytes = weights + (chunks * 32 * kXBytes<T> > kBaseBytes<O> ? chunks * 32 * kXBytes<T> : kBaseBytes<O>);
+    static constexpr int stages = G <= 2 ? 4 : sizeof(O) == 4 ? 2 : 3, ring = FEW_WARPS * stages * bytes;
+    static size_t smem(int cluster) { return (size_t)ring + (size_t)(FEW_WARPS + cluster) * FEW_ROWS * G * GROUP * sizeof(float); }
 };
 
-template <typename T, typename O>
+template <typename T, typename O, int G>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1)
 adapter_few_kernel(const FewParams p)
 {
@@ -1128,10 +1137,10 @@ adapter_few_kernel(const FewParams p)
     __shared__ unsigned entry_mask[MOST];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rank = p.cluster > 1 ? (int)ptx::cluster_ctarank() : 0, row0 = (int)(blockIdx.x / (unsigned)p.cluster) * p.rows;
-    const FewStage<T, O> st(p.d.groups);
-    const int rank_pad = st.groups * GROUP, numbers = FEW_ROWS * rank_pad;
-    uint8_t* ring = smem + (size_t)warp * st.stages * st.bytes;
-    float* parts = reinterpret_cast<float*>(smem + st.ring());           // [warp][row][rank_pad]
+    using St = FewStage<T, O, G>;
+    constexpr int rank_pad = G * GROUP, numbers = FEW_ROWS * rank_pad;
+    uint8_t* ring = smem + warp * St::stages * St::bytes;
+    float* parts = reinterpret_cast<float*>(smem + St::ring);           // [warp][row][rank_pad]
     float* z_all = parts + FEW_WARPS * numbers;                          // [block of the cluster][row][rank_pad]
     uint8_t* zs = reinterpret_cast<uint8_t*>(parts);                     // over the parts, once they are added up: [group][Z]
     pdl_wait();
@@ -1200,61 +1209,89 @@ adapter_few_kernel(const FewParams p)
     };
 
     // ---- the copies ----
+    const Run first_up = begin(true);
     Run run = begin(false);
-    bool up = false;
+    bool up = run.e == entries;
+    if (up) run = first_up;
+    Run mine = run, mine_up = first_up;
+    const bool has_down = !up;
     int unit = 0, fs = 0;                                    // up: the groups of the block that are on their way
-    if (run.e == entries) { up = true; run = begin(true); }
+    // of the run's adapter: its groups, whether this lane's row is its (up: bits of its two rows), its weights, and x or base
+    int f_groups = 0;
+    unsigned f_rows = 0;
+    const uint8_t* f_weights = nullptr;
+    const T* f_x = nullptr;
+    const O* f_base = nullptr;
+    auto aim = [&]() {
+        if (run.e >= (up ? all : entries)) return;
+        f_groups = entry_groups[run.e];
+        f_rows = entry_mask[run.e] >> (up ? 2 * t : g);
+        if (up) {
+            f_weights = p.u.B + (size_t)entry_slot[run.e] * p.u.b_slot + (size_t)run.at * f_groups * 2048 + lane * 16;
+            f_base = (const O*)p.u.base + (long long)(row0 + 2 * t) * p.u.ldb + run.at * BLOCK + 8 * g;
+        } else {
+            f_weights = p.d.A + (size_t)entry_slot[run.e] * p.d.a_slot + (size_t)run.at * f_groups * 1024 + lane * 16;
+            f_x = (const T*)p.d.x + (long long)(row0 + g) * p.d.ldx + run.at * CHUNK + 8 * t;
+        }
+    };
     auto fetch = [&]() {
-        uint8_t* to = ring + fs * st.bytes;
+        uint8_t* to = ring + fs * St::bytes;
+        const uint32_t to32 = ptx::smem_u32(to) + lane * 16;
         if (!up) {
-            const int groups = entry_groups[run.e], n = min(st.chunks, run.end - run.at);
-            const uint8_t* a = p.d.A + (size_t)entry_slot[run.e] * p.d.a_slot + (size_t)run.at * groups * 1024 + lane * 16;
+            const int n = min(St::chunks, run.end - run.at);
 #pragma unroll
-            for (int i = 0; i < 2 * FEW_GROUPS; ++i)
-                if (i < 2 * n * groups) copy16(to + i * 512 + lane * 16, a + i * 512);
-            if (entry_mask[run.e] >> g & 1)
-                for (int c = 0; c < n; ++c) {
+            for (int i = 0; i < St::weights / 512; ++i)
+                if (i < 2 * n * f_groups) copy16(to32 + i * 512, f_weights + i * 512);
+            f_weights += n * f_groups * 1024;
+            const bool whole = p.d.aligned && (run.at + n) * CHUNK <= p.d.N;
+            for (int c = 0; c < n; ++c, f_x += CHUNK) {
+                uint8_t* dst = to + St::weights + c * 32 * kXBytes<T>;
+                if (whole) {
+                    if (f_rows & 1) {
+                        if constexpr (sizeof(T) == 1) {
+                            copy8(to32 - lane * 8 + (uint32_t)(St::weights + c * 32 * kXBytes<T>), f_x);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kXBytes<T> / 16; ++i) copy16(to32 + (uint32_t)(St::weights + c * 32 * kXBytes<T>) + i * 512, f_x + i * (16 / (int)sizeof(T)));
+                        }
+                    }
+                } else if (f_rows & 1) {
                     const int col = (run.at + c) * CHUNK + 8 * t;
-                    copy_x<T>(to + st.weights + c * 32 * kXBytes<T>, p.d.x, p.d.ldx, row0 + g, p.d.rows.n_rows, col, p.d.N - col, p.d.aligned, lane);
+                    copy_x<T>(dst, p.d.x, p.d.ldx, row0 + g, p.d.rows.n_rows, col, p.d.N - col, p.d.aligned, lane);
                 }
+            }
             if ((run.at += n) >= run.end) {
                 advance(run, false);
-                if (run.e == entries) { up = true; run = begin(true); }
+                if (run.e == entries) { up = true; run = first_up; }
+                aim();
             }
         } else if (run.e < all) {
-            const int groups = entry_groups[run.e], n = min(st.units, groups - unit);
-            if (groups) {
-                const uint8_t* b = p.u.B + (size_t)entry_slot[run.e] * p.u.b_slot + ((size_t)run.at * groups + unit) * 2048 + lane * 16;
+            const int n = min(St::units, f_groups - unit);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < 4 * n) copy16(to + i * 512 + lane * 16, b + i * 512);
-            }
+            for (int i = 0; i < 4 * St::units; ++i)
+                if (i < 4 * n) copy16(to32 + i * 512, f_weights + i * 512);
+            f_weights += n * 2048;
             unit += n;
-            if (unit >= groups) {                            // with the block's last ones, base
+            if (unit >= f_groups) {                          // with the block's last ones, base
                 if (p.u.base)
-                    copy_base<O>(to + st.weights, (const O*)p.u.base + (long long)(row0 + 2 * t) * p.u.ldb + run.at * BLOCK + 8 * g, p.u.ldb,
-                                 entry_mask[run.e] >> (2 * t), p.u.M - run.at * BLOCK - 8 * g, p.u.vec && (run.at + 1) * BLOCK <= p.u.M, lane);
+                    copy_base<O>(to + St::weights, f_base, p.u.ldb, f_rows, p.u.M - run.at * BLOCK - 8 * g, p.u.vec && (run.at + 1) * BLOCK <= p.u.M, lane);
+                f_base += BLOCK;
                 unit = 0;
-                if (++run.at >= run.end) advance(run, true);
+                if (++run.at >= run.end) { advance(run, true); aim(); }
             }
         }
         copies_commit();
-        if (++fs == st.stages) fs = 0;
+        if (++fs == St::stages) fs = 0;
     };
+    aim();
     // (a stage's copies are one group, and stages - 2 groups may follow the one that is needed)
-    auto arrived = [&]() {
-        if (st.stages == 4) copies_wait<2>();
-        else if (st.stages == 3) copies_wait<1>();
-        else copies_wait<0>();
-    };
+    auto arrived = [&]() { copies_wait<St::stages - 2>(); };
     int stage = 0;
     auto done = [&]() {
         fetch();
-        if (++stage == st.stages) stage = 0;
+        if (++stage == St::stages) stage = 0;
     };
-    Run mine = run, mine_up = up ? run : begin(true);
-    const bool has_down = !up;
-    for (int i = 0; i < st.stages - 1; ++i) fetch();
+    for (int i = 0; i < St::stages - 1; ++i) fetch();
     for (int i = lane; i < numbers; i += 32) parts[warp * numbers + i] = 0.0f;
     __syncwarp();
 
@@ -1263,20 +1300,20 @@ adapter_few_kernel(const FewParams p)
         while (mine.e < entries) {
             const int groups = entry_groups[mine.e];
             const unsigned mask = entry_mask[mine.e];
-            float acc[FEW_GROUPS][4];
+            float acc[G][4];
 #pragma unroll
-            for (int i = 0; i < FEW_GROUPS; ++i)
+            for (int i = 0; i < G; ++i)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[i][k] = 0.0f;
             while (mine.at < mine.end) {
-                const int n = min(st.chunks, mine.end - mine.at);
+                const int n = min(St::chunks, mine.end - mine.at);
                 arrived();
-                const uint8_t* from = ring + stage * st.bytes;
+                const uint8_t* from = ring + stage * St::bytes;
                 for (int c = 0; c < n; ++c) {
                     Terms<T> x{};
-                    if (mask >> g & 1) x.read(from + st.weights + c * 32 * kXBytes<T> + lane * (sizeof(T) == 1 ? 8 : 16));
+                    if (mask >> g & 1) x.read(from + St::weights + c * 32 * kXBytes<T> + lane * (sizeof(T) == 1 ? 8 : 16));
 #pragma unroll
-                    for (int i = 0; i < FEW_GROUPS; ++i)
+                    for (int i = 0; i < G; ++i)
                         if (i < groups) {
                             const uint8_t* w = from + (c * groups + i) * 1024 + lane * 16;
                             const uint4 a0 = *reinterpret_cast<const uint4*>(w), a1 = *reinterpret_cast<const uint4*>(w + 512);
@@ -1295,7 +1332,7 @@ adapter_few_kernel(const FewParams p)
                 const int row = 2 * t + (k & 1);
                 if (mask >> row & 1)
 #pragma unroll
-                    for (int i = 0; i < FEW_GROUPS; ++i)
+                    for (int i = 0; i < G; ++i)
                         if (i < groups) parts[warp * numbers + row * rank_pad + i * GROUP + g + (k & 2 ? 8 : 0)] = acc[i][k];
             }
             advance(mine, false);
@@ -1319,7 +1356,7 @@ adapter_few_kernel(const FewParams p)
     else __syncthreads();
 
     // ---- z, scaled, as bf16 terms in the order of the product's second operand ----
-    for (int i = threadIdx.x; i < st.groups * 32; i += FEW_WARPS * 32) {
+    for (int i = threadIdx.x; i < G * 32; i += FEW_WARPS * 32) {
         const int ln = i & 31, group = i >> 5, row = ln >> 2, slot = slot_s[row];
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (slot >= 0) {
@@ -1339,31 +1376,41 @@ adapter_few_kernel(const FewParams p)
 
     while (mine_up.e < all) {
         const int groups = entry_groups[mine_up.e];
-        const unsigned mask = entry_mask[mine_up.e];
-        for (; mine_up.at < mine_up.end; ++mine_up.at) {
+        const unsigned rows = entry_mask[mine_up.e] >> (2 * t);
+        O* out = (O*)p.u.out + (long long)(row0 + 2 * t) * p.u.ldo + mine_up.at * BLOCK + 8 * g;
+        for (; mine_up.at < mine_up.end; ++mine_up.at, out += BLOCK) {
             Sums<O> sums;
-            sums.zero();
             int i = 0;
             do {
                 arrived();
                 __syncwarp();                                    // (weights are the other lanes' copies too)
-                const uint8_t* from = ring + stage * st.bytes;
-                const int n = min(st.units, groups - i);
-                if (i + n >= groups && p.u.base) {               // (the block's last stage brings base: what is there already is kept beside it)
-                    if constexpr (sizeof(O) == 4) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sums.base[k] = *reinterpret_cast<const uint4*>(from + st.weights + k * 512 + lane * 16);
-                    } else {
-                        Sums<O> b;
-                        b.begin(from + st.weights, lane);
+                const uint8_t* from = ring + stage * St::bytes;
+                const int n = G == 1 ? min(1, groups) : min(St::units, groups - i);
+                if (p.u.base && i + n >= groups && (i == 0 || sizeof(O) == 4)) {
+                    // the block's last stage brings base
+                    float kept[4][4];
+                    if (i > 0) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) sums.acc[q][k] += b.acc[q][k];
+                            for (int k = 0; k < 4; ++k) kept[q][k] = sums.acc[q][k];
                     }
-                } else if (sizeof(O) == 4) {
+                    sums.begin(from + St::weights, lane);
+                    if (i > 0) {
 #pragma unroll
-                    for (int k = 0; k < (int)sizeof(O); ++k) sums.base[k < (int)(sizeof(sums.base) / 16) ? k : 0] = make_uint4(0, 0, 0, 0);
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) sums.acc[q][k] = kept[q][k];
+                    }
+                } else if (i == 0) {
+                    sums = Sums<O>{};
+                } else if (p.u.base && i + n >= groups) {
+                    Sums<O> b;
+                    b.begin(from + St::weights, lane);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sums.acc[q][k] += b.acc[q][k];
                 }
                 for (int c = 0; c < n; ++c, ++i) {
                     ZTerms<TERMS> z;
@@ -1375,10 +1422,7 @@ adapter_few_kernel(const FewParams p)
                         for (int k = TERMS - 1; k >= 0; --k) mma_bf16(sums.acc[q], w, z.w[k][0], z.w[k][1]);
                     }
                 }
-                if (i >= groups) {
-                    sums.store((O*)p.u.out + (long long)(row0 + 2 * t) * p.u.ldo + mine_up.at * BLOCK + 8 * g, p.u.ldo, mask >> (2 * t),
-                               p.u.M - mine_up.at * BLOCK - 8 * g, p.u.vec && (mine_up.at + 1) * BLOCK <= p.u.M);
-                }
+                if (i >= groups) sums.store(out, p.u.ldo, rows, p.u.M - mine_up.at * BLOCK - 8 * g, p.u.vec && (mine_up.at + 1) * BLOCK <= p.u.M);
                 done();
             } while (i < groups);
         }
@@ -1439,7 +1483,9 @@ cudaError_t down_type(const DownParams& p, bool wide, cudaStream_t st)
 template <typename T, typename O>
 cudaError_t prepare_few()
 {
-    return cudaFuncSetAttribute(adapter_few_kernel<T, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+    for (const void* kernel : {(const void*)adapter_few_kernel<T, O, 1>, (const void*)adapter_few_kernel<T, O, 2>, (const void*)adapter_few_kernel<T, O, 4>})
+        if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024); e != cudaSuccess) return e;
+    return cudaSuccess;
 }
 
 struct FewLaunch {
@@ -1461,15 +1507,21 @@ struct FewLaunch {
     }
 };
 
+template <typename T, typename O, int G>
+cudaError_t few_as(const FewParams& p, unsigned tiles, cudaStream_t st)
+{
+    FewLaunch l(tiles, p.cluster, FewStage<T, O, G>::smem(p.cluster), st);
+    return cudaLaunchKernelEx(&l.cfg, adapter_few_kernel<T, O, G>, p);
+}
+template <typename T, typename O>
+cudaError_t few_ranks(const FewParams& p, unsigned tiles, cudaStream_t st)
+{
+    return p.d.groups == 1 ? few_as<T, O, 1>(p, tiles, st) : p.d.groups == 2 ? few_as<T, O, 2>(p, tiles, st) : few_as<T, O, 4>(p, tiles, st);
+}
 template <typename T>
 cudaError_t few(const FewParams& p, unsigned tiles, bool out_f32, cudaStream_t st)
 {
-    if (out_f32) {
-        FewLaunch l(tiles, p.cluster, FewStage<T, float>(p.d.groups).smem(p.cluster), st);
-        return cudaLaunchKernelEx(&l.cfg, adapter_few_kernel<T, float>, p);
-    }
-    FewLaunch l(tiles, p.cluster, FewStage<T, __nv_bfloat16>(p.d.groups).smem(p.cluster), st);
-    return cudaLaunchKernelEx(&l.cfg, adapter_few_kernel<T, __nv_bfloat16>, p);
+    return out_f32 ? few_ranks<T, float>(p, tiles, st) : few_ranks<T, __nv_bfloat16>(p, tiles, st);
 }
 
 cudaError_t prepare()
@@ -1636,11 +1688,15 @@ extern "C" tsvd_status_t tsvd_adapters_create(int N, int M, int max_rank, int n_
     if (e == cudaSuccess) e = prepare();
     if (h->groups <= FEW_GROUPS)
         for (int c = 1; c <= 8 && e == cudaSuccess; c *= 2) {
-            FewLaunch l((unsigned)(h->sms / 8 * 8), c, FewStage<float, float>(h->groups).smem(c), nullptr);
+            // (one block an SM, whatever the types)
+            const size_t smem = h->groups == 1 ? FewStage<float, float, 1>::smem(c) : h->groups == 2 ? FewStage<float, float, 2>::smem(c) : FewStage<float, float, 4>::smem(c);
+            FewLaunch l((unsigned)(h->sms / 8 * 8), c, smem, nullptr);
             l.cfg.numAttrs = 0;
             if (c > 1) { l.attr[0] = l.attr[1]; l.cfg.numAttrs = 1; }
             h->few[c] = h->sms;
-            if (c > 1) e = cudaOccupancyMaxActiveClusters(&h->few[c], adapter_few_kernel<float, float>, &l.cfg);
+            const void* kernel = h->groups == 1 ? (const void*)adapter_few_kernel<float, float, 1> : h->groups == 2 ? (const void*)adapter_few_kernel<float, float, 2>
+                                                                                                       : (const void*)adapter_few_kernel<float, float, 4>;
+            if (c > 1) e = cudaOccupancyMaxActiveClusters(&h->few[c], kernel, &l.cfg);
         }
     if (e != cudaSuccess) {
         release(h);
