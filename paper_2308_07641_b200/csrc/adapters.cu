@@ -463,6 +463,7 @@ struct UpParams {
     int vec;                 // rows of base and out on 16-byte boundaries
     int in_place;            // out is base: rows without an adapter are as they should be
     int M, blocks, per_warp; // per_warp: blocks of 64 channels that a warp takes
+    int columns;             // the kernel for many rows: blocks of threads that share a tile of rows
     int tile_rows;           // rows of a block of threads: at most UP_ROWS
     const uint8_t* B;
     size_t b_slot;
@@ -791,15 +792,12 @@ adapter_up_kernel(const UpParams p)
 }
 
 // ---- the same for many rows, on tcgen05 --------------------------------------------------------------------------------------
-// A block: 128 rows, blocks of 64 channels one after another, of each the adapters that the rows ask for (a job).  D = Z B^T, 128 x 64,
-// in tensor memory, with the terms of z side by side along the contraction (128-byte swizzle, 64 ranks an atom) and the same
-// weights against each:
-//   warp 8     brings a job's weights into shared memory (in the order they lie in: one bulk copy), and issues its products
+// A block: up to 128 rows of one sequence, blocks of 64 channels one after another.  D = Z B^T, 128 x 64, in tensor memory, with the
+// terms of z side by side along the contraction and the same weights against each:
+//   warp 8     brings the weights into shared memory (in the order they lie in: one bulk copy), and issues the products
 //   warps 0-7  one row and 32 channels a thread: base, copied ahead into the warp's own place, plus D, by way of that place to out
-// Warp-level products of this size would set the pace: an m16n8k16 was measured to take some 28 clocks a scheduler here, a seventh of
-// which this form needs.
 
-constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32, MANY_D = 4, MANY_B = 3;   // accumulators of 64 columns; jobs whose weights are there or on their way
+constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32, MANY_D = 4, MANY_B = 3;   // accumulators of 64 columns; blocks of channels whose weights are there or on their way
 
 // 32 lanes x 4 consecutive 32-bit columns.
 __device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4])  // whole warp
@@ -846,6 +844,41 @@ struct Many {
     __host__ __device__ size_t smem() const { return (size_t)base() + 8 * kStages * kStage + 1024; }
 };
 
+// The rows of a tile: a sequence is cut evenly into as few tiles of up to MANY_ROWS rows as it takes, and they are counted sequence by
+// sequence.  One warp.
+struct SeqTile { int row0, rows, slot; };
+__device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
+{
+    const int lane = threadIdx.x & 31;
+    SeqTile found{0, 0, kNoRow};
+    for (int s0 = 0, before = 0; s0 < r.n_seq; s0 += 32) {
+        const int s = s0 + lane;
+        const int begin = s < r.n_seq ? min(max(0, r.q_start[s]), r.n_rows) : 0, end = s < r.n_seq ? min(max(0, r.q_start[s + 1]), r.n_rows) : 0;
+        const int mine = max(0, end - begin + MANY_ROWS - 1) / MANY_ROWS;
+        int scan = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += v;
+        }
+        const unsigned holds = __ballot_sync(0xffffffffu, before + scan > tile);
+        if (holds) {
+            const int in = __ffs(holds) - 1, each = mine ? (end - begin + mine - 1) / mine : 0, at = begin + (tile - before - (scan - mine)) * each;
+            found.row0 = __shfl_sync(0xffffffffu, at, in);
+            found.rows = __shfl_sync(0xffffffffu, min(each, end - at), in);
+            int slot = r.slots[s0 + in];
+            if (slot < -1 || slot >= r.n_slots) {
+                if (lane == 0) atomicOr(r.status, KV4_DEV_INDEX);
+                slot = kNoAdapter;
+            }
+            if (slot >= 0 && r.ranks[slot] == 0) slot = kNoAdapter;
+            found.slot = slot;
+            return found;
+        }
+        before += __shfl_sync(0xffffffffu, scan, 31);
+    }
+    return found;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(MANY_THREADS, 2)
 adapter_many_kernel(const UpParams p)
@@ -859,9 +892,7 @@ adapter_many_kernel(const UpParams p)
     __shared__ uint64_t d_full[MANY_D], d_free[MANY_D], b_full[MANY_B], b_done[MANY_B], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ int ctl_[2];
-    __shared__ int slot_s[MANY_ROWS], entry_slot[MANY_ROWS + 1], entries_s;
-    __shared__ unsigned char entry_groups[MANY_ROWS + 1];
-    __shared__ unsigned entry_mask[MANY_ROWS + 1][4];
+    __shared__ SeqTile tile_s;
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -874,108 +905,94 @@ adapter_many_kernel(const UpParams p)
     }
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
     if (warp == 8) { tmem_alloc(&tmem_slot, MANY_D * 64); tmem_relinquish(); }
-    const int row0 = blockIdx.x * MANY_ROWS;
     // Adapters, slots and base are there: the first kernel let this one start after its own wait.  z is behind this one's wait.
-    find_slots<MANY_ROWS, MANY_THREADS / 32>(p.rows, row0, slot_s);
     if (warp == 0) {
-        int slot[4], entries = 0;
-        unsigned rest[4], in[4] = {};
-        auto add = [&](int which) {
-            if (lane < 4) entry_mask[entries][lane] = lane == 0 ? in[0] : lane == 1 ? in[1] : lane == 2 ? in[2] : in[3];
-            if (lane == 0) {
-                entry_slot[entries] = which;
-                entry_groups[entries] = (unsigned char)(which < 0 ? 0 : (p.rows.ranks[which] + GROUP - 1) / GROUP);
-            }
-            ++entries;
-        };
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            slot[i] = slot_s[32 * i + lane];
-            rest[i] = __ballot_sync(0xffffffffu, slot[i] >= 0);
-        }
-        while (rest[0] | rest[1] | rest[2] | rest[3]) {
-            int which = 0;
-#pragma unroll
-            for (int i = 3; i >= 0; --i)
-                if (rest[i]) which = __shfl_sync(0xffffffffu, slot[i], __ffs(rest[i]) - 1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                in[i] = __ballot_sync(0xffffffffu, slot[i] == which);
-                rest[i] &= ~in[i];
-            }
-            add(which);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) in[i] = __ballot_sync(0xffffffffu, slot[i] == kNoAdapter);
-        if ((in[0] | in[1] | in[2] | in[3]) && !p.in_place) add(kNoAdapter);     // rows without one: base is copied
-        if (lane == 0) entries_s = entries;
+        const SeqTile found = find_tile(p.rows, (int)blockIdx.x / p.columns);
+        if (lane == 0) tile_s = found;
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    const int entries = entries_s, b0 = blockIdx.y * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
+    const SeqTile tile = tile_s;
+    pdl_launch_dependents();
+    const bool real = tile.slot >= 0;
+    if (tile.rows == 0 || (!real && p.in_place)) {
+        pdl_wait();              // (whoever waits for this kernel waits for those before it)
+        if (warp == 8) tmem_dealloc(tmem, MANY_D * 64);
+        return;
+    }
+    const int row0 = tile.row0, b0 = (int)blockIdx.x % p.columns * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
+    const int rank = real ? p.rows.ranks[tile.slot] : 0, groups = (rank + GROUP - 1) / GROUP, eights = 2 * groups;
 
-    // ---- base of the next job into the warp's next stage: the rows in the adapter's mask, a row's 32 channels by LANES lanes ----
+    // ---- base of the next 64 channels into the warp's next stage: its rows, 32 channels of each by LANES lanes ----
     const int quarter = warp & 3, half = warp >> 2 & 1, mine0 = row0 + 32 * quarter;         // its rows (the tensor memory's lanes) and channels
+    const int mine = max(0, min(32, tile.rows - 32 * quarter));
     uint8_t* place = smem + lay.base() + (warp & 7) * (L::kStages * L::kStage);
     const int sub = lane / LANES, u = lane % LANES, ch_in = 32 * half + u * E;
-    int my_first = 0;            // the first adapter that the warp has rows of
-    while (my_first < entries && entry_mask[my_first][quarter] == 0) ++my_first;
-    int fb = b0, fe = my_first, fs = 0;
+    int fb = b0, fs = 0;
     auto fetch = [&]() {
-        if (fb < b1 && my_first < entries) {
-            if (p.base) {
-                const unsigned mask = entry_mask[fe][quarter] >> sub;
-                const int ch = fb * BLOCK + ch_in, left = p.M - ch;
-                const T* from = (const T*)p.base + (long long)(mine0 + sub) * p.ldb + ch;
-                uint8_t* to = place + fs * L::kStage;
-                if (p.vec && (fb + 1) * BLOCK <= p.M) {
+        if (fb < b1 && p.base) {
+            const int ch = fb * BLOCK + ch_in, left = p.M - ch;
+            const T* from = (const T*)p.base + (long long)(mine0 + sub) * p.ldb + ch;
+            uint8_t* to = place + fs * L::kStage;
+            if (p.vec && (fb + 1) * BLOCK <= p.M) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
-                        if (mask >> i & 1) copy16(smem_u32(to) + L::unit_at(i + sub, u), from);
-                } else {
-                    for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
-                        if (mask >> i & 1) {
-                            T* unit = reinterpret_cast<T*>(to + L::unit_at(i + sub, u));
-                            for (int e = 0; e < E; ++e) unit[e] = e < left ? from[e] : T(0.0f);
-                        }
+                for (int i = 0; i < 32; i += PER, from += PER * p.ldb)
+                    if (i + sub < mine) copy16(smem_u32(to) + L::unit_at(i + sub, u), from);
+            } else {
+                for (int i = sub; i < mine; i += PER, from += PER * p.ldb) {
+                    T* unit = reinterpret_cast<T*>(to + L::unit_at(i, u));
+                    for (int e = 0; e < E; ++e) unit[e] = e < left ? from[e] : T(0.0f);
                 }
             }
-            do ++fe; while (fe < entries && entry_mask[fe][quarter] == 0);
-            if (fe == entries) { fe = my_first; ++fb; }
         }
+        ++fb;
         copies_commit();
         if (++fs == L::kStages) fs = 0;
     };
     if (warp < 8)
         for (int i = 0; i < L::kStages - 1; ++i) fetch();
+    // ---- weights of the next 64 channels: one thread ----
+    int wb = b0;
+    auto ask = [&]() {
+        if (wb < b1) {
+            const int buf = (wb - b0) % MANY_B;
+            mbar_arrive_expect_tx(&b_full[buf], (uint32_t)groups * 2048);
+            bulk_g2s(smem + lay.z_bytes() + buf * lay.b_bytes(), p.B + (size_t)tile.slot * p.b_slot + (size_t)wb * groups * 2048, (uint32_t)groups * 2048, &b_full[buf]);
+            ++wb;
+        }
+    };
+    if (real && threadIdx.x == 8 * 32)
+        for (int i = 0; i < MANY_B - 1; ++i) ask();
 
     // ---- z, scaled, as bf16 terms, each at its ranks behind those of the term before ----
-    pdl_launch_dependents();
     pdl_wait();
-    // (four lanes take 32 ranks of a row, two its 16: between loads of whole lines and stores without conflicts)
-    const int rank_pad = p.groups * GROUP, eights = 2 * p.groups, wide = p.groups == 1 ? 2 : 4, across = (eights + wide - 1) / wide;
+    if (real) {
+        // (four lanes take 32 ranks of a row, two its 16: between loads of whole lines and stores without conflicts)
+        const int rank_pad = p.groups * GROUP, wide = groups == 1 ? 2 : 4, across = (eights + wide - 1) / wide;
+        const float factor = p.scales[tile.slot];
 #pragma unroll 2
-    for (int i = threadIdx.x; i < MANY_ROWS * across * wide; i += MANY_THREADS) {
-        const int piece = i / (MANY_ROWS * wide), rest = i - piece * (MANY_ROWS * wide), r = rest / wide, eight = piece * wide + rest % wide;
-        if (eight >= eights) continue;
-        const int first = 8 * eight, slot = slot_s[r], have = slot >= 0 ? p.rows.ranks[slot] - first : 0;     // z is written for the adapter's own ranks only
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (have > 0) {
-            const float4* at = reinterpret_cast<const float4*>(p.z + (size_t)(row0 + r) * rank_pad + first);
-            const float4 lo = __ldcg(at), hi = __ldcg(at + 1);
-            const float c = p.scales[slot] * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
-            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        for (int i = threadIdx.x; i < MANY_ROWS * across * wide; i += MANY_THREADS) {
+            const int piece = i / (MANY_ROWS * wide), rest = i - piece * (MANY_ROWS * wide), r = rest / wide, eight = piece * wide + rest % wide;
+            if (eight >= eights) continue;
+            const int first = 8 * eight, have = r < tile.rows ? rank - first : 0;              // z is written for the adapter's own ranks only
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (have > 0) {
+                const float4* at = reinterpret_cast<const float4*>(p.z + (size_t)(row0 + r) * rank_pad + first);
+                const float4 lo = __ldcg(at), hi = __ldcg(at + 1);
+                const float c = factor * (p.x_scale ? p.x_scale[row0 + r] : 1.0f);
+                v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k < have ? v[k] * c : 0.0f;
-        }
+                for (int k = 0; k < 8; ++k) v[k] = k < have ? v[k] * c : 0.0f;
+            }
 #pragma unroll
-        for (int k = 0; k < TERMS; ++k) {
-            uint32_t w[4];
+            for (int k = 0; k < TERMS; ++k) {
+                uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = k + 1 == TERMS ? rounded(v[2 * j], v[2 * j + 1]) : cut(v[2 * j], v[2 * j + 1]);
-            *reinterpret_cast<uint4*>(smem + (k * eights + eight) * 2048 + r * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int j = 0; j < 4; ++j) w[j] = k + 1 == TERMS ? rounded(v[2 * j], v[2 * j + 1]) : cut(v[2 * j], v[2 * j + 1]);
+                *reinterpret_cast<uint4*>(smem + (k * eights + eight) * 2048 + r * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
     }
     fence_proxy_async_smem();
@@ -983,44 +1000,30 @@ adapter_many_kernel(const UpParams p)
 
     bool ok = true;
     if (warp == 8) {
-        // ================= weights and products =================
-        if (elect_one()) {
-            const int real = entries > 0 && entry_slot[entries - 1] == kNoAdapter ? entries - 1 : entries;
+        // ================= products =================
+        if (real && lane == 0) {
             const uint64_t desc_z = umma_desc_k_plain(smem_u32(smem), 2048), desc_b = umma_desc_k_plain(smem_u32(smem + lay.z_bytes()), 1024);
             constexpr uint32_t kDesc = idesc_bf16(MANY_ROWS, BLOCK);
-            int wb = b0, we = 0, wj = 0;                                       // the job whose weights are asked for next
-            auto ask = [&]() {
-                if (wb >= b1 || real == 0) return;
-                const int groups = entry_groups[we], buf = wj % MANY_B;
-                mbar_arrive_expect_tx(&b_full[buf], (uint32_t)groups * 2048);
-                bulk_g2s(smem + lay.z_bytes() + buf * lay.b_bytes(), p.B + (size_t)entry_slot[we] * p.b_slot + (size_t)wb * groups * 2048,
-                         (uint32_t)groups * 2048, &b_full[buf]);
-                ++wj;
-                if (++we == real) { we = 0; ++wb; }
-            };
-            for (int i = 0; i < MANY_B - 1; ++i) ask();
-            int job = 0;
-            for (int b = b0; b < b1 && ok; ++b)
-                for (int e = 0; e < real && ok; ++e, ++job) {
-                    const int buf = job % MANY_B, d = job % MANY_D, groups = entry_groups[e];
-                    // (the place of the job after next was the last one's)
-                    if (job > 0 && !(ok = mbar_wait(&b_done[(job - 1) % MANY_B], (uint32_t)((job - 1) / MANY_B & 1), ctl))) break;
-                    ask();
-                    if (!(ok = mbar_wait(&b_full[buf], (uint32_t)(job / MANY_B & 1), ctl))) break;
-                    if (!(ok = mbar_wait(&d_free[d], (uint32_t)(job / MANY_D & 1) ^ 1, ctl))) break;
-                    tc_fence_after_sync();
-                    const uint64_t weights = desc_b + (uint32_t)(buf * (lay.b_bytes() >> 4));
-                    for (int k = TERMS - 1; k >= 0; --k)
-                        for (int i = 0; i < groups; ++i)
-                            umma_bf16_ss(tmem + 64u * d, desc_z + (uint32_t)((k * p.groups + i) * (4096 >> 4)), weights + (uint32_t)(i * (2048 >> 4)), kDesc,
-                                         k != TERMS - 1 || i > 0);
-                    umma_commit(&b_done[buf]);
-                    umma_commit(&d_full[d]);
-                }
+            for (int job = 0; job < b1 - b0; ++job) {
+                const int buf = job % MANY_B, d = job % MANY_D;
+                // (the place of the weights after next was the last one's)
+                if (job > 0 && !(ok = mbar_wait(&b_done[(job - 1) % MANY_B], (uint32_t)((job - 1) / MANY_B & 1), ctl))) break;
+                ask();
+                if (!(ok = mbar_wait(&b_full[buf], (uint32_t)(job / MANY_B & 1), ctl))) break;
+                if (!(ok = mbar_wait(&d_free[d], (uint32_t)(job / MANY_D & 1) ^ 1, ctl))) break;
+                tc_fence_after_sync();
+                const uint64_t weights = desc_b + (uint32_t)(buf * (lay.b_bytes() >> 4));
+                for (int k = TERMS - 1; k >= 0; --k)
+                    for (int i = 0; i < groups; ++i)
+                        umma_bf16_ss(tmem + 64u * d, desc_z + (uint32_t)((k * groups + i) * (4096 >> 4)), weights + (uint32_t)(i * (2048 >> 4)), kDesc,
+                                     k != TERMS - 1 || i > 0);
+                umma_commit(&b_done[buf]);
+                umma_commit(&d_full[d]);
+            }
             // every copy has landed and every product ended before the block does
             if (!ok)
                 for (int i = 0; i < MANY_B; ++i)
-                    if (wj > i) mbar_drain(&b_full[i], (uint32_t)((wj - 1 - i) / MANY_B & 1));
+                    if (wb - b0 > i) mbar_drain(&b_full[i], (uint32_t)((wb - b0 - 1 - i) / MANY_B & 1));
             umma_commit(&drained);
             mbar_drain(&drained, 0);
         }
@@ -1028,70 +1031,62 @@ adapter_many_kernel(const UpParams p)
     } else {
         // ================= rows: one a thread =================
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + 4u * half;
-        int job = 0, stage = 0;
-        for (int b = b0; b < b1 && ok; ++b)
-            for (int e = 0; e < entries && ok; ++e) {
-                const unsigned mask = entry_mask[e][quarter];
-                const bool real = entry_slot[e] != kNoAdapter;
-                uint32_t v[8][4] = {};                       // channel 8 n + j is column 8 j + n: [j][n % 4] of the half's n
-                if (real) {
-                    const int d = job % MANY_D;
-                    if (!(ok = mbar_wait_warp(&d_full[d], (uint32_t)(job / MANY_D & 1), ctl))) break;
-                    tc_fence_after_sync();
-                    if (mask) {
+        int stage = 0;
+        for (int b = b0; b < b1; ++b) {
+            const int job = b - b0, d = job % MANY_D;
+            uint32_t v[8][4] = {};                           // channel 8 n + j is column 8 j + n: [j][n % 4] of the half's n
+            if (real) {
+                if (!(ok = mbar_wait_warp(&d_full[d], (uint32_t)(job / MANY_D & 1), ctl))) break;
+                tc_fence_after_sync();
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) tmem_ld4(lanes + 64u * d + 8u * j, v[j]);
-                        tmem_ld_wait();
-                    }
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&d_free[d]);
-                    ++job;
-                }
-                if (mask == 0) continue;
-                uint8_t* here = place + stage * L::kStage;
-                copies_wait<L::kStages - 2>();
+                for (int j = 0; j < 8; ++j) tmem_ld4(lanes + 64u * d + 8u * j, v[j]);
+                tmem_ld_wait();
+                tc_fence_before_sync();
                 __syncwarp();
-                if (mask >> lane & 1) {
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-#pragma unroll
-                        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-                            uint4* unit = reinterpret_cast<uint4*>(here + L::unit_at(lane, n * ((int)sizeof(T) / 2) + h));
-                            uint4 x = p.base ? *unit : make_uint4(0, 0, 0, 0);
-                            uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if constexpr (sizeof(T) == 2)
-                                    w[k] = rounded(__uint_as_float(w[k] << 16) + __uint_as_float(v[2 * k][n]),
-                                                   __uint_as_float(w[k] & 0xffff0000u) + __uint_as_float(v[2 * k + 1][n]));
-                                else
-                                    w[k] = __float_as_uint(__uint_as_float(w[k]) + __uint_as_float(v[4 * h + k][n]));
-                            }
-                            *unit = x;
-                        }
-                    }
-                }
-                __syncwarp();
-                const int ch = b * BLOCK + ch_in, left = p.M - ch;
-                T* to = (T*)p.out + (long long)(mine0 + sub) * p.ldo + ch;
-                if (p.vec && (b + 1) * BLOCK <= p.M) {
-                    uint4 x[32 / PER];
-#pragma unroll
-                    for (int i = 0; i < 32; i += PER) x[i / PER] = *reinterpret_cast<const uint4*>(here + L::unit_at(i + sub, u));
-#pragma unroll
-                    for (int i = 0; i < 32; i += PER, to += PER * p.ldo)
-                        if (mask >> (i + sub) & 1) *reinterpret_cast<uint4*>(to) = x[i / PER];
-                } else {
-                    for (int i = 0; i < 32; i += PER, to += PER * p.ldo)
-                        if (mask >> (i + sub) & 1)
-                            for (int e = 0; e < E; ++e)
-                                if (e < left) to[e] = reinterpret_cast<const T*>(here + L::unit_at(i + sub, u))[e];
-                }
-                __syncwarp();
-                fetch();
-                if (++stage == L::kStages) stage = 0;
+                if (lane == 0) mbar_arrive(&d_free[d]);
             }
+            uint8_t* here = place + stage * L::kStage;
+            copies_wait<L::kStages - 2>();
+            __syncwarp();
+            if (lane < mine) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+#pragma unroll
+                    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+                        uint4* unit = reinterpret_cast<uint4*>(here + L::unit_at(lane, n * ((int)sizeof(T) / 2) + h));
+                        uint4 x = p.base ? *unit : make_uint4(0, 0, 0, 0);
+                        uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if constexpr (sizeof(T) == 2)
+                                w[k] = rounded(__uint_as_float(w[k] << 16) + __uint_as_float(v[2 * k][n]),
+                                               __uint_as_float(w[k] & 0xffff0000u) + __uint_as_float(v[2 * k + 1][n]));
+                            else
+                                w[k] = __float_as_uint(__uint_as_float(w[k]) + __uint_as_float(v[4 * h + k][n]));
+                        }
+                        *unit = x;
+                    }
+                }
+            }
+            __syncwarp();
+            const int ch = b * BLOCK + ch_in, left = p.M - ch;
+            T* to = (T*)p.out + (long long)(mine0 + sub) * p.ldo + ch;
+            if (p.vec && (b + 1) * BLOCK <= p.M) {
+                uint4 x[32 / PER];
+#pragma unroll
+                for (int i = 0; i < 32; i += PER) x[i / PER] = *reinterpret_cast<const uint4*>(here + L::unit_at(i + sub, u));
+#pragma unroll
+                for (int i = 0; i < 32; i += PER, to += PER * p.ldo)
+                    if (i + sub < mine) *reinterpret_cast<uint4*>(to) = x[i / PER];
+            } else {
+                for (int i = sub; i < mine; i += PER, to += PER * p.ldo)
+                    for (int e = 0; e < E; ++e)
+                        if (e < left) to[e] = reinterpret_cast<const T*>(here + L::unit_at(i, u))[e];
+            }
+            __syncwarp();
+            fetch();
+            if (++stage == L::kStages) stage = 0;
+        }
         copies_wait<0>();
     }
     tc_fence_before_sync();
@@ -1571,11 +1566,14 @@ cudaError_t many(UpParams& p, int sms, cudaStream_t st)
 {
     // Blocks of channels of a block of threads: so many that all run in one round.
     const Many<T> lay{p.groups};
-    const int tiles = (p.rows.n_rows + MANY_ROWS - 1) / MANY_ROWS, at_once = (lay.smem() <= 109 * 1024 ? 2 : 1) * sms;
+    // (the tiles of sequences of equal length; there are never more than `most`)
+    const int each = (p.rows.n_rows + p.rows.n_seq - 1) / p.rows.n_seq, tiles = p.rows.n_seq * ((each + MANY_ROWS - 1) / MANY_ROWS);
+    const int most = p.rows.n_rows / MANY_ROWS + p.rows.n_seq;
+    const int at_once = (lay.smem() <= 109 * 1024 ? 2 : 1) * sms;
     p.per_warp = (int)(((long long)p.blocks * tiles + at_once - 1) / at_once);
     while ((long long)tiles * ((p.blocks + p.per_warp - 1) / p.per_warp) > at_once && p.per_warp < p.blocks) ++p.per_warp;
-    PdlLaunch l((unsigned)tiles, MANY_THREADS, lay.smem(), st);
-    l.cfg.gridDim.y = (unsigned)((p.blocks + p.per_warp - 1) / p.per_warp);
+    p.columns = (p.blocks + p.per_warp - 1) / p.per_warp;
+    PdlLaunch l((unsigned)(most * p.columns), MANY_THREADS, lay.smem(), st);         // (those of tiles that are not there come last)
     return cudaLaunchKernelEx(&l.cfg, adapter_many_kernel<T>, p);
 }
 
@@ -1798,8 +1796,8 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
     // with few rows there are few tiles.
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows > 256 ? 16 : 8;
-    // tcgen05 from 512 rows on, where a tile of 128 holds few adapters, as far as the number of sequences tells (each is a job of its
-    // own for the whole tile): 2048 rows of four sequences, ranks of 64, 12288 channels 26 us against 62; 1000 rows of fifty 42 against 26.
+    // tcgen05 from 512 rows on, where sequences fill tiles of 128, as far as their number tells: 2048 rows of four, ranks of 64, 12288
+    // channels 26 us against 62; of 2048 rows by 64, 32 and 16 for each sequence, ranks of 16, 8192 channels 31, 39 and 65 against 32, 34 and 39.
     if (n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH) {
         if (out_dtype == TSVD_F32) TSVD_CUDA_OK(many<float>(u, h->sms, st));
         else TSVD_CUDA_OK(many<__nv_bfloat16>(u, h->sms, st));
