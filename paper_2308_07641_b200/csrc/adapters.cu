@@ -28,7 +28,7 @@ struct tsvd_adapters_s {
     int groups = 0;                  // of 16 ranks, of the largest rank
     int chunks = 0, blocks = 0;      // of 32 columns of A, of 64 channels of B
     size_t a_slot = 0, b_slot = 0;   // bytes of a slot
-    uint8_t* A = nullptr;            // [slot][chunk][its groups][2][32 lanes][16]
+    uint8_t* A = nullptr;            // [slot][chunk][its groups][2][4][8 ranks][16]: see adapter_set_kernel
     uint8_t* B = nullptr;            // [slot][block][its groups][2][64 rows][16]: see adapter_set_kernel
     int* ranks = nullptr;            // [slot], 0: empty
     float* scales = nullptr;         // [slot]
@@ -123,6 +123,16 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint4& a, uint32_t
         : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
+// 16 ranks by the 32 columns of a chunk: eight columns of rank g (lo) and of rank g + 8 (hi) a lane.
+__device__ __forceinline__ void mma_a(float (&d)[4], const uint4& lo, const uint4& hi, const uint32_t (&x)[4])
+{
+    mma_bf16(d, make_uint4(lo.x, hi.x, lo.y, hi.y), x[0], x[1]);
+    mma_bf16(d, make_uint4(lo.z, hi.z, lo.w, hi.w), x[2], x[3]);
+}
+// Where the 16 bytes at columns 8 t and rank g of a group's half lie in shared memory: copied in their order (lane 8 t + g) and read by
+// lane 4 g + t, both without a bank met twice.
+__device__ __forceinline__ int a_place(int g, int t) { return (8 * t + (g ^ 2 * t)) * 16; }
+
 // The leading bf16 of two numbers, cut off (not rounded), as a pair; what remains of them is exact in fp32.
 __device__ __forceinline__ uint32_t cut(float& lo, float& hi)
 {
@@ -156,12 +166,14 @@ __global__ void adapter_set_kernel(const T* A, long long lda, const T* B, long l
     if (first == 0) { *rank_out = rank; *scale_out = scale; }
     for (long long i = first; i < na + nb; i += step) {
         if (i < na) {
-            const int lane = (int)(i & 31), half = (int)(i >> 5 & 1), g = lane >> 2, t = lane & 3;
+            // Eight columns of a row are 16 bytes, eight rows in a row one matrix, four of them (the chunk's columns) before the next
+            // eight ranks.
+            const int g = (int)(i & 7), t = (int)(i >> 3 & 3), half = (int)(i >> 5 & 1);
             const long long piece = i >> 6;
             const int group = (int)(piece % groups), chunk = (int)(piece / groups);
-            const int r = group * GROUP + g, c = chunk * CHUNK + 8 * t + 4 * half;
-            a_out[i] = make_uint4(pair_of(A, lda, r, c, rank, N), pair_of(A, lda, r + 8, c, rank, N),
-                                  pair_of(A, lda, r, c + 2, rank, N), pair_of(A, lda, r + 8, c + 2, rank, N));
+            const int r = group * GROUP + 8 * half + g, c = chunk * CHUNK + 8 * t;
+            a_out[i] = make_uint4(pair_of(A, lda, r, c, rank, N), pair_of(A, lda, r, c + 2, rank, N), pair_of(A, lda, r, c + 4, rank, N),
+                                  pair_of(A, lda, r, c + 6, rank, N));
         } else {
             const long long k = i - na;
             const int row = (int)(k & 63), half = (int)(k >> 6 & 1);
@@ -212,9 +224,13 @@ template <> struct Terms<int8_t> {
     __device__ __forceinline__ void read(const uint8_t* at)
     {
         const uint2 u = *reinterpret_cast<const uint2*>(at);
+        make({u.x, u.y});
+    }
+    __device__ __forceinline__ void make(const uint32_t (&u)[2])
+    {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t v = (i < 2 ? u.x : u.y) >> (16 * (i & 1));
+            const uint32_t v = u[i >> 1] >> (16 * (i & 1));
             w[0][i] = rounded((float)(int8_t)(v & 0xff), (float)(int8_t)(v >> 8 & 0xff));       // exact
         }
     }
@@ -225,8 +241,14 @@ template <> struct Terms<float> {
     __device__ __forceinline__ void read(const uint8_t* at)
     {
         // (the halves of a row's eight columns lie 512 bytes apart)
-        const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 512);
-        float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at + 512);
+        make({a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w});
+    }
+    __device__ __forceinline__ void make(const uint32_t (&u)[8])
+    {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[0][i] = cut(v[2 * i], v[2 * i + 1]);
@@ -302,6 +324,7 @@ adapter_down_kernel(const DownParams p)
     uint8_t* ring = smem + (size_t)warp * STAGES * STAGE;
     float* parts = reinterpret_cast<float*>(smem + (size_t)DOWN_WARPS * STAGES * STAGE);     // [warp][row][here_pad]
 
+    const uint32_t a_put = (uint32_t)a_place(lane & 7, lane >> 3);
     // ---- the next item (adapter, groups, chunk) into a stage ----
     int fe = 0, fg = first_group, fc = c0 + warp, fs = 0, f_here = 0;
     const uint8_t* fa = nullptr;
@@ -322,7 +345,7 @@ adapter_down_kernel(const DownParams p)
             const uint32_t to32 = ptx::smem_u32(to) + lane * 16;
 #pragma unroll
             for (int i = 0; i < 2 * RG; ++i)
-                if (i < 2 * f_here) copy16(to32 + i * 512, fa + i * 512);
+                if (i < 2 * f_here) copy16(ptx::smem_u32(to) + a_put + i * 512, fa + i * 512);
             const bool whole = p.aligned && (fc + 1) * CHUNK <= p.N && row0 + ROWS <= p.rows.n_rows;
             const T* x = xp + fc * CHUNK;
 #pragma unroll
@@ -376,8 +399,8 @@ adapter_down_kernel(const DownParams p)
 #pragma unroll
                     for (int i = 0; i < RG; ++i)
                         if (i < here) {
-                            a[i][0] = *reinterpret_cast<const uint4*>(from + i * 1024 + lane * 16);
-                            a[i][1] = *reinterpret_cast<const uint4*>(from + i * 1024 + 512 + lane * 16);
+                            a[i][0] = *reinterpret_cast<const uint4*>(from + i * 1024 + a_place(g, t));
+                            a[i][1] = *reinterpret_cast<const uint4*>(from + i * 1024 + 512 + a_place(g, t));
                         }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -388,10 +411,7 @@ adapter_down_kernel(const DownParams p)
                         for (int i = 0; i < RG; ++i)
                             if (i < here) {
 #pragma unroll
-                                for (int k = Terms<T>::n - 1; k >= 0; --k) {
-                                    mma_bf16(acc[i][n], a[i][0], x.w[k][0], x.w[k][1]);
-                                    mma_bf16(acc[i][n], a[i][1], x.w[k][2], x.w[k][3]);
-                                }
+                                for (int k = Terms<T>::n - 1; k >= 0; --k) mma_a(acc[i][n], a[i][0], a[i][1], x.w[k]);
                             }
                     }
                     fetch();
@@ -446,6 +466,285 @@ adapter_down_kernel(const DownParams p)
         }
         p.z[(size_t)(row0 + row) * rank_pad + r] = sums[j];
     }
+}
+
+// ---- the same for many rows, on tcgen05 -----------------------------------------------------------------------------------
+// A block: up to 128 rows of one sequence, a share of the columns, 64 of them a stage.  D = X A^T, 128 x the ranks, in tensor memory:
+//   warps 0-7  x as bf16 (its terms one after another), rows of 128 bytes swizzled; bf16 is copied as it is, the other types are turned
+//              in registers, the next stage's on their way meanwhile.  Warp 0 also asks for the weights (one bulk copy: their order)
+//   warp 8     issues the products
+// The blocks that share a tile's columns are a cluster; each adds the parts of its share of the rows, in their order.
+
+constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32;
+
+// 32 lanes x 4 consecutive 32-bit columns.
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4])  // whole warp
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void umma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// kind::f16, both operands bf16 and K-major, fp32 sums
+__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// K-major without swizzle: eight rows of 16 bytes a matrix, the next eight rows `rows` bytes on, the next 16 bytes of a row `along`.
+__device__ __forceinline__ uint64_t umma_desc_k_plain(uint32_t smem_addr, uint32_t along, uint32_t rows)
+{
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(along >> 4) << 16;
+    d |= (uint64_t)(rows >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    return d;
+}
+
+// The rows of a tile: a sequence is cut evenly into as few tiles of up to MANY_ROWS rows as it takes, and they are counted sequence by
+// sequence.  One warp.
+struct SeqTile { int row0, rows, slot; };
+__device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
+{
+    const int lane = threadIdx.x & 31;
+    SeqTile found{0, 0, kNoRow};
+    for (int s0 = 0, before = 0; s0 < r.n_seq; s0 += 32) {
+        const int s = s0 + lane;
+        const int begin = s < r.n_seq ? min(max(0, r.q_start[s]), r.n_rows) : 0, end = s < r.n_seq ? min(max(0, r.q_start[s + 1]), r.n_rows) : 0;
+        const int mine = max(0, end - begin + MANY_ROWS - 1) / MANY_ROWS;
+        int scan = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += v;
+        }
+        const unsigned holds = __ballot_sync(0xffffffffu, before + scan > tile);
+        if (holds) {
+            const int in = __ffs(holds) - 1, each = mine ? (end - begin + mine - 1) / mine : 0, at = begin + (tile - before - (scan - mine)) * each;
+            found.row0 = __shfl_sync(0xffffffffu, at, in);
+            found.rows = __shfl_sync(0xffffffffu, min(each, end - at), in);
+            int slot = r.slots[s0 + in];
+            if (slot < -1 || slot >= r.n_slots) {
+                if (lane == 0) atomicOr(r.status, KV4_DEV_INDEX);
+                slot = kNoAdapter;
+            }
+            if (slot >= 0 && r.ranks[slot] == 0) slot = kNoAdapter;
+            found.slot = slot;
+            return found;
+        }
+        before += __shfl_sync(0xffffffffu, scan, 31);
+    }
+    return found;
+}
+
+template <typename T>
+struct DownMany {
+    static constexpr int kStages = sizeof(T) == 4 ? 3 : 4, kX = Terms<T>::n * MANY_ROWS * 128, kRaw = 2 * (int)sizeof(T);     // words of eight columns
+    __host__ __device__ static constexpr int stage(int groups) { return kX + groups * 2048; }
+    // (the parts lie over the stages; 16 bytes more a row, so that rows beside each other meet no bank twice)
+    __host__ __device__ static constexpr int pitch(int groups) { return groups * GROUP * 4 + 16; }
+    __host__ __device__ static constexpr size_t smem(int groups) { return (size_t)kStages * stage(groups) + 1024; }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(MANY_THREADS, sizeof(T) == 4 ? 1 : 2)
+adapter_down_many_kernel(const DownParams p)
+{
+    using namespace ptx;
+    using L = DownMany<T>;
+    constexpr int TERMS = Terms<T>::n, STAGES = L::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    __shared__ uint64_t x_full[STAGES], w_full[STAGES], freed[STAGES], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int ctl_[2];
+    __shared__ SeqTile tile_s;
+    volatile int* ctl = ctl_;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&x_full[i], 8); mbar_init(&w_full[i], 1); mbar_init(&freed[i], 1); }
+        mbar_init(&drained, 1);
+        ctl[0] = 0;
+        ctl[1] = kWaitLimitDefault;
+        fence_mbar_init();
+    }
+    // Tensor memory before the kernel after this one may start (see PdlLaunch).
+    const uint32_t columns = p.groups <= 2 ? 32u : p.groups <= 4 ? 64u : 128u;
+    if (warp == 8) { tmem_alloc(&tmem_slot, columns); tmem_relinquish(); }
+    // What the kernel ahead has written is there before the next kernel starts: that one reads it ahead of its own wait.
+    pdl_wait();
+    pdl_launch_dependents();
+    if (warp == 0) {
+        const SeqTile found = find_tile(p.rows, (int)blockIdx.x);
+        if (lane == 0) tile_s = found;
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    const SeqTile tile = tile_s;
+    if (tile.slot < 0 || tile.rows == 0) {           // (all blocks of the cluster)
+        if (warp == 8) tmem_dealloc(tmem, columns);
+        return;
+    }
+    const int groups = (p.rows.ranks[tile.slot] + GROUP - 1) / GROUP, stage_bytes = L::stage(groups), all = (p.chunks + 1) / 2;
+    const int s0 = (int)((long long)all * blockIdx.y / p.splits), n = (int)((long long)all * (blockIdx.y + 1) / p.splits) - s0;
+    auto chunks_of = [&](int i) { return min(2, p.chunks - 2 * (s0 + i)); };
+    bool ok = true;
+    if (warp < 8) {
+        // ================= x and the weights =================
+        const int r0 = 16 * warp + (lane >> 3), u = lane & 7;            // its rows: r0 + 4 i
+        const T* from = (const T*)p.x + (long long)(tile.row0 + r0) * p.ldx + s0 * 64 + 8 * u;
+        const uint8_t* weights = p.A + (size_t)tile.slot * p.a_slot + (size_t)s0 * 2 * groups * 1024;
+        const long long ldx4 = 4 * p.ldx;
+        auto place = [&](int i, int k) { return (uint32_t)((i % STAGES) * stage_bytes + (r0 + 4 * k) * 128 + ((u ^ ((r0 + 4 * k) & 7)) << 4)); };
+        auto room = [&](int i) {                     // the stage's place is free again, and its weights are on their way
+            const int at = i % STAGES;
+            if (i >= STAGES && !(ok = mbar_wait_warp(&freed[at], (uint32_t)(i / STAGES & 1) ^ 1, ctl))) return false;
+            if (threadIdx.x == 0) {
+                const uint32_t bytes = (uint32_t)(chunks_of(i) * groups * 1024);
+                mbar_arrive_expect_tx(&w_full[at], bytes);
+                bulk_g2s(smem + at * stage_bytes + L::kX, weights + (size_t)i * 2 * groups * 1024, bytes, &w_full[at]);
+            }
+            return true;
+        };
+        auto filled = [&](int i) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&x_full[i % STAGES]);
+        };
+        int asked = 0;                               // stages
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t base = smem_u32(smem);
+            for (int i = 0; i < n + STAGES - 1; ++i) {
+                if (i < n) {
+                    if (!room(i)) break;
+                    ++asked;
+                    const int left = p.N - (s0 + i) * 64 - 8 * u;
+                    const T* x = from + i * 64;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k, x += ldx4)
+                        if (r0 + 4 * k < tile.rows) {
+                            if (left >= 8) copy16(base + place(i, k), x);
+                            else copy16(smem + place(i, k), left > 0 ? x : (const T*)p.x, max(0, left) * 2);
+                        }
+                }
+                copies_commit();
+                copies_wait<STAGES - 1>();
+                if (i >= STAGES - 1) filled(i - (STAGES - 1));
+            }
+            copies_wait<0>();
+        } else {
+            uint32_t raw[4][L::kRaw];
+            auto load = [&](int i) {
+                const int left = p.N - (s0 + i) * 64 - 8 * u;
+                const T* x = from + i * 64;
+#pragma unroll
+                for (int k = 0; k < 4; ++k, x += ldx4) {
+                    const int have = r0 + 4 * k < tile.rows ? left : 0;
+                    if (have >= 8) {
+                        if constexpr (sizeof(T) == 1) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(x);
+                            raw[k][0] = v.x; raw[k][1] = v.y;
+                        } else {
+                            const uint4 a = reinterpret_cast<const uint4*>(x)[0], b = reinterpret_cast<const uint4*>(x)[1];
+                            raw[k][0] = a.x; raw[k][1] = a.y; raw[k][2] = a.z; raw[k][3] = a.w;
+                            raw[k][4] = b.x; raw[k][5] = b.y; raw[k][6] = b.z; raw[k][7] = b.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < L::kRaw; ++e) raw[k][e] = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < have) {
+                                if constexpr (sizeof(T) == 1) raw[k][e / 4] |= (uint32_t)(uint8_t)x[e] << (8 * (e & 3));
+                                else raw[k][e] = __float_as_uint(x[e]);
+                            }
+                    }
+                }
+            };
+            load(0);
+            for (int i = 0; i < n; ++i) {
+                if (!room(i)) break;
+                ++asked;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    Terms<T> x;
+                    x.make(raw[k]);
+#pragma unroll
+                    for (int j = 0; j < TERMS; ++j)
+                        *reinterpret_cast<uint4*>(smem + place(i, k) + j * (MANY_ROWS * 128)) = make_uint4(x.w[j][0], x.w[j][1], x.w[j][2], x.w[j][3]);
+                }
+                if (i + 1 < n) load(i + 1);
+                filled(i);
+            }
+        }
+        // (the weights have all landed before the block ends)
+        if (!ok && threadIdx.x == 0)
+            for (int i = max(0, asked - STAGES); i < asked; ++i) mbar_drain(&w_full[i % STAGES], (uint32_t)(i / STAGES & 1));
+    } else if (lane == 0) {
+        // ================= products =================
+        const uint64_t desc_x = umma_desc_k_sw128(smem_u32(smem)), desc_a = umma_desc_k_plain(smem_u32(smem + L::kX), 128, 512);
+        const uint32_t kDesc = idesc_bf16(MANY_ROWS, groups * GROUP);
+        for (int i = 0; i < n; ++i) {
+            const int at = i % STAGES;
+            if (!(ok = mbar_wait(&w_full[at], (uint32_t)(i / STAGES & 1), ctl))) break;
+            if (!(ok = mbar_wait(&x_full[at], (uint32_t)(i / STAGES & 1), ctl))) break;
+            tc_fence_after_sync();
+            const uint32_t here = (uint32_t)(at * (stage_bytes >> 4));
+            const int steps = 2 * chunks_of(i);                          // of 16 columns
+            for (int k = TERMS - 1; k >= 0; --k)
+                for (int j = 0; j < steps; ++j)
+                    umma_bf16_ss(tmem, desc_x + here + (uint32_t)(k * (MANY_ROWS * 128 >> 4) + 2 * j), desc_a + here + (uint32_t)((j >> 1) * groups * (1024 >> 4) + (j & 1) * (256 >> 4)),
+                                 kDesc, i > 0 || k < TERMS - 1 || j > 0);
+            umma_commit(&freed[at]);
+        }
+        // every product has ended before its place is used again
+        umma_commit(&drained);
+        mbar_drain(&drained, 0);
+    }
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    // ---- the parts: one row and half of the ranks a thread ----
+    const int pitch = L::pitch(groups);
+    if (warp < 8) {
+        const int quarter = warp & 3, half = warp >> 2, row = 32 * quarter + lane;
+        for (int j = half * groups; j < (half + 1) * groups; ++j) {      // of eight ranks
+            uint32_t v[8];
+            tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + 8u * j, v);
+            tmem_ld_wait();
+            if (row < tile.rows) {
+                uint4* to = reinterpret_cast<uint4*>(smem + row * pitch + j * 32);
+                to[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                to[1] = make_uint4(v[4], v[5], v[6], v[7]);
+            }
+        }
+    }
+    __syncthreads();
+    if (p.splits > 1) cluster_sync_all();
+    const int first = tile.rows * (int)blockIdx.y / p.splits, rows = tile.rows * (int)(blockIdx.y + 1) / p.splits - first, quads = groups * (GROUP / 4);
+    for (int i = threadIdx.x; i < rows * quads; i += MANY_THREADS) {
+        const int row = first + i / quads, quad = i % quads;
+        const uint32_t at = smem_u32(smem + row * pitch + quad * 16);
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < p.splits; ++k) {
+            float4 v;
+            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_map_u32(at, (uint32_t)k)) : "memory");
+            sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        }
+        *reinterpret_cast<float4*>(p.z + (size_t)(tile.row0 + row) * (p.groups * GROUP) + quad * 4) = sum;
+    }
+    if (p.splits > 1) cluster_sync_all();            // (a block's parts stay until the others have read them)
+    if (threadIdx.x == 0 && ctl[0]) atomicOr(p.rows.status, KV4_DEV_TIMEOUT);
+    if (warp == 8) tmem_dealloc(tmem, columns);
 }
 
 // ---- out = base + c B z ---------------------------------------------------------------------------------------------------
@@ -797,38 +1096,7 @@ adapter_up_kernel(const UpParams p)
 //   warp 8     brings the weights into shared memory (in the order they lie in: one bulk copy), and issues the products
 //   warps 0-7  one row and 32 channels a thread: base, copied ahead into the warp's own place, plus D, by way of that place to out
 
-constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32, MANY_D = 4, MANY_B = 3;   // accumulators of 64 columns; blocks of channels whose weights are there or on their way
-
-// 32 lanes x 4 consecutive 32-bit columns.
-__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4])  // whole warp
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void umma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate)
-{
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate)
-        : "memory");
-}
-// kind::f16, both operands bf16 and K-major, fp32 sums
-__host__ __device__ constexpr uint32_t idesc_bf16(int m, int n)
-{
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-
-// K-major without swizzle: eight rows of 16 bytes a matrix, the next eight rows 128 bytes on, the next eight ranks `apart`.
-__device__ __forceinline__ uint64_t umma_desc_k_plain(uint32_t smem_addr, uint32_t apart)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(apart >> 4) << 16;
-    d |= (uint64_t)(128u >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    return d;
-}
+constexpr int MANY_D = 4, MANY_B = 3;   // accumulators of 64 columns; blocks of channels whose weights are there or on their way
 
 // Shared memory (1024-aligned): Z [eight ranks of a term][128 rows][16 B] | B [MANY_B][groups][2 KB] | base [8 warps][stages][32 rows][32 channels],
 // the 16-byte unit u of row r turned by r (see unit_at)
@@ -843,41 +1111,6 @@ struct Many {
     __host__ __device__ int base() const { return z_bytes() + MANY_B * b_bytes(); }
     __host__ __device__ size_t smem() const { return (size_t)base() + 8 * kStages * kStage + 1024; }
 };
-
-// The rows of a tile: a sequence is cut evenly into as few tiles of up to MANY_ROWS rows as it takes, and they are counted sequence by
-// sequence.  One warp.
-struct SeqTile { int row0, rows, slot; };
-__device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
-{
-    const int lane = threadIdx.x & 31;
-    SeqTile found{0, 0, kNoRow};
-    for (int s0 = 0, before = 0; s0 < r.n_seq; s0 += 32) {
-        const int s = s0 + lane;
-        const int begin = s < r.n_seq ? min(max(0, r.q_start[s]), r.n_rows) : 0, end = s < r.n_seq ? min(max(0, r.q_start[s + 1]), r.n_rows) : 0;
-        const int mine = max(0, end - begin + MANY_ROWS - 1) / MANY_ROWS;
-        int scan = mine;
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += v;
-        }
-        const unsigned holds = __ballot_sync(0xffffffffu, before + scan > tile);
-        if (holds) {
-            const int in = __ffs(holds) - 1, each = mine ? (end - begin + mine - 1) / mine : 0, at = begin + (tile - before - (scan - mine)) * each;
-            found.row0 = __shfl_sync(0xffffffffu, at, in);
-            found.rows = __shfl_sync(0xffffffffu, min(each, end - at), in);
-            int slot = r.slots[s0 + in];
-            if (slot < -1 || slot >= r.n_slots) {
-                if (lane == 0) atomicOr(r.status, KV4_DEV_INDEX);
-                slot = kNoAdapter;
-            }
-            if (slot >= 0 && r.ranks[slot] == 0) slot = kNoAdapter;
-            found.slot = slot;
-            return found;
-        }
-        before += __shfl_sync(0xffffffffu, scan, 31);
-    }
-    return found;
-}
 
 template <typename T>
 __global__ void __launch_bounds__(MANY_THREADS, 2)
@@ -1002,7 +1235,7 @@ adapter_many_kernel(const UpParams p)
     if (warp == 8) {
         // ================= products =================
         if (real && lane == 0) {
-            const uint64_t desc_z = umma_desc_k_plain(smem_u32(smem), 2048), desc_b = umma_desc_k_plain(smem_u32(smem + lay.z_bytes()), 1024);
+            const uint64_t desc_z = umma_desc_k_plain(smem_u32(smem), 2048, 128), desc_b = umma_desc_k_plain(smem_u32(smem + lay.z_bytes()), 1024, 128);
             constexpr uint32_t kDesc = idesc_bf16(MANY_ROWS, BLOCK);
             for (int job = 0; job < b1 - b0; ++job) {
                 const int buf = job % MANY_B, d = job % MANY_D;
@@ -1217,6 +1450,7 @@ adapter_few_kernel(const FewParams p)
     const uint8_t* f_weights = nullptr;
     const T* f_x = nullptr;
     const O* f_base = nullptr;
+    const uint32_t a_put = (uint32_t)a_place(lane & 7, lane >> 3);
     auto aim = [&]() {
         if (run.e >= (up ? all : entries)) return;
         f_groups = entry_groups[run.e];
@@ -1236,7 +1470,7 @@ adapter_few_kernel(const FewParams p)
             const int n = min(St::chunks, run.end - run.at);
 #pragma unroll
             for (int i = 0; i < St::weights / 512; ++i)
-                if (i < 2 * n * f_groups) copy16(to32 + i * 512, f_weights + i * 512);
+                if (i < 2 * n * f_groups) copy16(ptx::smem_u32(to) + a_put + i * 512, f_weights + i * 512);
             f_weights += n * f_groups * 1024;
             const bool whole = p.d.aligned && (run.at + n) * CHUNK <= p.d.N;
             for (int c = 0; c < n; ++c, f_x += CHUNK) {
@@ -1310,13 +1544,10 @@ adapter_few_kernel(const FewParams p)
 #pragma unroll
                     for (int i = 0; i < G; ++i)
                         if (i < groups) {
-                            const uint8_t* w = from + (c * groups + i) * 1024 + lane * 16;
+                            const uint8_t* w = from + (c * groups + i) * 1024 + a_place(g, t);
                             const uint4 a0 = *reinterpret_cast<const uint4*>(w), a1 = *reinterpret_cast<const uint4*>(w + 512);
 #pragma unroll
-                            for (int k = Terms<T>::n - 1; k >= 0; --k) {
-                                mma_bf16(acc[i], a0, x.w[k][0], x.w[k][1]);
-                                mma_bf16(acc[i], a1, x.w[k][2], x.w[k][3]);
-                            }
+                            for (int k = Terms<T>::n - 1; k >= 0; --k) mma_a(acc[i], a0, a1, x.w[k]);
                         }
                 }
                 mine.at += n;
@@ -1467,6 +1698,34 @@ cudaError_t down(const DownParams& p, cudaStream_t st)
     return cudaLaunchKernelEx(&l.cfg, adapter_down_kernel<T, NT, RG>, p);
 }
 
+// Sequences cut into tiles: as many as there are if all have the same length, and how many there are at most.
+struct Tiles { int about, most; };
+Tiles tiles_of(const Rows& r)
+{
+    const int each = (r.n_rows + r.n_seq - 1) / r.n_seq;
+    return {r.n_seq * ((each + MANY_ROWS - 1) / MANY_ROWS), r.n_rows / MANY_ROWS + r.n_seq};
+}
+
+template <typename T>
+cudaError_t down_many(DownParams& p, int sms, cudaStream_t st)
+{
+    // Blocks that share a contraction: as many as run in one round with the other tiles', and as there are stages for.
+    const size_t smem = DownMany<T>::smem(p.groups);
+    const Tiles tiles = tiles_of(p.rows);
+    const int at_once = (smem <= 109 * 1024 ? 2 : 1) * sms, stages = (p.chunks + 1) / 2;
+    p.splits = 1;
+    while (p.splits < MAX_SPLITS && 2 * p.splits <= stages && (long long)tiles.about * p.splits * 2 <= at_once) p.splits *= 2;
+    PdlLaunch l((unsigned)tiles.most, MANY_THREADS, smem, st);                       // (those of tiles that are not there come last)
+    cudaLaunchAttribute attr[2] = {l.attr[0], {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.y = (unsigned)p.splits;
+    l.cfg.attrs = attr;
+    l.cfg.numAttrs = p.splits > 1 ? 2 : 1;
+    l.cfg.gridDim.y = (unsigned)p.splits;
+    return cudaLaunchKernelEx(&l.cfg, adapter_down_many_kernel<T>, p);
+}
+
 template <typename T>
 cudaError_t down_type(const DownParams& p, bool wide, cudaStream_t st)
 {
@@ -1534,7 +1793,8 @@ cudaError_t prepare()
                                (const void*)adapter_up_kernel<float, 8>, (const void*)adapter_up_kernel<__nv_bfloat16, 1>,
                                (const void*)adapter_up_kernel<__nv_bfloat16, 2>, (const void*)adapter_up_kernel<__nv_bfloat16, 4>,
                                (const void*)adapter_up_kernel<__nv_bfloat16, 8>, (const void*)adapter_many_kernel<float>,
-                               (const void*)adapter_many_kernel<__nv_bfloat16>})
+                               (const void*)adapter_many_kernel<__nv_bfloat16>, (const void*)adapter_down_many_kernel<float>,
+                               (const void*)adapter_down_many_kernel<__nv_bfloat16>, (const void*)adapter_down_many_kernel<int8_t>})
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
     return e;
 }
@@ -1566,14 +1826,12 @@ cudaError_t many(UpParams& p, int sms, cudaStream_t st)
 {
     // Blocks of channels of a block of threads: so many that all run in one round.
     const Many<T> lay{p.groups};
-    // (the tiles of sequences of equal length; there are never more than `most`)
-    const int each = (p.rows.n_rows + p.rows.n_seq - 1) / p.rows.n_seq, tiles = p.rows.n_seq * ((each + MANY_ROWS - 1) / MANY_ROWS);
-    const int most = p.rows.n_rows / MANY_ROWS + p.rows.n_seq;
+    const Tiles tiles = tiles_of(p.rows);
     const int at_once = (lay.smem() <= 109 * 1024 ? 2 : 1) * sms;
-    p.per_warp = (int)(((long long)p.blocks * tiles + at_once - 1) / at_once);
-    while ((long long)tiles * ((p.blocks + p.per_warp - 1) / p.per_warp) > at_once && p.per_warp < p.blocks) ++p.per_warp;
+    p.per_warp = (int)(((long long)p.blocks * tiles.about + at_once - 1) / at_once);
+    while ((long long)tiles.about * ((p.blocks + p.per_warp - 1) / p.per_warp) > at_once && p.per_warp < p.blocks) ++p.per_warp;
     p.columns = (p.blocks + p.per_warp - 1) / p.per_warp;
-    PdlLaunch l((unsigned)(most * p.columns), MANY_THREADS, lay.smem(), st);         // (those of tiles that are not there come last)
+    PdlLaunch l((unsigned)(tiles.most * p.columns), MANY_THREADS, lay.smem(), st);         // (those of tiles that are not there come last)
     return cudaLaunchKernelEx(&l.cfg, adapter_many_kernel<T>, p);
 }
 
@@ -1784,11 +2042,18 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     }
     const tsvd_status_t grown = grow(h, z_bytes(h, n_rows));
     if (grown != TSVD_OK) return grown;
-    const Shape s = shape_of(h, n_rows);
-    d.splits = s.splits;
     d.z = h->z;
     u.z = h->z;
-    if (dtype == TSVD_F32) TSVD_CUDA_OK(down_type<float>(d, s.wide, st));
+    // tcgen05 from 512 rows on, where sequences fill tiles of 128, as far as their number tells: 2048 rows of four, ranks of 64, 12288
+    // channels 26 us against 62; of 2048 rows by 64, 32 and 16 for each sequence, ranks of 16, 8192 channels 31, 39 and 65 against 32, 34 and 39.
+    const bool many_rows = n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH;
+    const Shape s = shape_of(h, n_rows);
+    d.splits = s.splits;
+    if (many_rows && d.aligned) {
+        if (dtype == TSVD_F32) TSVD_CUDA_OK(down_many<float>(d, h->sms, st));
+        else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_many<__nv_bfloat16>(d, h->sms, st));
+        else TSVD_CUDA_OK(down_many<int8_t>(d, h->sms, st));
+    } else if (dtype == TSVD_F32) TSVD_CUDA_OK(down_type<float>(d, s.wide, st));
     else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_type<__nv_bfloat16>(d, s.wide, st));
     else TSVD_CUDA_OK(down_type<int8_t>(d, s.wide, st));
     tsvd_count_launch();
@@ -1796,9 +2061,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
     // with few rows there are few tiles.
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows > 256 ? 16 : 8;
-    // tcgen05 from 512 rows on, where sequences fill tiles of 128, as far as their number tells: 2048 rows of four, ranks of 64, 12288
-    // channels 26 us against 62; of 2048 rows by 64, 32 and 16 for each sequence, ranks of 16, 8192 channels 31, 39 and 65 against 32, 34 and 39.
-    if (n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH) {
+    if (many_rows) {
         if (out_dtype == TSVD_F32) TSVD_CUDA_OK(many<float>(u, h->sms, st));
         else TSVD_CUDA_OK(many<__nv_bfloat16>(u, h->sms, st));
     } else if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_type<float>(u, h->sms, st));
