@@ -509,16 +509,16 @@ __device__ __forceinline__ uint64_t umma_desc_k_plain(uint32_t smem_addr, uint32
 }
 
 // The rows of a tile: a sequence is cut evenly into as few tiles of up to MANY_ROWS rows as it takes, and they are counted sequence by
-// sequence.  One warp.
-struct SeqTile { int row0, rows, slot; };
+// sequence.  A warp.  (What a sequence's adapter is comes with its ends: a load's time less.)
+struct SeqTile { int row0, rows, slot, rank; };
 __device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
 {
     const int lane = threadIdx.x & 31;
-    SeqTile found{0, 0, kNoRow};
+    SeqTile found{0, 0, kNoRow, 0};
     for (int s0 = 0, before = 0; s0 < r.n_seq; s0 += 32) {
         const int s = s0 + lane;
         const int begin = s < r.n_seq ? min(max(0, r.q_start[s]), r.n_rows) : 0, end = s < r.n_seq ? min(max(0, r.q_start[s + 1]), r.n_rows) : 0;
-        const int mine = max(0, end - begin + MANY_ROWS - 1) / MANY_ROWS;
+        const int mine = max(0, end - begin + MANY_ROWS - 1) / MANY_ROWS, its = s < r.n_seq ? r.slots[s] : kNoAdapter;
         int scan = mine;
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, scan, o);
@@ -529,13 +529,13 @@ __device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
             const int in = __ffs(holds) - 1, each = mine ? (end - begin + mine - 1) / mine : 0, at = begin + (tile - before - (scan - mine)) * each;
             found.row0 = __shfl_sync(0xffffffffu, at, in);
             found.rows = __shfl_sync(0xffffffffu, min(each, end - at), in);
-            int slot = r.slots[s0 + in];
+            int slot = __shfl_sync(0xffffffffu, its, in);
             if (slot < -1 || slot >= r.n_slots) {
                 if (lane == 0) atomicOr(r.status, KV4_DEV_INDEX);
                 slot = kNoAdapter;
             }
-            if (slot >= 0 && r.ranks[slot] == 0) slot = kNoAdapter;
-            found.slot = slot;
+            found.rank = slot >= 0 ? r.ranks[slot] : 0;
+            found.slot = found.rank ? slot : kNoAdapter;
             return found;
         }
         before += __shfl_sync(0xffffffffu, scan, 31);
@@ -564,7 +564,6 @@ adapter_down_many_kernel(const DownParams p)
     __shared__ uint64_t x_full[STAGES], w_full[STAGES], freed[STAGES], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ int ctl_[2];
-    __shared__ SeqTile tile_s;
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -580,28 +579,25 @@ adapter_down_many_kernel(const DownParams p)
     // What the kernel ahead has written is there before the next kernel starts: that one reads it ahead of its own wait.
     pdl_wait();
     pdl_launch_dependents();
-    if (warp == 0) {
-        const SeqTile found = find_tile(p.rows, (int)blockIdx.x);
-        if (lane == 0) tile_s = found;
-    }
+    const SeqTile tile = find_tile(p.rows, (int)blockIdx.x);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    const SeqTile tile = tile_s;
     if (tile.slot < 0 || tile.rows == 0) {           // (all blocks of the cluster)
         if (warp == 8) tmem_dealloc(tmem, columns);
         return;
     }
-    const int groups = (p.rows.ranks[tile.slot] + GROUP - 1) / GROUP, stage_bytes = L::stage(groups), all = (p.chunks + 1) / 2;
-    const int s0 = (int)((long long)all * blockIdx.y / p.splits), n = (int)((long long)all * (blockIdx.y + 1) / p.splits) - s0;
-    auto chunks_of = [&](int i) { return min(2, p.chunks - 2 * (s0 + i)); };
+    const int groups = (tile.rank + GROUP - 1) / GROUP, stage_bytes = L::stage(groups), all = (p.chunks + 1) / 2;
+    // Stage i of block y is the i splits + y-th of the row: what the cluster reads at a time lies side by side.
+    const int n = (all - (int)blockIdx.y + p.splits - 1) / p.splits, apart = 64 * p.splits, col0 = 64 * (int)blockIdx.y;
+    auto chunks_of = [&](int i) { return min(2, p.chunks - 2 * (i * p.splits + (int)blockIdx.y)); };
     bool ok = true;
     if (warp < 8) {
         // ================= x and the weights =================
         const int r0 = 16 * warp + (lane >> 3), u = lane & 7;            // its rows: r0 + 4 i
-        const T* from = (const T*)p.x + (long long)(tile.row0 + r0) * p.ldx + s0 * 64 + 8 * u;
-        const uint8_t* weights = p.A + (size_t)tile.slot * p.a_slot + (size_t)s0 * 2 * groups * 1024;
+        const T* from = (const T*)p.x + (long long)(tile.row0 + r0) * p.ldx + col0 + 8 * u;
+        const uint8_t* weights = p.A + (size_t)tile.slot * p.a_slot + (size_t)blockIdx.y * 2 * groups * 1024;
         const long long ldx4 = 4 * p.ldx;
         auto place = [&](int i, int k) { return (uint32_t)((i % STAGES) * stage_bytes + (r0 + 4 * k) * 128 + ((u ^ ((r0 + 4 * k) & 7)) << 4)); };
         auto room = [&](int i) {                     // the stage's place is free again, and its weights are on their way
@@ -610,7 +606,7 @@ adapter_down_many_kernel(const DownParams p)
             if (threadIdx.x == 0) {
                 const uint32_t bytes = (uint32_t)(chunks_of(i) * groups * 1024);
                 mbar_arrive_expect_tx(&w_full[at], bytes);
-                bulk_g2s(smem + at * stage_bytes + L::kX, weights + (size_t)i * 2 * groups * 1024, bytes, &w_full[at]);
+                bulk_g2s(smem + at * stage_bytes + L::kX, weights + (size_t)i * p.splits * 2 * groups * 1024, bytes, &w_full[at]);
             }
             return true;
         };
@@ -626,8 +622,8 @@ adapter_down_many_kernel(const DownParams p)
                 if (i < n) {
                     if (!room(i)) break;
                     ++asked;
-                    const int left = p.N - (s0 + i) * 64 - 8 * u;
-                    const T* x = from + i * 64;
+                    const int left = p.N - i * apart - col0 - 8 * u;
+                    const T* x = from + i * apart;
 #pragma unroll
                     for (int k = 0; k < 4; ++k, x += ldx4)
                         if (r0 + 4 * k < tile.rows) {
@@ -643,8 +639,8 @@ adapter_down_many_kernel(const DownParams p)
         } else {
             uint32_t raw[4][L::kRaw];
             auto load = [&](int i) {
-                const int left = p.N - (s0 + i) * 64 - 8 * u;
-                const T* x = from + i * 64;
+                const int left = p.N - i * apart - col0 - 8 * u;
+                const T* x = from + i * apart;
 #pragma unroll
                 for (int k = 0; k < 4; ++k, x += ldx4) {
                     const int have = r0 + 4 * k < tile.rows ? left : 0;
@@ -734,12 +730,15 @@ adapter_down_many_kernel(const DownParams p)
     for (int i = threadIdx.x; i < rows * quads; i += MANY_THREADS) {
         const int row = first + i / quads, quad = i % quads;
         const uint32_t at = smem_u32(smem + row * pitch + quad * 16);
-        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = 0; k < p.splits; ++k) {
-            float4 v;
-            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_map_u32(at, (uint32_t)k)) : "memory");
-            sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-        }
+        float4 v[MAX_SPLITS], sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < MAX_SPLITS; ++k)
+            if (k < p.splits)
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                             : "=f"(v[k].x), "=f"(v[k].y), "=f"(v[k].z), "=f"(v[k].w) : "r"(cluster_map_u32(at, (uint32_t)k)) : "memory");
+#pragma unroll
+        for (int k = 0; k < MAX_SPLITS; ++k)
+            if (k < p.splits) { sum.x += v[k].x; sum.y += v[k].y; sum.z += v[k].z; sum.w += v[k].w; }
         *reinterpret_cast<float4*>(p.z + (size_t)(tile.row0 + row) * (p.groups * GROUP) + quad * 4) = sum;
     }
     if (p.splits > 1) cluster_sync_all();            // (a block's parts stay until the others have read them)
@@ -1125,7 +1124,6 @@ adapter_many_kernel(const UpParams p)
     __shared__ uint64_t d_full[MANY_D], d_free[MANY_D], b_full[MANY_B], b_done[MANY_B], drained;
     __shared__ uint32_t tmem_slot;
     __shared__ int ctl_[2];
-    __shared__ SeqTile tile_s;
     volatile int* ctl = ctl_;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -1139,15 +1137,11 @@ adapter_many_kernel(const UpParams p)
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
     if (warp == 8) { tmem_alloc(&tmem_slot, MANY_D * 64); tmem_relinquish(); }
     // Adapters, slots and base are there: the first kernel let this one start after its own wait.  z is behind this one's wait.
-    if (warp == 0) {
-        const SeqTile found = find_tile(p.rows, (int)blockIdx.x / p.columns);
-        if (lane == 0) tile_s = found;
-    }
+    const SeqTile tile = find_tile(p.rows, (int)blockIdx.x / p.columns);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    const SeqTile tile = tile_s;
     pdl_launch_dependents();
     const bool real = tile.slot >= 0;
     if (tile.rows == 0 || (!real && p.in_place)) {
@@ -1156,7 +1150,7 @@ adapter_many_kernel(const UpParams p)
         return;
     }
     const int row0 = tile.row0, b0 = (int)blockIdx.x % p.columns * p.per_warp, b1 = min(b0 + p.per_warp, p.blocks);
-    const int rank = real ? p.rows.ranks[tile.slot] : 0, groups = (rank + GROUP - 1) / GROUP, eights = 2 * groups;
+    const int rank = tile.rank, groups = (rank + GROUP - 1) / GROUP, eights = 2 * groups;
 
     // ---- base of the next 64 channels into the warp's next stage: its rows, 32 channels of each by LANES lanes ----
     const int quarter = warp & 3, half = warp >> 2 & 1, mine0 = row0 + 32 * quarter;         // its rows (the tensor memory's lanes) and channels
@@ -2049,7 +2043,11 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     const bool many_rows = n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH;
     const Shape s = shape_of(h, n_rows);
     d.splits = s.splits;
-    if (many_rows && d.aligned) {
+    // The first product there too: its time hardly grows with the rank, and a tile has one adapter (2048 rows of four sequences, 4096
+    // columns, both products: ranks of 16, 32, 48 in 21.9, 21.9, 23.7 us against 20.5, 25.5, 31.2; five of 120 rows, 16 ranks, 13.0 against 18.0;
+    // 8192 rows 47.6 against 55.3).  fp32 is turned into terms in registers, with fewer loads under way: ranks of 16 from 4096 rows
+    // on (2048 rows 44 against 34, 8192 95 against 108).
+    if (many_rows && d.aligned && (dtype != TSVD_F32 || h->groups > 1 || n_rows >= 4096)) {
         if (dtype == TSVD_F32) TSVD_CUDA_OK(down_many<float>(d, h->sms, st));
         else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_many<__nv_bfloat16>(d, h->sms, st));
         else TSVD_CUDA_OK(down_many<int8_t>(d, h->sms, st));
