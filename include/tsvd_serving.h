@@ -136,7 +136,7 @@ tsvd_status_t tsvd_adapters_set(tsvd_adapters_t h, int slot, const void* A, long
  *   out       device, row i at out + i*ldo (ldo >= M), TSVD_F32 or TSVD_BF16.  May be base itself (same pointer and stride)
  *   slots     device, int32 [n_seq]: the slot of each sequence; -1 or an empty slot: none, the row becomes base's.  A number
  *             below -1 or from n_slots on counts as none and makes tsvd_adapters_last_status report TSVD_E_INDEX
- *   q_start   device, int32 [n_seq + 1]: the rows q_start[s] .. q_start[s+1]-1 belong to sequence s; NULL: one row each.  Rows
+ *   q_start   device, int32 [n_seq + 1], ascending: the rows q_start[s] .. q_start[s+1]-1 belong to sequence s; NULL: one row each.  Rows
  *             below q_start[0] or from q_start[n_seq] on belong to none and are not written
  * Weights are bf16; sums, A x and the result's addition fp32 (see adapters.cu); one rounding of the result.  Rows and
  * adapters do not disturb each other: what is not finite in one stays there.

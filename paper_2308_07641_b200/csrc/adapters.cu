@@ -1,15 +1,22 @@
 // Low-rank adapters of many requests beside a shared projection:  out_i = base_i + c_s B_s (A_s x_i),  s the adapter of row i's
 // sequence (A_s [rank, N], B_s [M, rank] in bf16).
 //
-// Two launches, the second a programmatic dependent of the first: z_i = A_s x_i (down), then out_i = base_i + c_s B_s z_i (up).
-// Both walk over tiles of consecutive rows, whatever sequences they belong to, and inside a tile over the adapters that its
-// rows ask for, each once; so one kernel serves single tokens with an adapter each, prompts of one adapter, and anything
-// between.  A row's result depends on its own numbers and adapter only: what the products of an adapter give for rows of
-// another one is dropped, never added.
+// z_i = A_s x_i (down), then out_i = base_i + c_s B_s z_i (up).  Three forms, chosen in tsvd_adapters_forward:
+//   few rows      one launch; a cluster of blocks takes up to eight rows through both products (adapter_few_kernel)
+//   more          two launches, the second a programmatic dependent of the first, on mma.sync: tiles of consecutive rows, whatever
+//                 sequences they belong to, and inside a tile the adapters that its rows ask for, each once (adapter_down_kernel,
+//                 adapter_up_kernel).  What the products of an adapter give for rows of another one is dropped, never added
+//   many rows of  two launches on tcgen05: tiles of up to 128 rows of one sequence, so of one adapter (adapter_down_many_kernel,
+//   a sequence    adapter_many_kernel)
+// In all of them a row's result depends on its own numbers and adapter only.
 //
-// The weights lie in the order in which the lanes of a warp hand them to mma.sync m16n8k16, 16 bytes a lane, so that a lane
-// copies (cp.async, some stages ahead) just what it will read, and nothing is exchanged between lanes.  What bounds both
-// kernels is bytes: the adapters' for single tokens, x and base and out for prompts; the products are small beside them.
+// The weights lie as tcgen05 takes them: eight rows of 16 bytes one after another, and are brought by bulk copies for it; the lanes
+// of a warp that uses mma.sync copy the 16 bytes that they will read (cp.async, some stages ahead), and nothing is exchanged.
+//
+// What bounds them, in time of the device alone (the bytes' at 6.55 TB/s in brackets): 64 tokens with 48 adapters of rank 16, 4096 to
+// 12288, 13.9 us (4.4; one token 5.9 us, so launch, two chains of loads and a cluster's exchange are most of it; of rank 64 26.2 (15.9): bytes);
+// 2046 rows of five sequences, rank 64, 38.7 us (19.5): the second product 26, base and out being 15 of the bytes' 19.5, the first
+// one 13, with 64 KB of x on their way to an SM.
 //
 // Arithmetic: bf16 operands, fp32 sums.  8-bit x is exact in bf16.  fp32 x is cut into three bf16 terms that add up to it
 // exactly.  z stays fp32 between the kernels, and enters the second product as two bf16 terms (2^-17 of it is lost, the result's
@@ -473,7 +480,10 @@ adapter_down_kernel(const DownParams p)
 //   warps 0-7  x as bf16 (its terms one after another), rows of 128 bytes swizzled; bf16 is copied as it is, the other types are turned
 //              in registers, the next stage's on their way meanwhile.  Warp 0 also asks for the weights (one bulk copy: their order)
 //   warp 8     issues the products
-// The blocks that share a tile's columns are a cluster; each adds the parts of its share of the rows, in their order.
+// The blocks that share a tile's columns are a cluster; each adds the parts of its share of the rows, in their order.  Four stages, two
+// blocks an SM: with six or eight of ranks of 64 one block fits, and clusters of eight find no place for each of sixteen tiles at once (2048
+// rows of four sequences, 4096 to 4096, both products 25.0 us against 34.4 and 34.3).  Parts sent to the block that adds them, instead of
+// fetched by it, need a place of their own, for a stage less: 36.4 against 36.1 us for five prompts.
 
 constexpr int MANY_ROWS = 128, MANY_THREADS = 9 * 32;
 
@@ -545,7 +555,7 @@ __device__ __forceinline__ SeqTile find_tile(const Rows& r, int tile)
 
 template <typename T>
 struct DownMany {
-    static constexpr int kStages = sizeof(T) == 4 ? 3 : 4, kX = Terms<T>::n * MANY_ROWS * 128, kRaw = 2 * (int)sizeof(T);     // words of eight columns
+    static constexpr int kStages = sizeof(T) == 4 ? 3 : 4, kX = Terms<T>::n * MANY_ROWS * 128;
     __host__ __device__ static constexpr int stage(int groups) { return kX + groups * 2048; }
     // (the parts lie over the stages; 16 bytes more a row, so that rows beside each other meet no bank twice)
     __host__ __device__ static constexpr int pitch(int groups) { return groups * GROUP * 4 + 16; }
@@ -637,7 +647,8 @@ adapter_down_many_kernel(const DownParams p)
             }
             copies_wait<0>();
         } else {
-            uint32_t raw[4][L::kRaw];
+            constexpr int RAW = 2 * (int)sizeof(T);              // words of eight columns
+            uint32_t raw[4][RAW];
             auto load = [&](int i) {
                 const int left = p.N - i * apart - col0 - 8 * u;
                 const T* x = from + i * apart;
@@ -655,7 +666,7 @@ adapter_down_many_kernel(const DownParams p)
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < L::kRaw; ++e) raw[k][e] = 0;
+                        for (int e = 0; e < RAW; ++e) raw[k][e] = 0;
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             if (e < have) {
@@ -695,7 +706,7 @@ adapter_down_many_kernel(const DownParams p)
             tc_fence_after_sync();
             const uint32_t here = (uint32_t)(at * (stage_bytes >> 4));
             const int steps = 2 * chunks_of(i);                          // of 16 columns
-            for (int k = TERMS - 1; k >= 0; --k)
+            for (int k = TERMS - 1; k >= 0; --k)                         // (the smallest terms first)
                 for (int j = 0; j < steps; ++j)
                     umma_bf16_ss(tmem, desc_x + here + (uint32_t)(k * (MANY_ROWS * 128 >> 4) + 2 * j), desc_a + here + (uint32_t)((j >> 1) * groups * (1024 >> 4) + (j & 1) * (256 >> 4)),
                                  kDesc, i > 0 || k < TERMS - 1 || j > 0);
@@ -1833,10 +1844,14 @@ struct Shape {
     bool wide;           // the first kernel's tiles have 32 rows, else 8
     int splits;          // blocks that share a contraction
 };
-Shape shape_of(const tsvd_adapters_s* h, int rows)
+// Tiles of 32 rows where sequences fill them, or where there are many: a tile goes over the columns once for each of its adapters, and with
+// tiles of 8 the weights are read four times as often.  Both products, 4096 to 4096, tiles of 8 and of 32: 900 rows by 20 for each sequence,
+// ranks of 32, 32.7 and 41.3 us; 300 by 10, ranks of 128, 49.2 and 58.6; 200 by 50, ranks of 128, 33.1 and 31.4; 4000 by 30, ranks of 16, 52.6
+// and 50.5.
+Shape shape_of(const tsvd_adapters_s* h, int rows, int n_seq)
 {
     Shape s;
-    s.wide = rows >= 256;
+    s.wide = rows >= 4000 || (rows >= 192 && rows / n_seq >= 32);
     const int tiles = (rows + (s.wide ? 31 : 7)) / (s.wide ? 32 : 8);
     // wide: one block an SM, in one round; else two; a chunk for every warp
     const int want = s.wide ? (h->sms > tiles ? h->sms / tiles : 1) : (2 * h->sms + tiles - 1) / tiles, most = (h->chunks + DOWN_WARPS - 1) / DOWN_WARPS;
@@ -2041,7 +2056,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     // tcgen05 from 512 rows on, where sequences fill tiles of 128, as far as their number tells: 2048 rows of four, ranks of 64, 12288
     // channels 26 us against 62; of 2048 rows by 64, 32 and 16 for each sequence, ranks of 16, 8192 channels 31, 39 and 65 against 32, 34 and 39.
     const bool many_rows = n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH;
-    const Shape s = shape_of(h, n_rows);
+    const Shape s = shape_of(h, n_rows, n_seq);
     d.splits = s.splits;
     // The first product there too: its time hardly grows with the rank, and a tile has one adapter (2048 rows of four sequences, 4096
     // columns, both products: ranks of 16, 32, 48 in 21.9, 21.9, 23.7 us against 20.5, 25.5, 31.2; five of 120 rows, 16 ranks, 13.0 against 18.0;
@@ -2057,8 +2072,9 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     tsvd_count_launch();
 
     // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
-    // with few rows there are few tiles.
-    u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows > 256 ? 16 : 8;
+    // with few rows there are few tiles (8, 16, 64 rows: 32 single tokens with ranks of 128, 4096 to 4096, 45.8, 67.8, 110 us; 200 rows by 50
+    // for each sequence 33.3, 28.4, 34.3; 900 by 20, ranks of 32, 49.0, 41.4, 45.4; 4000 by 30, ranks of 16, 80, 58, 51).
+    u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows >= 192 ? 16 : 8;
     if (many_rows) {
         if (out_dtype == TSVD_F32) TSVD_CUDA_OK(many<float>(u, h->sms, st));
         else TSVD_CUDA_OK(many<__nv_bfloat16>(u, h->sms, st));

@@ -211,3 +211,14 @@ def test_what_is_read_ahead_of_the_wait_is_there():
     assert "return" not in re.sub(r"auto \w+ = \[&\].*?\n    \};", "", up[:up.index("pdl_wait()")], flags=re.S)      # every block waits
     assert up.index("pdl_wait()") < up.index("p.z +") and up.index("pdl_wait()") < up.index("pdl_launch_dependents()")
     assert "pdl_launch_dependents" not in put and "pdl_wait" not in put
+
+
+def test_the_same_for_many_rows():
+    down, up = _body("adapters.cu", "adapter_down_many_kernel"), _body("adapters.cu", "adapter_many_kernel")
+    assert down.index("tmem_alloc(") < down.index("pdl_wait()") < down.index("pdl_launch_dependents()") < down.index("find_tile(")
+    assert up.index("tmem_alloc(") < up.index("pdl_launch_dependents()") and up.index("pdl_wait();\n    if (real)") < up.index("p.z +")
+    early = [m.start() for m in re.finditer(r"\breturn;", up)]
+    assert len(early) == 1 and "pdl_wait();" in up[early[0] - 200:early[0]]                                            # every block waits
+    # every wait of theirs has a limit, and what was under way has ended before a block does
+    for body in (down, up):
+        assert "mbar_try_wait" not in body and body.count("mbar_wait") >= 3 and "mbar_drain(&drained" in body and "KV4_DEV_TIMEOUT" in body

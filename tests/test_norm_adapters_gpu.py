@@ -254,6 +254,98 @@ def test_adapters(N, M, ranks, slots, new, kind, out):
     assert a.h.status() == 0
 
 
+MANY = [
+    # N, M, ranks, slots, rows of each sequence: at least 512 rows, 64 a sequence as a mean; tiles of up to 128 rows, stages of 64 columns
+    (32, 64, [16], [0], [512]), (64, 1, [1], [0], [513]), (96, 130, [128, 3], [0, 1, 0], [129, 255, 128]), (8, 72, [8, 8], [1, 0], [127, 640]),
+    (1001, 770, [9, 64, 33], [2, 0, -1, 1, 0, 1], [349, 1, 100, 0, 255, 90]), (4096, 192, [16, 100], [0, 1, -1, 0, 1], [1, 2, 600, 5, 900]),
+    (520, 328, [64] * 8, list(range(8)), [64, 65, 63, 1, 127, 128, 129, 60]), (200, 4100, [32], [-1, 0, -1], [300, 256, 44]),
+    (640, 640, [0, 0, 20], [0, 1], [400, 200]),
+]
+
+
+@pytest.mark.parametrize("N,M,ranks,slots,new", MANY)
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f32", "f32"), ("i8", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("i8", "bf16")])
+def test_adapters_many_rows(N, M, ranks, slots, new, kind, out):
+    """Whole sequences in tiles: rows of nobody ahead, behind and between stay as they were; in place; no base; x that cannot be copied
+    sixteen bytes at a time."""
+    import torch
+    g = _gen(N + M + len(new))
+    a = Adapters(N, M, ranks, dtype="f32" if kind == "f32" else "bf16")
+    n = sum(new)
+    for pad in (-N % 16, 1 - N % 2):
+        x, x_scale = _rows(kind, n, N, g, pad)
+        base = torch.randn(n, M + -M % 8, generator=g, device="cuda").to(_dtype(out))[:, :M]
+        want = a.check(x, base, slots, new, x_scale)
+        over = base.clone()
+        start = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
+        ids = torch.tensor(slots, dtype=torch.int32, device="cuda")
+        a.h(x, over, ids, start, x_scale=x_scale, out=over)
+        assert torch.equal(over, want)
+        start = start.clamp(3, n - 2)                          # (borders ascend)
+        left = torch.full((n + 1, M + 1), 7.0, device="cuda").to(_dtype(out))
+        a.h(x, base, ids, start, x_scale=x_scale, out=left[:n, :M])
+        assert (left[:3] == 7).all() and (left[n - 2:] == 7).all() and (left[:, M] == 7).all()
+        assert torch.isfinite(left).all()
+        if (kind == "bf16") == (out == "bf16"):
+            a.check(x, None, slots, new, x_scale)
+    assert a.h.status() == 0
+
+
+def test_adapters_many_rows_keep_to_themselves():
+    """What is not finite in a row or an adapter stays with it, in tiles that other rows share too."""
+    import torch
+    g = _gen(18)
+    a = Adapters(328, 200, [8, 8, 20])
+    a.h.set(1, torch.full((8, 328), float("nan"), device="cuda"), torch.full((200, 8), float("inf"), device="cuda"))
+    x, base = torch.randn(700, 328, generator=g, device="cuda").bfloat16(), torch.randn(700, 200, generator=g, device="cuda").bfloat16()
+    x[3], x[517] = float("nan"), float("inf")
+    new, slots = [150, 250, 300], [0, 1, 2]
+    start = torch.tensor([0, 150, 400, 700], dtype=torch.int32, device="cuda")
+    out = a.h(x, base, torch.tensor(slots, dtype=torch.int32, device="cuda"), start)
+    ok = torch.ones(700, dtype=torch.bool, device="cuda")
+    ok[150:400] = ok[3] = ok[517] = False
+    assert torch.isfinite(out[ok]).all() and not torch.isfinite(out[~ok]).any()
+    x[3] = x[517] = 0
+    clean = a.check(x[:150], base[:150], [0], [150])
+    assert ((clean.double() - out[:150].double()).abs()[ok[:150]] <= 4 * U8 * clean.double().abs()[ok[:150]] + 1e-2).all()
+    a.h.clear(1)
+    again = a.check(x, base, [0, -1, 2], new)
+    assert torch.equal(again[150:400], base[150:400])
+
+
+def test_adapters_many_rows_move_under_a_graph():
+    """The number of tiles is counted on the device: borders that move, also beyond the rows, and slots that are not there."""
+    import torch
+    from paper_2308_07641_b200 import binding
+    g = _gen(19)
+    a = Adapters(256, 320, [24, 64, 5])
+    n = 700
+    x, base = torch.randn(n, 256, generator=g, device="cuda").bfloat16(), torch.randn(n, 320, generator=g, device="cuda").bfloat16()
+    start = torch.tensor([0, 128, 256, 384, 512, 640, 700], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([0, 1, 2, 0, 1, 2], dtype=torch.int32, device="cuda")
+    a.h.reserve(n)
+    out = torch.empty_like(base)
+    a.h(x, base, slots, start, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.h(x, base, slots, start, out=out)
+    for new, ids in (([128, 128, 128, 128, 128, 60], [0, 1, 2, 0, 1, 2]), ([129, 1, 129, 1, 129, 311], [2, 1, 0, -1, 1, 0]),
+                     ([0, 0, 700, 0, 0, 0], [0, 1, 1, 2, 0, 1]), ([1, 1, 1, 1, 1, 695], [0, 1, 2, 0, -1, 2]), ([117] * 5 + [115], [-1] * 6)):
+        start.copy_(torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32))
+        slots.copy_(torch.tensor(ids, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(out, a.check(x, base, ids, new))
+    # beyond the rows: cut off; slots that are not there: base, and a status
+    want = a.check(x, base, [0, 1, 2, -1, -1, 0], [100, 100, 100, 100, 100, 200])
+    start.copy_(torch.tensor([-9, 100, 200, 300, 400, 500, 2 ** 31 - 1], dtype=torch.int32))
+    slots.copy_(torch.tensor([0, 1, 2, 3, -2 ** 31, 0], dtype=torch.int32))
+    assert a.h.status() == 0
+    graph.replay()
+    assert torch.equal(out, want)
+    assert a.h.status() == binding.TSVD_E_INDEX and a.h.status() == 0
+
+
 def test_adapters_in_place_and_bounds():
     """out is base; rows of an out with padding; rows of no sequence, and what lies beside the rows, stay as they were."""
     import torch
