@@ -1827,7 +1827,7 @@ cudaError_t up_type(UpParams& p, int sms, cudaStream_t st)
 }
 
 template <typename T>
-cudaError_t many(UpParams& p, int sms, cudaStream_t st)
+cudaError_t up_many(UpParams& p, int sms, cudaStream_t st)
 {
     // Blocks of channels of a block of threads: so many that all run in one round.
     const Many<T> lay{p.groups};
@@ -1862,7 +1862,6 @@ Shape shape_of(const tsvd_adapters_s* h, int rows, int n_seq)
 // How the kernel for few rows serves a call of so many, if it does (else cluster = 0): clusters of as many blocks as have a chunk
 // or a block of channels for each of their warps, eight at most, or half or a quarter of that where this lets more blocks run; as few
 // rows each as are served by the clusters that run at a time (a second round would cost what the other kernels' second launch does).
-constexpr int MANY_FROM = 512, MANY_EACH = 64;
 struct Few { int cluster, rows; };
 Few few_of(const tsvd_adapters_s* h, int rows)
 {
@@ -1881,7 +1880,19 @@ Few few_of(const tsvd_adapters_s* h, int rows)
         }
     return best;
 }
-size_t z_bytes(const tsvd_adapters_s* h, int rows) { return few_of(h, rows).cluster ? 0 : (size_t)rows * h->groups * GROUP * sizeof(float); }
+// The kernels on tcgen05 where sequences have rows for a tile of 128, as far as their number tells: half of one, a quarter where ranks above
+// 48 make the warps' products long.  2048 rows by 64 and 32 for each sequence, 2048 to 8192, ranks of 16: 30 and 48 us against 32 and 34; 4096 to
+// 4096, ranks of 32, 1024 rows by 32 25.6 against 26.7; ranks of 64, 4000 rows by 50 and 20 63 and 134 against 95 and 116; of 128, 300 rows by 40 22
+// against 41.
+constexpr int MANY_FROM = 192;
+bool many_rows(const tsvd_adapters_s* h, int rows, int n_seq) { return rows >= MANY_FROM && rows / n_seq >= (h->groups >= 4 ? 32 : 64); }
+// What both could serve is the kernel's for few rows (512 rows of four sequences, 4096 to 4096, ranks of 16 10.8 us against 16.5, of 64 17.1
+// against 19.4), but for ranks above 48 where its clusters leave a third of the device idle (300 rows of three, 4096 to 12288, 40.6 against 20.2).
+bool prefers_many(const tsvd_adapters_s* h, const Few& how, int rows, int n_seq)
+{
+    return h->groups >= 4 && many_rows(h, rows, n_seq) && 3 * ((rows + how.rows - 1) / how.rows) * how.cluster < 2 * h->sms;
+}
+size_t z_bytes(const tsvd_adapters_s* h, int rows) { return (size_t)rows * h->groups * GROUP * sizeof(float); }
 
 tsvd_status_t grow(tsvd_adapters_s* h, size_t need)
 {
@@ -2001,8 +2012,8 @@ extern "C" tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max)
     if (!h) return TSVD_E_NULL;
     if (rows_max < 1) return TSVD_E_SHAPE;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
-    const size_t need = (size_t)rows_max * h->groups * GROUP * sizeof(float);
-    return few_of(h, rows_max).cluster ? TSVD_OK : grow(h, need);
+    const bool none = few_of(h, rows_max).cluster && (h->groups < 4 || rows_max < MANY_FROM);          // no call of so many rows or fewer needs it
+    return none ? TSVD_OK : grow(h, z_bytes(h, rows_max));
 }
 
 extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
@@ -2040,7 +2051,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     u.blocks = h->blocks;
     u.B = h->B;
     u.b_slot = h->b_slot;
-    if (const Few how = few_of(h, n_rows); how.cluster) {
+    if (const Few how = few_of(h, n_rows); how.cluster && !prefers_many(h, how, n_rows, n_seq)) {
         const FewParams f{d, u, how.cluster, how.rows};
         const unsigned tiles = (unsigned)((n_rows + how.rows - 1) / how.rows);
         if (dtype == TSVD_F32) TSVD_CUDA_OK(few<float>(f, tiles, out_dtype == TSVD_F32, st));
@@ -2053,16 +2064,14 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     if (grown != TSVD_OK) return grown;
     d.z = h->z;
     u.z = h->z;
-    // tcgen05 from 512 rows on, where sequences fill tiles of 128, as far as their number tells: 2048 rows of four, ranks of 64, 12288
-    // channels 26 us against 62; of 2048 rows by 64, 32 and 16 for each sequence, ranks of 16, 8192 channels 31, 39 and 65 against 32, 34 and 39.
-    const bool many_rows = n_rows >= MANY_FROM && n_rows / n_seq >= MANY_EACH;
+    const bool many = many_rows(h, n_rows, n_seq);
     const Shape s = shape_of(h, n_rows, n_seq);
     d.splits = s.splits;
     // The first product there too: its time hardly grows with the rank, and a tile has one adapter (2048 rows of four sequences, 4096
     // columns, both products: ranks of 16, 32, 48 in 21.9, 21.9, 23.7 us against 20.5, 25.5, 31.2; five of 120 rows, 16 ranks, 13.0 against 18.0;
     // 8192 rows 47.6 against 55.3).  fp32 is turned into terms in registers, with fewer loads under way: ranks of 16 from 4096 rows
     // on (2048 rows 44 against 34, 8192 95 against 108).
-    if (many_rows && d.aligned && (dtype != TSVD_F32 || h->groups > 1 || n_rows >= 4096)) {
+    if (many && d.aligned && (dtype != TSVD_F32 || h->groups > 1 || n_rows >= 4096)) {
         if (dtype == TSVD_F32) TSVD_CUDA_OK(down_many<float>(d, h->sms, st));
         else if (dtype == TSVD_BF16) TSVD_CUDA_OK(down_many<__nv_bfloat16>(d, h->sms, st));
         else TSVD_CUDA_OK(down_many<int8_t>(d, h->sms, st));
@@ -2075,9 +2084,9 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     // with few rows there are few tiles (8, 16, 64 rows: 32 single tokens with ranks of 128, 4096 to 4096, 45.8, 67.8, 110 us; 200 rows by 50
     // for each sequence 33.3, 28.4, 34.3; 900 by 20, ranks of 32, 49.0, 41.4, 45.4; 4000 by 30, ranks of 16, 80, 58, 51).
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows >= 192 ? 16 : 8;
-    if (many_rows) {
-        if (out_dtype == TSVD_F32) TSVD_CUDA_OK(many<float>(u, h->sms, st));
-        else TSVD_CUDA_OK(many<__nv_bfloat16>(u, h->sms, st));
+    if (many) {
+        if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_many<float>(u, h->sms, st));
+        else TSVD_CUDA_OK(up_many<__nv_bfloat16>(u, h->sms, st));
     } else if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_type<float>(u, h->sms, st));
     else TSVD_CUDA_OK(up_type<__nv_bfloat16>(u, h->sms, st));
     tsvd_count_launch();

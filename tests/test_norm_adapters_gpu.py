@@ -255,11 +255,12 @@ def test_adapters(N, M, ranks, slots, new, kind, out):
 
 
 MANY = [
-    # N, M, ranks, slots, rows of each sequence: at least 512 rows, 64 a sequence as a mean; tiles of up to 128 rows, stages of 64 columns
+    # N, M, ranks, slots, rows of each sequence: 600 rows or so, 64 a sequence as a mean (ranks above 48: 200, 32); tiles of up to 128 rows,
+    # stages of 64 columns
     (32, 64, [16], [0], [512]), (64, 1, [1], [0], [513]), (96, 130, [128, 3], [0, 1, 0], [129, 255, 128]), (8, 72, [8, 8], [1, 0], [127, 640]),
     (1001, 770, [9, 64, 33], [2, 0, -1, 1, 0, 1], [349, 1, 100, 0, 255, 90]), (4096, 192, [16, 100], [0, 1, -1, 0, 1], [1, 2, 600, 5, 900]),
     (520, 328, [64] * 8, list(range(8)), [64, 65, 63, 1, 127, 128, 129, 60]), (200, 4100, [32], [-1, 0, -1], [300, 256, 44]),
-    (640, 640, [0, 0, 20], [0, 1], [400, 200]),
+    (640, 640, [0, 0, 20], [0, 1], [400, 200]), (328, 2100, [64, 50], [0, 1, 0], [66, 100, 51]), (264, 200, [128, 70], [1, 0, 1, -1], [40, 31, 90, 40]),
 ]
 
 
