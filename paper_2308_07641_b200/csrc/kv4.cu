@@ -177,7 +177,11 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* k, long long ldk, const T* v, 
 // Pairs (u, v) of a head's first `turned` numbers become (u cos - v sin, v cos + u sin), every product and sum rounded to fp32,
 // and go on in fp32: keys into the cache's codes, queries rounded once to their type.  The table holds, for each position, the
 // cosines of its turned / 2 angles and then their sines, so nothing here knows how the angles were chosen, and far positions
-// are as exact as near ones.
+// are as exact as near ones.  A row's cosines and sines are one line of the table, which its heads share from the caches.
+//
+// Bound by instructions, as the append without it is: 4095 rows of 32 heads of 128, keys, values and queries, 49 us (floor 24; the
+// append alone 33).  Read twice, once for either half of a pair, it took 64.  One token of 64 sequences, 32 heads on 8, and
+// the read of it 6.1 us: two launches, each two round trips to memory.
 struct Turn {
     const float* table;      // [positions][turned]
     int turned, positions;

@@ -24,6 +24,10 @@
 // persistent blocks whose copies run ahead into the next pair (57: the row loop needs more registers and a step takes 2300).
 // With one row tile alone the codes bound it, 2 us per 128 positions: both groups of row warps on one tile gained nothing.
 //
+// With first positions beside a window (SINKS, kernels of their own) a block walks over the tiles of both as one run, and each row tile
+// leaves out the steps that only the other one's window holds: a prompt of 4096 tokens, 32 heads of 128, window 1024 and 16 first ones
+// 118 us (floor 39; 512 blocks on 148 SMs are 3.5 rounds of 3.8 us of start and 2 of end); seven pieces of 16 heads of 64 on 4, 32 us.
+//
 // Arithmetic: q as fp16 times a power of two for each row that brings its largest number to 2^15 (a bf16 number is then exact
 // down to 2^-32 of it; the power goes into the row's factor c), keys and values as fp16 (one rounding), probabilities as fp16,
 // sums in fp32 (that of the probabilities before their rounding).  The roundings, 2^-12 of a term at most, are what fp16
@@ -660,7 +664,7 @@ kv4_prefill_kernel(const PreParams p)
             const int blk = (SINKS && k >= front ? k + gap : k) * (PRE_KEYS / KV4_BLOCK) + (lane & 7);
             const uint8_t* src = nullptr;
             // (with SINKS, blocks that no row of the pair sees may lie in pages that are gone)
-            const bool seen = !SINKS || blk * KV4_BLOCK < p.sinks || blk * KV4_BLOCK + KV4_BLOCK > token_lo(row_base / p.group);
+            const bool seen = !SINKS || (long long)blk * KV4_BLOCK < p.sinks || (long long)(blk + 1) * KV4_BLOCK > token_lo(row_base / p.group);
             if (seen && (long long)blk * KV4_BLOCK < len_in) {
                 const int page = p.b.table[(long long)s * p.b.max_pages + blk / per_page];
                 if (page >= 0 && page < p.g.n_pages) src = p.g.block(page, head, blk % per_page * KV4_BLOCK);
