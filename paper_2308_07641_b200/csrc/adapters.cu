@@ -401,6 +401,7 @@ adapter_down_kernel(const DownParams p)
                         for (int k = 0; k < 4; ++k) acc[i][n][k] = 0.0f;
                 for (int c = c0 + warp; c < c1; c += DOWN_WARPS) {
                     copies_wait<STAGES - 2>();
+                    __syncwarp();                    // (weights are the other lanes' copies too; and the place that fetch fills has been read)
                     const uint8_t* from = ring + stage * STAGE;
                     uint4 a[RG][2];
 #pragma unroll
@@ -1542,6 +1543,7 @@ adapter_few_kernel(const FewParams p)
             while (mine.at < mine.end) {
                 const int n = min(St::chunks, mine.end - mine.at);
                 arrived();
+                __syncwarp();                                    // (weights are the other lanes' copies too)
                 const uint8_t* from = ring + stage * St::bytes;
                 for (int c = 0; c < n; ++c) {
                     Terms<T> x{};

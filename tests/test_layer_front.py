@@ -222,3 +222,13 @@ def test_the_same_for_many_rows():
     # every wait of theirs has a limit, and what was under way has ended before a block does
     for body in (down, up):
         assert "mbar_try_wait" not in body and body.count("mbar_wait") >= 3 and "mbar_drain(&drained" in body and "KV4_DEV_TIMEOUT" in body
+
+
+def test_lanes_that_read_what_others_copied_wait_for_them():
+    """The adapters' rings: a lane's wait covers its own copies only, so the warp meets before it reads (and with that before the place
+    read last is filled again)."""
+    for name, waits in (("adapter_down_kernel", 1), ("adapter_few_kernel", 2)):
+        after = re.findall(r"(?:arrived\(\)|copies_wait<STAGES - 2>\(\));\s*(\S+)", _body("adapters.cu", name))
+        assert after == ["__syncwarp();"] * waits, name
+    many = re.findall(r"copies_wait<L::kStages - 2>\(\);\s*(\S+)", _body("adapters.cu", "adapter_many_kernel"))
+    assert many == ["__syncwarp();"]
