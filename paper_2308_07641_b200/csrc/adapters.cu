@@ -1889,10 +1889,13 @@ Few few_of(const tsvd_adapters_s* h, int rows)
 constexpr int MANY_FROM = 192;
 bool many_rows(const tsvd_adapters_s* h, int rows, int n_seq) { return rows >= MANY_FROM && rows / n_seq >= (h->groups >= 4 ? 32 : 64); }
 // What both could serve is the kernel's for few rows (512 rows of four sequences, 4096 to 4096, ranks of 16 10.8 us against 16.5, of 64 17.1
-// against 19.4), but for ranks above 48 where its clusters leave a third of the device idle (300 rows of three, 4096 to 12288, 40.6 against 20.2).
+// against 19.4), but for adapters of half a megabyte and more where its clusters, each of which reads them, leave a third of the device idle
+// (300 rows of three sequences: 4096 to 4096, ranks of 16 and 32 13.2 and 17.6 against 14.1 and 15.4; 4096 to 12288, ranks of 16, 32 and 64 21.8,
+// 30.8 and 40.6 against 17.4, 18.4 and 20.2).
+bool large(const tsvd_adapters_s* h) { return h->a_slot + h->b_slot >= 512 * 1024; }
 bool prefers_many(const tsvd_adapters_s* h, const Few& how, int rows, int n_seq)
 {
-    return h->groups >= 4 && many_rows(h, rows, n_seq) && 3 * ((rows + how.rows - 1) / how.rows) * how.cluster < 2 * h->sms;
+    return large(h) && many_rows(h, rows, n_seq) && 3 * ((rows + how.rows - 1) / how.rows) * how.cluster < 2 * h->sms;
 }
 size_t z_bytes(const tsvd_adapters_s* h, int rows) { return (size_t)rows * h->groups * GROUP * sizeof(float); }
 
@@ -2014,7 +2017,7 @@ extern "C" tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max)
     if (!h) return TSVD_E_NULL;
     if (rows_max < 1) return TSVD_E_SHAPE;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
-    const bool none = few_of(h, rows_max).cluster && (h->groups < 4 || rows_max < MANY_FROM);          // no call of so many rows or fewer needs it
+    const bool none = few_of(h, rows_max).cluster && (!large(h) || rows_max < MANY_FROM);          // no call of so many rows or fewer needs it
     return none ? TSVD_OK : grow(h, z_bytes(h, rows_max));
 }
 

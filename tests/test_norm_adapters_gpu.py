@@ -347,6 +347,24 @@ def test_adapters_many_rows_move_under_a_graph():
     assert a.h.status() == binding.TSVD_E_INDEX and a.h.status() == 0
 
 
+@pytest.mark.parametrize("rank", [16, 32, 64, 128])
+def test_adapters_reserved_rows_need_no_memory(rank):
+    """A first call under capture, whichever way it takes: nothing is allocated after reserve."""
+    import torch
+    g = _gen(rank)
+    a = Adapters(4096, 4096, [rank, rank])
+    a.h.reserve(300)
+    for n, new in ((300, [100, 200]), (300, [1] * 300), (200, [150, 50]), (40, [40]), (1, [1])):
+        x, base = (torch.randn(n, 4096, generator=g, device="cuda").bfloat16() for _ in range(2))
+        slots = torch.tensor([i % 2 for i in range(len(new))], dtype=torch.int32, device="cuda")
+        start = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = a.h(x, base, slots, start)
+        graph.replay()
+        assert torch.equal(out, a.check(x, base, slots.tolist(), new))
+
+
 def test_adapters_in_place_and_bounds():
     """out is base; rows of an out with padding; rows of no sequence, and what lies beside the rows, stay as they were."""
     import torch
