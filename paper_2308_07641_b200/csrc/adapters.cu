@@ -587,14 +587,14 @@ adapter_down_many_kernel(const DownParams p)
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
     const uint32_t columns = p.groups <= 2 ? 32u : p.groups <= 4 ? 64u : 128u;
     if (warp == 8) { tmem_alloc(&tmem_slot, columns); tmem_relinquish(); }
-    // What the kernel ahead has written is there before the next kernel starts: that one reads it ahead of its own wait.
     pdl_wait();
-    pdl_launch_dependents();
     const SeqTile tile = find_tile(p.rows, (int)blockIdx.x);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
+    // (behind the wait as well: what the kernel ahead has written is there before the next kernel, which reads it ahead of its own)
+    pdl_launch_dependents();
     if (tile.slot < 0 || tile.rows == 0) {           // (all blocks of the cluster)
         if (warp == 8) tmem_dealloc(tmem, columns);
         return;

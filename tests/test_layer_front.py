@@ -215,8 +215,10 @@ def test_what_is_read_ahead_of_the_wait_is_there():
 
 def test_the_same_for_many_rows():
     down, up = _body("adapters.cu", "adapter_down_many_kernel"), _body("adapters.cu", "adapter_many_kernel")
-    assert down.index("tmem_alloc(") < down.index("pdl_wait()") < down.index("pdl_launch_dependents()") < down.index("find_tile(")
-    assert up.index("tmem_alloc(") < up.index("pdl_launch_dependents()") and up.index("pdl_wait();\n    if (real)") < up.index("p.z +")
+    for body in (down, up):                  # the whole block has its tensor memory, not only the warp that asks for it
+        assert body.index("tmem_alloc(") < body.index("__syncthreads()") < body.index("pdl_launch_dependents()")
+    assert down.index("tmem_alloc(") < down.index("pdl_wait()") < down.index("find_tile(") and down.index("pdl_wait()") < down.index("pdl_launch_dependents()")
+    assert up.index("pdl_wait();\n    if (real)") < up.index("p.z +")
     early = [m.start() for m in re.finditer(r"\breturn;", up)]
     assert len(early) == 1 and "pdl_wait();" in up[early[0] - 200:early[0]]                                            # every block waits
     # every wait of theirs has a limit, and what was under way has ended before a block does
