@@ -736,7 +736,11 @@ adapter_down_many_kernel(const DownParams p)
             }
         }
     }
+    tc_fence_before_sync();
     __syncthreads();
+    tc_fence_after_sync();
+    // The tensor memory goes back before the cluster meets: its blocks share SMs with others that may wait for it (see PdlLaunch).
+    if (warp == 8) tmem_dealloc(tmem, columns);
     if (p.splits > 1) cluster_sync_all();
     const int first = tile.rows * (int)blockIdx.y / p.splits, rows = tile.rows * (int)(blockIdx.y + 1) / p.splits - first, quads = groups * (GROUP / 4);
     for (int i = threadIdx.x; i < rows * quads; i += MANY_THREADS) {
@@ -755,7 +759,6 @@ adapter_down_many_kernel(const DownParams p)
     }
     if (p.splits > 1) cluster_sync_all();            // (a block's parts stay until the others have read them)
     if (threadIdx.x == 0 && ctl[0]) atomicOr(p.rows.status, KV4_DEV_TIMEOUT);
-    if (warp == 8) tmem_dealloc(tmem, columns);
 }
 
 // ---- out = base + c B z ---------------------------------------------------------------------------------------------------

@@ -146,8 +146,9 @@ constexpr int TSVD_DEV_BOUNDS = 4;    // checked builds (-DTSVD_CHECK_BOUNDS): a
 // still has to get.
 //
 // Blocks of a cluster that wait for one another while they hold tensor memory: were two such blocks to share an SM, each of
-// two clusters (of one launch, or of two streams) could hold the columns that the other one waits for.  Their launches ask
-// for more than half of an SM's shared memory, so that no two of them ever do.
+// two clusters (of one launch, or of two streams) could hold the columns that the other one waits for.  So their launches ask
+// for more than half of an SM's shared memory, and no two of them ever do; or, where blocks are to share an SM, a block gives
+// its columns back before it first waits for its cluster: it then comes to that point whatever the others do.
 constexpr size_t TSVD_SM_SMEM = 228 * 1024;
 constexpr size_t TSVD_ALONE_SMEM = 116 * 1024;
 static_assert(2 * TSVD_ALONE_SMEM > TSVD_SM_SMEM, "two blocks of cluster kernels would fit one SM");
