@@ -604,6 +604,7 @@ adapter_down_many_kernel(const DownParams p)
     const int n = (all - (int)blockIdx.y + p.splits - 1) / p.splits, apart = 64 * p.splits, col0 = 64 * (int)blockIdx.y;
     auto chunks_of = [&](int i) { return min(2, p.chunks - 2 * (i * p.splits + (int)blockIdx.y)); };
     bool ok = true;
+    int asked = 0;                                   // stages whose weights were asked for
     if (warp < 8) {
         // ================= x and the weights =================
         const int r0 = 16 * warp + (lane >> 3), u = lane & 7;            // its rows: r0 + 4 i
@@ -626,7 +627,6 @@ adapter_down_many_kernel(const DownParams p)
             __syncwarp();
             if (lane == 0) mbar_arrive(&x_full[i % STAGES]);
         };
-        int asked = 0;                               // stages
         if constexpr (sizeof(T) == 2) {
             const uint32_t base = smem_u32(smem);
             for (int i = 0; i < n + STAGES - 1; ++i) {
@@ -693,9 +693,6 @@ adapter_down_many_kernel(const DownParams p)
                 filled(i);
             }
         }
-        // (the weights have all landed before the block ends)
-        if (!ok && threadIdx.x == 0)
-            for (int i = max(0, asked - STAGES); i < asked; ++i) mbar_drain(&w_full[i % STAGES], (uint32_t)(i / STAGES & 1));
     } else if (lane == 0) {
         // ================= products =================
         const uint64_t desc_x = umma_desc_k_sw128(smem_u32(smem)), desc_a = umma_desc_k_plain(smem_u32(smem + L::kX), 128, 512);
@@ -721,6 +718,12 @@ adapter_down_many_kernel(const DownParams p)
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    // Whoever gave up a wait, weights may still be on their way: they land before the parts lie over the stages, and the block ends.
+    if (ctl[0]) {
+        if (threadIdx.x == 0)
+            for (int i = max(0, asked - STAGES); i < asked; ++i) mbar_drain(&w_full[i % STAGES], (uint32_t)(i / STAGES & 1));
+        __syncthreads();
+    }
     // ---- the parts: one row and half of the ranks a thread ----
     const int pitch = L::pitch(groups);
     if (warp < 8) {
