@@ -147,6 +147,14 @@ tsvd_status_t tsvd_adapters_set(tsvd_adapters_t h, int slot, const void* A, long
 tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
                                     const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
                                     const int* slots, const int* q_start, int n_seq, int n_rows, void* stream);
+/*
+ * tsvd_adapters_forward_ex -- the same with flags: 0 or TSVD_FLAG_TEST_STALL (tsvd.h).  With that the weights never reach the products
+ * of sequences of many rows (those on tcgen05), their waits run out after some milliseconds, out is unspecified and
+ * tsvd_adapters_last_status reports TSVD_E_TIMEOUT; the other forms wait for nothing and take no notice of it.
+ */
+tsvd_status_t tsvd_adapters_forward_ex(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
+                                       const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
+                                       const int* slots, const int* q_start, int n_seq, int n_rows, unsigned flags, void* stream);
 /* Scratch for calls of up to rows_max rows, so that none of them allocates. */
 tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max);
 tsvd_status_t tsvd_adapters_info(tsvd_adapters_t h, int* N, int* M, int* max_rank, int* n_slots, size_t* bytes);

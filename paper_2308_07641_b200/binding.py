@@ -49,8 +49,8 @@ EXPORTS = ("tsvd_pack", "tsvd_forward", "tsvd_forward_ex", "tsvd_forward_host", 
            "tsvd_i8_last_status", "tsvd_i8_destroy", "tsvd_kv4_create", "tsvd_kv4_append", "tsvd_kv4_read",
            "tsvd_kv4_attend", "tsvd_kv4_info", "tsvd_kv4_last_status", "tsvd_kv4_destroy",
            "tsvd_rms_norm", "tsvd_kv4_append_rotated", "tsvd_rotary_table", "tsvd_kv4_attend_sinks",
-           "tsvd_adapters_create", "tsvd_adapters_set", "tsvd_adapters_forward", "tsvd_adapters_reserve", "tsvd_adapters_info",
-           "tsvd_adapters_last_status", "tsvd_adapters_destroy")
+           "tsvd_adapters_create", "tsvd_adapters_set", "tsvd_adapters_forward", "tsvd_adapters_forward_ex", "tsvd_adapters_reserve",
+           "tsvd_adapters_info", "tsvd_adapters_last_status", "tsvd_adapters_destroy")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -140,6 +140,7 @@ def lib() -> ctypes.CDLL:
         L.tsvd_adapters_create.argtypes = [ci, ci, ci, ci, ctypes.POINTER(vp)]
         L.tsvd_adapters_set.argtypes = [vp, ci, vp, ll, vp, ll, ci, ci, ctypes.c_float, vp]
         L.tsvd_adapters_forward.argtypes = [vp, vp, ll, vp, ci, vp, ll, vp, ll, ci, vp, vp, ci, ci, vp]
+        L.tsvd_adapters_forward_ex.argtypes = [vp, vp, ll, vp, ci, vp, ll, vp, ll, ci, vp, vp, ci, ci, cu, vp]
         L.tsvd_adapters_reserve.argtypes = [vp, ci]
         L.tsvd_adapters_info.argtypes = [vp] + [ctypes.POINTER(ci)] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
         L.tsvd_adapters_last_status.argtypes = [vp]
@@ -149,7 +150,7 @@ def lib() -> ctypes.CDLL:
         L.tsvd_kv4_destroy.argtypes = [vp]
         for f in ("quantize", "dequantize", "i8_pack", "i8_forward", "i8_reserve", "i8_info", "i8_last_status", "kv4_create",
                   "kv4_append", "kv4_read", "kv4_attend", "kv4_info", "kv4_last_status", "rms_norm", "kv4_append_rotated", "rotary_table",
-                  "kv4_attend_sinks", "adapters_create", "adapters_set", "adapters_forward", "adapters_reserve", "adapters_info",
+                  "kv4_attend_sinks", "adapters_create", "adapters_set", "adapters_forward", "adapters_forward_ex", "adapters_reserve", "adapters_info",
                   "adapters_last_status"):
             getattr(L, "tsvd_" + f).restype = ci
         L.tsvd_i8_destroy.restype = None
@@ -411,6 +412,13 @@ def tsvd_adapters_forward(h: int, x_ptr: int, ldx: int, x_scale_ptr: int, dtype:
                           out_dtype: int, slots_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, stream: int = 0) -> None:
     _check(lib().tsvd_adapters_forward(h, x_ptr, ldx, x_scale_ptr or None, dtype, base_ptr or None, ldb, out_ptr, ldo, out_dtype, slots_ptr,
                                        q_start_ptr or None, n_seq, n_rows, stream or None), "tsvd_adapters_forward")
+
+
+def tsvd_adapters_forward_ex(h: int, x_ptr: int, ldx: int, x_scale_ptr: int, dtype: int, base_ptr: int, ldb: int, out_ptr: int, ldo: int,
+                             out_dtype: int, slots_ptr: int, q_start_ptr: int, n_seq: int, n_rows: int, flags: int = 0,
+                             stream: int = 0) -> None:
+    _check(lib().tsvd_adapters_forward_ex(h, x_ptr, ldx, x_scale_ptr or None, dtype, base_ptr or None, ldb, out_ptr, ldo, out_dtype, slots_ptr,
+                                          q_start_ptr or None, n_seq, n_rows, flags, stream or None), "tsvd_adapters_forward_ex")
 
 
 def tsvd_adapters_reserve(h: int, rows_max: int) -> None:

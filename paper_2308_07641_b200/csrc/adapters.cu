@@ -206,6 +206,7 @@ struct DownParams {
     const uint8_t* A;
     size_t a_slot;
     float* z;
+    int test_stall;          // test hook (tcgen05): the weights are never copied, so the waits must give up
 };
 
 template <typename T> constexpr int kXBytes = 8 * (int)sizeof(T);    // of a lane: eight columns of a row
@@ -581,7 +582,7 @@ adapter_down_many_kernel(const DownParams p)
         for (int i = 0; i < STAGES; ++i) { mbar_init(&x_full[i], 8); mbar_init(&w_full[i], 1); mbar_init(&freed[i], 1); }
         mbar_init(&drained, 1);
         ctl[0] = 0;
-        ctl[1] = kWaitLimitDefault;
+        ctl[1] = p.test_stall ? kWaitLimitStall : kWaitLimitDefault;
         fence_mbar_init();
     }
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
@@ -615,7 +616,7 @@ adapter_down_many_kernel(const DownParams p)
         auto room = [&](int i) {                     // the stage's place is free again, and its weights are on their way
             const int at = i % STAGES;
             if (i >= STAGES && !(ok = mbar_wait_warp(&freed[at], (uint32_t)(i / STAGES & 1) ^ 1, ctl))) return false;
-            if (threadIdx.x == 0) {
+            if (threadIdx.x == 0 && !p.test_stall) {
                 const uint32_t bytes = (uint32_t)(chunks_of(i) * groups * 1024);
                 mbar_arrive_expect_tx(&w_full[at], bytes);
                 bulk_g2s(smem + at * stage_bytes + L::kX, weights + (size_t)i * p.splits * 2 * groups * 1024, bytes, &w_full[at]);
@@ -783,6 +784,7 @@ struct UpParams {
     int tile_rows;           // rows of a block of threads: at most UP_ROWS
     const uint8_t* B;
     size_t b_slot;
+    int test_stall;          // test hook (tcgen05): the weights are never copied, so the waits must give up
 };
 
 template <typename T> constexpr int kTerms = sizeof(T) == 2 ? 2 : 3;
@@ -1149,7 +1151,7 @@ adapter_many_kernel(const UpParams p)
         for (int i = 0; i < MANY_B; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_done[i], 1); }
         mbar_init(&drained, 1);
         ctl[0] = 0;
-        ctl[1] = kWaitLimitDefault;
+        ctl[1] = p.test_stall ? kWaitLimitStall : kWaitLimitDefault;
         fence_mbar_init();
     }
     // Tensor memory before the kernel after this one may start (see PdlLaunch).
@@ -1201,7 +1203,7 @@ adapter_many_kernel(const UpParams p)
     // ---- weights of the next 64 channels: one thread ----
     int wb = b0;
     auto ask = [&]() {
-        if (wb < b1) {
+        if (wb < b1 && !p.test_stall) {
             const int buf = (wb - b0) % MANY_B;
             mbar_arrive_expect_tx(&b_full[buf], (uint32_t)groups * 2048);
             bulk_g2s(smem + lay.z_bytes() + buf * lay.b_bytes(), p.B + (size_t)tile.slot * p.b_slot + (size_t)wb * groups * 2048, (uint32_t)groups * 2048, &b_full[buf]);
@@ -2031,11 +2033,19 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
                                                const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
                                                const int* slots, const int* q_start, int n_seq, int n_rows, void* stream)
 {
+    return tsvd_adapters_forward_ex(h, x, ldx, x_scale, dtype, base, ldb, out, ldo, out_dtype, slots, q_start, n_seq, n_rows, 0, stream);
+}
+
+extern "C" tsvd_status_t tsvd_adapters_forward_ex(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
+                                                  const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
+                                                  const int* slots, const int* q_start, int n_seq, int n_rows, unsigned flags, void* stream)
+{
     if (!h) return TSVD_E_NULL;
     if (n_rows < 0 || n_seq < 1 || (!q_start && n_rows != n_seq) || ldx < h->N || (base && ldb < h->M) || ldo < h->M) return TSVD_E_SHAPE;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16 && dtype != TSVD_I8) return TSVD_E_DTYPE;
     if (out_dtype != TSVD_F32 && out_dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (x_scale && dtype != TSVD_I8) return TSVD_E_DTYPE;
+    if (flags & ~TSVD_FLAG_TEST_STALL) return TSVD_E_DTYPE;
     if (n_rows == 0) return TSVD_OK;
     if (!x || !out || !slots) return TSVD_E_NULL;
     const size_t size = dtype == TSVD_F32 ? 4 : dtype == TSVD_BF16 ? 2 : 1, out_size = out_dtype == TSVD_F32 ? 4 : 2;
@@ -2045,7 +2055,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     const Rows rows{slots, q_start, n_seq, n_rows, h->n_slots, h->ranks, h->dev_status};
     const size_t step = dtype == TSVD_I8 ? 8 : 16;
     DownParams d{rows, x, ldx, !off(x, step) && (n_rows == 1 || ldx * (long long)size % (long long)step == 0), h->N, h->chunks, 0, h->groups,
-                 h->A, h->a_slot, nullptr};
+                 h->A, h->a_slot, nullptr, (flags & TSVD_FLAG_TEST_STALL) != 0};
     auto even = [&](const void* p, long long ld) { return !p || (!off(p, 16) && (n_rows == 1 || ld * (long long)out_size % 16 == 0)); };
     UpParams u{};
     u.rows = rows;
@@ -2062,6 +2072,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x,
     u.blocks = h->blocks;
     u.B = h->B;
     u.b_slot = h->b_slot;
+    u.test_stall = d.test_stall;
     if (const Few how = few_of(h, n_rows); how.cluster && !prefers_many(h, how, n_rows, n_seq)) {
         const FewParams f{d, u, how.cluster, how.rows};
         const unsigned tiles = (unsigned)((n_rows + how.rows - 1) / how.rows);

@@ -267,7 +267,7 @@ class LowRankAdapters:
     def reserve(self, rows_max: int) -> None:
         binding.tsvd_adapters_reserve(self.handle, rows_max)
 
-    def forward(self, x, base, slots, q_start=None, x_scale=None, out=None):
+    def forward(self, x, base, slots, q_start=None, x_scale=None, out=None, flags: int = 0):
         """base + scale * B (A x) for every row: x [rows, N] float32, bfloat16, or int8 with x_scale float32 [rows] (None: ones),
         base [rows, M] float32 or bfloat16 (None: zeros, float32 unless x is bfloat16), slots int32 [n_seq] (-1: no adapter),
         q_start int32 [n_seq + 1] (None: one row per sequence); all CUDA tensors, rows with any stride.  out may be base.
@@ -304,9 +304,9 @@ class LowRankAdapters:
             raise TSVDError(binding.TSVD_E_DTYPE if out.dtype != dtype else binding.TSVD_E_SHAPE, what)
         else:
             ldo = _rows(out, what)[2]
-        err = binding.lib().tsvd_adapters_forward(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else None, code,
-                                                  base.data_ptr() if base is not None else None, ldb, out.data_ptr(), ldo,
-                                                  _code(dtype, what), slots.data_ptr(), start, n_seq, rows, stream)
+        err = binding.lib().tsvd_adapters_forward_ex(self.handle, x.data_ptr(), ldx, x_scale.data_ptr() if x_scale is not None else None, code,
+                                                     base.data_ptr() if base is not None else None, ldb, out.data_ptr(), ldo,
+                                                     _code(dtype, what), slots.data_ptr(), start, n_seq, rows, flags, stream)
         if err:
             raise TSVDError(err, "tsvd_adapters_forward")
         return out
