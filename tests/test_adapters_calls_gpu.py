@@ -1,4 +1,6 @@
-"""The adapters where a call meets its surroundings: waits that give up, results that are exact.  (Tolerances: test_norm_adapters_gpu.)"""
+"""The adapters where a call meets its surroundings: waits that give up, results that are exact, whole sequences and mixed
+batches, slots far larger than their adapters, a ternary projection beside them, the one-to-one functions of `binding`.
+(Tolerances: test_norm_adapters_gpu.)"""
 import numpy as np
 import pytest
 
@@ -96,3 +98,141 @@ def test_selected_numbers_come_through_exactly(N, M, rank, new, aligned, kind, o
         assert torch.equal(h(x, base, slots, start, x_scale=x_scale), base + want)
     torch.cuda.synchronize()
     assert h.status() == 0
+
+
+# ---- batches of every kind ----------------------------------------------------------------------------------------------
+
+# More rows than the one-launch form takes at these sizes, and sequences long enough for tiles of their own (64 rows a sequence, 32 with ranks above
+# 48): both products on tcgen05 (fp32 x of one group of ranks: the first one from 4096 rows on), with one to eight groups of 16 ranks
+WHOLE = [(32, 64, [16], [0], [1300]), (1001, 770, [9, 16, 3], [2, 0, -1, 1, 0], [349, 700, 100, 1, 255]), (520, 328, [32, 17], [0, 1, 0], [640, 127, 700]),
+         (256, 2100, [48, 20], [1, 0, -1, 0], [66, 1100, 100, 51]), (640, 640, [64, 0, 50, 5], [0, 1, 2, 3], [400, 200, 129, 700]),
+         (96, 130, [80, 3], [0, 1, 0], [129, 255, 128]), (264, 200, [96], [0, 0, -1], [100, 31, 129]), (72, 72, [112], [0, 0], [256, 1]),
+         (328, 129, [128], [0], [193]), (72, 70, [16, 2], [0, 1], [4000, 200])]
+
+
+@pytest.mark.parametrize("N,M,ranks,slots,new", WHOLE)
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f32", "f32"), ("i8", "f32"), ("i8", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+def test_whole_sequences(N, M, ranks, slots, new, kind, out):
+    """As wide as the ranks need; that the kernels on tcgen05 take the call is seen by their waits, which give up on request."""
+    import torch
+    from paper_2308_07641_b200 import binding
+    g = _gen(N + M)
+    a = Adapters(N, M, ranks, dtype="f32" if kind == "f32" else "bf16")
+    x, x_scale = _rows(kind, sum(new), N, g, -N % 16)
+    base = torch.randn(sum(new), M + -M % 8, generator=g, device="cuda").to(_dtype(out))[:, :M]
+    want = a.check(x, base, slots, new, x_scale)
+    over, ids = base.clone(), torch.tensor(slots, dtype=torch.int32, device="cuda")
+    a.h(x, over, ids, _start(new), x_scale=x_scale, out=over)
+    assert torch.equal(over, want)
+    assert a.h.status() == 0
+    a.h(x, base, ids, _start(new), x_scale=x_scale, flags=binding.TSVD_FLAG_TEST_STALL)
+    torch.cuda.synchronize()
+    assert a.h.status() == binding.TSVD_E_TIMEOUT
+    assert torch.equal(a.check(x, base, slots, new, x_scale), want) and a.h.status() == 0
+
+
+@pytest.mark.parametrize("tokens,prompts", [(63, [1024]), (15, [1024]), (31, [700, 1, 300]), (200, [64]), (7, [130])])
+@pytest.mark.parametrize("N,M,ranks", [(1024, 1536, [16, 8, 64, 3]), (512, 700, [128, 5])])
+def test_prompts_among_single_tokens(N, M, ranks, tokens, prompts):
+    """What a serving loop submits; the form is chosen for the whole call."""
+    import torch
+    g = _gen(tokens)
+    a = Adapters(N, M, ranks)
+    new = [1] * (tokens // 2) + prompts + [1] * (tokens - tokens // 2)
+    x, base = torch.randn(sum(new), N, generator=g, device="cuda").bfloat16(), torch.randn(sum(new), M, generator=g, device="cuda").bfloat16()
+    a.check(x, base, [i % (len(ranks) + 1) - 1 for i in range(len(new))], new)
+    assert a.h.status() == 0
+
+
+@pytest.mark.parametrize("max_rank", [17, 64, 65, 128])
+@pytest.mark.parametrize("new", [[1], [1] * 9, [5, 1, 17], [40] * 20, [300, 1000], [900, 1, 500]])
+def test_slots_larger_than_their_adapters(max_rank, new):
+    """The handle's largest rank chooses the form; the adapters in it are small, of unlike ranks, or not there."""
+    import torch
+    g = _gen(max_rank)
+    a = Adapters(328, 200, [16, 1, 0, 9], max_rank=max_rank)
+    for kind in ("bf16", "f32"):
+        x, _ = _rows(kind, sum(new), 328, g)
+        base = torch.randn(sum(new), 200, generator=g, device="cuda").to(_dtype(kind))
+        a.check(x, base, [i % 5 - 1 for i in range(len(new))], new)
+        a.check(x, base, [(i + 1) % 4 for i in range(len(new))], new)
+    assert a.h.status() == 0
+
+
+@pytest.mark.parametrize("new", [[1], [1] * 16, [3, 1, 28], [130, 70], [1500, 100]])
+@pytest.mark.parametrize("rank", [8, 100])
+def test_beside_a_ternary_layer(new, rank):
+    """The ternary product's result is the base, in place, each call a programmatic dependent of the one ahead, on a side stream."""
+    import torch
+    from paper_2308_07641_b200 import TSVDLinear
+    N, M, K = 512, 384, 256
+    rng = np.random.default_rng(rank)
+    layer = TSVDLinear(rng.integers(-1, 2, (M, K), dtype=np.int8), rng.random(K, dtype=np.float32) / 64, rng.integers(-1, 2, (K, N), dtype=np.int8))
+    n, g = sum(new), _gen(rank)
+    a = Adapters(N, M, [rank, 4])
+    layer.reserve(n, "bf16")
+    a.h.reserve(n)
+    xs = [torch.randn(n, N, generator=g, device="cuda").bfloat16() for _ in range(6)]
+    slots = [i % 3 - 1 for i in range(len(new))]
+    ids, start = torch.tensor(slots, dtype=torch.int32, device="cuda"), _start(new)
+    wants = []
+    for x in xs:
+        base = layer(x)
+        torch.cuda.synchronize()
+        wants.append(a.check(x, base, slots, new))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            outs = []
+            for x in xs:
+                y = layer(x)
+                outs.append(a.h(x, y, ids, start, out=y))
+            side.synchronize()
+            assert all(torch.equal(y, want) for y, want in zip(outs, wants))
+    assert a.h.status() == 0
+
+
+def test_binding_entry_points():
+    """The one-to-one functions of `binding`, with raw pointers on the current stream, against the torch front."""
+    import torch
+    from paper_2308_07641_b200 import KV4Cache, binding, rotary_table
+    g = _gen(5)
+    F32, BF16, stream = binding.TSVD_F32, binding.TSVD_BF16, torch.cuda.current_stream().cuda_stream
+    # adapters
+    a = Adapters(200, 130, [16, 5])
+    x, base = torch.randn(9, 200, generator=g, device="cuda"), torch.randn(9, 130, generator=g, device="cuda")
+    slots, start = torch.tensor([1, 0], dtype=torch.int32, device="cuda"), torch.tensor([0, 4, 9], dtype=torch.int32, device="cuda")
+    want = a.h(x, base, slots, start)
+    h = binding.tsvd_adapters_create(200, 130, 16, 2)
+    try:
+        for s in range(2):
+            A, B = a.A[s].float().contiguous(), a.B[s].float().contiguous()
+            binding.tsvd_adapters_set(h, s, A.data_ptr(), 200, B.data_ptr(), A.shape[0], F32, A.shape[0], a.c[s], stream)
+        for call in (binding.tsvd_adapters_forward, lambda *p: binding.tsvd_adapters_forward_ex(*p[:-1], 0, p[-1])):
+            out = torch.zeros_like(want)
+            call(h, x.data_ptr(), 200, 0, F32, base.data_ptr(), 130, out.data_ptr(), 130, F32, slots.data_ptr(), start.data_ptr(), 2, 9, stream)
+            assert torch.equal(out, want)
+        assert binding.tsvd_adapters_info(h)["max_rank"] == 16 and binding.tsvd_adapters_last_status(h) == 0
+    finally:
+        binding.tsvd_adapters_destroy(h)
+    # rotation and the window with first positions
+    rates = 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64, device="cuda") / 64)
+    table = torch.zeros(300, 64, device="cuda")
+    binding.tsvd_rotary_table(table.data_ptr(), 300, 64, rates.data_ptr(), 1.0, stream)
+    assert torch.equal(table, rotary_table(300, 64, rates=rates))
+    caches = [KV4Cache(2, 64, 20, 16) for _ in range(2)]
+    q, k, v = (torch.randn(300, heads, 64, generator=g, device="cuda").bfloat16() for heads in (4, 2, 2))
+    pages, n = torch.arange(20, dtype=torch.int32, device="cuda").view(1, 20), torch.tensor([300], dtype=torch.int32, device="cuda")
+    first = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    turned = caches[0].append_rotated(q, k, v, table, pages, n, first)
+    want = caches[0].attend(turned, pages, n, first, max_q=300, window=70, sinks=5)
+    turned2, out = torch.zeros_like(turned), torch.zeros_like(want)
+    batch = (pages.data_ptr(), 20, n.data_ptr(), first.data_ptr(), 1, 300)
+    binding.tsvd_kv4_append_rotated(caches[1].handle, q.data_ptr(), 256, turned2.data_ptr(), 256, 4, k.data_ptr(), 128, v.data_ptr(), 128, BF16,
+                                    table.data_ptr(), 300, 64, 0, *batch, stream)
+    binding.tsvd_kv4_attend_sinks(caches[1].handle, turned2.data_ptr(), 256, out.data_ptr(), 256, 4, BF16, *batch, 300, 0, 0.125, 70, 5,
+                                  binding.TSVD_FLAG_CAUSAL, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(turned2, turned) and torch.equal(out, want)
+    assert all(c.status() == 0 for c in caches)
