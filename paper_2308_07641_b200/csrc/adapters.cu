@@ -22,6 +22,7 @@
 // exactly.  z stays fp32 between the kernels, and enters the second product as two bf16 terms (2^-17 of it is lost, the result's
 // own rounding being 2^-9) for bf16 results, as three (exactly) for fp32.  The parts of a contraction that blocks share are
 // added in their order.
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -1814,26 +1815,30 @@ cudaError_t prepare()
     return e;
 }
 
+constexpr int kUpStatic = 2560;      // shared memory that the second kernel declares, and what the system keeps of a block's
 template <typename T, int G>
-cudaError_t up(const UpParams& p, unsigned tiles, unsigned columns, cudaStream_t st)
+cudaError_t up(UpParams& p, int sms, cudaStream_t st)
 {
+    // Channel blocks a warp: so many that the blocks run in one round (they read z again each), as many an SM as registers and shared memory
+    // leave, and four or three where those leave more.  With four or three whatever they leave, fp32 results and ranks above 64 took rounds
+    // more: 4096 to 4096, 4000 rows by 20, ranks of 128, 262 us in place of 224 (fp32 383 and 344); 700 single rows of rank 64 in fp32 280 and
+    // 239; 300 by 10, ranks of 128, whose second round was eight blocks, 50.4 in place of 53.3.
     const size_t smem = (size_t)(p.tile_rows + 15) / 16 * 2 * p.groups * 256 * kTerms<T> + (size_t)UP_WARPS * (p.groups * 2048 + 2 * UP_STAGES * kBaseBytes<T>);
-    PdlLaunch l(tiles, UP_WARPS * 32, smem, st);
-    l.cfg.gridDim.y = columns;
+    const int fit = (int)(TSVD_SM_SMEM / (smem + kUpStatic)), most = p.groups <= 2 ? 4 : 3;
+    const int at_once = sms * std::max(1, std::min({fit, kUpBlocks<T, G>, most}));
+    const int tiles = (p.rows.n_rows + p.tile_rows - 1) / p.tile_rows;
+    auto columns = [&] { return (p.blocks + UP_WARPS * p.per_warp - 1) / (UP_WARPS * p.per_warp); };
+    p.per_warp = 1;
+    while ((long long)tiles * columns() > at_once && p.per_warp < p.blocks) ++p.per_warp;
+    PdlLaunch l((unsigned)tiles, UP_WARPS * 32, smem, st);
+    l.cfg.gridDim.y = (unsigned)columns();
     return cudaLaunchKernelEx(&l.cfg, adapter_up_kernel<T, G>, p);
 }
 
 template <typename T>
 cudaError_t up_type(UpParams& p, int sms, cudaStream_t st)
 {
-    // Channel blocks a warp: so many that the blocks run in one round, three or four an SM (they read z again each).
-    const int at_once = (p.groups <= 2 ? 4 : 3) * sms;
-    const int tiles = (p.rows.n_rows + p.tile_rows - 1) / p.tile_rows;
-    auto columns = [&] { return (p.blocks + UP_WARPS * p.per_warp - 1) / (UP_WARPS * p.per_warp); };
-    p.per_warp = 1;
-    while ((long long)tiles * columns() > at_once && p.per_warp < p.blocks) ++p.per_warp;
-    const unsigned x = (unsigned)tiles, y = (unsigned)columns();
-    return p.groups == 1 ? up<T, 1>(p, x, y, st) : p.groups == 2 ? up<T, 2>(p, x, y, st) : p.groups <= 4 ? up<T, 4>(p, x, y, st) : up<T, 8>(p, x, y, st);
+    return p.groups == 1 ? up<T, 1>(p, sms, st) : p.groups == 2 ? up<T, 2>(p, sms, st) : p.groups <= 4 ? up<T, 4>(p, sms, st) : up<T, 8>(p, sms, st);
 }
 
 template <typename T>
