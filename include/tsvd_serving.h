@@ -31,7 +31,7 @@ extern "C" {
  * A row that holds a NaN or an infinity gets a scale that is not finite (and unspecified q), so that what is
  * computed from it is not finite either.  rows = 0 does nothing (and looks at no pointer).  Any alignment that the types allow; 16-byte
  * aligned rows are read 16 bytes at a time.
- * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN (a pointer is not a multiple of its type's size), E_CUDA.
+ * Errors: E_NULL, E_SHAPE, E_TOOBIG (cols above 2^31 - 2^16), E_DTYPE, E_ALIGN (a pointer is not a multiple of its type's size), E_CUDA.
  */
 tsvd_status_t tsvd_quantize(const void* x, tsvd_dtype_t dtype, long long rows, int cols, long long ldx, int8_t* q,
                             long long ldq, float* scale, void* stream);
@@ -60,7 +60,7 @@ tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const float* scale
  *   q, scale  device, row b at q + b*ldq (ldq >= cols), scale float [rows]; NULL where y is given.  One of the two results.
  * A row with a NaN or an infinity gets results that are not all finite (in 8 bits a scale that is not finite); no other row does.
  * A row whose a_b is below 2^-100 becomes q = 0.  rows = 0 does nothing.
- * Errors: E_NULL (also both results, or none), E_SHAPE, E_DTYPE, E_VALUE (eps), E_ALIGN, E_CUDA.
+ * Errors: E_NULL (also both results, or none), E_SHAPE, E_TOOBIG (cols above 2^31 - 2^16), E_DTYPE, E_VALUE (eps), E_ALIGN, E_CUDA.
  */
 tsvd_status_t tsvd_rms_norm(const void* x, tsvd_dtype_t dtype, long long rows, int cols, long long ldx, const void* residual,
                             long long ldr, void* h, long long ldh, const void* weight, tsvd_dtype_t weight_dtype, float eps,
@@ -142,7 +142,7 @@ tsvd_status_t tsvd_adapters_set(tsvd_adapters_t h, int slot, const void* A, long
  * adapters do not disturb each other: what is not finite in one stays there.
  * Calls on one handle share its scratch and must be ordered; it grows on the first call with more rows unless
  * tsvd_adapters_reserve has sized it (outgrown scratch lives as long as the handle: captured graphs stay valid).
- * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_NOMEM, E_CUDA.
+ * Errors: E_NULL, E_SHAPE, E_TOOBIG (n_rows or n_seq above 2^30), E_DTYPE, E_ALIGN, E_NOMEM, E_CUDA.
  */
 tsvd_status_t tsvd_adapters_forward(tsvd_adapters_t h, const void* x, long long ldx, const float* x_scale, tsvd_dtype_t dtype,
                                     const void* base, long long ldb, void* out, long long ldo, tsvd_dtype_t out_dtype,
@@ -187,7 +187,7 @@ typedef struct tsvd_kv4_s* tsvd_kv4_t; /* opaque; owns device memory on one GPU 
  * sequence longer than its pages makes tsvd_kv4_last_status report TSVD_E_INDEX, and so does a row before position 0 in
  * append and read; such a position is not written (append), reads as zeros (read) and is not seen (attend).  An unused
  * slot of a batch (seq_len 0 with a row) is therefore fine in attend, which gives it zeros.
- * Calls on one handle must be ordered on one stream (or otherwise serialised).
+ * Calls on one handle must be ordered on one stream (or otherwise serialised).  More than 2^31 - 2^16 sequences or rows: E_TOOBIG.
  * Synchronous.  Errors: E_NULL, E_SHAPE, E_TOOBIG (n_pages * page_tokens above 2^31 - 1, page_tokens above 2^24), E_NOMEM, E_CUDA.
  */
 tsvd_status_t tsvd_kv4_create(int n_kv_heads, int head_dim, int page_tokens, long long n_pages, tsvd_kv4_t* out);

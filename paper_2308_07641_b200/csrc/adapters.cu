@@ -56,6 +56,7 @@ constexpr int MAX_RANK = 128;
 constexpr int DOWN_WARPS = 8, UP_WARPS = 4;
 constexpr int UP_ROWS = 64;      // rows of a tile of the second kernel at most
 constexpr int MAX_SPLITS = 8;      // a cluster
+constexpr int MOST_ROWS = 1 << 30; // and sequences: their numbers are added in 32 bits
 
 struct Rows {                    // which adapter a row has
     const int* slots;            // [n_seq]
@@ -2029,6 +2030,7 @@ extern "C" tsvd_status_t tsvd_adapters_reserve(tsvd_adapters_t h, int rows_max)
 {
     if (!h) return TSVD_E_NULL;
     if (rows_max < 1) return TSVD_E_SHAPE;
+    if (rows_max > MOST_ROWS) return TSVD_E_TOOBIG;
     if (const tsvd_status_t on = on_current_device(h->device); on != TSVD_OK) return on;
     const bool none = few_of(h, rows_max).cluster && (!large(h) || rows_max < MANY_FROM);          // no call of so many rows or fewer needs it
     return none ? TSVD_OK : grow(h, z_bytes(h, rows_max));
@@ -2047,6 +2049,7 @@ extern "C" tsvd_status_t tsvd_adapters_forward_ex(tsvd_adapters_t h, const void*
 {
     if (!h) return TSVD_E_NULL;
     if (n_rows < 0 || n_seq < 1 || (!q_start && n_rows != n_seq) || ldx < h->N || (base && ldb < h->M) || ldo < h->M) return TSVD_E_SHAPE;
+    if (n_rows > MOST_ROWS || n_seq > MOST_ROWS) return TSVD_E_TOOBIG;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16 && dtype != TSVD_I8) return TSVD_E_DTYPE;
     if (out_dtype != TSVD_F32 && out_dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (x_scale && dtype != TSVD_I8) return TSVD_E_DTYPE;

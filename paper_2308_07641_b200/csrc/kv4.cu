@@ -398,6 +398,7 @@ tsvd_status_t check_batch(const tsvd_kv4_s* h, const int* page_table, int max_pa
 {
     if (!h || !page_table || !seq_len) return TSVD_E_NULL;
     if (max_pages < 1 || n_seq < 1 || n_rows < 0 || (!q_start && n_rows != n_seq)) return TSVD_E_SHAPE;
+    if (n_seq > TSVD_COUNT_MOST || n_rows > TSVD_COUNT_MOST) return TSVD_E_TOOBIG;
     if (((uintptr_t)page_table | (uintptr_t)seq_len | (uintptr_t)q_start) & 3) return TSVD_E_ALIGN;
     return TSVD_OK;
 }

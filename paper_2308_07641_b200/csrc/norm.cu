@@ -342,6 +342,7 @@ extern "C" tsvd_status_t tsvd_rms_norm(const void* x, tsvd_dtype_t dtype, long l
 {
     if (rows < 0 || rows > 0x7fffffffLL || cols < 1 || ldx < cols || (residual && (ldr < cols || ldh < cols)) || (y && ldy < cols) || (q && ldq < cols))
         return TSVD_E_SHAPE;
+    if (cols > TSVD_COUNT_MOST) return TSVD_E_TOOBIG;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (weight_dtype != TSVD_F32 && weight_dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (!(eps >= 1e-12f && eps <= FLT_MAX)) return TSVD_E_VALUE;

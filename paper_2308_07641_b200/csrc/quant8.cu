@@ -58,6 +58,7 @@ extern "C" tsvd_status_t tsvd_quantize(const void* x, tsvd_dtype_t dtype, long l
                                        long long ldq, float* scale, void* stream)
 {
     if (rows < 0 || rows > TSVD_ROWS_MOST || cols < 1 || ldx < cols || ldq < cols) return TSVD_E_SHAPE;
+    if (cols > TSVD_COUNT_MOST) return TSVD_E_TOOBIG;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (rows == 0) return TSVD_OK;
     if (!x || !q || !scale) return TSVD_E_NULL;
@@ -72,6 +73,7 @@ extern "C" tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const f
                                          tsvd_dtype_t dtype, long long ldy, void* stream)
 {
     if (rows < 0 || rows > TSVD_ROWS_MOST || cols < 1 || ldy < cols || ldq < cols) return TSVD_E_SHAPE;
+    if (cols > TSVD_COUNT_MOST) return TSVD_E_TOOBIG;
     if (dtype != TSVD_F32 && dtype != TSVD_BF16) return TSVD_E_DTYPE;
     if (rows == 0) return TSVD_OK;
     if (!q || !scale || !y) return TSVD_E_NULL;

@@ -110,6 +110,10 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 #endif
 
+// Columns, rows and sequences are counted in 32 bits, some beyond the last one (up to a block's share of them); calls whose counts
+// would not fit are refused.
+constexpr int TSVD_COUNT_MOST = 0x7fffffff - 0xffff;
+
 // A handle's memory lies on one device; its calls launch on the current one.
 inline tsvd_status_t on_current_device(int device)
 {
