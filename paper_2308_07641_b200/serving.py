@@ -54,6 +54,12 @@ def _stream(what: str, x, *others) -> int:
     return _raw_stream(index)
 
 
+def _count(n, what: str) -> None:
+    """A number of the caller's that the library takes in 32 bits: ctypes would cut a larger one without a word."""
+    if not -0x80000000 <= n <= 0x7fffffff:
+        raise TSVDError(binding.TSVD_E_SHAPE, what)
+
+
 def _rows(x, what: str):
     """A CUDA tensor [rows, cols] with contiguous rows; returns (rows, cols, row stride).  The stride of a single row says
     nothing and is taken as cols; any other is handed on as it is, and the library refuses one below cols (rows that overlap,
@@ -151,6 +157,7 @@ def rotary_table(positions: int, turned: int, base: float = 10000.0, rates=None,
     import torch
     if not _CODES:
         _load()
+    _count(positions, "rotary_table")
     if positions < 1 or turned < 2 or turned % 2:
         raise TSVDError(binding.TSVD_E_SHAPE, "rotary_table")
     device = torch.device(device if device is not None else "cuda")
@@ -251,13 +258,19 @@ class LowRankAdapters:
         (rank, N, lda), (M, rank_b, ldb) = _rows(A, what), _rows(B, what)
         if N != self.N or M != self.M or rank != rank_b or not 0 < rank <= self.max_rank:
             raise TSVDError(binding.TSVD_E_SHAPE, what)
+        self._slot(slot, what)
         stream = _stream(what, A, B)
         err = binding.lib().tsvd_adapters_set(self.handle, slot, A.data_ptr(), lda, B.data_ptr(), ldb, _code(A.dtype, what), rank, scale, stream)
         if err:
             raise TSVDError(err, "tsvd_adapters_set")
 
+    def _slot(self, slot: int, what: str) -> None:
+        if not 0 <= slot < self.n_slots:
+            raise TSVDError(binding.TSVD_E_INDEX, what)
+
     def clear(self, slot: int) -> None:
         """Empty a slot, on torch's current stream."""
+        self._slot(slot, "LowRankAdapters.clear")
         if not _CODES:
             _load()
         err = binding.lib().tsvd_adapters_set(self.handle, slot, None, 0, None, 0, TSVD_BF16, 0, 0.0, _raw_stream(_device()))
@@ -265,6 +278,7 @@ class LowRankAdapters:
             raise TSVDError(err, "tsvd_adapters_set")
 
     def reserve(self, rows_max: int) -> None:
+        _count(rows_max, "LowRankAdapters.reserve")
         binding.tsvd_adapters_reserve(self.handle, rows_max)
 
     def forward(self, x, base, slots, q_start=None, x_scale=None, out=None, flags: int = 0):
@@ -438,6 +452,8 @@ class KV4Cache:
         stream = _stream("KV4Cache.attend", q, out, page_table, seq_len, q_start)
         if max_q is None:
             max_q = 1 if q_start is None else max(1, rows)
+        if (max_q | (max_kv or 0) | window | sinks) >> 31 not in (0, -1):    # (_count of all four; the library refuses those below 0)
+            raise TSVDError(binding.TSVD_E_SHAPE, "KV4Cache.attend")
         if out is None:
             ldo = n_heads * self.head_dim
             out = _empty((rows, n_heads, self.head_dim), (ldo, self.head_dim, 1), dtype=q.dtype, device=q.device)
