@@ -58,7 +58,8 @@ tsvd_status_t tsvd_dequantize(const int8_t* q, long long ldq, const float* scale
  *   eps       1e-12 or more
  *   y         device, like x, or NULL; may be x itself, where there is no residual
  *   q, scale  device, row b at q + b*ldq (ldq >= cols), scale float [rows]; NULL where y is given.  One of the two results.
- * A row with a NaN or an infinity gets results that are not all finite (in 8 bits a scale that is not finite); no other row does.
+ * A row with a NaN or an infinity gets results that are not all finite (in 8 bits a scale that is not finite); with finite weights
+ * no other row does, but for 8-bit rows one of whose products t leaves fp32's range: a_b, and with it scale_b, is then infinite.
  * A row whose a_b is below 2^-100 becomes q = 0.  rows = 0 does nothing.
  * Errors: E_NULL (also both results, or none), E_SHAPE, E_TOOBIG (cols above 2^31 - 2^16), E_DTYPE, E_VALUE (eps), E_ALIGN, E_CUDA.
  */
