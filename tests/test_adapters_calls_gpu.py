@@ -236,3 +236,36 @@ def test_binding_entry_points():
     torch.cuda.synchronize()
     assert torch.equal(turned2, turned) and torch.equal(out, want)
     assert all(c.status() == 0 for c in caches)
+
+
+def test_beside_other_cluster_kernels_on_two_streams():
+    """The first product of whole sequences, whose blocks share SMs, on one stream; on the other the ternary kernel for 5 to 32 tokens and
+    the 8-bit product of few tokens, whose clusters hold tensor memory while they wait for one another.  Same bits as one by one."""
+    import torch
+    from paper_2308_07641_b200 import Int8Linear, TSVDLinear, quantize
+    g, rng = _gen(31), np.random.default_rng(31)
+    N = 2048
+    ternary = TSVDLinear(rng.integers(-1, 2, (4096, 1024), dtype=np.int8), rng.random(1024, dtype=np.float32) / 64, rng.integers(-1, 2, (1024, N), dtype=np.int8))
+    dense = Int8Linear(*quantize(torch.randn(2304, N, generator=g, device="cuda")))
+    a = Adapters(N, 640, [128, 20, 64])
+    new, slots = [130, 300, 70, 200], [0, 1, -1, 2]
+    x = torch.randn(sum(new), N, generator=g, device="cuda").bfloat16()
+    base = torch.randn(sum(new), 640, generator=g, device="cuda").bfloat16()
+    ids, start, few = torch.tensor(slots, dtype=torch.int32, device="cuda"), _start(new), x[:16].clone()
+    ternary.reserve(16, "bf16")
+    dense.reserve(16, "bf16")
+    want_a = a.check(x, base, slots, new)
+    want_t, want_d = ternary(few), dense(few)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = [[], []]
+        for _ in range(10):
+            with torch.cuda.stream(streams[0]):
+                got[0].append(a.h(x, base, ids, start))
+            with torch.cuda.stream(streams[1]):
+                got[1] += [(ternary(few), dense(few))]
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want_a) for y in got[0])
+        assert all(torch.equal(t, want_t) and torch.equal(d, want_d) for t, d in got[1])
+    assert a.h.status() == 0 and dense.status() == 0
