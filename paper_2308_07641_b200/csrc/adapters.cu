@@ -8,19 +8,21 @@
 //                 adapter_up_kernel).  What the products of an adapter give for rows of another one is dropped, never added
 //   many rows of  two launches on tcgen05: tiles of up to 128 rows of one sequence, so of one adapter (adapter_down_many_kernel,
 //   a sequence    adapter_many_kernel)
-// In all of them a row's result depends on its own numbers and adapter only.
+// In all of them a row's result is made of its own numbers and adapter only.  How its sums are cut, and with that their last bits, goes
+// by the call: its rows and sequences choose the form, and a cluster of the first form shares its work out by the adapters of all its rows.
+// The same call gives the same bits.
 //
 // The weights lie as tcgen05 takes them: eight rows of 16 bytes one after another, and are brought by bulk copies for it; the lanes
 // of a warp that uses mma.sync copy the 16 bytes that they will read (cp.async, some stages ahead), and nothing is exchanged.
 //
 // What bounds them, in time of the device alone (the bytes' at 6.55 TB/s in brackets): 64 tokens with 48 adapters of rank 16, 4096 to
 // 12288, 13.9 us (4.4; one token 5.9 us, so launch, two chains of loads and a cluster's exchange are most of it; of rank 64 26.2 (15.9): bytes);
-// 2046 rows of five sequences, rank 64, 38.7 us (19.5): the second product 26, base and out being 15 of the bytes' 19.5, the first
-// one 13, with 64 KB of x on their way to an SM.
+// 2046 rows of five sequences, all of rank 64, 38.5 us (19.5), base and out being 15 of the bytes' 19.5; of unlike ranks, 64 and below, 36 to
+// 38.  Under ncu, each alone, the second product takes 30 and the first one 16, with 64 KB of x on their way to an SM.
 //
 // Arithmetic: bf16 operands, fp32 sums.  8-bit x is exact in bf16.  fp32 x is cut into three bf16 terms that add up to it
-// exactly.  z stays fp32 between the kernels, and enters the second product as two bf16 terms (2^-17 of it is lost, the result's
-// own rounding being 2^-9) for bf16 results, as three (exactly) for fp32.  The parts of a contraction that blocks share are
+// exactly.  z stays fp32 between the kernels, and enters the second product as two bf16 terms (off by 2^-16 of it at most, the
+// result's own rounding by 2^-8) for bf16 results, as three (exactly) for fp32.  The parts of a contraction that blocks share are
 // added in their order.
 #include <algorithm>
 #include <new>
@@ -1862,8 +1864,8 @@ struct Shape {
 };
 // Tiles of 32 rows where sequences fill them, or where there are many: a tile goes over the columns once for each of its adapters, and with
 // tiles of 8 the weights are read four times as often.  Both products, 4096 to 4096, tiles of 8 and of 32: 900 rows by 20 for each sequence,
-// ranks of 32, 32.7 and 41.3 us; 300 by 10, ranks of 128, 49.2 and 58.6; 200 by 50, ranks of 128, 33.1 and 31.4; 4000 by 30, ranks of 16, 52.6
-// and 50.5.
+// ranks of 32, 32.9 and 41.5 us; 300 by 10, ranks of 128, 53.3 and 62.4; 200 by 50, ranks of 128, 28.5 and 26.5; 4000 by 30, ranks of 16, 53.2
+// and 50.6.
 Shape shape_of(const tsvd_adapters_s* h, int rows, int n_seq)
 {
     Shape s;
@@ -1898,8 +1900,8 @@ Few few_of(const tsvd_adapters_s* h, int rows)
 }
 // The kernels on tcgen05 where sequences have rows for a tile of 128, as far as their number tells: half of one, a quarter where ranks above
 // 48 make the warps' products long.  2048 rows by 64 and 32 for each sequence, 2048 to 8192, ranks of 16: 30 and 48 us against 32 and 34; 4096 to
-// 4096, ranks of 32, 1024 rows by 32 25.6 against 26.7; ranks of 64, 4000 rows by 50 and 20 63 and 134 against 95 and 116; of 128, 300 rows by 40 22
-// against 41.
+// 4096, ranks of 32, 1024 rows by 32 26.0 against 26.7; ranks of 64, 4000 rows by 50 and 20 63 and 135 against 96 and 117; of 128, 300 rows by 40 22
+// against 44.
 constexpr int MANY_FROM = 192;
 bool many_rows(const tsvd_adapters_s* h, int rows, int n_seq) { return rows >= MANY_FROM && rows / n_seq >= (h->groups >= 4 ? 32 : 64); }
 // What both could serve is the kernel's for few rows (512 rows of four sequences, 4096 to 4096, ranks of 16 10.8 us against 16.5, of 64 17.1
@@ -2111,8 +2113,8 @@ extern "C" tsvd_status_t tsvd_adapters_forward_ex(tsvd_adapters_t h, const void*
     tsvd_count_launch();
 
     // Rows of a tile: a warp's weights serve all of them, but with many sequences a tile holds many adapters, one after another, and
-    // with few rows there are few tiles (8, 16, 64 rows: 32 single tokens with ranks of 128, 4096 to 4096, 45.8, 67.8, 110 us; 200 rows by 50
-    // for each sequence 33.3, 28.4, 34.3; 900 by 20, ranks of 32, 49.0, 41.4, 45.4; 4000 by 30, ranks of 16, 80, 58, 51).
+    // with few rows there are few tiles (8, 16, 64 rows: 32 single tokens with ranks of 128, 4096 to 4096, 45.9, 67.6, 109 us; 200 rows by 50
+    // for each sequence 32.3, 26.4, 33.1; 900 by 20, ranks of 32, 40.1, 32.7, 36.9; 4000 by 30, ranks of 16, 80, 58, 51, fp32 318, 117, 88).
     u.tile_rows = n_rows >= 1024 ? UP_ROWS : n_rows >= 192 ? 16 : 8;
     if (many) {
         if (out_dtype == TSVD_F32) TSVD_CUDA_OK(up_many<float>(u, h->sms, st));

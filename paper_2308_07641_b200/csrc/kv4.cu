@@ -179,9 +179,10 @@ kv4_append_kernel(Kv4Geom g, Kv4Batch b, const T* k, long long ldk, const T* v, 
 // cosines of its turned / 2 angles and then their sines, so nothing here knows how the angles were chosen, and far positions
 // are as exact as near ones.  A row's cosines and sines are one line of the table, which its heads share from the caches.
 //
-// Bound by instructions, as the append without it is: 4095 rows of 32 heads of 128, keys, values and queries, 49 us (floor 24; the
-// append alone 33).  Read twice, once for either half of a pair, it took 64.  One token of 64 sequences, 32 heads on 8, and
-// the read of it 6.1 us: two launches, each two round trips to memory.
+// Bound by loads that start late, behind the search for the row's place, and by instructions: 4095 rows of 32 heads of 128, keys,
+// values and queries, 49 us (floor 24; the append alone 33), 3.1 stalls an issue on loads, issue slots 54% busy.  Read twice, once for
+// either half of a pair, it took 64.  One token of 64 sequences, 32 heads on 8, and the read of it 6.1 us: two launches, each two round
+// trips to memory.
 struct Turn {
     const float* table;      // [positions][turned]
     int turned, positions;

@@ -19,7 +19,7 @@
 // number is exact down to 2^-23 of the row's largest, and off by at most 2^-31 of it below).  Values become fp16 numbers
 // code * step + base (one rounding); probabilities fp16, relative to a reference that moves only when a score passes the one
 // it was set by by more than 5 (in units of log2): no exchange between lanes otherwise.  Both roundings are what the fp16
-// operands of the second product cost: 2^-12 of a term at most, up or down, where the result's own to bf16 is 2^-9; the
+// operands of the second product cost: 2^-11 of a term at most, up or down, where the result's own to bf16 is 2^-8; the
 // sum of probabilities is taken before their rounding.  Error against 64 bits 0.0017 of the results' size, 0.0016 to 0.0017
 // for fp32 throughout with the same last rounding.
 //

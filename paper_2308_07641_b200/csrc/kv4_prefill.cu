@@ -30,8 +30,8 @@
 //
 // Arithmetic: q as fp16 times a power of two for each row that brings its largest number to 2^15 (a bf16 number is then exact
 // down to 2^-32 of it; the power goes into the row's factor c), keys and values as fp16 (one rounding), probabilities as fp16,
-// sums in fp32 (that of the probabilities before their rounding).  The roundings, 2^-12 of a term at most, are what fp16
-// operands of the tensor cores cost; the result's own to bf16 is 2^-9.  Error against 64 bits 0.0017 of the results' size,
+// sums in fp32 (that of the probabilities before their rounding).  The roundings, 2^-11 of a term at most, are what fp16
+// operands of the tensor cores cost; the result's own to bf16 is 2^-8.  Error against 64 bits 0.0017 of the results' size,
 // 0.0016 to 0.0017 for fp32 throughout with the same last rounding.
 #include <algorithm>
 

@@ -37,8 +37,8 @@ struct NormArgs {
 
 // How the rows lie.  ALIGNED: on 16-byte boundaries, all of them and w; a thread's unit is 16 bytes.  PAIRS (bf16), SINGLES: on
 // boundaries of two numbers, or anyhow; a unit is as many numbers, spread over the row two or one at a time, neighbouring
-// threads on neighbouring ones.  (Cutting units out of aligned words, through registers or shared memory, was slower: 2048 x 1001 bf16
-// with residual to 8 bits 12.3 us, number by number 9.0; 4097 columns the other way round, 26 and 30.)
+// threads on neighbouring ones.  (Cutting units out of aligned words, through registers or shared memory, gains on wide rows what it loses
+// on narrow ones: 2048 x 1001 bf16 with residual to 8 bits 12.3 us in place of 9.0, 2048 x 4097 26 in place of 30.  Single numbers serve both.)
 enum Mode { ALIGNED, PAIRS, SINGLES };
 
 // The numbers of a unit, and back (rounded).

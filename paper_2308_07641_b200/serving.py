@@ -285,7 +285,7 @@ class LowRankAdapters:
         """base + scale * B (A x) for every row: x [rows, N] float32, bfloat16, or int8 with x_scale float32 [rows] (None: ones),
         base [rows, M] float32 or bfloat16 (None: zeros, float32 unless x is bfloat16), slots int32 [n_seq] (-1: no adapter),
         q_start int32 [n_seq + 1] (None: one row per sequence); all CUDA tensors, rows with any stride.  out may be base.
-        Returns [rows, M] of base's type."""
+        Returns [rows, M] of base's type; rows of no sequence are not written."""
         what = "LowRankAdapters.forward"
         rows, N, ldx = _rows(x, what)
         code = _code(x.dtype, what)
